@@ -30,7 +30,9 @@ typedef enum {
     MLT_ERR_ARCH = 5,        /* current device is not compute capability 10.x */
     MLT_ERR_TIMEOUT = 6,     /* a bounded device-side wait expired (reported by mlt_last_device_error) */
     MLT_ERR_BAD_BLOCK = 7,   /* a block-table entry outside [0, num_blocks) was met (reported by mlt_last_device_error) */
-    MLT_ERR_SCRATCH_LIMIT = 8 /* mlt_paged_attn_decode_static: the call needs more than MLT_PAGED_STATIC_SCRATCH_BYTES */
+    MLT_ERR_SCRATCH_LIMIT = 8, /* mlt_paged_attn_decode_static: the call needs more than MLT_PAGED_STATIC_SCRATCH_BYTES */
+    MLT_ERR_BAD_POSITION = 9 /* mlt_kv_append*: a sequence's token offsets or positions lie outside the call's tokens or the
+                                cos / sin tables (reported by mlt_last_device_error) */
 } mlt_status;
 
 /*
@@ -175,6 +177,110 @@ int mlt_paged_attn_decode_static(const void* Q, const void* K_cache, const void*
                                  void* stream);
 
 /*
+ * ---- The 8-bit serving path (library additions; the paper's workloads have no 8-bit form) ----
+ *
+ * E4M3 values are passed as bytes.  A decoding step runs them in this order: mlt_quantize_f8 (activations) ->
+ * mlt_gemm_f8 (projections) -> mlt_kv_append_f8 -> mlt_paged_attn_decode_f8 -> mlt_quantize_f8 -> mlt_gemm_f8.
+ *
+ * Scales that the library makes are powers of two: s = 2^e with the smallest e >= -64 for which amax <= 448 * s (amax
+ * over finite values; 2^-64 for a block of zeros).  E4M3's relative step does not depend on s, x / s is exact, and a
+ * stored value has one rounding (to nearest even).  Infinities are stored as +-448 * s, NaN as NaN.  Scales that it
+ * reads may be any FP32 values.
+ */
+
+/*
+ * Q = round(X / s) in E4M3 with one scale s per block of `block_rows` x 128 elements.
+ *
+ *   X       device, BF16, M x K row-major, pitch ldx in elements, a multiple of 8; 16-byte aligned
+ *   Q       device, E4M3 out, M x K row-major, pitch ldq in bytes, a multiple of 16; 16-byte aligned
+ *   scales  device, FP32 out.  block_rows 1 (activations): scales[kb * lds + i] for row i and K block kb, lds >= M.
+ *           block_rows 128 (weights): scales[rb * lds + kb] for row block rb, lds >= ceil(K / 128).
+ * The last blocks may be ragged; nothing outside M x K (and its blocks' scales) is written.  M == 0 or K == 0: MLT_OK,
+ * nothing launched.  MLT_ERR_UNSUPPORTED for another block_rows.
+ */
+int mlt_quantize_f8(const void* X, void* Q, float* scales, int64_t M, int64_t K, int64_t ldx, int64_t ldq, int64_t lds,
+                    int block_rows, void* stream);
+
+/*
+ * C[i][j] = sum over K blocks kb of 128: sa[kb][i] * sb[j / 128][kb] * sum over k in kb of A[i][k] * B[j][k]
+ * (B is stored with K contiguous, as the weights of a linear layer are).
+ *
+ *   A, B     device, E4M3, M x K and N x K, pitches lda, ldb in bytes, multiples of 16; 16-byte aligned
+ *   scale_a  device, FP32, scale_a[kb * ldsa + i], ldsa >= M                    (mlt_quantize_f8 with block_rows 1)
+ *   scale_b  device, FP32, scale_b[(j / 128) * ldsb + kb], ldsb >= ceil(K / 128)  (block_rows 128)
+ *   C        device, BF16 out, M x N, pitch ldc in elements, a multiple of 8; 16-byte aligned
+ * Products of a K block are summed in the tensor core's FP32, weighted, and summed over the blocks in FP32 in a fixed
+ * order; one rounding to nearest even.  K need not be a multiple of 128.  M == 0 or N == 0: MLT_OK, nothing launched;
+ * K == 0: C is zero-filled.  Needs no scratch.
+ */
+int mlt_gemm_f8(const void* A, const float* scale_a, const void* B, const float* scale_b, void* C,
+                int64_t M, int64_t N, int64_t K, int64_t lda, int64_t ldb, int64_t ldc, int64_t ldsa, int64_t ldsb,
+                void* stream);
+
+/*
+ * Appends the keys and values of new tokens to the paged cache that mlt_paged_attn_decode reads (mlt_kv_append, BF16) or
+ * that mlt_paged_attn_decode_f8 reads (mlt_kv_append_f8, E4M3), and rotates queries and keys by their positions.
+ *
+ * Sequence s has the new tokens cu_tokens[s] .. cu_tokens[s + 1] - 1 (none is allowed), which follow the context_lens[s]
+ * tokens that its cache holds: token t sits at position p = context_lens[s] + t - cu_tokens[s], in block
+ * block_table[s][p / block_size] at offset p % block_size.
+ *
+ *   Q, K, V      device, BF16; token t, head h, element d at t * ld + h * D + d (pitches ldq, ldk, ldv in elements,
+ *                multiples of 8; views of one fused projection work).  Q may be NULL: then only the cache is written.
+ *   cos_table, sin_table  device, FP32, [max_position, rotary_dim / 2]: row p holds the angles of position p
+ *   rotary_dim   elements of each head that are rotated, a multiple of 16, 0 (none: the tables may be NULL) .. D.
+ *                Pair i is (i, i + rotary_dim / 2), or with `interleaved` (2 i, 2 i + 1); (a, b) becomes
+ *                (a cos_i - b sin_i, b cos_i + a sin_i).  The other elements pass through.
+ *   cu_tokens    device, int32, [num_seqs + 1], ascending from 0;  context_lens device, int32, [num_seqs]
+ *   block_table  device, int32, [num_seqs, max_blocks_per_seq].  The blocks that one call writes must differ between
+ *                sequences (a shared block is copied before a sequence appends to it); where two share one all the
+ *                same, what its tokens hold afterwards is undefined.
+ *   Q_out        device, BF16 out, pitch ldqo; may be Q itself with the same pitch
+ *   K_cache, V_cache  device, [num_blocks, H_kv, block_size, D]
+ *   k_scale, v_scale  device, FP32, [num_blocks, H_kv] (E4M3 cache).  A block's scale becomes the larger of the scale it
+ *                had, if it holds tokens of the sequence already, and the power of two that its new tokens need; if it
+ *                grows, the tokens already there are rescaled (exact for powers of two unless a value underflows).  Scales
+ *                of blocks that hold tokens must be positive.
+ * D in {64, 128}, block_size in {8, 16, 32}.  Tokens from cu_tokens[num_seqs] on (a padded batch), their rows of
+ * Q_out and all cache positions without a new token are left as they were.  A block-table entry outside
+ * [0, num_blocks) or beyond the table's row is not written and reported (MLT_ERR_BAD_BLOCK); a sequence whose
+ * cu_tokens reach outside [0, num_tokens] or whose positions are negative or reach max_position is left out and
+ * reported (MLT_ERR_BAD_POSITION), both through mlt_last_device_error.  num_tokens == 0 or num_seqs == 0: MLT_OK,
+ * nothing launched.
+ */
+int mlt_kv_append(const void* Q, const void* K, const void* V, const float* cos_table, const float* sin_table,
+                  const int32_t* cu_tokens, const int32_t* context_lens, const int32_t* block_table,
+                  void* Q_out, void* K_cache, void* V_cache,
+                  int num_tokens, int num_seqs, int H, int H_kv, int D, int rotary_dim, int interleaved,
+                  int block_size, int max_blocks_per_seq, int num_blocks, int max_position,
+                  int64_t ldq, int64_t ldk, int64_t ldv, int64_t ldqo, void* stream);
+int mlt_kv_append_f8(const void* Q, const void* K, const void* V, const float* cos_table, const float* sin_table,
+                     const int32_t* cu_tokens, const int32_t* context_lens, const int32_t* block_table,
+                     void* Q_out, void* K_cache, void* V_cache, float* k_scale, float* v_scale,
+                     int num_tokens, int num_seqs, int H, int H_kv, int D, int rotary_dim, int interleaved,
+                     int block_size, int max_blocks_per_seq, int num_blocks, int max_position,
+                     int64_t ldq, int64_t ldk, int64_t ldv, int64_t ldqo, void* stream);
+
+/*
+ * mlt_paged_attn_decode over an E4M3 cache: key element = k_scale[block][head] * K_cache value, and likewise for V.
+ * Arguments as there, but
+ *   K_cache, V_cache  device, E4M3, [num_blocks, H_kv, block_size, D];  k_scale, v_scale  device, FP32, [num_blocks, H_kv]
+ *   workspace    device scratch, 16-byte aligned; mlt_paged_attn_f8_workspace_bytes is always enough.  With less the
+ *                work is cut into fewer shares, with NULL (or less than num_seqs * H_kv + 2 partials of
+ *                (H / H_kv) * (4 D + 8) bytes) one CTA works on each (sequence, KV head).  Calls that overlap on the
+ *                GPU must not share it.
+ * num_blocks * H_kv must be below 2^31.  The tokens of a bad block-table entry are left out and reported.  The maximum, the
+ * sum and the output accumulate in FP32; the probabilities are rounded to FP16 for the second product.
+ */
+size_t mlt_paged_attn_f8_workspace_bytes(int num_seqs, int H, int H_kv, int D);
+int mlt_paged_attn_decode_f8(const void* Q, const void* K_cache, const void* V_cache, const float* k_scale, const float* v_scale,
+                             const int32_t* block_table, const int32_t* seq_lens,
+                             void* O, float* LSE,
+                             int num_seqs, int H, int H_kv, int D,
+                             int block_size, int max_blocks_per_seq, int num_blocks, float scale,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * The SM clock the last GEMM (which = 0) or attention (which = 1) launch on the current device really ran at, in
  * MHz: CTA 0 of those kernels notes the SM cycle counter and the nanosecond timer at its start and at its end.  (No
  * counterpart in the paper; a measurement aid: under tensor-core load this part runs well below the clock NVML
@@ -202,7 +308,7 @@ int mlt_debug_gemm_plan(int64_t M, int64_t N, int64_t K, size_t workspace_bytes,
  * Device-side health word.  Kernels never trap: a wait that exceeds its bound
  * records {code, barrier id, block} in a per-device status word and the kernel
  * drains and returns.  This call synchronises the current device, reads and
- * clears that word, and returns MLT_OK, MLT_ERR_TIMEOUT, MLT_ERR_BAD_BLOCK or MLT_ERR_CUDA.
+ * clears that word, and returns MLT_OK, MLT_ERR_TIMEOUT, MLT_ERR_BAD_BLOCK, MLT_ERR_BAD_POSITION or MLT_ERR_CUDA.
  * detail (host, may be NULL) receives 4 words: code, barrier id, block, aux.
  * (Library addition; the paper has no counterpart.)
  */

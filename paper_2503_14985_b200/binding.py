@@ -15,11 +15,12 @@ LIB_PATH = os.path.join(_HERE, "libmlt.so")
 MLT_OK = 0
 STATUS_NAMES = {0: "MLT_OK", 1: "MLT_ERR_INVALID_ARG", 2: "MLT_ERR_UNSUPPORTED", 3: "MLT_ERR_ALIGNMENT",
                 4: "MLT_ERR_CUDA", 5: "MLT_ERR_ARCH", 6: "MLT_ERR_TIMEOUT", 7: "MLT_ERR_BAD_BLOCK",
-                8: "MLT_ERR_SCRATCH_LIMIT"}
+                8: "MLT_ERR_SCRATCH_LIMIT", 9: "MLT_ERR_BAD_POSITION"}
 PAGED_STATIC_SCRATCH_BYTES = 16 * 1024 * 1024
 
 EXPORTS = ("mlt_gemm", "mlt_gemm_f16", "mlt_gemm_ex", "mlt_gemm_workspace_bytes", "mlt_mha_fwd", "mlt_paged_attn_decode", "mlt_paged_attn_decode_static",
            "mlt_paged_attn_workspace_bytes",
+           "mlt_quantize_f8", "mlt_gemm_f8", "mlt_kv_append", "mlt_kv_append_f8", "mlt_paged_attn_decode_f8", "mlt_paged_attn_f8_workspace_bytes",
            "mlt_last_device_error", "mlt_debug_wait_timeout_selftest", "mlt_debug_last_clock_mhz", "mlt_debug_gemm_plan", "mlt_status_string",
            "mlt_version")
 
@@ -64,6 +65,18 @@ def load() -> ctypes.CDLL:
         lib.mlt_paged_attn_decode_static.argtypes = [p, p, p, p, p, p, p, i32, i32, i32, i32, i32, i32, i32,
                                                      ctypes.c_float, p]
         lib.mlt_paged_attn_decode_static.restype = i32
+        lib.mlt_quantize_f8.argtypes = [p, p, p, i64, i64, i64, i64, i64, i32, p]
+        lib.mlt_quantize_f8.restype = i32
+        lib.mlt_gemm_f8.argtypes = [p, p, p, p, p, i64, i64, i64, i64, i64, i64, i64, i64, p]
+        lib.mlt_gemm_f8.restype = i32
+        lib.mlt_kv_append.argtypes = [p] * 11 + [i32] * 11 + [i64] * 4 + [p]
+        lib.mlt_kv_append.restype = i32
+        lib.mlt_kv_append_f8.argtypes = [p] * 13 + [i32] * 11 + [i64] * 4 + [p]
+        lib.mlt_kv_append_f8.restype = i32
+        lib.mlt_paged_attn_f8_workspace_bytes.argtypes = [i32, i32, i32, i32]
+        lib.mlt_paged_attn_f8_workspace_bytes.restype = ctypes.c_size_t
+        lib.mlt_paged_attn_decode_f8.argtypes = [p] * 9 + [i32] * 7 + [ctypes.c_float, p, ctypes.c_size_t, p]
+        lib.mlt_paged_attn_decode_f8.restype = i32
         lib.mlt_last_device_error.argtypes = [p]
         lib.mlt_last_device_error.restype = i32
         lib.mlt_status_string.argtypes = [i32]
@@ -132,6 +145,52 @@ def paged_attn_decode_static_raw(Q: int, K_cache: int, V_cache: int, block_table
     """mlt_paged_attn_decode_static (scratch inside the library, nothing allocated) with raw device addresses."""
     return int(load().mlt_paged_attn_decode_static(Q, K_cache, V_cache, block_table, seq_lens, O, LSE, num_seqs, H,
                                                    H_kv, D, block_size, max_blocks, num_blocks, scale, stream))
+
+
+def quantize_f8_raw(X: int, Q: int, scales: int, M: int, K: int, ldx: int, ldq: int, lds: int, block_rows: int,
+                    stream: int = 0) -> int:
+    """mlt_quantize_f8 with raw device addresses; returns the status code."""
+    return load().mlt_quantize_f8(X, Q, scales, M, K, ldx, ldq, lds, block_rows, stream)
+
+
+def gemm_f8_raw(A: int, scale_a: int, B: int, scale_b: int, C: int, M: int, N: int, K: int, lda: int, ldb: int, ldc: int,
+                ldsa: int, ldsb: int, stream: int = 0) -> int:
+    """mlt_gemm_f8 with raw device addresses; returns the status code."""
+    return load().mlt_gemm_f8(A, scale_a, B, scale_b, C, M, N, K, lda, ldb, ldc, ldsa, ldsb, stream)
+
+
+def kv_append_raw(Q: int, K: int, V: int, cos: int, sin: int, cu_tokens: int, context_lens: int, block_table: int,
+                  Q_out: int, K_cache: int, V_cache: int, num_tokens: int, num_seqs: int, H: int, H_kv: int, D: int,
+                  rotary_dim: int, interleaved: int, block_size: int, max_blocks: int, num_blocks: int, max_position: int,
+                  ldq: int, ldk: int, ldv: int, ldqo: int, stream: int = 0) -> int:
+    """mlt_kv_append (BF16 cache) with raw device addresses; returns the status code."""
+    return load().mlt_kv_append(Q, K, V, cos, sin, cu_tokens, context_lens, block_table, Q_out, K_cache, V_cache, num_tokens,
+                                num_seqs, H, H_kv, D, rotary_dim, interleaved, block_size, max_blocks, num_blocks,
+                                max_position, ldq, ldk, ldv, ldqo, stream)
+
+
+def kv_append_f8_raw(Q: int, K: int, V: int, cos: int, sin: int, cu_tokens: int, context_lens: int, block_table: int,
+                     Q_out: int, K_cache: int, V_cache: int, k_scale: int, v_scale: int, num_tokens: int, num_seqs: int,
+                     H: int, H_kv: int, D: int, rotary_dim: int, interleaved: int, block_size: int, max_blocks: int,
+                     num_blocks: int, max_position: int, ldq: int, ldk: int, ldv: int, ldqo: int, stream: int = 0) -> int:
+    """mlt_kv_append_f8 (E4M3 cache) with raw device addresses; returns the status code."""
+    return load().mlt_kv_append_f8(Q, K, V, cos, sin, cu_tokens, context_lens, block_table, Q_out, K_cache, V_cache, k_scale,
+                                   v_scale, num_tokens, num_seqs, H, H_kv, D, rotary_dim, interleaved, block_size,
+                                   max_blocks, num_blocks, max_position, ldq, ldk, ldv, ldqo, stream)
+
+
+def paged_attn_f8_workspace_bytes(num_seqs: int, H: int, H_kv: int, D: int) -> int:
+    return int(load().mlt_paged_attn_f8_workspace_bytes(num_seqs, H, H_kv, D))
+
+
+def paged_attn_decode_f8_raw(Q: int, K_cache: int, V_cache: int, k_scale: int, v_scale: int, block_table: int,
+                             seq_lens: int, O: int, LSE: int, num_seqs: int, H: int, H_kv: int, D: int, block_size: int,
+                             max_blocks: int, num_blocks: int, scale: float, workspace: int = 0, workspace_bytes: int = 0,
+                             stream: int = 0) -> int:
+    """mlt_paged_attn_decode_f8 with raw device addresses; returns the status code."""
+    return load().mlt_paged_attn_decode_f8(Q, K_cache, V_cache, k_scale, v_scale, block_table, seq_lens, O, LSE, num_seqs, H,
+                                           H_kv, D, block_size, max_blocks, num_blocks, scale, workspace, workspace_bytes,
+                                           stream)
 
 
 def last_device_error():
@@ -243,4 +302,216 @@ def paged_attn_decode(Q, K_cache, V_cache, block_table, seq_lens, *, scale: floa
                                _stream(stream))
     if rc != MLT_OK:
         raise MltError(rc, "mlt_paged_attn_decode")
+    return O, LSE
+
+
+def _on_device(tensors, stream, call):
+    """Runs call(stream address) with the tensors' device current; they must all be CUDA tensors of one device."""
+    import torch
+    index = tensors[0].device.index
+    for t in tensors:
+        if not t.is_cuda or t.device.index != index:
+            raise ValueError("all tensors must be on one CUDA device")
+    if torch.cuda.current_device() == index:
+        return call(_stream(stream))
+    with torch.cuda.device(index):
+        return call(_stream(stream))
+
+
+def _f8():
+    import torch
+    return torch.float8_e4m3fn
+
+
+def _pitch(t, width):
+    """Row pitch of a 2-D tensor with unit inner stride (of a single row: any pitch serves)."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("matrices must be 2-D with unit inner stride")
+    return t.stride(0) if t.shape[0] > 1 else width
+
+
+def quantize_f8(X, *, block_rows: int = 1, Q=None, scales=None, stream=None):
+    """X [M, K] bfloat16 -> (Q [M, K] float8_e4m3fn, scales float32), one power-of-two scale per block.
+
+    block_rows 1 (activations): 1 x 128 blocks, scales [ceil(K / 128), M].  block_rows 128 (weights): 128 x 128 blocks,
+    scales [ceil(M / 128), ceil(K / 128)].  Both are what gemm_f8 takes.  Row pitches come from the tensors' strides; the
+    pitch of a new Q is K rounded up to 16.
+    """
+    import torch
+    if X.dtype != torch.bfloat16:
+        raise TypeError("X must be bfloat16")
+    if block_rows not in (1, 128):
+        raise ValueError("block_rows must be 1 or 128")
+    M, K = X.shape
+    up16 = (K + 15) // 16 * 16
+    kb = (K + 127) // 128
+    shape = (kb, M) if block_rows == 1 else ((M + 127) // 128, kb)
+    if Q is None:
+        Q = torch.empty((M, up16), dtype=_f8(), device=X.device)
+        if up16 != K:
+            Q = Q[:, :K]
+    if scales is None:
+        scales = torch.empty(shape, dtype=torch.float32, device=X.device)
+    if Q.dtype != _f8() or scales.dtype != torch.float32:
+        raise TypeError("Q must be float8_e4m3fn and scales float32")
+    if tuple(Q.shape) != (M, K) or tuple(scales.shape) != shape:
+        raise ValueError("shape mismatch")
+    ldx, ldq, lds = _pitch(X, (K + 7) // 8 * 8), _pitch(Q, up16), _pitch(scales, shape[1])
+    rc = _on_device((X, Q, scales), stream, lambda st: quantize_f8_raw(X.data_ptr(), Q.data_ptr(), scales.data_ptr(), M, K, ldx, ldq,
+                                                                       lds, block_rows, st))
+    if rc != MLT_OK:
+        raise MltError(rc, "mlt_quantize_f8")
+    return Q, scales
+
+
+def gemm_f8(A, scale_a, B, scale_b, C=None, *, stream=None):
+    """C = (A scaled) @ (B scaled).T in bfloat16 for float8_e4m3fn A [M, K] and B [N, K] with K contiguous.
+
+    scale_a [ceil(K / 128), M] and scale_b [ceil(N / 128), ceil(K / 128)], float32 (see quantize_f8).  Row pitches come
+    from the tensors' strides (A, B: multiples of 16 bytes; C: of 8 elements; a new C has N rounded up to 8).
+    """
+    import torch
+    if A.dtype != _f8() or B.dtype != _f8() or scale_a.dtype != torch.float32 or scale_b.dtype != torch.float32:
+        raise TypeError("A and B must be float8_e4m3fn, the scales float32")
+    (M, K), N = A.shape, B.shape[0]
+    kb = (K + 127) // 128
+    if B.shape[1] != K or tuple(scale_a.shape) != (kb, M) or tuple(scale_b.shape) != ((N + 127) // 128, kb):
+        raise ValueError("shape mismatch")
+    up8, up16 = (N + 7) // 8 * 8, (K + 15) // 16 * 16
+    if C is None:
+        C = torch.empty((M, up8), dtype=torch.bfloat16, device=A.device)
+        if up8 != N:
+            C = C[:, :N]
+    elif C.dtype != torch.bfloat16 or tuple(C.shape) != (M, N):
+        raise ValueError("C must be bfloat16 [M, N]")
+    lda, ldb, ldc, ldsa, ldsb = _pitch(A, up16), _pitch(B, up16), _pitch(C, up8), _pitch(scale_a, M), _pitch(scale_b, kb)
+    rc = _on_device((A, scale_a, B, scale_b, C), stream,
+                    lambda st: gemm_f8_raw(A.data_ptr(), scale_a.data_ptr(), B.data_ptr(), scale_b.data_ptr(), C.data_ptr(), M, N, K,
+                                           lda, ldb, ldc, ldsa, ldsb, st))
+    if rc != MLT_OK:
+        raise MltError(rc, "mlt_gemm_f8")
+    return C
+
+
+def _rows(t, heads, D):
+    """Token pitch of [T, heads, D] whose heads lie side by side."""
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != D or t.stride(2) != 1 or (heads > 1 and t.stride(1) != D):
+        raise ValueError("queries, keys and values must be [tokens, heads, D] with a token's heads side by side")
+    return t.stride(0) if t.shape[0] > 1 else heads * D
+
+
+def _kv_append(name, Q, K, V, cos, sin, cu_tokens, context_lens, block_table, K_cache, V_cache, scales, interleaved, Q_out, stream):
+    import torch
+    bf16, cache_type = torch.bfloat16, _f8() if scales else torch.bfloat16
+    if K.dtype != bf16 or V.dtype != bf16 or (Q is not None and Q.dtype != bf16):
+        raise TypeError("Q, K and V must be bfloat16")
+    if K_cache.dtype != cache_type or V_cache.dtype != cache_type or not K_cache.is_contiguous() or not V_cache.is_contiguous():
+        raise TypeError(f"the caches must be contiguous {cache_type} tensors")
+    num_blocks, H_kv, block_size, D = K_cache.shape
+    T = K.shape[0]
+    if V_cache.shape != K_cache.shape or V.shape != K.shape or (Q is not None and Q.shape[0] != T):
+        raise ValueError("shape mismatch")
+    for t in (cu_tokens, context_lens, block_table):
+        if t.dtype != torch.int32 or not t.is_contiguous():
+            raise TypeError("cu_tokens, context_lens and block_table must be contiguous int32 tensors")
+    S = context_lens.shape[0]
+    if cu_tokens.shape[0] != S + 1 or block_table.dim() != 2 or block_table.shape[0] != S:
+        raise ValueError("cu_tokens must be [sequences + 1], block_table [sequences, blocks]")
+    for t in scales:
+        if t.dtype != torch.float32 or not t.is_contiguous() or tuple(t.shape) != (num_blocks, H_kv):
+            raise TypeError("k_scale and v_scale must be contiguous float32 [num_blocks, H_kv] tensors")
+    ldk, ldv = _rows(K, H_kv, D), _rows(V, H_kv, D)
+    H = ldq = ldqo = rotary = top = 0
+    held = [K, V, K_cache, V_cache, cu_tokens, context_lens, block_table, *scales]
+    if Q is not None:
+        H = Q.shape[1]
+        ldq = _rows(Q, H, D)
+        if Q_out is None:
+            Q_out = torch.empty((T, H, D), dtype=bf16, device=Q.device)
+        elif Q_out.dtype != bf16 or Q_out.shape != Q.shape:
+            raise ValueError("Q_out must be bfloat16 of Q's shape")
+        ldqo = _rows(Q_out, H, D)
+        held += [Q, Q_out]
+    if (cos is None) != (sin is None):
+        raise ValueError("cos and sin come together")
+    if cos is not None:
+        if cos.dtype != torch.float32 or sin.dtype != torch.float32 or not cos.is_contiguous() or not sin.is_contiguous():
+            raise TypeError("cos and sin must be contiguous float32 tensors")
+        if cos.dim() != 2 or cos.shape != sin.shape:
+            raise ValueError("cos and sin must be [positions, rotary_dim / 2]")
+        top, rotary = cos.shape[0], 2 * cos.shape[1]
+        held += [cos, sin]
+
+    def ptr(t):
+        return t.data_ptr() if t is not None else 0
+
+    raw = kv_append_f8_raw if scales else kv_append_raw
+    rc = _on_device(held, stream, lambda st: raw(
+        ptr(Q), K.data_ptr(), V.data_ptr(), ptr(cos), ptr(sin), cu_tokens.data_ptr(), context_lens.data_ptr(), block_table.data_ptr(),
+        ptr(Q_out) if Q is not None else 0, K_cache.data_ptr(), V_cache.data_ptr(), *[t.data_ptr() for t in scales], T, S, H, H_kv, D, rotary,
+        int(bool(interleaved)), block_size, block_table.shape[1], num_blocks, top, ldq, ldk, ldv, ldqo, st))
+    if rc != MLT_OK:
+        raise MltError(rc, name)
+    return Q_out if Q is not None else None
+
+
+def kv_append(Q, K, V, cos, sin, cu_tokens, context_lens, block_table, K_cache, V_cache, *, interleaved: bool = False,
+              Q_out=None, stream=None):
+    """Rotates Q and K by their positions and appends K and V to a bfloat16 paged cache; returns the rotated Q.
+
+    Q [T, H, D] (or None: only the cache is written), K and V [T, H_kv, D] bfloat16, a token's heads side by side (views
+    of one fused projection work); cos, sin [positions, rotary_dim / 2] float32 (both None: no rotation); cu_tokens
+    [S + 1], context_lens [S], block_table [S, max_blocks] int32; caches [num_blocks, H_kv, block_size, D].  Tokens from
+    cu_tokens[S] on are left out.  Q_out may be Q.
+    """
+    return _kv_append("mlt_kv_append", Q, K, V, cos, sin, cu_tokens, context_lens, block_table, K_cache, V_cache, (),
+                      interleaved, Q_out, stream)
+
+
+def kv_append_f8(Q, K, V, cos, sin, cu_tokens, context_lens, block_table, K_cache, V_cache, k_scale, v_scale, *,
+                 interleaved: bool = False, Q_out=None, stream=None):
+    """kv_append into a float8_e4m3fn cache with one float32 scale per block and head: k_scale, v_scale [num_blocks, H_kv]."""
+    return _kv_append("mlt_kv_append_f8", Q, K, V, cos, sin, cu_tokens, context_lens, block_table, K_cache, V_cache,
+                      (k_scale, v_scale), interleaved, Q_out, stream)
+
+
+def paged_attn_decode_f8(Q, K_cache, V_cache, k_scale, v_scale, block_table, seq_lens, *, scale: float, workspace=None, O=None,
+                         LSE=None, return_lse: bool = True, stream=None):
+    """paged_attn_decode over float8_e4m3fn caches with float32 scales k_scale, v_scale [num_blocks, H_kv].
+
+    `workspace` is an optional uint8 CUDA tensor (see paged_attn_f8_workspace_bytes).  Returns (O [S,H,D] bfloat16,
+    LSE [S,H] float32 or None).
+    """
+    import torch
+    if Q.dtype != torch.bfloat16 or not Q.is_contiguous() or Q.dim() != 3:
+        raise TypeError("Q must be a contiguous [S, H, D] bfloat16 tensor")
+    for t in (K_cache, V_cache):
+        if t.dtype != _f8() or not t.is_contiguous() or t.dim() != 4:
+            raise TypeError("the caches must be contiguous 4-D float8_e4m3fn tensors")
+    for t in (block_table, seq_lens):
+        if t.dtype != torch.int32 or not t.is_contiguous():
+            raise TypeError("block_table and seq_lens must be contiguous int32 tensors")
+    S, H, D = Q.shape
+    NB, H_kv, bs, _ = K_cache.shape
+    for t in (k_scale, v_scale):
+        if t.dtype != torch.float32 or not t.is_contiguous() or tuple(t.shape) != (NB, H_kv):
+            raise TypeError("k_scale and v_scale must be contiguous float32 [num_blocks, H_kv] tensors")
+    if V_cache.shape != K_cache.shape or K_cache.shape[3] != D or seq_lens.shape[0] != S or block_table.dim() != 2 or block_table.shape[0] != S:
+        raise ValueError("shape mismatch")
+    if O is None:
+        O = torch.empty_like(Q)
+    elif O.dtype != torch.bfloat16 or O.shape != Q.shape or not O.is_contiguous():
+        raise ValueError("O must be contiguous bfloat16 of Q's shape")
+    if LSE is None and return_lse:
+        LSE = torch.empty((S, H), dtype=torch.float32, device=Q.device)
+    elif LSE is not None and (LSE.dtype != torch.float32 or tuple(LSE.shape) != (S, H) or not LSE.is_contiguous()):
+        raise ValueError("LSE must be contiguous float32 [S, H]")
+    held = [Q, K_cache, V_cache, k_scale, v_scale, block_table, seq_lens, O]
+    held += [t for t in (LSE, workspace) if t is not None]
+    rc = _on_device(held, stream, lambda st: paged_attn_decode_f8_raw(
+        Q.data_ptr(), K_cache.data_ptr(), V_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), block_table.data_ptr(),
+        seq_lens.data_ptr(), O.data_ptr(), LSE.data_ptr() if LSE is not None else 0, S, H, H_kv, D, bs, block_table.shape[1], NB, float(scale),
+        workspace.data_ptr() if workspace is not None else 0, workspace.numel() * workspace.element_size() if workspace is not None else 0, st))
+    if rc != MLT_OK:
+        raise MltError(rc, "mlt_paged_attn_decode_f8")
     return O, LSE

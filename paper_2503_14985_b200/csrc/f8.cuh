@@ -1,0 +1,53 @@
+// E4M3 helpers shared by the 8-bit kernels (quantiser, cache append, scaled GEMM, decode over an 8-bit cache).
+//
+// Scales made here are powers of two, s = 2^e with the smallest e >= -64 for which amax <= 448 * s.  E4M3 is a
+// floating format: its relative step does not depend on s, so a power of two costs no precision against amax / 448,
+// x / s is exact (the stored value has one rounding), and values that were stored under one scale move to a larger one
+// without a second rounding unless they underflow.
+#pragma once
+
+#include "ptx.cuh"
+
+namespace mlt {
+
+constexpr int kF8MinExp = -64;
+
+// {hi, lo} -> two E4M3 codes, round to nearest even; magnitudes beyond 448 (infinities too) become 448, NaN stays NaN
+__device__ __forceinline__ uint32_t f8x2_from_f32(float lo, float hi) {
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ uint32_t f8x4_from_f32(float a, float b, float c, float d) {
+    return f8x2_from_f32(a, b) | (f8x2_from_f32(c, d) << 16);
+}
+// two E4M3 codes -> two FP16 values (exact: FP16 holds every E4M3 value), low code in the low half
+__device__ __forceinline__ uint32_t f16x2_from_f8x2(uint16_t v) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(v));
+    return r;
+}
+__device__ __forceinline__ void f16x2_from_f8x4(uint32_t v, uint32_t& lo, uint32_t& hi) {
+    lo = f16x2_from_f8x2(static_cast<uint16_t>(v & 0xFFFFu));
+    hi = f16x2_from_f8x2(static_cast<uint16_t>(v >> 16));
+}
+__device__ __forceinline__ float2 f32x2_from_f16x2(uint32_t v) {
+    float2 f;
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, h;\n\t}" : "=f"(f.x), "=f"(f.y) : "r"(v));
+    return f;
+}
+
+// Exponent e of the scale for a finite amax >= 0 (448 = 1.75 * 2^8).
+__device__ __forceinline__ int f8_scale_exp(float amax) {
+    const uint32_t b = __float_as_uint(amax);
+    const int e = static_cast<int>(b >> 23) - 127 - 8 + ((b & 0x7FFFFFu) > 0x600000u ? 1 : 0);  // FP32 subnormals give e < -64
+    return max(kF8MinExp, e);  // at most 127 - 8 + 1 = 120
+}
+__device__ __forceinline__ float pow2f(int e) { return __uint_as_float(static_cast<uint32_t>(e + 127) << 23); }  // -126 <= e <= 127
+
+__device__ __forceinline__ float abs_if_finite(float x) {
+    const float a = fabsf(x);
+    return a <= 3.402823466e38f ? a : 0.0f;  // infinities and NaN do not set a scale
+}
+
+}  // namespace mlt

@@ -11,9 +11,13 @@
 #include <mutex>
 
 #include "../../include/mlt.h"
+#include "append.cuh"
 #include "gemm.cuh"
+#include "gemm_f8.cuh"
 #include "mha.cuh"
 #include "paged.cuh"
+#include "paged_f8.cuh"
+#include "quantize.cuh"
 
 namespace {
 
@@ -96,7 +100,9 @@ int get_device(DeviceInfo* out) {
             }
             d.cluster_slots[i] = clusters * S;
         }
-        if (paged_configure() != 0) return MLT_ERR_CUDA;
+        if (paged_configure() != 0 || !paged_f8_configure()) return MLT_ERR_CUDA;
+        if (set_smem(gemm_f8_kernel<64, 3>, kGemmF8NarrowSmem) != MLT_OK || set_smem(gemm_f8_kernel<128, 1>, kGemmF8WideSmem) != MLT_OK)
+            return MLT_ERR_CUDA;
         const int mha_rc = mha_configure();
         if (mha_rc == 1) return MLT_ERR_CUDA;
         d.mha_ok = mha_rc == 0;
@@ -106,9 +112,9 @@ int get_device(DeviceInfo* out) {
     return MLT_OK;
 }
 
-// BF16 tensor map with 128-byte swizzle.  dims / strides innermost first; strides[0] is implicit.
+// Tensor map with 128-byte swizzle (64-byte where asked for).  dims / strides innermost first; strides[0] is implicit.
 int encode_bf16(CUtensorMap* map, const void* base, int rank, const uint64_t* dims, const uint64_t* strides_bytes,
-                const uint32_t* box, int dtype = 0 /* 0 BF16, 1 FP16, 2 FP32 */) {
+                const uint32_t* box, int dtype = 0 /* 0 BF16, 1 FP16, 2 FP32, 3 bytes */, bool swizzle64 = false) {
     EncodeTiledFn enc;
     int rc = get_encoder(&enc);
     if (rc != MLT_OK) return rc;
@@ -126,11 +132,13 @@ int encode_bf16(CUtensorMap* map, const void* base, int rank, const uint64_t* di
             gstride[i - 1] = strides_bytes[i - 1];
         }
     }
-    const CUtensorMapDataType dt = dtype == 2   ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+    const CUtensorMapDataType dt = dtype == 3   ? CU_TENSOR_MAP_DATA_TYPE_UINT8
+                                   : dtype == 2 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
                                    : dtype == 1 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
                                                 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
     CUresult r = enc(map, dt, static_cast<cuuint32_t>(rank), const_cast<void*>(base),
-                     gdim, gstride, gbox, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                     gdim, gstride, gbox, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                     swizzle64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? MLT_OK : MLT_ERR_CUDA;
 }
@@ -144,14 +152,15 @@ int forced_variant() {
     return v;
 }
 
-// Debug only: tuning overrides read once from the environment (0 = not set).  MLT_GEMM_GROUP_M: M-tiles per raster
+// Debug only: tuning overrides read once from the environment (0 = not set).  MLT_F8_BN / MLT_F8_SPLIT: tile width and CTAs
+// per tile of the scaled GEMM.  MLT_GEMM_GROUP_M: M-tiles per raster
 // group of the pair kernel; MLT_GEMM_NO_HALF: no half tiles in the last wave; MLT_MHA_HEAD_GROUP / MLT_MHA_GRID: item
 // list grouping and CTA count of the attention kernel; MLT_PAGED_SPLITS: CTAs per (sequence, KV head);
 // MLT_GEMM_WIDE_RATIO: per cent of the current plan's cost below which 128 x 256 tiles in clusters are taken (1: never);
 // MLT_GEMM_NO_EVEN: uniform K slices through scratch instead of the even hand-out; MLT_GEMM_NO_SKINNY_MODEL: the
 // rule-based plan for problems of one tile row instead of the time model; MLT_GEMM_NO_CLUSTER: no K cut inside clusters.
 struct DebugEnv {
-    int gemm_group_m, gemm_no_half, mha_head_group, mha_grid, paged_splits, gemm_wide_ratio, gemm_no_even, gemm_no_skinny_model, gemm_no_cluster;
+    int gemm_group_m, gemm_no_half, mha_head_group, mha_grid, paged_splits, gemm_wide_ratio, gemm_no_even, gemm_no_skinny_model, gemm_no_cluster, f8_bn, f8_split;
 };
 const DebugEnv& debug_env() {
     static const DebugEnv env = [] {
@@ -161,7 +170,7 @@ const DebugEnv& debug_env() {
             return v > 0 ? v : 0;
         };
         return DebugEnv{get("MLT_GEMM_GROUP_M"), get("MLT_GEMM_NO_HALF"), get("MLT_MHA_HEAD_GROUP"), get("MLT_MHA_GRID"),
-                        get("MLT_PAGED_SPLITS"), get("MLT_GEMM_WIDE_RATIO"), get("MLT_GEMM_NO_EVEN"), get("MLT_GEMM_NO_SKINNY_MODEL"), get("MLT_GEMM_NO_CLUSTER")};
+                        get("MLT_PAGED_SPLITS"), get("MLT_GEMM_WIDE_RATIO"), get("MLT_GEMM_NO_EVEN"), get("MLT_GEMM_NO_SKINNY_MODEL"), get("MLT_GEMM_NO_CLUSTER"), get("MLT_F8_BN"), get("MLT_F8_SPLIT")};
     }();
     return env;
 }
@@ -199,6 +208,7 @@ const char* mlt_status_string(int status) {
         case MLT_ERR_ARCH: return "device is not compute capability 10.x (sm_100a required)";
         case MLT_ERR_TIMEOUT: return "a bounded device-side wait expired";
         case MLT_ERR_BAD_BLOCK: return "a block-table entry outside [0, num_blocks) was met";
+        case MLT_ERR_BAD_POSITION: return "a sequence's token offsets or positions lie outside the call's tokens or the cos / sin tables";
         case MLT_ERR_SCRATCH_LIMIT: return "the call needs more scratch than the built-in array of mlt_paged_attn_decode_static holds";
         default: return "unknown status";
     }
@@ -242,7 +252,9 @@ int mlt_last_device_error(uint32_t* detail) {
     if (host[0] != 0) {
         unsigned int zero[4] = {0, 0, 0, 0};
         if (cudaMemcpyToSymbol(g_status, zero, sizeof zero) != cudaSuccess) return MLT_ERR_CUDA;
-        return host[0] == kStatusTimeout ? MLT_ERR_TIMEOUT : host[0] == kStatusBadBlock ? MLT_ERR_BAD_BLOCK : MLT_ERR_CUDA;
+        return host[0] == kStatusTimeout ? MLT_ERR_TIMEOUT : host[0] == kStatusBadBlock ? MLT_ERR_BAD_BLOCK
+               : host[0] == kStatusBadPosition                     ? MLT_ERR_BAD_POSITION
+                                                                   : MLT_ERR_CUDA;
     }
     return MLT_OK;
 }
@@ -831,3 +843,285 @@ extern "C" int mlt_paged_attn_decode_static(const void* Q, const void* K_cache, 
     // nothing in the array has to start at zero: every partial the combine step reads was written by this call
     return paged_launch(p, D, scratch, static_cast<cudaStream_t>(stream));
 }
+
+// ---------------------------------------------------------------------------------------------------------
+// The 8-bit serving path: quantiser, scaled GEMM, cache append (BF16 and E4M3), decode over an E4M3 cache
+// ---------------------------------------------------------------------------------------------------------
+namespace {
+
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+// Launch plan of the scaled GEMM.
+struct GemmF8Plan {
+    int bn;       // tile width
+    int cluster;  // CTAs per tile that cut K
+    int kb_per_split;
+    int a_rows, stages;
+};
+
+GemmF8Plan gemm_f8_plan(int64_t M, int64_t N, int64_t K, int sm_count) {
+    const int num_kb = static_cast<int>((K + kF8BK - 1) / kF8BK);
+    GemmF8Plan plan;
+    plan.bn = M <= 128 ? 64 : 128;
+    if (debug_env().f8_bn == 64 || debug_env().f8_bn == 128) plan.bn = debug_env().f8_bn;
+    plan.a_rows = static_cast<int>(std::min<int64_t>(128, (M + 7) / 8 * 8));
+    const int smem = plan.bn == 64 ? kGemmF8NarrowSmem : kGemmF8WideSmem;
+    const int stage = plan.a_rows * kF8BK + plan.bn * kF8BK;
+    plan.stages = std::min(kF8MaxStages, (smem - 1024 - GemmF8Smem<64>::kBarrierBytes) / stage);
+    const int64_t tiles = ((M + 127) / 128) * ((N + plan.bn - 1) / plan.bn);
+    const int64_t slots = static_cast<int64_t>(sm_count) * (plan.bn == 64 ? 3 : 1);
+    plan.cluster = 1;
+    int64_t best = INT64_MAX;
+    for (int S = 1; S <= 8; S *= 2) {
+        const int kbps = (num_kb + S - 1) / S;
+        if (S > 1 && (kbps < 2 || static_cast<int64_t>(kbps) * (S - 1) >= num_kb)) continue;  // too short, or an empty slice
+        const int64_t cost = (tiles * S + slots - 1) / slots * (kbps + (S > 1 ? 10 : 6));
+        if (cost < best) { best = cost; plan.cluster = S; }
+    }
+    if (debug_env().f8_split) plan.cluster = debug_env().f8_split;
+    plan.kb_per_split = (num_kb + plan.cluster - 1) / plan.cluster;
+    return plan;
+}
+
+}  // namespace
+
+extern "C" {
+
+int mlt_quantize_f8(const void* X, void* Q, float* scales, int64_t M, int64_t K, int64_t ldx, int64_t ldq, int64_t lds,
+                    int block_rows, void* stream) {
+    if (M < 0 || K < 0) return MLT_ERR_INVALID_ARG;
+    if (block_rows != 1 && block_rows != 128) return MLT_ERR_UNSUPPORTED;
+    if (M == 0 || K == 0) return MLT_OK;
+    if (!X || !Q || !scales || ldx < K || ldq < K || lds < (block_rows == 1 ? M : (K + 127) / 128)) return MLT_ERR_INVALID_ARG;
+    if (M > INT32_MAX - 256 || K > INT32_MAX - 256) return MLT_ERR_UNSUPPORTED;
+    if (!aligned16(X) || !aligned16(Q) || !aligned4(scales) || ldx % 8 != 0 || ldq % 16 != 0) return MLT_ERR_ALIGNMENT;
+    DeviceInfo dev;
+    const int rc = get_device(&dev);
+    if (rc != MLT_OK) return rc;
+    const QuantizeParams p = {static_cast<const __nv_bfloat16*>(X), static_cast<uint8_t*>(Q), scales, ldx, ldq, lds,
+                              static_cast<int>(M), static_cast<int>(K)};
+    return quantize_launch(p, block_rows, static_cast<cudaStream_t>(stream));
+}
+
+int mlt_gemm_f8(const void* A, const float* scale_a, const void* B, const float* scale_b, void* C, int64_t M, int64_t N,
+                int64_t K, int64_t lda, int64_t ldb, int64_t ldc, int64_t ldsa, int64_t ldsb, void* stream) {
+    if (M < 0 || N < 0 || K < 0) return MLT_ERR_INVALID_ARG;
+    if (M == 0 || N == 0) return MLT_OK;
+    if (!C || ldc < N) return MLT_ERR_INVALID_ARG;
+    if (K > 0 && (!A || !B || !scale_a || !scale_b || lda < K || ldb < K || ldsa < M || ldsb < (K + 127) / 128)) return MLT_ERR_INVALID_ARG;
+    if (M > INT32_MAX - 256 || N > INT32_MAX - 256 || K > INT32_MAX - 256) return MLT_ERR_UNSUPPORTED;
+    if (!aligned16(C) || ldc % 8 != 0) return MLT_ERR_ALIGNMENT;
+    if (K > 0 && (!aligned16(A) || !aligned16(B) || !aligned4(scale_a) || !aligned4(scale_b) || lda % 16 != 0 || ldb % 16 != 0))
+        return MLT_ERR_ALIGNMENT;
+    DeviceInfo dev;
+    int rc = get_device(&dev);
+    if (rc != MLT_OK) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (K == 0) {
+        const int blocks = static_cast<int>(std::min<int64_t>((M * N + 255) / 256, 4 * dev.sm_count));
+        gemm_zero_fill_kernel<<<blocks, 256, 0, st>>>(static_cast<__nv_bfloat16*>(C), ldc, static_cast<int>(M), static_cast<int>(N));
+        return cudaGetLastError() == cudaSuccess ? MLT_OK : MLT_ERR_CUDA;
+    }
+    const GemmF8Plan plan = gemm_f8_plan(M, N, K, dev.sm_count);
+    CUtensorMap ta, tb;
+    {
+        const uint64_t dims[2] = {static_cast<uint64_t>(K), static_cast<uint64_t>(M)};
+        const uint64_t strides[1] = {static_cast<uint64_t>(lda)};
+        const uint32_t box[2] = {kF8BK, static_cast<uint32_t>(plan.a_rows)};
+        rc = encode_bf16(&ta, A, 2, dims, strides, box, 3);
+        if (rc != MLT_OK) return rc;
+    }
+    {
+        const uint64_t dims[2] = {static_cast<uint64_t>(K), static_cast<uint64_t>(N)};
+        const uint64_t strides[1] = {static_cast<uint64_t>(ldb)};
+        const uint32_t box[2] = {kF8BK, static_cast<uint32_t>(plan.bn)};
+        rc = encode_bf16(&tb, B, 2, dims, strides, box, 3);
+        if (rc != MLT_OK) return rc;
+    }
+    const int64_t tiles_m = (M + 127) / 128, tiles_n = (N + plan.bn - 1) / plan.bn;
+    if (tiles_m * tiles_n * plan.cluster > INT32_MAX) return MLT_ERR_UNSUPPORTED;
+    GemmF8Params p;
+    p.C = static_cast<__nv_bfloat16*>(C);
+    p.sa = scale_a;
+    p.sb = scale_b;
+    p.ldc = ldc;
+    p.ldsa = ldsa;
+    p.ldsb = ldsb;
+    p.M = static_cast<int>(M);
+    p.N = static_cast<int>(N);
+    p.K = static_cast<int>(K);
+    p.tiles_m = static_cast<int>(tiles_m);
+    p.tiles_n = static_cast<int>(tiles_n);
+    p.group_m = 16;
+    p.kb_per_split = plan.kb_per_split;
+    p.a_rows = plan.a_rows;
+    p.stages = plan.stages;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(tiles_m * tiles_n * plan.cluster));
+    cfg.blockDim = dim3(kF8Threads);
+    cfg.stream = st;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = static_cast<unsigned>(plan.cluster);
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    cudaError_t e;
+    if (plan.bn == 64) {
+        cfg.dynamicSmemBytes = GemmF8Smem<64>::bytes(plan.a_rows, plan.stages);
+        e = cudaLaunchKernelEx(&cfg, gemm_f8_kernel<64, 3>, ta, tb, p);
+    } else {
+        cfg.dynamicSmemBytes = GemmF8Smem<128>::bytes(plan.a_rows, plan.stages);
+        e = cudaLaunchKernelEx(&cfg, gemm_f8_kernel<128, 1>, ta, tb, p);
+    }
+    return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? MLT_OK : MLT_ERR_CUDA;
+}
+
+}  // extern "C"
+
+namespace {
+int append_run(const void* Q, const void* K, const void* V, const float* cosv, const float* sinv, const int32_t* cu_tokens,
+               const int32_t* context_lens, const int32_t* block_table, void* Q_out, void* K_cache, void* V_cache, float* k_scale,
+               float* v_scale, int num_tokens, int num_seqs, int H, int H_kv, int D, int rotary_dim, int interleaved, int block_size,
+               int max_blocks_per_seq, int num_blocks, int max_position, int64_t ldq, int64_t ldk, int64_t ldv, int64_t ldqo, bool f8,
+               void* stream) {
+    if (num_tokens < 0 || num_seqs < 0 || H < 0 || H_kv < 0 || rotary_dim < 0 || max_blocks_per_seq < 0 || num_blocks < 0 || max_position < 0)
+        return MLT_ERR_INVALID_ARG;
+    if (num_tokens == 0 || num_seqs == 0) return MLT_OK;
+    if (!K || !V || !K_cache || !V_cache || !cu_tokens || !context_lens || !block_table || H_kv == 0) return MLT_ERR_INVALID_ARG;
+    if (f8 && (!k_scale || !v_scale)) return MLT_ERR_INVALID_ARG;
+    if (Q && (!Q_out || H == 0)) return MLT_ERR_INVALID_ARG;
+    if (D != 64 && D != 128) return MLT_ERR_UNSUPPORTED;
+    if (block_size != 8 && block_size != 16 && block_size != 32) return MLT_ERR_UNSUPPORTED;
+    if (rotary_dim > D || (rotary_dim > 0 && (!cosv || !sinv))) return MLT_ERR_INVALID_ARG;
+    if (rotary_dim % 16 != 0) return MLT_ERR_UNSUPPORTED;
+    const int64_t kv_width = static_cast<int64_t>(H_kv) * D, q_width = static_cast<int64_t>(H) * D;
+    if (ldk < kv_width || ldv < kv_width || (Q && (ldq < q_width || ldqo < q_width))) return MLT_ERR_INVALID_ARG;
+    if (!aligned16(K) || !aligned16(V) || !aligned16(K_cache) || !aligned16(V_cache) || ldk % 8 != 0 || ldv % 8 != 0) return MLT_ERR_ALIGNMENT;
+    if (Q && (!aligned16(Q) || !aligned16(Q_out) || ldq % 8 != 0 || ldqo % 8 != 0)) return MLT_ERR_ALIGNMENT;
+    if (rotary_dim > 0 && (!aligned16(cosv) || !aligned16(sinv))) return MLT_ERR_ALIGNMENT;
+    const int64_t tasks = 2ll * H_kv + (Q ? H : 0);
+    if (num_tokens / block_size + 2ll * num_seqs > INT32_MAX || tasks > 65535) return MLT_ERR_UNSUPPORTED;
+    DeviceInfo dev;
+    const int rc = get_device(&dev);
+    if (rc != MLT_OK) return rc;
+    AppendParams p;
+    p.Q = static_cast<const __nv_bfloat16*>(Q);
+    p.K = static_cast<const __nv_bfloat16*>(K);
+    p.V = static_cast<const __nv_bfloat16*>(V);
+    p.Qo = static_cast<__nv_bfloat16*>(Q_out);
+    p.cosv = cosv;
+    p.sinv = sinv;
+    p.cu = cu_tokens;
+    p.ctx = context_lens;
+    p.table = block_table;
+    p.Kc = K_cache;
+    p.Vc = V_cache;
+    p.ks = k_scale;
+    p.vs = v_scale;
+    p.ldq = ldq;
+    p.ldk = ldk;
+    p.ldv = ldv;
+    p.ldqo = ldqo;
+    p.T = num_tokens;
+    p.S = num_seqs;
+    p.H = H;
+    p.H_kv = H_kv;
+    p.R = rotary_dim;
+    p.max_blocks = max_blocks_per_seq;
+    p.num_blocks = num_blocks;
+    p.max_pos = max_position;
+    return append_launch(p, D, block_size, f8, interleaved != 0, static_cast<cudaStream_t>(stream));
+}
+}  // namespace
+
+extern "C" {
+
+int mlt_kv_append(const void* Q, const void* K, const void* V, const float* cos_table, const float* sin_table,
+                  const int32_t* cu_tokens, const int32_t* context_lens, const int32_t* block_table, void* Q_out, void* K_cache,
+                  void* V_cache, int num_tokens, int num_seqs, int H, int H_kv, int D, int rotary_dim, int interleaved,
+                  int block_size, int max_blocks_per_seq, int num_blocks, int max_position, int64_t ldq, int64_t ldk,
+                  int64_t ldv, int64_t ldqo, void* stream) {
+    return append_run(Q, K, V, cos_table, sin_table, cu_tokens, context_lens, block_table, Q_out, K_cache, V_cache, nullptr, nullptr,
+                      num_tokens, num_seqs, H, H_kv, D, rotary_dim, interleaved, block_size, max_blocks_per_seq, num_blocks,
+                      max_position, ldq, ldk, ldv, ldqo, false, stream);
+}
+
+int mlt_kv_append_f8(const void* Q, const void* K, const void* V, const float* cos_table, const float* sin_table,
+                     const int32_t* cu_tokens, const int32_t* context_lens, const int32_t* block_table, void* Q_out, void* K_cache,
+                     void* V_cache, float* k_scale, float* v_scale, int num_tokens, int num_seqs, int H, int H_kv, int D,
+                     int rotary_dim, int interleaved, int block_size, int max_blocks_per_seq, int num_blocks, int max_position,
+                     int64_t ldq, int64_t ldk, int64_t ldv, int64_t ldqo, void* stream) {
+    return append_run(Q, K, V, cos_table, sin_table, cu_tokens, context_lens, block_table, Q_out, K_cache, V_cache, k_scale, v_scale,
+                      num_tokens, num_seqs, H, H_kv, D, rotary_dim, interleaved, block_size, max_blocks_per_seq, num_blocks,
+                      max_position, ldq, ldk, ldv, ldqo, true, stream);
+}
+
+size_t mlt_paged_attn_f8_workspace_bytes(int num_seqs, int H, int H_kv, int D) {
+    if (num_seqs <= 0 || H <= 0 || H_kv <= 0 || D <= 0 || H % H_kv != 0) return 0;
+    return (static_cast<size_t>(num_seqs) * H_kv + kPagedF8MaxCtas) * paged_f8_slot_bytes(H / H_kv, D);
+}
+
+int mlt_paged_attn_decode_f8(const void* Q, const void* K_cache, const void* V_cache, const float* k_scale, const float* v_scale,
+                             const int32_t* block_table, const int32_t* seq_lens, void* O, float* LSE, int num_seqs, int H,
+                             int H_kv, int D, int block_size, int max_blocks_per_seq, int num_blocks, float scale,
+                             void* workspace, size_t workspace_bytes, void* stream) {
+    if (num_seqs < 0 || H < 0 || H_kv < 0 || max_blocks_per_seq < 0 || num_blocks < 0) return MLT_ERR_INVALID_ARG;
+    if (num_seqs == 0 || H == 0) return MLT_OK;
+    if (!Q || !K_cache || !V_cache || !k_scale || !v_scale || !block_table || !seq_lens || !O) return MLT_ERR_INVALID_ARG;
+    if (H_kv == 0 || H % H_kv != 0) return MLT_ERR_INVALID_ARG;
+    if (!(scale > 0.0f) || scale > 3.0e38f) return MLT_ERR_INVALID_ARG;
+    const int G = H / H_kv;
+    if (D != 64 && D != 128) return MLT_ERR_UNSUPPORTED;
+    if (G != 1 && G != 2 && G != 4 && G != 8) return MLT_ERR_UNSUPPORTED;
+    if (block_size != 8 && block_size != 16 && block_size != 32) return MLT_ERR_UNSUPPORTED;
+    if (static_cast<int64_t>(num_blocks) * H_kv > INT32_MAX || static_cast<int64_t>(num_seqs) * H > INT32_MAX) return MLT_ERR_UNSUPPORTED;
+    if (!aligned16(Q) || !aligned16(K_cache) || !aligned16(V_cache) || !aligned16(O) || (workspace && !aligned16(workspace)))
+        return MLT_ERR_ALIGNMENT;
+    DeviceInfo dev;
+    int rc = get_device(&dev);
+    if (rc != MLT_OK) return rc;
+    CUtensorMap tk, tv;
+    {
+        const uint64_t dims[3] = {static_cast<uint64_t>(D), static_cast<uint64_t>(block_size),
+                                  std::max<uint64_t>(1, static_cast<uint64_t>(num_blocks) * H_kv)};
+        const uint64_t strides[2] = {static_cast<uint64_t>(D), static_cast<uint64_t>(D) * block_size};
+        const uint32_t box[3] = {static_cast<uint32_t>(D), static_cast<uint32_t>(block_size), 1};
+        rc = encode_bf16(&tk, K_cache, 3, dims, strides, box, 3, D == 64);
+        if (rc != MLT_OK) return rc;
+        rc = encode_bf16(&tv, V_cache, 3, dims, strides, box, 3, D == 64);
+        if (rc != MLT_OK) return rc;
+    }
+    PagedF8Params p;
+    p.Q = static_cast<const __nv_bfloat16*>(Q);
+    p.ks = k_scale;
+    p.vs = v_scale;
+    p.block_table = block_table;
+    p.seq_lens = seq_lens;
+    p.O = static_cast<__nv_bfloat16*>(O);
+    p.LSE = LSE;
+    p.num_seqs = num_seqs;
+    p.H = H;
+    p.H_kv = H_kv;
+    p.max_blocks = max_blocks_per_seq;
+    p.num_blocks = num_blocks;
+    p.scale_log2e = scale * 1.4426950408889634f;
+    p.part_o = nullptr;
+    p.part_ml = nullptr;
+    p.ctas = 0;
+    const int64_t rows = static_cast<int64_t>(num_seqs) * H_kv;
+    if (workspace && num_seqs <= kPagedBalanceMaxSeqs) {
+        const int64_t slots = static_cast<int64_t>(workspace_bytes / paged_f8_slot_bytes(G, D));
+        const int64_t chunks = rows * ((static_cast<int64_t>(max_blocks_per_seq) * block_size + kPagedChunkTokens - 1) / kPagedChunkTokens);
+        const int64_t ctas = std::min<int64_t>({static_cast<int64_t>(kPagedF8CtasPerSm) * dev.sm_count, kPagedF8MaxCtas, chunks, slots - rows});
+        if (ctas > 1) {
+            p.ctas = static_cast<int>(ctas);
+            p.part_o = static_cast<float*>(workspace);
+            p.part_ml = reinterpret_cast<float2*>(p.part_o + static_cast<size_t>(rows + ctas) * G * D);
+        }
+    }
+    return D == 64 ? paged_f8_launch<64>(tk, tv, p, block_size, static_cast<cudaStream_t>(stream))
+                   : paged_f8_launch<128>(tk, tv, p, block_size, static_cast<cudaStream_t>(stream));
+}
+
+}  // extern "C"

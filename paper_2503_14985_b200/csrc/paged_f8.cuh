@@ -1,0 +1,577 @@
+// Paged-attention decode over an E4M3 cache with one FP32 scale per (cache block, KV head), for K and for V:
+//   O = softmax(scale * q . (ks K)) (vs V),  LSE in natural log.
+//
+// Bound by HBM: 2 * len * D bytes per (sequence, KV head), half of the BF16 cache's.  At the copy bandwidth an SM gets
+// about 23 cache elements per clock, too many for the FP32 pipe (convert, multiply, add for each query head), so both
+// products run on warp-level tensor-core MMAs (m16n8k16, FP16) for every group size, with the group's query heads as rows.
+// E4M3 to FP16 is exact (one conversion instruction per two elements).
+//   * Q is scaled by a power of two per row into FP16's range (its 8 significant bits fit), exact but for elements more
+//     than 2^28 below the row's largest.
+//   * K's scale multiplies the scores of its block's tokens.  A tile of 8 tokens lies in one block.
+//   * V's scale multiplies the probabilities before they become the FP16 operand, relative to the largest V scale the
+//     warp has met (v_ref, kept like a running maximum: the accumulators are rescaled when it grows).  Probabilities
+//     are held times 2^14, so that weights down to 2^-28 of the largest keep FP16's full precision.
+//   * Scores, maxima, sums and outputs are FP32; the sum takes the probabilities before their rounding to FP16.
+//
+// Data path: tensor copies (TMA) of whole (block, head) pieces into a two-deep ring of 32-token units per warp, swizzled so
+// that the fragment loads meet no bank conflict at D = 128 (a lane's 16 bytes of K cover 16 elements of one token: the
+// order of an MMA's summation index is free as long as both operands agree, as is the order of its output columns).
+//
+// Work split: the live chunks of 128 tokens of all (sequence, KV head) rows are numbered in row order and cut into equal
+// contiguous shares, one per CTA (the lengths are only known on the device: every CTA scans them).  A row inside one
+// share is finished by its CTA; otherwise each CTA that meets row r writes an unnormalised partial into slot
+// r + (its own index) -- strictly increasing along the line, so rows + CTAs slots are enough -- and a second kernel
+// combines them in ascending order.  Without scratch, or beyond 1024 sequences, one CTA works on each row.
+#pragma once
+
+#include "f8.cuh"
+#include "paged.cuh"
+
+namespace mlt {
+
+struct PagedF8Params {
+    const __nv_bfloat16* Q;  // [num_seqs, H, D]
+    const float *ks, *vs;    // [num_blocks, H_kv]
+    const int *block_table, *seq_lens;
+    __nv_bfloat16* O;        // [num_seqs, H, D]
+    float* LSE;              // [num_seqs, H] or null
+    float* part_o;           // [num_seqs * H_kv + ctas][G][D]
+    float2* part_ml;         // [num_seqs * H_kv + ctas][G] {m in log2 units, l}
+    int num_seqs, H, H_kv, max_blocks, num_blocks;
+    int ctas;                // CTAs of the balanced split; 0: one CTA per row
+    float scale_log2e;
+};
+
+constexpr int kPagedF8Unit = 32;   // tokens per warp and ring stage
+constexpr int kPagedF8CtasPerSm = 3;
+constexpr int kPagedF8MaxCtas = 1024;  // bound on the balanced split's CTAs that the workspace formula uses
+
+template <int D>
+constexpr int paged_f8_smem_bytes() {
+    return kPagedWarps * kPagedRing * 2 * kPagedF8Unit * D + 1024;
+}
+
+__device__ __forceinline__ void mma_f16_16816(float (&c)[4], uint32_t a0, uint32_t a2, uint32_t b0, uint32_t b1) {  // rows 8..15 of A are zero
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(0u), "r"(a2), "r"(0u), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+__device__ __forceinline__ int paged_f8_len(const PagedF8Params& p, int s, int bs) {  // cut at the table's end
+    return static_cast<int>(max(0ll, min(static_cast<long long>(p.seq_lens[s]), static_cast<long long>(p.max_blocks) * bs)));
+}
+__device__ __forceinline__ int paged_f8_chunks(const PagedF8Params& p, int s, int bs) {
+    return (paged_f8_len(p, s, bs) + kPagedChunkTokens - 1) / kPagedChunkTokens;
+}
+// chunks per CTA
+__device__ __forceinline__ long long paged_f8_quota(long long n, int ctas) { return max(1ll, (n + ctas - 1) / ctas); }
+
+template <int D, int G, int BS>
+__global__ void __launch_bounds__(kPagedThreads, kPagedF8CtasPerSm)
+paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const PagedF8Params p) {
+    pdl_launch_dependents();
+    static_assert(kPagedRing == 2, "the loop below keeps one unit in use and one in flight");
+    constexpr int U = kPagedF8Unit;
+    constexpr int PP = D / 64;       // 16-byte pieces of a token's K per lane
+    constexpr int NT = D / 8;        // column tiles of the output
+    constexpr int NB = U / BS;       // cache blocks per unit
+    constexpr int kUnitBytes = 2 * U * D;
+    __shared__ float2 sm_ml[kPagedWarps][G];
+    __shared__ int sm_pre[kPagedBalanceMaxSeqs + 1];
+    __shared__ int sm_red[kPagedWarps];
+    __shared__ uint64_t ring_bar[kPagedWarps][kPagedRing];
+    __shared__ uint32_t ring_abort;
+    extern __shared__ uint8_t ring_raw[];
+    uint8_t* ring_base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(ring_raw) + 1023) & ~uintptr_t(1023));
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int g = lane >> 2, tg = lane & 3;
+    uint8_t* my_ring = ring_base + warp * kPagedRing * kUnitBytes;
+    if (lane == 0) {
+#pragma unroll
+        for (int i = 0; i < kPagedRing; ++i) mbar_init(&ring_bar[warp][i], 1);
+        if (warp == 0) ring_abort = 0;
+        fence_mbar_init();
+        prefetch_tensormap(&tmap_k);
+        prefetch_tensormap(&tmap_v);
+    }
+
+    // ---- which segments (row, token range) this CTA works on ----
+    int seg_s, seg_kvh = 0, seg_tok_begin = 0, seg_tok_end = 0;
+    bool seg_whole = true;  // the row lies inside this CTA's share
+    long long bal_i = 0, bal_hi = 0, bal_q = 1;
+    if (p.ctas == 0) {
+        seg_s = blockIdx.x / p.H_kv;
+        seg_kvh = blockIdx.x % p.H_kv;
+        seg_tok_end = paged_f8_len(p, seg_s, BS);
+        __syncthreads();  // the ring barriers are initialised
+    } else {
+        const int S = p.num_seqs;
+        const int per = (S + kPagedThreads - 1) / kPagedThreads;
+        const int s_lo = min(S, static_cast<int>(threadIdx.x) * per), s_hi = min(S, s_lo + per);
+        int sum = 0;
+        for (int s2 = s_lo; s2 < s_hi; ++s2) sum += paged_f8_chunks(p, s2, BS);
+        int incl = sum;
+#pragma unroll
+        for (int w = 1; w < 32; w <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, incl, w);
+            if (lane >= w) incl += v;
+        }
+        if (lane == 31) sm_red[warp] = incl;
+        __syncthreads();  // also: the ring barriers are initialised
+        int before = incl - sum, total = 0;
+#pragma unroll
+        for (int w = 0; w < kPagedWarps; ++w) {
+            if (w < warp) before += sm_red[w];
+            total += sm_red[w];
+        }
+        if (threadIdx.x == 0) sm_pre[0] = 0;
+        for (int s2 = s_lo; s2 < s_hi; ++s2) {
+            before += paged_f8_chunks(p, s2, BS);
+            sm_pre[s2 + 1] = before;
+        }
+        __syncthreads();
+        const long long n = static_cast<long long>(total) * p.H_kv;
+        bal_q = paged_f8_quota(n, p.ctas);
+        bal_i = blockIdx.x * bal_q;
+        bal_hi = min(n, bal_i + bal_q);
+        if (bal_i >= n) return;
+        int lo = 0, hi = S;  // H_kv * pre[lo] <= bal_i < H_kv * pre[hi]
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (static_cast<long long>(sm_pre[mid]) * p.H_kv <= bal_i) lo = mid; else hi = mid;
+        }
+        seg_s = lo;
+    }
+    auto next_segment = [&]() -> bool {
+        if (bal_i >= bal_hi) return false;
+        while (static_cast<long long>(sm_pre[seg_s + 1]) * p.H_kv <= bal_i) ++seg_s;  // skips empty sequences too
+        const int n_s = sm_pre[seg_s + 1] - sm_pre[seg_s];
+        const long long r = bal_i - static_cast<long long>(sm_pre[seg_s]) * p.H_kv;
+        seg_kvh = static_cast<int>(r / n_s);
+        const int ch0 = static_cast<int>(r % n_s);
+        const int ch1 = static_cast<int>(min(static_cast<long long>(n_s), ch0 + (bal_hi - bal_i)));
+        seg_tok_begin = ch0 * kPagedChunkTokens;
+        seg_tok_end = min(paged_f8_len(p, seg_s, BS), ch1 * kPagedChunkTokens);
+        seg_whole = ch0 == 0 && ch1 == n_s;
+        bal_i += ch1 - ch0;
+        return true;
+    };
+    if (p.ctas != 0 && !next_segment()) return;
+
+    uint32_t kbase = 0;        // units this warp has been through (the ring stage follows it)
+    uint32_t ring_parity = 0;  // bit st: parity of the next completion of stage st's barrier
+    bool ok = true;
+    for (;;) {
+    // =============================== one segment ===============================
+    const int s = seg_s, kvh = seg_kvh, tok_begin = seg_tok_begin, tok_end = seg_tok_end;
+    const int head0 = kvh * G;
+
+    // Q as A fragments in FP16: lane (g, tg) holds elements tg * D / 4 .. of head g, scaled by 2^-qexp
+    uint32_t qa[PP][4][2];
+    float c_row;  // scores of row g in log2 units, before K's scale
+    {
+        uint4 v[2 * PP];
+#pragma unroll
+        for (int i = 0; i < 2 * PP; ++i) {
+            v[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (g < G) v[i] = *reinterpret_cast<const uint4*>(p.Q + (static_cast<int64_t>(s) * p.H + head0 + g) * D + tg * (D / 4) + i * 8);
+        }
+        float amax = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 2 * PP; ++i) {
+            float f[8];
+            bf16x8_to_f32(v[i], f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) amax = fmaxf(amax, abs_if_finite(f[e]));
+        }
+        amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+        amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+        const int qexp = max(-100, static_cast<int>(__float_as_uint(amax) >> 23) - 127 - 14);  // the largest element becomes 2^14 .. 2^15
+        const float down = pow2f(-qexp);
+        c_row = p.scale_log2e * pow2f(qexp);
+#pragma unroll
+        for (int i = 0; i < 2 * PP; ++i) {
+            float f[8];
+            bf16x8_to_f32(v[i], f);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) qa[i >> 1][(i & 1) * 2 + (e >> 1)][e & 1] = pack_f16x2(f[2 * e] * down, f[2 * e + 1] * down);
+        }
+    }
+    float oacc[NT][4];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) oacc[nt][i] = 0.0f;
+    float m_run = -INFINITY, l_part = 0.0f;  // head g: running max (log2 units), this lane's share of the sum (times 2^14)
+    float v_ref = 0.0f;                      // the accumulators hold sums of p * 2^14 * vs / v_ref * V
+
+    const int* table = p.block_table + static_cast<int64_t>(s) * p.max_blocks;
+    struct Meta {  // of a unit whose copies are under way: which of its tokens count, and its blocks' scales
+        uint32_t vis;
+        float ks[NB], vs[NB];
+    };
+    // Unit k of this warp starts at token first + k * kStep.  The table entries and scales of 32 units at a time are
+    // read by one lane each and handed out by shuffles.
+    constexpr int kStep = kPagedWarps * U;
+    const int first = tok_begin + warp * U;
+    const int n_units = first < tok_end ? (tok_end - first + kStep - 1) / kStep : 0;
+    int tab[NB];
+    float tks[NB], tvs[NB];
+    int tab_base = -64;
+    auto issue_unit = [&](Meta& meta, int stage, int k) {
+        const int u0 = first + k * kStep;
+        if (k >= tab_base + 32) {
+            tab_base = k;
+            const int n = k + lane < n_units ? tok_end - (first + (k + lane) * kStep) : 0;  // tokens of unit k + lane and beyond
+#pragma unroll
+            for (int i = 0; i < NB; ++i) tab[i] = i * BS < n ? table[(first + (k + lane) * kStep) / BS + i] : 0;
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+                const bool there = i * BS < n && tab[i] >= 0 && tab[i] < p.num_blocks;
+                const int64_t at = static_cast<int64_t>(tab[i]) * p.H_kv + kvh;
+                tks[i] = there ? __ldg(p.ks + at) : 0.0f;
+                tvs[i] = there ? __ldg(p.vs + at) : 0.0f;
+            }
+        }
+        const int left = tok_end - u0;
+        meta.vis = left >= U ? 0xFFFFFFFFu : (1u << left) - 1u;
+        int phys[NB], blocks = 0;
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            phys[i] = __shfl_sync(0xffffffffu, tab[i], k - tab_base);
+            if (i * BS >= left) {
+                phys[i] = -1;
+            } else if (phys[i] < 0 || phys[i] >= p.num_blocks) {  // never dereference a bad table entry: report, leave its tokens out
+                if (lane == 0 && atomicCAS(&g_status[0], 0u, kStatusBadBlock) == 0u) {
+                    g_status[1] = static_cast<unsigned int>(u0 / BS + i);
+                    g_status[2] = static_cast<unsigned int>(s);
+                    g_status[3] = static_cast<unsigned int>(phys[i]);
+                }
+                phys[i] = -1;
+                meta.vis &= ~((BS == 32 ? 0xFFFFFFFFu : (1u << (BS & 31)) - 1u) << (i * BS));
+            } else {
+                ++blocks;
+            }
+        }
+        if (blocks > 0) {
+            __syncwarp();  // every lane is done reading the stage's previous contents
+            uint64_t* bar = &ring_bar[warp][stage];
+            if (lane == 0) mbar_arrive_expect_tx(bar, 2u * blocks * BS * D);
+            __syncwarp();
+            uint8_t* dst = my_ring + stage * kUnitBytes;
+#pragma unroll
+            for (int i = 0; i < NB; ++i)
+                if (phys[i] >= 0 && (lane >> 1) == i)
+                    tma_load_3d(dst + (lane & 1) * (U * D) + i * BS * D, (lane & 1) ? &tmap_v : &tmap_k, bar, 0, 0, phys[i] * p.H_kv + kvh);
+            __syncwarp();
+        }
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            meta.ks[i] = __shfl_sync(0xffffffffu, tks[i], k - tab_base);
+            meta.vs[i] = __shfl_sync(0xffffffffu, tvs[i], k - tab_base);
+        }
+    };
+    // byte offset of 16-byte piece c of token row r in a swizzled [tokens][D] tile
+    auto at16 = [](int r, int c) { return D == 128 ? r * 128 + ((c ^ (r & 7)) << 4) : r * 64 + ((c ^ ((r >> 1) & 3)) << 4); };
+    auto compute_unit = [&](const Meta& meta, int stage) {
+        const uint8_t* ku = my_ring + stage * kUnitBytes;
+        const uint8_t* vu = ku + U * D;
+        // ---- scores of head g for tokens 8 e + 2 tg, + 1 ----
+        float x[U / 8][2];
+#pragma unroll
+        for (int e = 0; e < U / 8; ++e) {
+            float sc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int pp = 0; pp < PP; ++pp) {
+                const uint4 w = *reinterpret_cast<const uint4*>(ku + at16(8 * e + g, PP * tg + pp));
+                const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t b0, b1;
+                    f16x2_from_f8x4(ww[j], b0, b1);
+                    mma_f16_16816(sc, qa[pp][j][0], qa[pp][j][1], b0, b1);
+                }
+            }
+            const float f = c_row * meta.ks[8 * e / BS];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) x[e][i] = (meta.vis >> (8 * e + 2 * tg + i)) & 1u ? sc[i] * f : -INFINITY;
+        }
+        float mb = fmaxf(x[0][0], x[0][1]);
+#pragma unroll
+        for (int e = 1; e < U / 8; ++e) mb = fmaxf(mb, fmaxf(x[e][0], x[e][1]));
+        mb = fmaxf(mb, __shfl_xor_sync(0xffffffffu, mb, 1));
+        mb = fmaxf(mb, __shfl_xor_sync(0xffffffffu, mb, 2));
+        const float mn = fmaxf(m_run, mb);
+        const float ref = mn == -INFINITY ? 0.0f : mn;
+        const float alpha = fast_exp2(m_run - ref);  // 0 while m_run = -inf
+        float vm = v_ref;
+#pragma unroll
+        for (int i = 0; i < NB; ++i) vm = fmaxf(vm, fabsf(meta.vs[i]));
+        if (__any_sync(0xffffffffu, mn != m_run) || vm != v_ref) {
+            const float f = vm > v_ref ? alpha * (v_ref / vm) : alpha;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                oacc[nt][0] *= f;
+                oacc[nt][1] *= f;
+            }
+            l_part *= alpha;
+            m_run = mn;
+            v_ref = vm;
+        }
+        float vw[NB];
+#pragma unroll
+        for (int i = 0; i < NB; ++i) vw[i] = v_ref > 0.0f ? meta.vs[i] / v_ref : 0.0f;
+        uint32_t pa[U / 8];
+#pragma unroll
+        for (int e = 0; e < U / 8; ++e) {
+            const float p0 = fast_exp2(x[e][0] - ref + 14.0f), p1 = fast_exp2(x[e][1] - ref + 14.0f);
+            l_part += p0 + p1;
+            const float w = vw[8 * e / BS];
+            pa[e] = pack_f16x2(p0 * w, p1 * w);
+        }
+        // ---- O += P V: column n = g of tile nt is element g * NT + nt of D ----
+#pragma unroll
+        for (int h = 0; h < U / 16; ++h) {
+            uint32_t w[4][NT / 4];  // tokens 16 h + {2 tg, 2 tg + 1, 2 tg + 8, 2 tg + 9}
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int t = 16 * h + 2 * tg + (i & 1) + (i >> 1) * 8;
+                if constexpr (D == 128) {
+                    const uint4 q = *reinterpret_cast<const uint4*>(vu + at16(t, g));
+                    w[i][0] = q.x; w[i][1] = q.y; w[i][2] = q.z; w[i][3] = q.w;
+                } else {
+                    const uint2 q = *reinterpret_cast<const uint2*>(vu + at16(t, g >> 1) + (g & 1) * 8);
+                    w[i][0] = q.x; w[i][1] = q.y;
+                }
+                if (meta.vis != 0xFFFFFFFFu && !((meta.vis >> t) & 1u)) {  // whatever lies there, weight 0 must not meet a NaN
+#pragma unroll
+                    for (int j = 0; j < NT / 4; ++j) w[i][j] = 0u;
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < NT / 4; ++j) {
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {  // elements 4 j + 2 q, + 1 of two tokens each
+                    const uint32_t sel = q ? 0x7362u : 0x5140u;
+                    uint32_t a0, a1, b0, b1;
+                    f16x2_from_f8x4(__byte_perm(w[0][j], w[1][j], sel), a0, a1);
+                    f16x2_from_f8x4(__byte_perm(w[2][j], w[3][j], sel), b0, b1);
+                    mma_f16_16816(oacc[4 * j + 2 * q], pa[2 * h], pa[2 * h + 1], a0, b0);
+                    mma_f16_16816(oacc[4 * j + 2 * q + 1], pa[2 * h], pa[2 * h + 1], a1, b1);
+                }
+            }
+        }
+    };
+    Meta cur, next;
+    cur.vis = next.vis = 0;
+    if (n_units > 0) issue_unit(cur, kbase & 1, 0);
+    for (int k = 0; k < n_units && ok; ++k) {
+        const uint32_t st = (kbase + k) & 1;
+        if (k + 1 < n_units) issue_unit(next, st ^ 1, k + 1);
+        if (cur.vis != 0) {  // (a unit all of whose blocks are bad has no copies and does not use its stage)
+            ok = __all_sync(0xffffffffu, mbar_wait(&ring_bar[warp][st], (ring_parity >> st) & 1, &ring_abort, 0x600 + warp)) != 0;
+            if (!ok) break;
+            ring_parity ^= 1u << st;
+            compute_unit(cur, st);
+        }
+        cur = next;
+    }
+    kbase += n_units;
+
+    // ---- the warps' results meet in shared memory, where the ring was (all copies have landed and been read) ----
+    __syncthreads();
+    float (*sm_o)[G][D] = reinterpret_cast<float (*)[G][D]>(ring_base);
+    static_assert(sizeof(float) * kPagedWarps * G * D <= kPagedWarps * kPagedRing * kUnitBytes, "partials fit the ring");
+    l_part += __shfl_xor_sync(0xffffffffu, l_part, 1);
+    l_part += __shfl_xor_sync(0xffffffffu, l_part, 2);
+    if (g < G) {
+        const float unit = v_ref * (1.0f / 16384.0f);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            sm_o[warp][g][(2 * tg) * NT + nt] = oacc[nt][0] * unit;
+            sm_o[warp][g][(2 * tg + 1) * NT + nt] = oacc[nt][1] * unit;
+        }
+        if (tg == 0) sm_ml[warp][g] = make_float2(m_run, l_part * (1.0f / 16384.0f));
+    }
+    __syncthreads();
+    for (int idx = threadIdx.x; idx < G * D; idx += kPagedThreads) {
+        const int gg = idx / D, d = idx % D;
+        float mt = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kPagedWarps; ++w) mt = fmaxf(mt, sm_ml[w][gg].x);
+        float lt = 0.0f, ot = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kPagedWarps; ++w) {
+            const float2 ml = sm_ml[w][gg];
+            const float sw = (ml.x == -INFINITY) ? 0.0f : fast_exp2(ml.x - mt);
+            lt += ml.y * sw;
+            ot += sm_o[w][gg][d] * sw;
+        }
+        if (seg_whole) {
+            const int64_t row = static_cast<int64_t>(s) * p.H + head0 + gg;
+            p.O[row * D + d] = __float2bfloat16(lt == 0.0f ? 0.0f : ot / lt);
+            if (d == 0 && p.LSE) p.LSE[row] = lt == 0.0f ? -INFINITY : (mt + log2f(lt)) * 0.6931471805599453f;
+        } else {
+            const int64_t slot = (static_cast<int64_t>(s) * p.H_kv + kvh + blockIdx.x) * G + gg;
+            p.part_o[slot * D + d] = ot;
+            if (d == 0) p.part_ml[slot] = make_float2(mt, lt);
+        }
+    }
+    if (p.ctas == 0 || !ok) break;
+    fence_proxy_async_smem();
+    __syncthreads();  // the results have left shared memory: copies may fill the ring again
+    if (!next_segment()) break;
+    }  // segments
+}
+
+// Rows that several CTAs worked on: sum of their partials, rescaled to the common maximum.  One CTA per (sequence, head),
+// blockDim.x / D groups of threads that take every blockDim.x / D-th partial.  Also writes the rows of empty sequences.
+constexpr int kPagedF8CombineBatch = 512;  // partials whose weights are in shared memory at a time
+template <int D, int BS>
+__global__ void paged_f8_combine_kernel(const PagedF8Params p) {
+    __shared__ float sm_w[kPagedF8CombineBatch];
+    __shared__ float sm_o[1024];
+    __shared__ int sm_i[2][32];
+    __shared__ float sm_f[2][32];
+    const int G = p.H / p.H_kv;
+    const int s = blockIdx.x / p.H, h = blockIdx.x % p.H, kvh = h / G, gg = h % G;
+    const int tid = threadIdx.x, lane = tid & 31, warps = blockDim.x >> 5;
+    int below = 0, total = 0;
+    for (int s2 = tid; s2 < p.num_seqs; s2 += blockDim.x) {
+        const int c = paged_f8_chunks(p, s2, BS);
+        total += c;
+        if (s2 < s) below += c;
+    }
+#pragma unroll
+    for (int w = 16; w > 0; w >>= 1) {
+        below += __shfl_xor_sync(0xffffffffu, below, w);
+        total += __shfl_xor_sync(0xffffffffu, total, w);
+    }
+    if (lane == 0) { sm_i[0][tid >> 5] = below; sm_i[1][tid >> 5] = total; }
+    __syncthreads();
+    below = total = 0;
+    for (int w = 0; w < warps; ++w) { below += sm_i[0][w]; total += sm_i[1][w]; }
+    const int n_s = paged_f8_chunks(p, s, BS);
+    const int64_t row = static_cast<int64_t>(s) * p.H + h;
+    cudaGridDependencySynchronize();  // (what was read so far are inputs)
+    if (n_s == 0) {  // nothing to see: O = 0, LSE = -inf
+        if (tid < D) p.O[row * D + tid] = __float2bfloat16(0.0f);
+        if (tid == 0 && p.LSE) p.LSE[row] = -INFINITY;
+        return;
+    }
+    const long long q = paged_f8_quota(static_cast<long long>(total) * p.H_kv, p.ctas);
+    const long long start = static_cast<long long>(below) * p.H_kv + static_cast<long long>(kvh) * n_s;
+    const int c0 = static_cast<int>(start / q), used = static_cast<int>((start + n_s - 1) / q) - c0 + 1;
+    if (used == 1) return;  // one CTA had the whole row and finished it
+    const int64_t slot0 = static_cast<int64_t>(s) * p.H_kv + kvh + c0;
+    const float2* ml = p.part_ml + slot0 * G + gg;
+    const float* po = p.part_o + (slot0 * G + gg) * D;
+    float mt = -INFINITY;
+    for (int i = tid; i < used; i += blockDim.x) mt = fmaxf(mt, ml[static_cast<int64_t>(i) * G].x);
+#pragma unroll
+    for (int w = 16; w > 0; w >>= 1) mt = fmaxf(mt, __shfl_xor_sync(0xffffffffu, mt, w));
+    if (lane == 0) sm_f[0][tid >> 5] = mt;
+    __syncthreads();
+    mt = -INFINITY;
+    for (int w = 0; w < warps; ++w) mt = fmaxf(mt, sm_f[0][w]);
+    const int d = tid % D, grp = tid / D, groups = blockDim.x / D;
+    float ot = 0.0f, lt = 0.0f;
+    for (int base = 0; base < used; base += kPagedF8CombineBatch) {
+        const int n = min(kPagedF8CombineBatch, used - base);
+        __syncthreads();
+        for (int i = tid; i < n; i += blockDim.x) {
+            const float2 v = ml[static_cast<int64_t>(base + i) * G];
+            const float w = v.x == -INFINITY ? 0.0f : fast_exp2(v.x - mt);
+            sm_w[i] = w;
+            lt += v.y * w;
+        }
+        __syncthreads();
+        const float* src = po + static_cast<int64_t>(base) * G * D + d;
+        int i = grp;
+        for (; i + 3 * groups < n; i += 4 * groups) {
+            float v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) v[u] = src[static_cast<int64_t>(i + u * groups) * G * D];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) ot = fmaf(v[u], sm_w[i + u * groups], ot);
+        }
+        for (; i < n; i += groups) ot = fmaf(src[static_cast<int64_t>(i) * G * D], sm_w[i], ot);
+    }
+#pragma unroll
+    for (int w = 16; w > 0; w >>= 1) lt += __shfl_xor_sync(0xffffffffu, lt, w);
+    if (lane == 0) sm_f[1][tid >> 5] = lt;
+    sm_o[tid] = ot;
+    __syncthreads();
+    if (tid < D) {
+        lt = 0.0f;
+        for (int w = 0; w < warps; ++w) lt += sm_f[1][w];
+        ot = 0.0f;
+        for (int k = 0; k < groups; ++k) ot += sm_o[k * D + tid];
+        p.O[row * D + tid] = __float2bfloat16(lt == 0.0f ? 0.0f : ot / lt);
+        if (tid == 0 && p.LSE) p.LSE[row] = lt == 0.0f ? -INFINITY : (mt + log2f(lt)) * 0.6931471805599453f;
+    }
+}
+
+inline size_t paged_f8_slot_bytes(int G, int D) { return static_cast<size_t>(G) * (static_cast<size_t>(D) * 4 + 8); }
+
+template <int D, int G, int BS>
+int paged_f8_launch_one(const CUtensorMap& tk, const CUtensorMap& tv, const PagedF8Params& p, cudaStream_t st) {
+    const int64_t grid = p.ctas ? p.ctas : static_cast<int64_t>(p.num_seqs) * p.H_kv;
+    if (grid > INT32_MAX || static_cast<int64_t>(p.num_seqs) * p.H > INT32_MAX) return 2;
+    paged_f8_decode_kernel<D, G, BS><<<static_cast<unsigned>(grid), kPagedThreads, paged_f8_smem_bytes<D>(), st>>>(tk, tv, p);
+    if (cudaGetLastError() != cudaSuccess) return 4;
+    if (p.ctas == 0) return 0;
+    const int64_t rows = static_cast<int64_t>(p.num_seqs) * p.H_kv;
+    int groups = 1;  // about four partials per thread where a row meets many CTAs
+    while (groups * D < 1024 && rows * groups * 4 < p.ctas) groups *= 2;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(p.num_seqs * p.H));
+    cfg.blockDim = dim3(static_cast<unsigned>(groups * D));
+    cfg.stream = st;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, paged_f8_combine_kernel<D, BS>, p) == cudaSuccess ? 0 : 4;
+}
+template <int D, int G>
+int paged_f8_launch_bs(const CUtensorMap& tk, const CUtensorMap& tv, const PagedF8Params& p, int block_size, cudaStream_t st) {
+    switch (block_size) {
+        case 8: return paged_f8_launch_one<D, G, 8>(tk, tv, p, st);
+        case 16: return paged_f8_launch_one<D, G, 16>(tk, tv, p, st);
+        case 32: return paged_f8_launch_one<D, G, 32>(tk, tv, p, st);
+        default: return 2;
+    }
+}
+template <int D>
+int paged_f8_launch(const CUtensorMap& tk, const CUtensorMap& tv, const PagedF8Params& p, int block_size, cudaStream_t st) {
+    switch (p.H / p.H_kv) {
+        case 1: return paged_f8_launch_bs<D, 1>(tk, tv, p, block_size, st);
+        case 2: return paged_f8_launch_bs<D, 2>(tk, tv, p, block_size, st);
+        case 4: return paged_f8_launch_bs<D, 4>(tk, tv, p, block_size, st);
+        case 8: return paged_f8_launch_bs<D, 8>(tk, tv, p, block_size, st);
+        default: return 2;
+    }
+}
+
+// Once per device: the ring is larger than the default shared-memory limit.
+template <int D, int G>
+bool paged_f8_configure_one() {
+    const int bytes = paged_f8_smem_bytes<D>();
+    return cudaFuncSetAttribute(paged_f8_decode_kernel<D, G, 8>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess &&
+           cudaFuncSetAttribute(paged_f8_decode_kernel<D, G, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess &&
+           cudaFuncSetAttribute(paged_f8_decode_kernel<D, G, 32>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess;
+}
+inline bool paged_f8_configure() {
+    return paged_f8_configure_one<64, 1>() && paged_f8_configure_one<64, 2>() && paged_f8_configure_one<64, 4>() && paged_f8_configure_one<64, 8>() &&
+           paged_f8_configure_one<128, 1>() && paged_f8_configure_one<128, 2>() && paged_f8_configure_one<128, 4>() && paged_f8_configure_one<128, 8>();
+}
+
+}  // namespace mlt
