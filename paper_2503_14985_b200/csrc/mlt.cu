@@ -101,7 +101,8 @@ int get_device(DeviceInfo* out) {
             d.cluster_slots[i] = clusters * S;
         }
         if (paged_configure() != 0 || !paged_f8_configure()) return MLT_ERR_CUDA;
-        if (set_smem(gemm_f8_kernel<64, 3>, kGemmF8NarrowSmem) != MLT_OK || set_smem(gemm_f8_kernel<128, 1>, kGemmF8WideSmem) != MLT_OK)
+        if (set_smem(gemm_f8_kernel<64, 3>, kGemmF8NarrowSmem) != MLT_OK || set_smem(gemm_f8_kernel<128, 1>, kGemmF8WideSmem) != MLT_OK ||
+            set_smem(gemm_f8_big_kernel<true>, GemmF8BigSmem<true>::kTotal) != MLT_OK || set_smem(gemm_f8_big_kernel<false>, GemmF8BigSmem<false>::kTotal) != MLT_OK)
             return MLT_ERR_CUDA;
         const int mha_rc = mha_configure();
         if (mha_rc == 1) return MLT_ERR_CUDA;
@@ -853,7 +854,8 @@ inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3
 
 // Launch plan of the scaled GEMM.
 struct GemmF8Plan {
-    int bn;       // tile width
+    int big;      // 2: CTA pairs on 256 x 256 tiles, 1: 128 x 256 tiles, 0: the kernel for smaller problems, with
+    int bn;       // its tile width
     int cluster;  // CTAs per tile that cut K
     int kb_per_split;
     int a_rows, stages;
@@ -862,6 +864,10 @@ struct GemmF8Plan {
 GemmF8Plan gemm_f8_plan(int64_t M, int64_t N, int64_t K, int sm_count) {
     const int num_kb = static_cast<int>((K + kF8BK - 1) / kF8BK);
     GemmF8Plan plan;
+    plan.big = 0;
+    if (M > 128 && N >= 128) plan.big = M > 1024 ? 2 : 1;
+    if (debug_env().f8_bn == 1 || debug_env().f8_bn == 2) plan.big = debug_env().f8_bn;
+    if (debug_env().f8_bn >= 64) plan.big = 0;
     plan.bn = M <= 128 ? 64 : 128;
     if (debug_env().f8_bn == 64 || debug_env().f8_bn == 128) plan.bn = debug_env().f8_bn;
     plan.a_rows = static_cast<int>(std::min<int64_t>(128, (M + 7) / 8 * 8));
@@ -923,23 +929,24 @@ int mlt_gemm_f8(const void* A, const float* scale_a, const void* B, const float*
         return cudaGetLastError() == cudaSuccess ? MLT_OK : MLT_ERR_CUDA;
     }
     const GemmF8Plan plan = gemm_f8_plan(M, N, K, dev.sm_count);
+    const int bm = plan.big == 2 ? 256 : 128, bn = plan.big ? 256 : plan.bn;
     CUtensorMap ta, tb;
     {
         const uint64_t dims[2] = {static_cast<uint64_t>(K), static_cast<uint64_t>(M)};
         const uint64_t strides[1] = {static_cast<uint64_t>(lda)};
-        const uint32_t box[2] = {kF8BK, static_cast<uint32_t>(plan.a_rows)};
+        const uint32_t box[2] = {kF8BK, static_cast<uint32_t>(plan.big ? 128 : plan.a_rows)};
         rc = encode_bf16(&ta, A, 2, dims, strides, box, 3);
         if (rc != MLT_OK) return rc;
     }
     {
         const uint64_t dims[2] = {static_cast<uint64_t>(K), static_cast<uint64_t>(N)};
         const uint64_t strides[1] = {static_cast<uint64_t>(ldb)};
-        const uint32_t box[2] = {kF8BK, static_cast<uint32_t>(plan.bn)};
+        const uint32_t box[2] = {kF8BK, static_cast<uint32_t>(plan.big ? 128 : plan.bn)};
         rc = encode_bf16(&tb, B, 2, dims, strides, box, 3);
         if (rc != MLT_OK) return rc;
     }
-    const int64_t tiles_m = (M + 127) / 128, tiles_n = (N + plan.bn - 1) / plan.bn;
-    if (tiles_m * tiles_n * plan.cluster > INT32_MAX) return MLT_ERR_UNSUPPORTED;
+    const int64_t tiles_m = (M + bm - 1) / bm, tiles_n = (N + bn - 1) / bn;
+    if (tiles_m * tiles_n * 8 > INT32_MAX) return MLT_ERR_UNSUPPORTED;
     GemmF8Params p;
     p.C = static_cast<__nv_bfloat16*>(C);
     p.sa = scale_a;
@@ -956,6 +963,36 @@ int mlt_gemm_f8(const void* A, const float* scale_a, const void* B, const float*
     p.kb_per_split = plan.kb_per_split;
     p.a_rows = plan.a_rows;
     p.stages = plan.stages;
+    if (plan.big) {
+        CUtensorMap tc;
+        const uint64_t dims[2] = {static_cast<uint64_t>(N) & ~7ull, static_cast<uint64_t>(M)};  // TMA stores work in 16-byte units
+        const uint64_t strides[1] = {static_cast<uint64_t>(ldc) * 2};
+        const uint32_t box[2] = {64, 32};
+        rc = encode_bf16(&tc, C, 2, dims, strides, box);
+        if (rc != MLT_OK) return rc;
+        p.group_m = tiles_n >= 32 && plan.big == 2 ? 16 : 8;
+        const int tiles = static_cast<int>(tiles_m * tiles_n);
+        cudaLaunchConfig_t big = {};
+        big.blockDim = dim3(kF8BigThreads);
+        big.stream = st;
+        cudaLaunchAttribute pair;
+        pair.id = cudaLaunchAttributeClusterDimension;
+        pair.val.clusterDim.x = plan.big;
+        pair.val.clusterDim.y = pair.val.clusterDim.z = 1;
+        big.attrs = &pair;
+        big.numAttrs = 1;
+        cudaError_t e;
+        if (plan.big == 2) {
+            big.gridDim = dim3(2 * std::min(tiles, dev.sm_count / 2));
+            big.dynamicSmemBytes = GemmF8BigSmem<true>::kTotal;
+            e = cudaLaunchKernelEx(&big, gemm_f8_big_kernel<true>, ta, tb, tc, p);
+        } else {
+            big.gridDim = dim3(std::min(tiles, dev.sm_count));
+            big.dynamicSmemBytes = GemmF8BigSmem<false>::kTotal;
+            e = cudaLaunchKernelEx(&big, gemm_f8_big_kernel<false>, ta, tb, tc, p);
+        }
+        return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? MLT_OK : MLT_ERR_CUDA;
+    }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(tiles_m * tiles_n * plan.cluster));
     cfg.blockDim = dim3(kF8Threads);
