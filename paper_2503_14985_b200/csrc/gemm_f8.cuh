@@ -9,9 +9,12 @@
 //
 //   warp 0      TMA producer: 128 bytes of K per stage for the tile's rows of A and of B (128-byte swizzle)
 //   warp 1      UMMA issuer, owner of the tensor-memory allocation
-//   warps 2..   promotion and epilogue
-// gemm_f8_big_kernel (256 columns per tile, persistent) for problems with enough tiles, gemm_f8_kernel otherwise.
+//   warps 4-11  promotion and epilogue
+// gemm_f8_big_kernel (256 columns per tile, persistent) for problems with enough tiles, gemm_f8_split_kernel otherwise.
 #pragma once
+
+#include <algorithm>
+#include <type_traits>
 
 #include "f8.cuh"
 #include "gemm.cuh"
@@ -19,6 +22,12 @@
 namespace mlt {
 
 constexpr int kF8BK = 128;  // elements (= bytes) of K per stage, and per scale
+// Twelve warps: producer, issuer, two that only hand their registers over, eight promotion warps (warps 4 .. 11).  The 128
+// sums and the 32 words on their way do not fit the 168 registers a thread starts with, and a spilled word costs an L2 access
+// (shared memory leaves no L1): with setmaxnreg the promotion warps take 208 and the others 88 of the launch's registers.
+constexpr int kF8Threads = 384;
+constexpr int kF8PromoteRegs = 208, kF8OtherRegs = 88, kF8LaunchRegs = 168;
+static_assert(8 * kF8PromoteRegs + 4 * kF8OtherRegs <= 12 * kF8LaunchRegs, "setmaxnreg budget exceeds the launch allocation");
 
 struct GemmF8Params {
     __nv_bfloat16* C;
@@ -26,234 +35,282 @@ struct GemmF8Params {
     int64_t ldc, ldsa, ldsb;
     int M, N, K;
     int tiles_m, tiles_n, group_m;
-    int kb_per_split;  // K blocks per CTA of a cluster
-    int a_rows;        // rows of A per stage (a multiple of 8; fewer than 128 when M is smaller)
+    // gemm_f8_split_kernel
+    int bn, bufs;  // tile width (a multiple of 16), accumulators in tensor memory (2 .. 4, bufs * bn <= 512)
+    int a_rows;    // rows of A per stage (a multiple of 8; fewer than 128 when M is smaller)
     int stages;
 };
 
-// ---------------------------------------------------------------------------------------------------------
-// 128 x BN tiles, K cut over the S CTAs of a cluster (S = 1: none), one tile per cluster.  The CTAs' FP32 tiles are
-// summed through distributed shared memory in ascending slice order (deterministic).
-// ---------------------------------------------------------------------------------------------------------
+// Scales travel through a ring in shared memory, four K blocks to a slot, filled by a warp of its own with 4-byte asynchronous
+// copies.  (Not by the producer: an arrival waits for the copies its thread has in flight.)
 constexpr int kF8MaxStages = 16;
-constexpr int kF8Threads = 192;
-template <int BN>
-struct GemmF8Smem {
-    static constexpr int kBBytes = BN * kF8BK;
-    static constexpr int kBarrierBytes = 512;
-    static constexpr int kPartPitch = BN + 4;  // FP32 words per row of the tile summed over the cluster
-    // A stages | B stages | barriers; the A descriptor always spans 128 rows, of which the first a_rows are loaded: the
-    // span may run on into whatever follows (rows that are never stored), so at least 16 KB follow the last A stage.
-    static constexpr int bytes(int a_rows, int stages) { return stages * (a_rows * kF8BK + kBBytes) + kBarrierBytes + 1024; }
+constexpr int kF8ScaleSlots = 4;
+struct GemmF8Scales {
+    float row[4][128];
+    float col[4][4];
 };
-
-constexpr int kGemmF8NarrowSmem = 75 * 1024;  // per CTA of the 64-wide kernel (three on an SM)
-constexpr int kGemmF8WideSmem = 200 * 1024;   // per CTA of the 128-wide kernel (one on an SM)
-
-// A load that stays where it is written (a prefetch that the compiler would move down to its use); 0 where `there` is false.
-__device__ __forceinline__ float ld_f32_if(const float* p, bool there) {
-    float v;
-    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\tmov.f32 %0, 0f00000000;\n\t@q ld.global.nc.f32 %0, [%1];\n\t}"
-                 : "=f"(v)
-                 : "l"(p), "r"(static_cast<int>(there)));
-    return v;
+__device__ __forceinline__ void cp_async_f32(float* smem_dst, const float* src, bool there) {  // 0 where `there` is false
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(smem_dst)), "l"(src), "r"(there ? 4 : 0) : "memory");
 }
-
-// One row's 32 consecutive results to BF16 C; a ragged right edge is stored element by element.
-__device__ __forceinline__ void gemm_f8_store32(__nv_bfloat16* crow, int col0, int N, const float* v) {
+__device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {  // arrives once this thread's copies so far have landed
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+// The scale warp's part for one tile: K blocks kb0 .. kb1 - 1, `sa` at the tile's first row, sb: this lane's column scale
+// (lanes 0 .. 3).  `slot` and `phase` run on from tile to tile.
+__device__ __forceinline__ bool gemm_f8_load_scales(GemmF8Scales* ring, uint64_t* full, uint64_t* empty, int& slot, uint32_t& phase,
+                                                    const float* sa, int64_t ldsa, int rows, const float* sb, int kb0, int kb1, int lane,
+                                                    volatile uint32_t* abort_flag) {
+    for (int kb = kb0; kb < kb1; kb += 4) {
+        if (!__all_sync(0xffffffffu, mbar_wait(&empty[slot], phase ^ 1, abort_flag, 0x600 + slot))) return false;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        const int col = col0 + q * 8;
-        if (col + 8 <= N) {
-            *reinterpret_cast<uint4*>(crow + col) = make_uint4(pack_bf16x2(v[q * 8], v[q * 8 + 1]), pack_bf16x2(v[q * 8 + 2], v[q * 8 + 3]),
-                                                               pack_bf16x2(v[q * 8 + 4], v[q * 8 + 5]), pack_bf16x2(v[q * 8 + 6], v[q * 8 + 7]));
-        } else {
+        for (int u = 0; u < 4; ++u) {
+            if (kb + u < kb1) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (col + j < N) crow[col + j] = __float2bfloat16(v[q * 8 + j]);
+                for (int i = 0; i < 4; ++i)
+                    if (i * 32 < rows) cp_async_f32(&ring[slot].row[u][i * 32 + lane], sa + (kb + u) * ldsa + i * 32 + lane, i * 32 + lane < rows);
+                if (lane < 4) cp_async_f32(&ring[slot].col[u][lane], sb + kb + u, true);
+            }
         }
+        cp_async_arrive(&full[slot]);
+        if (++slot == kF8ScaleSlots) { slot = 0; phase ^= 1; }
     }
+    return true;
 }
 
-// acc += s * (kCols accumulator columns of tensor memory), 16 columns at a time: the next 16 are on their way while these
-// are added, two columns per instruction.  `drained` runs when the last ones are in registers.
-template <int kCols, class F>
-__device__ __forceinline__ void gemm_f8_promote(float2 (&acc)[kCols / 2], uint32_t taddr, float s, F drained) {
-    const float2 s2 = make_float2(s, s);
+// acc += scale * (16 * kChunks accumulator columns of tensor memory), 16 columns at a time: the next 16 are on their way while
+// these are added, two columns per instruction.  The scale is s0 before chunk `cut` and s1 from it on.  `drained` runs when the
+// last columns are in registers.
+template <int kChunks, class F>
+__device__ __forceinline__ void gemm_f8_promote(float2 (&acc)[kChunks * 8], uint32_t taddr, float s0, float s1, int cut, F drained) {
     uint32_t v[2][16];
     tmem_ld_32x32b_x16(taddr, v[0]);
 #pragma unroll
-    for (int c = 0; c < kCols / 16; ++c) {
+    for (int c = 0; c < kChunks; ++c) {
         tmem_wait_ld_of(v[c & 1]);
-        if (c + 1 < kCols / 16)
+        if (c + 1 < kChunks)
             tmem_ld_32x32b_x16(taddr + (c + 1) * 16, v[(c + 1) & 1]);
         else
             drained();
+        const float s = c < cut ? s0 : s1;
+        const float2 s2 = make_float2(s, s);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             acc[c * 8 + i] = ffma2(s2, make_float2(__uint_as_float(v[c & 1][2 * i]), __uint_as_float(v[c & 1][2 * i + 1])), acc[c * 8 + i]);
     }
 }
 
-template <int BN, int kCtasPerSm>
-__global__ void __launch_bounds__(kF8Threads, kCtasPerSm)
-gemm_f8_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b, const GemmF8Params p) {
-    using L = GemmF8Smem<BN>;
+// ---------------------------------------------------------------------------------------------------------
+// Problems with few tiles (next-token shapes above all): one 128 x bn tile per cluster, bn any multiple of 16 up to 256, K
+// cut over the S CTAs of the cluster.  Such a problem is bound by how evenly the stream of B is spread over the SMs, so the
+// host picks bn and S together such that tiles x S comes close to the SM count from below.  The CTAs' FP32 tiles meet in
+// distributed shared memory (the stages are free by then) and are summed in ascending slice order (deterministic).
+// ---------------------------------------------------------------------------------------------------------
+constexpr int kF8SplitSmem = 208 * 1024;
+// A stages | B stages.  The A descriptor always spans 128 rows, of which the first a_rows are loaded: the span may
+// run on into whatever follows (rows that are never stored), so at least 16 KB follow the A stages.  The FP32 tile of up to
+// a_rows rows takes the stages' place at the end.
+inline int gemm_f8_split_smem(int bn, int a_rows, int stages) {
+    return std::max({stages * (a_rows + bn) * kF8BK, stages * a_rows * kF8BK + 16384, a_rows * (bn + 4) * 4}) + 1024;
+}
+
+__global__ void __launch_bounds__(kF8Threads, 1)
+gemm_f8_split_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b, const GemmF8Params p) {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    const int a_bytes = p.a_rows * kF8BK;
+    __shared__ uint64_t full[kF8MaxStages], empty[kF8MaxStages], acc_full[4], acc_empty[4], scale_full[kF8ScaleSlots], scale_empty[kF8ScaleSlots];
+    __shared__ GemmF8Scales scales[kF8ScaleSlots];
+    __shared__ uint32_t tmem_base_slot, abort_word;
+    volatile uint32_t* abort_flag = &abort_word;
+    const int bn = p.bn, bufs = p.bufs;
+    const int a_bytes = p.a_rows * kF8BK, b_bytes = bn * kF8BK;
     uint8_t* smem_b = smem + p.stages * a_bytes;
-    uint64_t* full = reinterpret_cast<uint64_t*>(smem_b + p.stages * L::kBBytes);
-    uint64_t* empty = full + kF8MaxStages;
-    uint64_t* acc_full = empty + kF8MaxStages;  // [2]
-    uint64_t* acc_empty = acc_full + 2;         // [2]
-    uint32_t* tmem_base_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
-    volatile uint32_t* abort_flag = tmem_base_slot + 1;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int S = static_cast<int>(cluster_nctarank());
     const int slice = static_cast<int>(cluster_ctarank());
     const int tile = static_cast<int>(blockIdx.x) / S;
     const int num_kb = (p.K + kF8BK - 1) / kF8BK;
-    const int kb0 = slice * p.kb_per_split, kb1 = min(num_kb, kb0 + p.kb_per_split);  // no slice is empty (host)
-    const int per_group = p.group_m * p.tiles_n;  // raster groups of group_m tile rows, rows fastest (L2 reuse)
-    const int first_m = tile / per_group * p.group_m;
-    const int rows_in_group = min(p.group_m, p.tiles_m - first_m);
-    const int m0 = (first_m + tile % per_group % rows_in_group) * 128, n0 = tile % per_group / rows_in_group * BN;
-    const int active = min(4, (p.M - m0 + 31) / 32);  // promotion warps whose rows exist
-    constexpr uint32_t kTmemCols = 2 * BN;
+    // slices differ by at most one K block (none is empty: S <= num_kb)
+    const int kb0 = static_cast<int>(static_cast<int64_t>(num_kb) * slice / S), kb1 = static_cast<int>(static_cast<int64_t>(num_kb) * (slice + 1) / S);
+    const int m0 = tile % p.tiles_m * 128, n0 = tile / p.tiles_m * bn;
+    const int rows = min(128, p.M - m0);
+    const int cols0 = (bn / 16 + 1) / 2 * 16;  // columns of the first four promotion warps; the others have the rest
+    const int quarters = (rows + 31) / 32, halves = bn > cols0 ? 2 : 1;  // promotion warps with something to do
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.stages; ++s) {
             mbar_init(&full[s], 1);
             mbar_init(&empty[s], 1);
         }
-        for (int a = 0; a < 2; ++a) {
+        for (int a = 0; a < bufs; ++a) {
             mbar_init(&acc_full[a], 1);
-            mbar_init(&acc_empty[a], active);
+            mbar_init(&acc_empty[a], quarters * halves);
         }
-        *abort_flag = 0;
+        for (int a = 0; a < kF8ScaleSlots; ++a) {
+            mbar_init(&scale_full[a], 32);
+            mbar_init(&scale_empty[a], quarters * halves);
+        }
+        abort_word = 0;
         fence_mbar_init();
+        if (blockIdx.x == 0) clock_probe(0, 0);
     }
     if (warp == 0 && lane == 0) {
         prefetch_tensormap(&tmap_a);
         prefetch_tensormap(&tmap_b);
     }
     if (warp == 1) {
-        tmem_alloc(tmem_base_slot, kTmemCols);
+        tmem_alloc(&tmem_base_slot, 512);
         tmem_relinquish();
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem_base = *tmem_base_slot;
-    const int quarter = warp & 3;  // tensor-memory lanes this warp may touch: 32 * quarter .. + 31
-    const int r = quarter * 32 + lane;
-    float2 acc[BN / 2];
-#pragma unroll
-    for (int i = 0; i < BN / 2; ++i) acc[i] = make_float2(0.0f, 0.0f);
+    const uint32_t tmem_base = tmem_base_slot;
+    float* part = reinterpret_cast<float*>(smem);  // [rows][bn + 4], written after the main loop
+    const int part_pitch = bn + 4;
 
     if (warp == 0) {
+        setmaxnreg_dec<kF8OtherRegs>();
         if (lane == 0) {
             int stage = 0;
             uint32_t phase = 0;
             for (int kb = kb0; kb < kb1; ++kb) {
                 if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag, 0x100 + stage)) break;
-                mbar_arrive_expect_tx(&full[stage], a_bytes + L::kBBytes);
+                mbar_arrive_expect_tx(&full[stage], a_bytes + b_bytes);
+                tma_load_2d(smem_b + stage * b_bytes, &tmap_b, &full[stage], kb * kF8BK, n0);
                 tma_load_2d(smem + stage * a_bytes, &tmap_a, &full[stage], kb * kF8BK, m0);
-                tma_load_2d(smem_b + stage * L::kBBytes, &tmap_b, &full[stage], kb * kF8BK, n0);
                 if (++stage == p.stages) { stage = 0; phase ^= 1; }
             }
         }
+        __syncwarp();
+        cluster_sync_all();
     } else if (warp == 1) {
+        setmaxnreg_dec<kF8OtherRegs>();
         const bool leader = elect_one();
-        constexpr uint32_t idesc = make_idesc_e4m3(128, BN);
+        const uint32_t idesc = make_idesc_e4m3(128, bn);
         const uint32_t a_lo0 = sdesc_lo(smem_u32(smem), 16), b_lo0 = sdesc_lo(smem_u32(smem_b), 16);
-        int stage = 0;
-        uint32_t phase = 0;
+        int stage = 0, buf = 0;
+        uint32_t phase = 0, acc_phase = 0;
         for (int kb = kb0; kb < kb1; ++kb) {
-            const int buf = (kb - kb0) & 1;
-            const uint32_t use = (kb - kb0) >> 1;  // uses of this accumulator before
-            bool ok = mbar_wait(&acc_empty[buf], (use & 1) ^ 1, abort_flag, 0x300 + buf);
-            ok = ok && mbar_wait(&full[stage], phase, abort_flag, 0x200 + stage);
+            bool ok = mbar_wait(&full[stage], phase, abort_flag, 0x200 + stage);
+            ok = ok && mbar_wait(&acc_empty[buf], acc_phase ^ 1, abort_flag, 0x300 + buf);
             if (!__all_sync(0xffffffffu, ok)) break;
             tc_fence_after();
             if (leader) {
-                const uint32_t a_lo = a_lo0 + stage * (a_bytes >> 4), b_lo = b_lo0 + stage * (L::kBBytes >> 4);
+                const uint32_t a_lo = a_lo0 + stage * (a_bytes >> 4), b_lo = b_lo0 + stage * (b_bytes >> 4);
 #pragma unroll
                 for (int k = 0; k < kF8BK / 32; ++k)
-                    umma_f8_ss_lo(tmem_base + buf * BN, a_lo + k * (32 >> 4), b_lo + k * (32 >> 4), idesc, k != 0);
+                    umma_f8_ss_lo(tmem_base + buf * bn, a_lo + k * (32 >> 4), b_lo + k * (32 >> 4), idesc, k != 0);
                 umma_commit(&empty[stage]);
                 umma_commit(&acc_full[buf]);
             }
             __syncwarp();
             if (++stage == p.stages) { stage = 0; phase ^= 1; }
+            if (++buf == bufs) { buf = 0; acc_phase ^= 1; }
         }
-    } else if (quarter < active) {
-        const bool live = m0 + r < p.M;
-        const float* sa = p.sa + m0 + r;
-        const float* sb = p.sb + static_cast<int64_t>(n0 / 128) * p.ldsb;
-        const uint32_t t_row = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16);
-        float s_next = live ? __ldg(sa + kb0 * p.ldsa) * __ldg(sb + kb0) : 0.0f;
-        for (int kb = kb0; kb < kb1; ++kb) {
-            const int buf = (kb - kb0) & 1;
-            const float s = s_next;
-            if (live && kb + 1 < kb1) s_next = __ldg(sa + (kb + 1) * p.ldsa) * __ldg(sb + kb + 1);
-            if (!__all_sync(0xffffffffu, mbar_wait(&acc_full[buf], ((kb - kb0) >> 1) & 1, abort_flag, 0x400 + buf))) break;
-            tc_fence_after();
-gemm_f8_promote<BN>(acc, t_row + buf * BN, s, [&] {  // the accumulator is in registers: the tensor core may refill it
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&acc_empty[buf]);
-            });
-        }
-    }
-
-    if (S == 1) {
-        if (warp >= 2 && m0 + r < p.M) {
-            __nv_bfloat16* crow = p.C + static_cast<int64_t>(m0 + r) * p.ldc;
-#pragma unroll
-            for (int c = 0; c < BN / 32; ++c) gemm_f8_store32(crow, n0 + c * 32, p.N, reinterpret_cast<const float*>(acc + c * 16));
-        }
-        tc_fence_before();
-        __syncthreads();
+        cluster_sync_all();
+    } else if (warp == 2) {
+        setmaxnreg_dec<kF8OtherRegs>();
+        // lane c < 4: the c-th column scale, of half c / 2: the first or second block of 128 its columns touch
+        const int block = min((n0 + (lane >> 1 & 1) * cols0) / 128 + (lane & 1), (p.N - 1) / 128);  // (columns beyond N are not stored)
+        int slot = 0;
+        uint32_t phase = 0;
+        gemm_f8_load_scales(scales, scale_full, scale_empty, slot, phase, p.sa + m0, p.ldsa, rows, p.sb + block * p.ldsb, kb0, kb1, lane, abort_flag);
+        cluster_sync_all();
+    } else if (warp == 3) {
+        setmaxnreg_dec<kF8OtherRegs>();
+        cluster_sync_all();
     } else {
-        // every UMMA of this CTA has read its operands once the last accumulator is full, which the promotion warps have
-        // waited for; the producer issued no load beyond them: the stages are free
-        float* part = reinterpret_cast<float*>(smem);
-        __syncthreads();
-        if (warp >= 2 && m0 + r < p.M) {
-            float4* dst = reinterpret_cast<float4*>(part + r * L::kPartPitch);
+        setmaxnreg_inc<kF8PromoteRegs>();
+        const int quarter = warp & 3, half = (warp - 4) >> 2;
+        const int col = half * cols0, chunks = ((half ? bn : cols0) - col) / 16;
+        if (quarter < quarters && chunks > 0) {
+            const int r = quarter * 32 + lane;
+            const uint32_t t_row = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + col;
+            float4* dst = reinterpret_cast<float4*>(part + r * part_pitch + col);
+            // One unrolled loop per number of chunks: a branch around every chunk costs more than the chunk.
+            auto promote = [&](auto count) {
+                constexpr int kChunks = decltype(count)::value;
+                // a warp's columns lie in one or two blocks of 128: the second begins at chunk `cut`
+                const int cut = (128 - (n0 + col) % 128) / 16;
+                float2 acc[kChunks * 8];
 #pragma unroll
-            for (int q = 0; q < BN / 4; ++q) dst[q] = make_float4(acc[2 * q].x, acc[2 * q].y, acc[2 * q + 1].x, acc[2 * q + 1].y);
+                for (int i = 0; i < kChunks * 8; ++i) acc[i] = make_float2(0.0f, 0.0f);
+                int buf = 0, slot = 0;
+                uint32_t acc_phase = 0, slot_phase = 0;
+                for (int kb = kb0; kb < kb1; ++kb) {
+                    const int u = (kb - kb0) & 3;
+                    bool ok = true;
+                    if (u == 0) ok = mbar_wait(&scale_full[slot], slot_phase, abort_flag, 0x500 + slot);
+                    const float row_scale = scales[slot].row[u][r];
+                    const float s0 = row_scale * scales[slot].col[u][half * 2], s1 = row_scale * scales[slot].col[u][half * 2 + 1];
+                    ok = ok && mbar_wait(&acc_full[buf], acc_phase, abort_flag, 0x400 + buf);
+                    if (!__all_sync(0xffffffffu, ok)) break;
+                    tc_fence_after();
+                    gemm_f8_promote<kChunks>(acc, t_row + buf * bn, s0, s1, cut, [&] {  // the tensor core may refill the accumulator
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) {
+                            mbar_arrive(&acc_empty[buf]);
+                            if (u == 3) mbar_arrive(&scale_empty[slot]);
+                        }
+                    });
+                    if (u == 3 && ++slot == kF8ScaleSlots) { slot = 0; slot_phase ^= 1; }
+                    if (++buf == bufs) { buf = 0; acc_phase ^= 1; }
+                }
+                // Every UMMA of this CTA has read its operands once the last accumulator is full, and the producer issued no load
+                // beyond them: the stages are free when all promotion warps are here.
+                asm volatile("bar.sync 1, %0;" ::"r"(32 * quarters * halves) : "memory");
+                if (r < rows) {
+#pragma unroll
+                    for (int q = 0; q < kChunks * 4; ++q) dst[q] = make_float4(acc[2 * q].x, acc[2 * q].y, acc[2 * q + 1].x, acc[2 * q + 1].y);
+                }
+            };
+            switch (chunks) {
+                case 1: promote(std::integral_constant<int, 1>()); break;
+                case 2: promote(std::integral_constant<int, 2>()); break;
+                case 3: promote(std::integral_constant<int, 3>()); break;
+                case 4: promote(std::integral_constant<int, 4>()); break;
+                case 5: promote(std::integral_constant<int, 5>()); break;
+                case 6: promote(std::integral_constant<int, 6>()); break;
+                case 7: promote(std::integral_constant<int, 7>()); break;
+                default: promote(std::integral_constant<int, 8>()); break;
+            }
         }
+        __syncwarp();
+        // Every CTA's tile is in its shared memory (or a wait expired there: its rows are then garbage and the status word says
+        // so): sum this CTA's share of the columns over the cluster.  (Only the promotion warps: code behind the roles' common
+        // end would have to do with the registers of the others.)
         tc_fence_before();
         cluster_sync_all();
-        const int groups = BN / S / 4;  // this CTA's share of the columns, four at a time
-        const int rows = min(128, p.M - m0);
+        const int g0 = bn / 4 * slice / S, groups = bn / 4 * (slice + 1) / S - g0;  // groups of four columns
         const uint32_t part_addr = smem_u32(part);
-        for (int idx = threadIdx.x; idx < rows * groups; idx += kF8Threads) {
-            const int row = idx / groups, c = slice * (BN / S) + (idx % groups) * 4;
+        for (int idx = threadIdx.x - 128; idx < rows * groups; idx += kF8Threads - 128) {
+            const int row = idx / groups, c = (g0 + idx % groups) * 4;
             float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             for (int s2 = 0; s2 < S; ++s2) {
-                const float4 v = ld_shared_cluster_f32x4(map_to_cta(part_addr + (row * L::kPartPitch + c) * 4, s2));
+                const float4 v = ld_shared_cluster_f32x4(map_to_cta(part_addr + (row * part_pitch + c) * 4, s2));
                 sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
             }
-            const int col = n0 + c;
-            __nv_bfloat16* dst = p.C + static_cast<int64_t>(m0 + row) * p.ldc + col;
-            if (col + 4 <= p.N) {
+            const int out = n0 + c;
+            __nv_bfloat16* dst = p.C + static_cast<int64_t>(m0 + row) * p.ldc + out;
+            if (out + 4 <= p.N) {
                 *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(sum.x, sum.y), pack_bf16x2(sum.z, sum.w));
             } else {
                 const float a[4] = {sum.x, sum.y, sum.z, sum.w};
-                for (int j = 0; j < 4 && col + j < p.N; ++j) dst[j] = __float2bfloat16(a[j]);
+                for (int j = 0; j < 4 && out + j < p.N; ++j) dst[j] = __float2bfloat16(a[j]);
             }
         }
-        cluster_sync_all();  // no CTA leaves while a peer may still read its shared memory
+        __syncwarp();
     }
+
+    tc_fence_before();
+    cluster_sync_all();  // no CTA leaves while a peer may still read its shared memory
+    if (blockIdx.x == 0 && threadIdx.x == 0) clock_probe(0, 1);
     if (warp == 1) {
         __syncwarp();
         tc_fence_after();
-        tmem_dealloc(tmem_base, kTmemCols);
+        tmem_dealloc(tmem_base, 512);
     }
 }
 
@@ -265,34 +322,33 @@ gemm_f8_promote<BN>(acc, t_row + buf * BN, s, [&] {  // the accumulator is in re
 //   else   one CTA owns a 128 x 256 tile
 // The two accumulators in tensor memory (2 x 256 columns) belong to alternate K blocks, across tile borders: while the
 // promotion warps round and store a tile, the tensor core is up to two K blocks into the next one.  Results leave through
-// 4 KB of shared memory per warp (32 rows x 64 columns, 128-byte swizzle) and TMA stores.
+// 2 KB of shared memory per warp (32 rows x 32 columns, 64-byte swizzle) and TMA stores.
 // ---------------------------------------------------------------------------------------------------------
-constexpr int kF8BigThreads = 320;  // 2 + 8 warps; 200 registers per thread
-template <bool kPair>
+template <bool kPair, int BN>
 struct GemmF8BigSmem {
     static constexpr int kABytes = 128 * kF8BK;
-    static constexpr int kBBytes = (kPair ? 128 : 256) * kF8BK;
+    static constexpr int kBBytes = (kPair ? BN / 2 : BN) * kF8BK;
     static constexpr int kStageBytes = kABytes + kBBytes;
-    static constexpr int kStages = kPair ? 6 : 4;
-    static constexpr int kTotal = kStages * kStageBytes + 8 * 4096 + 256 + 1024;
+    static constexpr int kStages = 192 * 1024 / kStageBytes;
+    static constexpr int kTotal = kStages * kStageBytes + 8 * 2048 + 1024;
 };
 
-template <bool kPair>
-__global__ void __launch_bounds__(kF8BigThreads, 1)
+template <bool kPair, int BN>
+__global__ void __launch_bounds__(kF8Threads, 1)
 gemm_f8_big_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b,
                    const __grid_constant__ CUtensorMap tmap_c, const GemmF8Params p) {
-    using L = GemmF8BigSmem<kPair>;
+    using L = GemmF8BigSmem<kPair, BN>;
     constexpr int kStages = L::kStages;
+    constexpr int kBufs = 512 / BN;     // accumulators in tensor memory
+    constexpr int kCols = BN / 2;       // columns of a promotion warp
     constexpr int kTileM = kPair ? 256 : 128;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t* staging = smem + kStages * L::kStageBytes;
-    uint64_t* full = reinterpret_cast<uint64_t*>(staging + 8 * 4096);
-    uint64_t* empty = full + kStages;
-    uint64_t* acc_full = empty + kStages;  // [2]
-    uint64_t* acc_empty = acc_full + 2;    // [2]
-    uint32_t* tmem_base_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
-    volatile uint32_t* abort_flag = tmem_base_slot + 1;
+    __shared__ uint64_t full[kStages], empty[kStages], acc_full[kBufs], acc_empty[kBufs], scale_full[kF8ScaleSlots], scale_empty[kF8ScaleSlots];
+    __shared__ GemmF8Scales scales[kF8ScaleSlots];
+    __shared__ uint32_t tmem_base_slot[1], abort_word;
+    volatile uint32_t* abort_flag = &abort_word;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (blockIdx.x == 0 && threadIdx.x == 0) clock_probe(0, 0);
@@ -305,7 +361,7 @@ gemm_f8_big_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
         const int first_m = tile / per_group * p.group_m;
         const int rows = min(p.group_m, p.tiles_m - first_m), r = tile % per_group;
         m0 = (first_m + r % rows) * kTileM + rank * 128;
-        n0 = r / rows * 256;
+        n0 = r / rows * BN;
     };
 
     if (threadIdx.x == 0) {
@@ -313,9 +369,13 @@ gemm_f8_big_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
             mbar_init(&full[s], 1);
             mbar_init(&empty[s], 1);
         }
-        for (int a = 0; a < 2; ++a) {
+        for (int a = 0; a < kBufs; ++a) {
             mbar_init(&acc_full[a], 1);
             mbar_init(&acc_empty[a], kPair ? 16 : 8);  // every promotion warp
+        }
+        for (int a = 0; a < kF8ScaleSlots; ++a) {
+            mbar_init(&scale_full[a], 32);
+            mbar_init(&scale_empty[a], 8);
         }
         *abort_flag = 0;
         fence_mbar_init();
@@ -340,6 +400,7 @@ gemm_f8_big_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
     const uint32_t tmem_base = *tmem_base_slot;
 
     if (warp == 0) {
+        setmaxnreg_dec<kF8OtherRegs>();
         if (lane == 0) {
             int stage = 0;
             uint32_t phase = 0;
@@ -350,36 +411,37 @@ gemm_f8_big_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
                 for (int kb = 0; kb < num_kb; ++kb) {
                     ok = mbar_wait(&empty[stage], phase ^ 1, abort_flag, 0x100 + stage);
                     if (!ok) break;
-                    uint8_t* sa = smem + stage * L::kStageBytes;
-                    uint8_t* sb = sa + L::kABytes;
+                    uint8_t* dst_a = smem + stage * L::kStageBytes;
+                    uint8_t* dst_b = dst_a + L::kABytes;
                     if constexpr (kPair) {
                         if (rank == 0) mbar_arrive_expect_tx(&full[stage], 2 * L::kStageBytes);
                         const uint32_t bar = map_to_cta(smem_u32(&full[stage]), 0);
-                        tma_load_2d_pair(sa, &tmap_a, bar, kb * kF8BK, m0);
-                        tma_load_2d_pair(sb, &tmap_b, bar, kb * kF8BK, n0 + rank * 128);
+                        tma_load_2d_pair(dst_a, &tmap_a, bar, kb * kF8BK, m0);
+                        tma_load_2d_pair(dst_b, &tmap_b, bar, kb * kF8BK, n0 + rank * (BN / 2));
                     } else {
                         mbar_arrive_expect_tx(&full[stage], L::kStageBytes);
-                        tma_load_2d(sa, &tmap_a, &full[stage], kb * kF8BK, m0);
-                        tma_load_2d(sb, &tmap_b, &full[stage], kb * kF8BK, n0);
-                        tma_load_2d(sb + 128 * kF8BK, &tmap_b, &full[stage], kb * kF8BK, n0 + 128);
+                        tma_load_2d(dst_a, &tmap_a, &full[stage], kb * kF8BK, m0);
+                        tma_load_2d(dst_b, &tmap_b, &full[stage], kb * kF8BK, n0);
+                        if constexpr (BN == 256) tma_load_2d(dst_b + 128 * kF8BK, &tmap_b, &full[stage], kb * kF8BK, n0 + 128);
                     }
                     if (++stage == kStages) { stage = 0; phase ^= 1; }
                 }
             }
         }
     } else if (warp == 1) {
+        setmaxnreg_dec<kF8OtherRegs>();
         if (rank == 0) {
             const bool issuer = elect_one();
-            constexpr uint32_t idesc = make_idesc_e4m3(kTileM, 256);
+            constexpr uint32_t idesc = make_idesc_e4m3(kTileM, BN);
             const uint32_t a_lo0 = sdesc_lo(smem_u32(smem), 16), b_lo0 = sdesc_lo(smem_u32(smem + L::kABytes), 16);
             int stage = 0;
             uint32_t phase = 0, use = 0;  // use: K blocks so far
             bool ok = true;
             for (int tile = first; tile < tiles && ok; tile += step) {
                 for (int kb = 0; kb < num_kb; ++kb, ++use) {
-                    const int buf = use & 1;
+                    const int buf = use % kBufs;
                     ok = mbar_wait(&full[stage], phase, abort_flag, 0x200 + stage);
-                    ok = ok && mbar_wait(&acc_empty[buf], ((use >> 1) & 1) ^ 1, abort_flag, 0x300 + buf);
+                    ok = ok && mbar_wait(&acc_empty[buf], ((use / kBufs) & 1) ^ 1, abort_flag, 0x300 + buf);
                     ok = __all_sync(0xffffffffu, ok) != 0;
                     if (!ok) break;
                     tc_fence_after();
@@ -388,9 +450,9 @@ gemm_f8_big_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
 #pragma unroll
                         for (int k = 0; k < kF8BK / 32; ++k) {
                             if constexpr (kPair)
-                                umma_f8_ss_pair_lo(tmem_base + buf * 256, a_lo + k * (32 >> 4), b_lo + k * (32 >> 4), idesc, k != 0);
+                                umma_f8_ss_pair_lo(tmem_base + buf * BN, a_lo + k * (32 >> 4), b_lo + k * (32 >> 4), idesc, k != 0);
                             else
-                                umma_f8_ss_lo(tmem_base + buf * 256, a_lo + k * (32 >> 4), b_lo + k * (32 >> 4), idesc, k != 0);
+                                umma_f8_ss_lo(tmem_base + buf * BN, a_lo + k * (32 >> 4), b_lo + k * (32 >> 4), idesc, k != 0);
                         }
                         if constexpr (kPair) {
                             umma_commit_pair(&empty[stage], 3);
@@ -405,84 +467,83 @@ gemm_f8_big_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
                 }
             }
         }
+    } else if (warp == 2) {
+        setmaxnreg_dec<kF8OtherRegs>();
+        int slot = 0;
+        uint32_t phase = 0;
+        for (int tile = first; tile < tiles; tile += step) {
+            int m0, n0;
+            coords(tile, m0, n0);
+            const int block = min((n0 + (lane >> 1 & 1) * kCols) / 128, (p.N - 1) / 128);  // lane c < 4: of half c / 2
+            if (!gemm_f8_load_scales(scales, scale_full, scale_empty, slot, phase, p.sa + m0, p.ldsa, min(128, p.M - m0), p.sb + block * p.ldsb, 0,
+                                     num_kb, lane, abort_flag))
+                break;
+        }
+    } else if (warp == 3) {
+        setmaxnreg_dec<kF8OtherRegs>();
     } else {
-        const int quarter = warp & 3, half = (warp - 2) >> 2;  // 32 rows, 128 columns
-        uint8_t* stg = staging + (warp - 2) * 4096;
-        const uint32_t t_row = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + half * 128;
-        uint32_t use = 0;
+        setmaxnreg_inc<kF8PromoteRegs>();
+        const int quarter = warp & 3, half = (warp - 4) >> 2;  // 32 rows, kCols columns
+        uint8_t* stg = staging + (warp - 4) * 2048;
+        const uint32_t t_row = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + half * kCols;
+        uint32_t use = 0, slot_phase = 0;
+        int slot = 0;
         bool ok = true;
         for (int tile = first; tile < tiles && ok; tile += step) {
             int m0, n0;
             coords(tile, m0, n0);
-            const int row0 = m0 + quarter * 32, col0 = n0 + half * 128;
-            const bool live = row0 + lane < p.M && col0 < p.N;
-            const float* sa = p.sa + row0 + lane;
-            const float* sb = p.sb + static_cast<int64_t>(col0 / 128) * p.ldsb;
-            float2 acc[64];
+            const int row0 = m0 + quarter * 32, col0 = n0 + half * kCols;
+            float2 acc[kCols / 2];
 #pragma unroll
-            for (int i = 0; i < 64; ++i) acc[i] = make_float2(0.0f, 0.0f);
-            // the scales of two K blocks at a time, requested two K blocks ahead
-            float s[2];
-#pragma unroll
-            for (int u = 0; u < 2; ++u) s[u] = ld_f32_if(sa + u * p.ldsa, live && u < num_kb) * ld_f32_if(sb + u, live && u < num_kb);
-            for (int kb2 = 0; kb2 < num_kb && ok; kb2 += 2) {
-                float xa[2], xb[2];
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const bool there = live && kb2 + 2 + u < num_kb;
-                    xa[u] = ld_f32_if(sa + (kb2 + 2 + u) * p.ldsa, there);
-                    xb[u] = ld_f32_if(sb + kb2 + 2 + u, there);
-                }
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    if (kb2 + u < num_kb && ok) {
-                        const int buf = use & 1;
-                        ok = __all_sync(0xffffffffu, mbar_wait(&acc_full[buf], (use >> 1) & 1, abort_flag, 0x400 + buf)) != 0;
-                        if (ok) {
-                            tc_fence_after();
-                            gemm_f8_promote<128>(acc, t_row + buf * 256, s[u], [&] {
-                                tc_fence_before();
-                                __syncwarp();
-                                if (lane == 0) {
-                                    if constexpr (kPair)
-                                        mbar_arrive_peer(map_to_cta(smem_u32(&acc_empty[buf]), 0));
-                                    else
-                                        mbar_arrive(&acc_empty[buf]);
-                                }
-                            });
-                            ++use;
-                        }
+            for (int i = 0; i < kCols / 2; ++i) acc[i] = make_float2(0.0f, 0.0f);
+            for (int kb = 0; kb < num_kb; ++kb, ++use) {
+                const int buf = use % kBufs, u = kb & 3;
+                const bool last_of_slot = u == 3 || kb == num_kb - 1;
+                if (u == 0) ok = mbar_wait(&scale_full[slot], slot_phase, abort_flag, 0x500 + slot);
+                const float s = scales[slot].row[u][quarter * 32 + lane] * scales[slot].col[u][half * 2];
+                ok = ok && mbar_wait(&acc_full[buf], (use / kBufs) & 1, abort_flag, 0x400 + buf);
+                ok = __all_sync(0xffffffffu, ok) != 0;
+                if (!ok) break;
+                tc_fence_after();
+                gemm_f8_promote<kCols / 16>(acc, t_row + buf * BN, s, s, kCols / 16, [&] {  // the tensor core may refill the accumulator
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if constexpr (kPair)
+                            mbar_arrive_peer(map_to_cta(smem_u32(&acc_empty[buf]), 0));
+                        else
+                            mbar_arrive(&acc_empty[buf]);
+                        if (last_of_slot) mbar_arrive(&scale_empty[slot]);
                     }
-                }
-#pragma unroll
-                for (int u = 0; u < 2; ++u) s[u] = xa[u] * xb[u];
+                });
+                if (last_of_slot && ++slot == kF8ScaleSlots) { slot = 0; slot_phase ^= 1; }
             }
             if (!ok) break;
-            // ---- round and store: 64 columns at a time ----
+            // ---- round and store: 32 columns at a time ----
             const int n8 = p.N & ~7;  // the tensor map of C ends here (16-byte units)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int h = 0; h < kCols / 32; ++h) {
+                const int col = col0 + h * 32;
                 if (lane == 0) tma_store_wait_read<0>();
                 __syncwarp();
 #pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    const float2* a = acc + h * 32 + q * 4;
-                    *reinterpret_cast<uint4*>(stg + lane * 128 + ((q ^ (lane & 7)) << 4)) =
+                for (int q = 0; q < 4; ++q) {
+                    const float2* a = acc + h * 16 + q * 4;
+                    *reinterpret_cast<uint4*>(stg + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4)) =
                         make_uint4(pack_bf16x2(a[0].x, a[0].y), pack_bf16x2(a[1].x, a[1].y), pack_bf16x2(a[2].x, a[2].y), pack_bf16x2(a[3].x, a[3].y));
                 }
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) {
-                    if (row0 < p.M && col0 + h * 64 < n8) tma_store_2d(&tmap_c, stg, col0 + h * 64, row0);
+                    if (row0 < p.M && col < n8) tma_store_2d(&tmap_c, stg, col, row0);
                     tma_store_commit();
                 }
-                if (n8 != p.N && col0 + h * 64 <= n8 && n8 < col0 + h * 64 + 64 && row0 + lane < p.M) {  // the up to seven columns beyond
+                if (n8 != p.N && col <= n8 && n8 < col + 32 && row0 + lane < p.M) {  // the up to seven columns beyond
                     __nv_bfloat16* crow = p.C + static_cast<int64_t>(row0 + lane) * p.ldc;
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        const int col = col0 + h * 64 + 2 * j;
-                        if (col >= n8 && col < p.N) crow[col] = __float2bfloat16(acc[h * 32 + j].x);
-                        if (col >= n8 && col + 1 < p.N) crow[col + 1] = __float2bfloat16(acc[h * 32 + j].y);
+                    for (int j = 0; j < 16; ++j) {
+                        if (col + 2 * j >= n8 && col + 2 * j < p.N) crow[col + 2 * j] = __float2bfloat16(acc[h * 16 + j].x);
+                        if (col + 2 * j + 1 >= n8 && col + 2 * j + 1 < p.N) crow[col + 2 * j + 1] = __float2bfloat16(acc[h * 16 + j].y);
                     }
                 }
             }
@@ -499,6 +560,21 @@ gemm_f8_big_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
         tc_fence_after();
         if constexpr (kPair) tmem_dealloc_pair(tmem_base, 512); else tmem_dealloc(tmem_base, 512);
     }
+}
+
+// Once per device.  0: ready, 1: a CUDA call failed, 2: a kernel was compiled with fewer registers than its hand-over moves
+// (it would wait for registers that never come: nothing may be launched).
+inline int gemm_f8_configure() {
+    auto one = [](auto kernel, int smem) {
+        cudaFuncAttributes attr;
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess ||
+            cudaFuncGetAttributes(&attr, kernel) != cudaSuccess)
+            return 1;
+        return attr.numRegs >= kF8LaunchRegs ? 0 : 2;
+    };
+    const int rc[] = {one(gemm_f8_split_kernel, kF8SplitSmem), one(gemm_f8_big_kernel<true, 256>, GemmF8BigSmem<true, 256>::kTotal),
+                      one(gemm_f8_big_kernel<false, 256>, GemmF8BigSmem<false, 256>::kTotal)};
+    return *std::max_element(rc, rc + 3);
 }
 
 }  // namespace mlt

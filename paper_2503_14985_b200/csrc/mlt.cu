@@ -32,6 +32,7 @@ struct DeviceInfo {
     int cc_major = 0;
     bool configured = false;
     bool mha_ok = false;  // the attention kernels' compiled register count covers their in-kernel register hand-over
+    bool gemm_f8_ok = false;  // likewise for the scaled GEMM
     // CTAs that can be resident at once as clusters of 2, 4 and 8 of the K-cutting GEMM kernel (a cluster must fit
     // one GPC, so this can be less than the SM count rounded down to a multiple of the cluster size)
     int cluster_slots[3] = {0, 0, 0};
@@ -101,9 +102,9 @@ int get_device(DeviceInfo* out) {
             d.cluster_slots[i] = clusters * S;
         }
         if (paged_configure() != 0 || !paged_f8_configure()) return MLT_ERR_CUDA;
-        if (set_smem(gemm_f8_kernel<64, 3>, kGemmF8NarrowSmem) != MLT_OK || set_smem(gemm_f8_kernel<128, 1>, kGemmF8WideSmem) != MLT_OK ||
-            set_smem(gemm_f8_big_kernel<true>, GemmF8BigSmem<true>::kTotal) != MLT_OK || set_smem(gemm_f8_big_kernel<false>, GemmF8BigSmem<false>::kTotal) != MLT_OK)
-            return MLT_ERR_CUDA;
+        const int f8_rc = gemm_f8_configure();
+        if (f8_rc == 1) return MLT_ERR_CUDA;
+        d.gemm_f8_ok = f8_rc == 0;
         const int mha_rc = mha_configure();
         if (mha_rc == 1) return MLT_ERR_CUDA;
         d.mha_ok = mha_rc == 0;
@@ -854,38 +855,52 @@ inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3
 
 // Launch plan of the scaled GEMM.
 struct GemmF8Plan {
-    int big;      // 2: CTA pairs on 256 x 256 tiles, 1: 128 x 256 tiles, 0: the kernel for smaller problems, with
-    int bn;       // its tile width
+    int big;      // 2: CTA pairs on 256 x bn tiles, 1: 128 x bn tiles, persistent; 0: one tile per cluster, K cut inside it
+    int bn;       // tile width
     int cluster;  // CTAs per tile that cut K
-    int kb_per_split;
-    int a_rows, stages;
+    int a_rows, stages, bufs;
 };
 
-GemmF8Plan gemm_f8_plan(int64_t M, int64_t N, int64_t K, int sm_count) {
+// cluster_slots: resident CTAs in clusters of 2, 4, 8 as the device reports them, or null for the SM count rounded down
+GemmF8Plan gemm_f8_plan(int64_t M, int64_t N, int64_t K, int sm_count, const int* cluster_slots) {
     const int num_kb = static_cast<int>((K + kF8BK - 1) / kF8BK);
-    GemmF8Plan plan;
-    plan.big = 0;
-    if (M > 128 && N >= 128) plan.big = M > 1024 ? 2 : 1;
-    if (debug_env().f8_bn == 1 || debug_env().f8_bn == 2) plan.big = debug_env().f8_bn;
-    if (debug_env().f8_bn >= 64) plan.big = 0;
-    plan.bn = M <= 128 ? 64 : 128;
-    if (debug_env().f8_bn == 64 || debug_env().f8_bn == 128) plan.bn = debug_env().f8_bn;
+    GemmF8Plan plan = {0, 16, 1, 128, 2, 2};
     plan.a_rows = static_cast<int>(std::min<int64_t>(128, (M + 7) / 8 * 8));
-    const int smem = plan.bn == 64 ? kGemmF8NarrowSmem : kGemmF8WideSmem;
-    const int stage = plan.a_rows * kF8BK + plan.bn * kF8BK;
-    plan.stages = std::min(kF8MaxStages, (smem - 1024 - GemmF8Smem<64>::kBarrierBytes) / stage);
-    const int64_t tiles = ((M + 127) / 128) * ((N + plan.bn - 1) / plan.bn);
-    const int64_t slots = static_cast<int64_t>(sm_count) * (plan.bn == 64 ? 3 : 1);
-    plan.cluster = 1;
-    int64_t best = INT64_MAX;
-    for (int S = 1; S <= 8; S *= 2) {
-        const int kbps = (num_kb + S - 1) / S;
-        if (S > 1 && (kbps < 2 || static_cast<int64_t>(kbps) * (S - 1) >= num_kb)) continue;  // too short, or an empty slice
-        const int64_t cost = (tiles * S + slots - 1) / slots * (kbps + (S > 1 ? 10 : 6));
-        if (cost < best) { best = cost; plan.cluster = S; }
+    const int64_t tiles_m = (M + 127) / 128;
+    auto slots_of = [&](int S) {
+        return S == 1 ? sm_count : cluster_slots ? cluster_slots[S == 2 ? 0 : S == 4 ? 1 : 2] : sm_count / S * S;
+    };
+    double best = 1e300;
+    for (int S = 1; S <= 8 && S <= num_kb; S *= 2) {
+        if (slots_of(S) < S) continue;
+        for (int bn = 16; bn <= 256; bn += 16) {
+            if (bn > 16 && bn - 16 >= N) break;
+            const int64_t tiles = tiles_m * ((N + bn - 1) / bn);
+            const int64_t rounds = (tiles * S + slots_of(S) - 1) / slots_of(S);
+            const double kbs = static_cast<double>((num_kb + S - 1) / S);
+            const double t_kb = std::max((bn + plan.a_rows) * 128.0 / 40.0, 300.0 + bn);
+            const double cost = rounds * (kbs * t_kb + 4000.0 + (S > 1 ? 2000.0 : 0.0));
+            if (cost < best) {
+                best = cost;
+                plan.bn = bn;
+                plan.cluster = S;
+            }
+        }
+    }
+    if (M > 128 && N >= 128) {
+        plan.big = M > 1024 ? 2 : 1;
+        plan.bn = 256;
+    }
+    if (debug_env().f8_bn) {  // development: thousands: which kernel, below: tile width
+        plan.big = debug_env().f8_bn / 1000;
+        plan.bn = debug_env().f8_bn % 1000;
     }
     if (debug_env().f8_split) plan.cluster = debug_env().f8_split;
-    plan.kb_per_split = (num_kb + plan.cluster - 1) / plan.cluster;
+    if (!plan.big) {
+        const int stage = (plan.a_rows + plan.bn) * kF8BK;
+        plan.stages = std::min({kF8MaxStages, (kF8SplitSmem - 1024) / stage, std::max(2, num_kb)});
+        plan.bufs = std::min(4, 512 / plan.bn);
+    }
     return plan;
 }
 
@@ -928,8 +943,9 @@ int mlt_gemm_f8(const void* A, const float* scale_a, const void* B, const float*
         gemm_zero_fill_kernel<<<blocks, 256, 0, st>>>(static_cast<__nv_bfloat16*>(C), ldc, static_cast<int>(M), static_cast<int>(N));
         return cudaGetLastError() == cudaSuccess ? MLT_OK : MLT_ERR_CUDA;
     }
-    const GemmF8Plan plan = gemm_f8_plan(M, N, K, dev.sm_count);
-    const int bm = plan.big == 2 ? 256 : 128, bn = plan.big ? 256 : plan.bn;
+    if (!dev.gemm_f8_ok) return MLT_ERR_UNSUPPORTED;  // this build of the kernels must not be launched (see gemm_f8_configure)
+    const GemmF8Plan plan = gemm_f8_plan(M, N, K, dev.sm_count, dev.cluster_slots);
+    const int bm = plan.big == 2 ? 256 : 128, bn = plan.bn;
     CUtensorMap ta, tb;
     {
         const uint64_t dims[2] = {static_cast<uint64_t>(K), static_cast<uint64_t>(M)};
@@ -941,7 +957,7 @@ int mlt_gemm_f8(const void* A, const float* scale_a, const void* B, const float*
     {
         const uint64_t dims[2] = {static_cast<uint64_t>(K), static_cast<uint64_t>(N)};
         const uint64_t strides[1] = {static_cast<uint64_t>(ldb)};
-        const uint32_t box[2] = {kF8BK, static_cast<uint32_t>(plan.big ? 128 : plan.bn)};
+        const uint32_t box[2] = {kF8BK, static_cast<uint32_t>(plan.big == 2 ? bn / 2 : plan.big ? std::min(bn, 128) : bn)};
         rc = encode_bf16(&tb, B, 2, dims, strides, box, 3);
         if (rc != MLT_OK) return rc;
     }
@@ -960,20 +976,21 @@ int mlt_gemm_f8(const void* A, const float* scale_a, const void* B, const float*
     p.tiles_m = static_cast<int>(tiles_m);
     p.tiles_n = static_cast<int>(tiles_n);
     p.group_m = 16;
-    p.kb_per_split = plan.kb_per_split;
+    p.bn = bn;
+    p.bufs = plan.bufs;
     p.a_rows = plan.a_rows;
     p.stages = plan.stages;
     if (plan.big) {
         CUtensorMap tc;
         const uint64_t dims[2] = {static_cast<uint64_t>(N) & ~7ull, static_cast<uint64_t>(M)};  // TMA stores work in 16-byte units
         const uint64_t strides[1] = {static_cast<uint64_t>(ldc) * 2};
-        const uint32_t box[2] = {64, 32};
-        rc = encode_bf16(&tc, C, 2, dims, strides, box);
+        const uint32_t box[2] = {32, 32};
+        rc = encode_bf16(&tc, C, 2, dims, strides, box, 0, /*swizzle64=*/true);
         if (rc != MLT_OK) return rc;
         p.group_m = tiles_n >= 32 && plan.big == 2 ? 16 : 8;
         const int tiles = static_cast<int>(tiles_m * tiles_n);
         cudaLaunchConfig_t big = {};
-        big.blockDim = dim3(kF8BigThreads);
+        big.blockDim = dim3(kF8Threads);
         big.stream = st;
         cudaLaunchAttribute pair;
         pair.id = cudaLaunchAttributeClusterDimension;
@@ -984,18 +1001,19 @@ int mlt_gemm_f8(const void* A, const float* scale_a, const void* B, const float*
         cudaError_t e;
         if (plan.big == 2) {
             big.gridDim = dim3(2 * std::min(tiles, dev.sm_count / 2));
-            big.dynamicSmemBytes = GemmF8BigSmem<true>::kTotal;
-            e = cudaLaunchKernelEx(&big, gemm_f8_big_kernel<true>, ta, tb, tc, p);
+            big.dynamicSmemBytes = GemmF8BigSmem<true, 256>::kTotal;
+            e = cudaLaunchKernelEx(&big, gemm_f8_big_kernel<true, 256>, ta, tb, tc, p);
         } else {
             big.gridDim = dim3(std::min(tiles, dev.sm_count));
-            big.dynamicSmemBytes = GemmF8BigSmem<false>::kTotal;
-            e = cudaLaunchKernelEx(&big, gemm_f8_big_kernel<false>, ta, tb, tc, p);
+            big.dynamicSmemBytes = GemmF8BigSmem<false, 256>::kTotal;
+            e = cudaLaunchKernelEx(&big, gemm_f8_big_kernel<false, 256>, ta, tb, tc, p);
         }
         return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? MLT_OK : MLT_ERR_CUDA;
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(tiles_m * tiles_n * plan.cluster));
     cfg.blockDim = dim3(kF8Threads);
+    cfg.dynamicSmemBytes = gemm_f8_split_smem(bn, plan.a_rows, plan.stages);
     cfg.stream = st;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeClusterDimension;
@@ -1003,14 +1021,7 @@ int mlt_gemm_f8(const void* A, const float* scale_a, const void* B, const float*
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    cudaError_t e;
-    if (plan.bn == 64) {
-        cfg.dynamicSmemBytes = GemmF8Smem<64>::bytes(plan.a_rows, plan.stages);
-        e = cudaLaunchKernelEx(&cfg, gemm_f8_kernel<64, 3>, ta, tb, p);
-    } else {
-        cfg.dynamicSmemBytes = GemmF8Smem<128>::bytes(plan.a_rows, plan.stages);
-        e = cudaLaunchKernelEx(&cfg, gemm_f8_kernel<128, 1>, ta, tb, p);
-    }
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, gemm_f8_split_kernel, ta, tb, p);
     return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? MLT_OK : MLT_ERR_CUDA;
 }
 
