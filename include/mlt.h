@@ -305,6 +305,13 @@ int mlt_debug_last_clock_mhz(int which, double* mhz);
 int mlt_debug_gemm_plan(int64_t M, int64_t N, int64_t K, size_t workspace_bytes, int sm_count, int* out4);
 
 /*
+ * The launch plan of mlt_gemm_f8 (likewise; sm_count as above).
+ *   out4[0]  0 = one 128 x out4[1] tile per cluster, 1 = 128 x 256 tiles, 2 = CTA pairs on 256 x 256 tiles
+ *   out4[1]  tile width    out4[2]  CTAs per cluster that cut K    out4[3]  shared memory of the first kind in bytes
+ */
+int mlt_debug_gemm_f8_plan(int64_t M, int64_t N, int64_t K, int sm_count, int* out4);
+
+/*
  * Device-side health word.  Kernels never trap: a wait that exceeds its bound
  * records {code, barrier id, block} in a per-device status word and the kernel
  * drains and returns.  This call synchronises the current device, reads and

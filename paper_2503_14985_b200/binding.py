@@ -21,7 +21,7 @@ PAGED_STATIC_SCRATCH_BYTES = 16 * 1024 * 1024
 EXPORTS = ("mlt_gemm", "mlt_gemm_f16", "mlt_gemm_ex", "mlt_gemm_workspace_bytes", "mlt_mha_fwd", "mlt_paged_attn_decode", "mlt_paged_attn_decode_static",
            "mlt_paged_attn_workspace_bytes",
            "mlt_quantize_f8", "mlt_gemm_f8", "mlt_kv_append", "mlt_kv_append_f8", "mlt_paged_attn_decode_f8", "mlt_paged_attn_f8_workspace_bytes",
-           "mlt_last_device_error", "mlt_debug_wait_timeout_selftest", "mlt_debug_last_clock_mhz", "mlt_debug_gemm_plan", "mlt_status_string",
+           "mlt_last_device_error", "mlt_debug_wait_timeout_selftest", "mlt_debug_last_clock_mhz", "mlt_debug_gemm_plan", "mlt_debug_gemm_f8_plan", "mlt_status_string",
            "mlt_version")
 
 _lib = None
@@ -49,6 +49,8 @@ def load() -> ctypes.CDLL:
         lib.mlt_debug_last_clock_mhz.restype = i32
         lib.mlt_debug_gemm_plan.argtypes = [i64, i64, i64, ctypes.c_size_t, i32, ctypes.POINTER(ctypes.c_int)]
         lib.mlt_debug_gemm_plan.restype = i32
+        lib.mlt_debug_gemm_f8_plan.argtypes = [i64, i64, i64, i32, ctypes.POINTER(ctypes.c_int)]
+        lib.mlt_debug_gemm_f8_plan.restype = i32
         lib.mlt_gemm_f16.argtypes = [p, p, p, i64, i64, i64, i64, i64, i64, i32, p]
         lib.mlt_gemm_f16.restype = i32
         lib.mlt_gemm_ex.argtypes = [p, p, p, i64, i64, i64, i64, i64, i64, p, ctypes.c_size_t, p]
@@ -217,6 +219,16 @@ def gemm_plan(M: int, N: int, K: int, workspace_bytes: int = 0, sm_count: int = 
     if rc != MLT_OK:
         raise MltError(rc, "mlt_debug_gemm_plan")
     return {"variant": out[0], "split_k": out[1], "cluster": out[2], "kb_per_split": out[3]}
+
+
+def gemm_f8_plan(M: int, N: int, K: int, sm_count: int = 148) -> dict:
+    """Launch plan of gemm_f8 for a shape: kernel (0: one tile per cluster, 1: 128 x 256 tiles, 2: CTA pairs), tile width, CTAs
+    per K-cutting cluster, shared memory of kernel 0.  sm_count as in gemm_plan."""
+    out = (ctypes.c_int * 4)()
+    rc = int(load().mlt_debug_gemm_f8_plan(M, N, K, sm_count, out))
+    if rc != MLT_OK:
+        raise MltError(rc, "mlt_debug_gemm_f8_plan")
+    return {"kernel": out[0], "tile_n": out[1], "cluster": out[2], "smem": out[3]}
 
 
 def _stream(stream) -> int:

@@ -314,6 +314,15 @@ gemm_f8_split_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_co
     }
 }
 
+// A load that stays where it is written (a prefetch that the compiler would move down to its use); 0 where `there` is false.
+__device__ __forceinline__ float ld_f32_if(const float* p, bool there) {
+    float v;
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\tmov.f32 %0, 0f00000000;\n\t@q ld.global.nc.f32 %0, [%1];\n\t}"
+                 : "=f"(v)
+                 : "l"(p), "r"(static_cast<int>(there)));
+    return v;
+}
+
 // ---------------------------------------------------------------------------------------------------------
 // Large problems: persistent, 256 columns per tile, eight promotion warps (a thread owns one row and 128 columns in
 // registers).
@@ -322,33 +331,34 @@ gemm_f8_split_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_co
 //   else   one CTA owns a 128 x 256 tile
 // The two accumulators in tensor memory (2 x 256 columns) belong to alternate K blocks, across tile borders: while the
 // promotion warps round and store a tile, the tensor core is up to two K blocks into the next one.  Results leave through
-// 2 KB of shared memory per warp (32 rows x 32 columns, 64-byte swizzle) and TMA stores.
+// 4 KB of shared memory per warp (32 rows x 64 columns, 128-byte swizzle) and TMA stores.
 // ---------------------------------------------------------------------------------------------------------
-template <bool kPair, int BN>
+constexpr int kF8BigThreads = 320;  // producer, issuer, eight promotion warps (168 registers per thread)
+template <bool kPair>
 struct GemmF8BigSmem {
     static constexpr int kABytes = 128 * kF8BK;
-    static constexpr int kBBytes = (kPair ? BN / 2 : BN) * kF8BK;
+    static constexpr int kBBytes = (kPair ? 128 : 256) * kF8BK;
     static constexpr int kStageBytes = kABytes + kBBytes;
-    static constexpr int kStages = 192 * 1024 / kStageBytes;
-    static constexpr int kTotal = kStages * kStageBytes + 8 * 2048 + 1024;
+    static constexpr int kStages = kPair ? 6 : 4;
+    static constexpr int kTotal = kStages * kStageBytes + 8 * 4096 + 256 + 1024;
 };
 
-template <bool kPair, int BN>
-__global__ void __launch_bounds__(kF8Threads, 1)
+template <bool kPair>
+__global__ void __launch_bounds__(kF8BigThreads, 1)
 gemm_f8_big_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b,
                    const __grid_constant__ CUtensorMap tmap_c, const GemmF8Params p) {
-    using L = GemmF8BigSmem<kPair, BN>;
+    using L = GemmF8BigSmem<kPair>;
     constexpr int kStages = L::kStages;
-    constexpr int kBufs = 512 / BN;     // accumulators in tensor memory
-    constexpr int kCols = BN / 2;       // columns of a promotion warp
     constexpr int kTileM = kPair ? 256 : 128;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t* staging = smem + kStages * L::kStageBytes;
-    __shared__ uint64_t full[kStages], empty[kStages], acc_full[kBufs], acc_empty[kBufs], scale_full[kF8ScaleSlots], scale_empty[kF8ScaleSlots];
-    __shared__ GemmF8Scales scales[kF8ScaleSlots];
-    __shared__ uint32_t tmem_base_slot[1], abort_word;
-    volatile uint32_t* abort_flag = &abort_word;
+    uint64_t* full = reinterpret_cast<uint64_t*>(staging + 8 * 4096);
+    uint64_t* empty = full + kStages;
+    uint64_t* acc_full = empty + kStages;  // [2]
+    uint64_t* acc_empty = acc_full + 2;    // [2]
+    uint32_t* tmem_base_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
+    volatile uint32_t* abort_flag = tmem_base_slot + 1;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (blockIdx.x == 0 && threadIdx.x == 0) clock_probe(0, 0);
@@ -361,7 +371,7 @@ gemm_f8_big_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
         const int first_m = tile / per_group * p.group_m;
         const int rows = min(p.group_m, p.tiles_m - first_m), r = tile % per_group;
         m0 = (first_m + r % rows) * kTileM + rank * 128;
-        n0 = r / rows * BN;
+        n0 = r / rows * 256;
     };
 
     if (threadIdx.x == 0) {
@@ -369,13 +379,9 @@ gemm_f8_big_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
             mbar_init(&full[s], 1);
             mbar_init(&empty[s], 1);
         }
-        for (int a = 0; a < kBufs; ++a) {
+        for (int a = 0; a < 2; ++a) {
             mbar_init(&acc_full[a], 1);
             mbar_init(&acc_empty[a], kPair ? 16 : 8);  // every promotion warp
-        }
-        for (int a = 0; a < kF8ScaleSlots; ++a) {
-            mbar_init(&scale_full[a], 32);
-            mbar_init(&scale_empty[a], 8);
         }
         *abort_flag = 0;
         fence_mbar_init();
@@ -400,7 +406,6 @@ gemm_f8_big_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
     const uint32_t tmem_base = *tmem_base_slot;
 
     if (warp == 0) {
-        setmaxnreg_dec<kF8OtherRegs>();
         if (lane == 0) {
             int stage = 0;
             uint32_t phase = 0;
@@ -411,37 +416,36 @@ gemm_f8_big_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
                 for (int kb = 0; kb < num_kb; ++kb) {
                     ok = mbar_wait(&empty[stage], phase ^ 1, abort_flag, 0x100 + stage);
                     if (!ok) break;
-                    uint8_t* dst_a = smem + stage * L::kStageBytes;
-                    uint8_t* dst_b = dst_a + L::kABytes;
+                    uint8_t* sa = smem + stage * L::kStageBytes;
+                    uint8_t* sb = sa + L::kABytes;
                     if constexpr (kPair) {
                         if (rank == 0) mbar_arrive_expect_tx(&full[stage], 2 * L::kStageBytes);
                         const uint32_t bar = map_to_cta(smem_u32(&full[stage]), 0);
-                        tma_load_2d_pair(dst_a, &tmap_a, bar, kb * kF8BK, m0);
-                        tma_load_2d_pair(dst_b, &tmap_b, bar, kb * kF8BK, n0 + rank * (BN / 2));
+                        tma_load_2d_pair(sa, &tmap_a, bar, kb * kF8BK, m0);
+                        tma_load_2d_pair(sb, &tmap_b, bar, kb * kF8BK, n0 + rank * 128);
                     } else {
                         mbar_arrive_expect_tx(&full[stage], L::kStageBytes);
-                        tma_load_2d(dst_a, &tmap_a, &full[stage], kb * kF8BK, m0);
-                        tma_load_2d(dst_b, &tmap_b, &full[stage], kb * kF8BK, n0);
-                        if constexpr (BN == 256) tma_load_2d(dst_b + 128 * kF8BK, &tmap_b, &full[stage], kb * kF8BK, n0 + 128);
+                        tma_load_2d(sa, &tmap_a, &full[stage], kb * kF8BK, m0);
+                        tma_load_2d(sb, &tmap_b, &full[stage], kb * kF8BK, n0);
+                        tma_load_2d(sb + 128 * kF8BK, &tmap_b, &full[stage], kb * kF8BK, n0 + 128);
                     }
                     if (++stage == kStages) { stage = 0; phase ^= 1; }
                 }
             }
         }
     } else if (warp == 1) {
-        setmaxnreg_dec<kF8OtherRegs>();
         if (rank == 0) {
             const bool issuer = elect_one();
-            constexpr uint32_t idesc = make_idesc_e4m3(kTileM, BN);
+            constexpr uint32_t idesc = make_idesc_e4m3(kTileM, 256);
             const uint32_t a_lo0 = sdesc_lo(smem_u32(smem), 16), b_lo0 = sdesc_lo(smem_u32(smem + L::kABytes), 16);
             int stage = 0;
             uint32_t phase = 0, use = 0;  // use: K blocks so far
             bool ok = true;
             for (int tile = first; tile < tiles && ok; tile += step) {
                 for (int kb = 0; kb < num_kb; ++kb, ++use) {
-                    const int buf = use % kBufs;
+                    const int buf = use & 1;
                     ok = mbar_wait(&full[stage], phase, abort_flag, 0x200 + stage);
-                    ok = ok && mbar_wait(&acc_empty[buf], ((use / kBufs) & 1) ^ 1, abort_flag, 0x300 + buf);
+                    ok = ok && mbar_wait(&acc_empty[buf], ((use >> 1) & 1) ^ 1, abort_flag, 0x300 + buf);
                     ok = __all_sync(0xffffffffu, ok) != 0;
                     if (!ok) break;
                     tc_fence_after();
@@ -450,9 +454,9 @@ gemm_f8_big_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
 #pragma unroll
                         for (int k = 0; k < kF8BK / 32; ++k) {
                             if constexpr (kPair)
-                                umma_f8_ss_pair_lo(tmem_base + buf * BN, a_lo + k * (32 >> 4), b_lo + k * (32 >> 4), idesc, k != 0);
+                                umma_f8_ss_pair_lo(tmem_base + buf * 256, a_lo + k * (32 >> 4), b_lo + k * (32 >> 4), idesc, k != 0);
                             else
-                                umma_f8_ss_lo(tmem_base + buf * BN, a_lo + k * (32 >> 4), b_lo + k * (32 >> 4), idesc, k != 0);
+                                umma_f8_ss_lo(tmem_base + buf * 256, a_lo + k * (32 >> 4), b_lo + k * (32 >> 4), idesc, k != 0);
                         }
                         if constexpr (kPair) {
                             umma_commit_pair(&empty[stage], 3);
@@ -467,83 +471,84 @@ gemm_f8_big_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
                 }
             }
         }
-    } else if (warp == 2) {
-        setmaxnreg_dec<kF8OtherRegs>();
-        int slot = 0;
-        uint32_t phase = 0;
-        for (int tile = first; tile < tiles; tile += step) {
-            int m0, n0;
-            coords(tile, m0, n0);
-            const int block = min((n0 + (lane >> 1 & 1) * kCols) / 128, (p.N - 1) / 128);  // lane c < 4: of half c / 2
-            if (!gemm_f8_load_scales(scales, scale_full, scale_empty, slot, phase, p.sa + m0, p.ldsa, min(128, p.M - m0), p.sb + block * p.ldsb, 0,
-                                     num_kb, lane, abort_flag))
-                break;
-        }
-    } else if (warp == 3) {
-        setmaxnreg_dec<kF8OtherRegs>();
     } else {
-        setmaxnreg_inc<kF8PromoteRegs>();
-        const int quarter = warp & 3, half = (warp - 4) >> 2;  // 32 rows, kCols columns
-        uint8_t* stg = staging + (warp - 4) * 2048;
-        const uint32_t t_row = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + half * kCols;
-        uint32_t use = 0, slot_phase = 0;
-        int slot = 0;
+        const int quarter = warp & 3, half = (warp - 2) >> 2;  // 32 rows, 128 columns
+        uint8_t* stg = staging + (warp - 2) * 4096;
+        const uint32_t t_row = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + half * 128;
+        uint32_t use = 0;
         bool ok = true;
         for (int tile = first; tile < tiles && ok; tile += step) {
             int m0, n0;
             coords(tile, m0, n0);
-            const int row0 = m0 + quarter * 32, col0 = n0 + half * kCols;
-            float2 acc[kCols / 2];
+            const int row0 = m0 + quarter * 32, col0 = n0 + half * 128;
+            const bool live = row0 + lane < p.M && col0 < p.N;
+            const float* sa = p.sa + row0 + lane;
+            const float* sb = p.sb + static_cast<int64_t>(col0 / 128) * p.ldsb;
+            float2 acc[64];
 #pragma unroll
-            for (int i = 0; i < kCols / 2; ++i) acc[i] = make_float2(0.0f, 0.0f);
-            for (int kb = 0; kb < num_kb; ++kb, ++use) {
-                const int buf = use % kBufs, u = kb & 3;
-                const bool last_of_slot = u == 3 || kb == num_kb - 1;
-                if (u == 0) ok = mbar_wait(&scale_full[slot], slot_phase, abort_flag, 0x500 + slot);
-                const float s = scales[slot].row[u][quarter * 32 + lane] * scales[slot].col[u][half * 2];
-                ok = ok && mbar_wait(&acc_full[buf], (use / kBufs) & 1, abort_flag, 0x400 + buf);
-                ok = __all_sync(0xffffffffu, ok) != 0;
-                if (!ok) break;
-                tc_fence_after();
-                gemm_f8_promote<kCols / 16>(acc, t_row + buf * BN, s, s, kCols / 16, [&] {  // the tensor core may refill the accumulator
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) {
-                        if constexpr (kPair)
-                            mbar_arrive_peer(map_to_cta(smem_u32(&acc_empty[buf]), 0));
-                        else
-                            mbar_arrive(&acc_empty[buf]);
-                        if (last_of_slot) mbar_arrive(&scale_empty[slot]);
+            for (int i = 0; i < 64; ++i) acc[i] = make_float2(0.0f, 0.0f);
+            // the scales of two K blocks at a time, requested two K blocks ahead
+            float s[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) s[u] = ld_f32_if(sa + u * p.ldsa, live && u < num_kb) * ld_f32_if(sb + u, live && u < num_kb);
+            for (int kb2 = 0; kb2 < num_kb && ok; kb2 += 2) {
+                float xa[2], xb[2];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const bool there = live && kb2 + 2 + u < num_kb;
+                    xa[u] = ld_f32_if(sa + (kb2 + 2 + u) * p.ldsa, there);
+                    xb[u] = ld_f32_if(sb + kb2 + 2 + u, there);
+                }
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    if (kb2 + u < num_kb && ok) {
+                        const int buf = use & 1;
+                        ok = __all_sync(0xffffffffu, mbar_wait(&acc_full[buf], (use >> 1) & 1, abort_flag, 0x400 + buf)) != 0;
+                        if (ok) {
+                            tc_fence_after();
+                            gemm_f8_promote<8>(acc, t_row + buf * 256, s[u], s[u], 8, [&] {
+                                tc_fence_before();
+                                __syncwarp();
+                                if (lane == 0) {
+                                    if constexpr (kPair)
+                                        mbar_arrive_peer(map_to_cta(smem_u32(&acc_empty[buf]), 0));
+                                    else
+                                        mbar_arrive(&acc_empty[buf]);
+                                }
+                            });
+                            ++use;
+                        }
                     }
-                });
-                if (last_of_slot && ++slot == kF8ScaleSlots) { slot = 0; slot_phase ^= 1; }
+                }
+#pragma unroll
+                for (int u = 0; u < 2; ++u) s[u] = xa[u] * xb[u];
             }
             if (!ok) break;
-            // ---- round and store: 32 columns at a time ----
+            // ---- round and store: 64 columns at a time ----
             const int n8 = p.N & ~7;  // the tensor map of C ends here (16-byte units)
 #pragma unroll
-            for (int h = 0; h < kCols / 32; ++h) {
-                const int col = col0 + h * 32;
+            for (int h = 0; h < 2; ++h) {
                 if (lane == 0) tma_store_wait_read<0>();
                 __syncwarp();
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const float2* a = acc + h * 16 + q * 4;
-                    *reinterpret_cast<uint4*>(stg + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4)) =
+                for (int q = 0; q < 8; ++q) {
+                    const float2* a = acc + h * 32 + q * 4;
+                    *reinterpret_cast<uint4*>(stg + lane * 128 + ((q ^ (lane & 7)) << 4)) =
                         make_uint4(pack_bf16x2(a[0].x, a[0].y), pack_bf16x2(a[1].x, a[1].y), pack_bf16x2(a[2].x, a[2].y), pack_bf16x2(a[3].x, a[3].y));
                 }
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) {
-                    if (row0 < p.M && col < n8) tma_store_2d(&tmap_c, stg, col, row0);
+                    if (row0 < p.M && col0 + h * 64 < n8) tma_store_2d(&tmap_c, stg, col0 + h * 64, row0);
                     tma_store_commit();
                 }
-                if (n8 != p.N && col <= n8 && n8 < col + 32 && row0 + lane < p.M) {  // the up to seven columns beyond
+                if (n8 != p.N && col0 + h * 64 <= n8 && n8 < col0 + h * 64 + 64 && row0 + lane < p.M) {  // the up to seven columns beyond
                     __nv_bfloat16* crow = p.C + static_cast<int64_t>(row0 + lane) * p.ldc;
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        if (col + 2 * j >= n8 && col + 2 * j < p.N) crow[col + 2 * j] = __float2bfloat16(acc[h * 16 + j].x);
-                        if (col + 2 * j + 1 >= n8 && col + 2 * j + 1 < p.N) crow[col + 2 * j + 1] = __float2bfloat16(acc[h * 16 + j].y);
+                    for (int j = 0; j < 32; ++j) {
+                        const int col = col0 + h * 64 + 2 * j;
+                        if (col >= n8 && col < p.N) crow[col] = __float2bfloat16(acc[h * 32 + j].x);
+                        if (col >= n8 && col + 1 < p.N) crow[col + 1] = __float2bfloat16(acc[h * 32 + j].y);
                     }
                 }
             }
@@ -562,19 +567,16 @@ gemm_f8_big_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
     }
 }
 
-// Once per device.  0: ready, 1: a CUDA call failed, 2: a kernel was compiled with fewer registers than its hand-over moves
-// (it would wait for registers that never come: nothing may be launched).
+// Once per device.  0: ready, 1: a CUDA call failed, 2: the split kernel was compiled with fewer registers than its hand-over
+// moves (it would wait for registers that never come: nothing may be launched).
 inline int gemm_f8_configure() {
-    auto one = [](auto kernel, int smem) {
-        cudaFuncAttributes attr;
-        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess ||
-            cudaFuncGetAttributes(&attr, kernel) != cudaSuccess)
-            return 1;
-        return attr.numRegs >= kF8LaunchRegs ? 0 : 2;
-    };
-    const int rc[] = {one(gemm_f8_split_kernel, kF8SplitSmem), one(gemm_f8_big_kernel<true, 256>, GemmF8BigSmem<true, 256>::kTotal),
-                      one(gemm_f8_big_kernel<false, 256>, GemmF8BigSmem<false, 256>::kTotal)};
-    return *std::max_element(rc, rc + 3);
+    cudaFuncAttributes attr;
+    if (cudaFuncSetAttribute(gemm_f8_split_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kF8SplitSmem) != cudaSuccess ||
+        cudaFuncSetAttribute(gemm_f8_big_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmF8BigSmem<true>::kTotal) != cudaSuccess ||
+        cudaFuncSetAttribute(gemm_f8_big_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmF8BigSmem<false>::kTotal) != cudaSuccess ||
+        cudaFuncGetAttributes(&attr, gemm_f8_split_kernel) != cudaSuccess)
+        return 1;
+    return attr.numRegs >= kF8LaunchRegs ? 0 : 2;
 }
 
 }  // namespace mlt

@@ -154,8 +154,8 @@ int forced_variant() {
     return v;
 }
 
-// Debug only: tuning overrides read once from the environment (0 = not set).  MLT_F8_BN / MLT_F8_SPLIT: tile width and CTAs
-// per tile of the scaled GEMM.  MLT_GEMM_GROUP_M: M-tiles per raster
+// Debug only: tuning overrides read once from the environment (0 = not set).  MLT_F8_BN / MLT_F8_SPLIT: kernel and
+// tile width, and CTAs per tile, of the scaled GEMM (see gemm_f8_plan).  MLT_GEMM_GROUP_M: M-tiles per raster
 // group of the pair kernel; MLT_GEMM_NO_HALF: no half tiles in the last wave; MLT_MHA_HEAD_GROUP / MLT_MHA_GRID: item
 // list grouping and CTA count of the attention kernel; MLT_PAGED_SPLITS: CTAs per (sequence, KV head);
 // MLT_GEMM_WIDE_RATIO: per cent of the current plan's cost below which 128 x 256 tiles in clusters are taken (1: never);
@@ -855,13 +855,20 @@ inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3
 
 // Launch plan of the scaled GEMM.
 struct GemmF8Plan {
-    int big;      // 2: CTA pairs on 256 x bn tiles, 1: 128 x bn tiles, persistent; 0: one tile per cluster, K cut inside it
+    int big;      // 2: CTA pairs on 256 x 256 tiles, 1: 128 x 256 tiles, both persistent; 0: one 128 x bn tile per cluster
     int bn;       // tile width
-    int cluster;  // CTAs per tile that cut K
+    int cluster;  // CTAs per tile that cut K (big = 0)
     int a_rows, stages, bufs;
 };
 
-// cluster_slots: resident CTAs in clusters of 2, 4, 8 as the device reports them, or null for the SM count rounded down
+// The fastest by a time model in nanoseconds, fitted to CUDA-event timings of each kernel on M = 16 .. 4096, N = 200 ..
+// 28672, K = 512 .. 28672 (within 15 % of them but for K that is no multiple of 128, where every kernel is slower):
+//   5 us of launch, fill and drain per round of tiles; one K block takes 500 (pairs) or 520 ns (128 x 256 tiles; 680 with a
+//   single tile row, whose scales come from HBM), 200 + 1.6 bn + 2 a_rows in the split kernel, whose reduction over a cluster
+//   adds 0.7 us; and never less than the operands at the copy bandwidth.
+// Measured where they part: 16 x 28672 x 4096 split kernel 26 us, 128 x 256 tiles 45; 128 x 28672 x 4096 33 against 27;
+// 200 x 5000 x 4200 18 against 26; 512 x 4096 x 4096 21 against 20; 4096^3 122, 128 x 256 tiles 72, pairs 69.
+// cluster_slots: resident CTAs in clusters of 2, 4, 8 as the device reports them, or null for the SM count rounded down.
 GemmF8Plan gemm_f8_plan(int64_t M, int64_t N, int64_t K, int sm_count, const int* cluster_slots) {
     const int num_kb = static_cast<int>((K + kF8BK - 1) / kF8BK);
     GemmF8Plan plan = {0, 16, 1, 128, 2, 2};
@@ -870,30 +877,37 @@ GemmF8Plan gemm_f8_plan(int64_t M, int64_t N, int64_t K, int sm_count, const int
     auto slots_of = [&](int S) {
         return S == 1 ? sm_count : cluster_slots ? cluster_slots[S == 2 ? 0 : S == 4 ? 1 : 2] : sm_count / S * S;
     };
+    auto rounds_of = [](int64_t tiles, int64_t slots) { return static_cast<double>((tiles + slots - 1) / slots); };
+    const double hbm = (static_cast<double>(M) * K + static_cast<double>(N) * K + 2.0 * M * N) / 6.3e3;
     double best = 1e300;
     for (int S = 1; S <= 8 && S <= num_kb; S *= 2) {
         if (slots_of(S) < S) continue;
-        for (int bn = 16; bn <= 256; bn += 16) {
-            if (bn > 16 && bn - 16 >= N) break;
-            const int64_t tiles = tiles_m * ((N + bn - 1) / bn);
-            const int64_t rounds = (tiles * S + slots_of(S) - 1) / slots_of(S);
+        for (int bn = 16; bn <= 256 && (bn == 16 || bn - 16 < N); bn += 16) {
             const double kbs = static_cast<double>((num_kb + S - 1) / S);
-            const double t_kb = std::max((bn + plan.a_rows) * 128.0 / 40.0, 300.0 + bn);
-            const double cost = rounds * (kbs * t_kb + 4000.0 + (S > 1 ? 2000.0 : 0.0));
-            if (cost < best) {
-                best = cost;
+            const double fixed = 5000.0 + (S > 1 ? 700.0 : 0.0);
+            const double t = rounds_of(tiles_m * ((N + bn - 1) / bn) * S, slots_of(S)) *
+                             (kbs * (200.0 + 1.6 * bn + 2.0 * plan.a_rows) + fixed);
+            if (std::max(t, hbm + fixed) < best) {
+                best = std::max(t, hbm + fixed);
                 plan.bn = bn;
                 plan.cluster = S;
             }
         }
     }
-    if (M > 128 && N >= 128) {
-        plan.big = M > 1024 ? 2 : 1;
-        plan.bn = 256;
+    const int split_bn = plan.bn;
+    if (N >= 128) {
+        const int64_t tiles_n = (N + 255) / 256;
+        const double t1 = std::max(rounds_of(tiles_m * tiles_n, sm_count) * num_kb * (M <= 128 ? 680.0 : 520.0), hbm) + 5000.0;
+        const double t2 = std::max(rounds_of((M + 255) / 256 * tiles_n, sm_count / 2) * num_kb * 500.0, hbm) + 5500.0;
+        if (std::min(t1, t2) < best) {
+            plan.big = t2 < t1 && sm_count >= 2 ? 2 : 1;
+            plan.bn = 256;
+            plan.cluster = 1;
+        }
     }
-    if (debug_env().f8_bn) {  // development: thousands: which kernel, below: tile width
-        plan.big = debug_env().f8_bn / 1000;
-        plan.bn = debug_env().f8_bn % 1000;
+    if (debug_env().f8_bn) {  // thousands: which kernel (3: the split kernel at its own width), below: tile width
+        plan.big = debug_env().f8_bn / 1000 % 3;
+        plan.bn = debug_env().f8_bn == 3000 ? split_bn : debug_env().f8_bn % 1000;
     }
     if (debug_env().f8_split) plan.cluster = debug_env().f8_split;
     if (!plan.big) {
@@ -922,6 +936,21 @@ int mlt_quantize_f8(const void* X, void* Q, float* scales, int64_t M, int64_t K,
     const QuantizeParams p = {static_cast<const __nv_bfloat16*>(X), static_cast<uint8_t*>(Q), scales, ldx, ldq, lds,
                               static_cast<int>(M), static_cast<int>(K)};
     return quantize_launch(p, block_rows, static_cast<cudaStream_t>(stream));
+}
+
+int mlt_debug_gemm_f8_plan(int64_t M, int64_t N, int64_t K, int sm_count, int* out4) {
+    if (!out4 || M <= 0 || N <= 0 || K <= 0 || sm_count == 1 || sm_count < 0) return MLT_ERR_INVALID_ARG;
+    DeviceInfo dev;
+    if (sm_count == 0) {  // the current device, with the cluster occupancy it reports
+        const int rc = get_device(&dev);
+        if (rc != MLT_OK) return rc;
+    }
+    const GemmF8Plan plan = gemm_f8_plan(M, N, K, sm_count ? sm_count : dev.sm_count, sm_count ? nullptr : dev.cluster_slots);
+    out4[0] = plan.big;
+    out4[1] = plan.bn;
+    out4[2] = plan.cluster;
+    out4[3] = plan.big ? 0 : gemm_f8_split_smem(plan.bn, plan.a_rows, plan.stages);
+    return MLT_OK;
 }
 
 int mlt_gemm_f8(const void* A, const float* scale_a, const void* B, const float* scale_b, void* C, int64_t M, int64_t N,
@@ -984,13 +1013,13 @@ int mlt_gemm_f8(const void* A, const float* scale_a, const void* B, const float*
         CUtensorMap tc;
         const uint64_t dims[2] = {static_cast<uint64_t>(N) & ~7ull, static_cast<uint64_t>(M)};  // TMA stores work in 16-byte units
         const uint64_t strides[1] = {static_cast<uint64_t>(ldc) * 2};
-        const uint32_t box[2] = {32, 32};
-        rc = encode_bf16(&tc, C, 2, dims, strides, box, 0, /*swizzle64=*/true);
+        const uint32_t box[2] = {64, 32};
+        rc = encode_bf16(&tc, C, 2, dims, strides, box);
         if (rc != MLT_OK) return rc;
         p.group_m = tiles_n >= 32 && plan.big == 2 ? 16 : 8;
         const int tiles = static_cast<int>(tiles_m * tiles_n);
         cudaLaunchConfig_t big = {};
-        big.blockDim = dim3(kF8Threads);
+        big.blockDim = dim3(kF8BigThreads);
         big.stream = st;
         cudaLaunchAttribute pair;
         pair.id = cudaLaunchAttributeClusterDimension;
@@ -1001,12 +1030,12 @@ int mlt_gemm_f8(const void* A, const float* scale_a, const void* B, const float*
         cudaError_t e;
         if (plan.big == 2) {
             big.gridDim = dim3(2 * std::min(tiles, dev.sm_count / 2));
-            big.dynamicSmemBytes = GemmF8BigSmem<true, 256>::kTotal;
-            e = cudaLaunchKernelEx(&big, gemm_f8_big_kernel<true, 256>, ta, tb, tc, p);
+            big.dynamicSmemBytes = GemmF8BigSmem<true>::kTotal;
+            e = cudaLaunchKernelEx(&big, gemm_f8_big_kernel<true>, ta, tb, tc, p);
         } else {
             big.gridDim = dim3(std::min(tiles, dev.sm_count));
-            big.dynamicSmemBytes = GemmF8BigSmem<false, 256>::kTotal;
-            e = cudaLaunchKernelEx(&big, gemm_f8_big_kernel<false, 256>, ta, tb, tc, p);
+            big.dynamicSmemBytes = GemmF8BigSmem<false>::kTotal;
+            e = cudaLaunchKernelEx(&big, gemm_f8_big_kernel<false>, ta, tb, tc, p);
         }
         return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? MLT_OK : MLT_ERR_CUDA;
     }
