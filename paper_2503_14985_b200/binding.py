@@ -317,29 +317,46 @@ def paged_attn_decode(Q, K_cache, V_cache, block_table, seq_lens, *, scale: floa
     return O, LSE
 
 
-def _on_device(tensors, stream, call):
-    """Runs call(stream address) with the tensors' device current; they must all be CUDA tensors of one device."""
-    import torch
-    index = tensors[0].device.index
-    for t in tensors:
-        if not t.is_cuda or t.device.index != index:
-            raise ValueError("all tensors must be on one CUDA device")
-    if torch.cuda.current_device() == index:
-        return call(_stream(stream))
-    with torch.cuda.device(index):
-        return call(_stream(stream))
+_f8_dtype = None
 
 
 def _f8():
+    global _f8_dtype
+    if _f8_dtype is None:
+        import torch
+        _f8_dtype = torch.float8_e4m3fn
+    return _f8_dtype
+
+
+def _call(name, fn, tensors, args, stream):
+    """fn(*args, stream address) with the tensors' device current; they must all be CUDA tensors of one device.
+
+    The stream is torch's current one of that device (asked for by its raw handle: building a torch.cuda.Stream object
+    takes 3 us), or the caller's.
+    """
     import torch
-    return torch.float8_e4m3fn
+    index = tensors[0].get_device()
+    for t in tensors:
+        if t.get_device() != index:
+            index = -1
+    if index < 0:
+        raise ValueError("all tensors must be on one CUDA device")
+    st = torch._C._cuda_getCurrentRawStream(index) if stream is None else _stream(stream)
+    if torch._C._cuda_getDevice() == index:
+        rc = fn(*args, st)
+    else:
+        with torch.cuda.device(index):
+            rc = fn(*args, st)
+    if rc != MLT_OK:
+        raise MltError(rc, name)
 
 
 def _pitch(t, width):
     """Row pitch of a 2-D tensor with unit inner stride (of a single row: any pitch serves)."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+    st = t.stride()
+    if len(st) != 2 or (st[1] != 1 and t.shape[1] > 1):
         raise ValueError("matrices must be 2-D with unit inner stride")
-    return t.stride(0) if t.shape[0] > 1 else width
+    return st[0] if t.shape[0] > 1 else width
 
 
 def quantize_f8(X, *, block_rows: int = 1, Q=None, scales=None, stream=None):
@@ -358,21 +375,29 @@ def quantize_f8(X, *, block_rows: int = 1, Q=None, scales=None, stream=None):
     up16 = (K + 15) // 16 * 16
     kb = (K + 127) // 128
     shape = (kb, M) if block_rows == 1 else ((M + 127) // 128, kb)
+    ldx = _pitch(X, (K + 7) // 8 * 8)
     if Q is None:
-        Q = torch.empty((M, up16), dtype=_f8(), device=X.device)
+        Q = X.new_empty((M, up16), dtype=_f8())
         if up16 != K:
             Q = Q[:, :K]
+        ldq = up16
+    elif Q.dtype != _f8():
+        raise TypeError("Q must be float8_e4m3fn")
+    elif Q.shape != X.shape:
+        raise ValueError("Q must have the shape of X")
+    else:
+        ldq = _pitch(Q, up16)
     if scales is None:
-        scales = torch.empty(shape, dtype=torch.float32, device=X.device)
-    if Q.dtype != _f8() or scales.dtype != torch.float32:
-        raise TypeError("Q must be float8_e4m3fn and scales float32")
-    if tuple(Q.shape) != (M, K) or tuple(scales.shape) != shape:
-        raise ValueError("shape mismatch")
-    ldx, ldq, lds = _pitch(X, (K + 7) // 8 * 8), _pitch(Q, up16), _pitch(scales, shape[1])
-    rc = _on_device((X, Q, scales), stream, lambda st: quantize_f8_raw(X.data_ptr(), Q.data_ptr(), scales.data_ptr(), M, K, ldx, ldq,
-                                                                       lds, block_rows, st))
-    if rc != MLT_OK:
-        raise MltError(rc, "mlt_quantize_f8")
+        scales = X.new_empty(shape, dtype=torch.float32)
+        lds = shape[1]
+    elif scales.dtype != torch.float32:
+        raise TypeError("scales must be float32")
+    elif tuple(scales.shape) != shape:
+        raise ValueError(f"scales must be {shape}")
+    else:
+        lds = _pitch(scales, shape[1])
+    _call("mlt_quantize_f8", load().mlt_quantize_f8, (X, Q, scales),
+          (X.data_ptr(), Q.data_ptr(), scales.data_ptr(), M, K, ldx, ldq, lds, block_rows), stream)
     return Q, scales
 
 
@@ -383,38 +408,41 @@ def gemm_f8(A, scale_a, B, scale_b, C=None, *, stream=None):
     from the tensors' strides (A, B: multiples of 16 bytes; C: of 8 elements; a new C has N rounded up to 8).
     """
     import torch
-    if A.dtype != _f8() or B.dtype != _f8() or scale_a.dtype != torch.float32 or scale_b.dtype != torch.float32:
+    f8, f32 = _f8(), torch.float32
+    if A.dtype != f8 or B.dtype != f8 or scale_a.dtype != f32 or scale_b.dtype != f32:
         raise TypeError("A and B must be float8_e4m3fn, the scales float32")
-    (M, K), N = A.shape, B.shape[0]
+    (M, K), (N, Kb) = A.shape, B.shape
     kb = (K + 127) // 128
-    if B.shape[1] != K or tuple(scale_a.shape) != (kb, M) or tuple(scale_b.shape) != ((N + 127) // 128, kb):
+    if Kb != K or tuple(scale_a.shape) != (kb, M) or tuple(scale_b.shape) != ((N + 127) // 128, kb):
         raise ValueError("shape mismatch")
     up8, up16 = (N + 7) // 8 * 8, (K + 15) // 16 * 16
     if C is None:
-        C = torch.empty((M, up8), dtype=torch.bfloat16, device=A.device)
+        C = A.new_empty((M, up8), dtype=torch.bfloat16)
         if up8 != N:
             C = C[:, :N]
+        ldc = up8
     elif C.dtype != torch.bfloat16 or tuple(C.shape) != (M, N):
         raise ValueError("C must be bfloat16 [M, N]")
-    lda, ldb, ldc, ldsa, ldsb = _pitch(A, up16), _pitch(B, up16), _pitch(C, up8), _pitch(scale_a, M), _pitch(scale_b, kb)
-    rc = _on_device((A, scale_a, B, scale_b, C), stream,
-                    lambda st: gemm_f8_raw(A.data_ptr(), scale_a.data_ptr(), B.data_ptr(), scale_b.data_ptr(), C.data_ptr(), M, N, K,
-                                           lda, ldb, ldc, ldsa, ldsb, st))
-    if rc != MLT_OK:
-        raise MltError(rc, "mlt_gemm_f8")
+    else:
+        ldc = _pitch(C, up8)
+    _call("mlt_gemm_f8", load().mlt_gemm_f8, (A, scale_a, B, scale_b, C),
+          (A.data_ptr(), scale_a.data_ptr(), B.data_ptr(), scale_b.data_ptr(), C.data_ptr(), M, N, K, _pitch(A, up16), _pitch(B, up16),
+           ldc, _pitch(scale_a, M), _pitch(scale_b, kb)), stream)
     return C
 
 
 def _rows(t, heads, D):
     """Token pitch of [T, heads, D] whose heads lie side by side."""
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != D or t.stride(2) != 1 or (heads > 1 and t.stride(1) != D):
+    st, sh = t.stride(), t.shape
+    if len(sh) != 3 or sh[1] != heads or sh[2] != D or st[2] != 1 or (heads > 1 and st[1] != D):
         raise ValueError("queries, keys and values must be [tokens, heads, D] with a token's heads side by side")
-    return t.stride(0) if t.shape[0] > 1 else heads * D
+    return st[0] if sh[0] > 1 else heads * D
 
 
 def _kv_append(name, Q, K, V, cos, sin, cu_tokens, context_lens, block_table, K_cache, V_cache, scales, interleaved, Q_out, stream):
     import torch
-    bf16, cache_type = torch.bfloat16, _f8() if scales else torch.bfloat16
+    bf16, f32, i32 = torch.bfloat16, torch.float32, torch.int32
+    cache_type = _f8() if scales else bf16
     if K.dtype != bf16 or V.dtype != bf16 or (Q is not None and Q.dtype != bf16):
         raise TypeError("Q, K and V must be bfloat16")
     if K_cache.dtype != cache_type or V_cache.dtype != cache_type or not K_cache.is_contiguous() or not V_cache.is_contiguous():
@@ -424,46 +452,48 @@ def _kv_append(name, Q, K, V, cos, sin, cu_tokens, context_lens, block_table, K_
     if V_cache.shape != K_cache.shape or V.shape != K.shape or (Q is not None and Q.shape[0] != T):
         raise ValueError("shape mismatch")
     for t in (cu_tokens, context_lens, block_table):
-        if t.dtype != torch.int32 or not t.is_contiguous():
+        if t.dtype != i32 or not t.is_contiguous():
             raise TypeError("cu_tokens, context_lens and block_table must be contiguous int32 tensors")
-    S = context_lens.shape[0]
-    if cu_tokens.shape[0] != S + 1 or block_table.dim() != 2 or block_table.shape[0] != S:
+    S, table = context_lens.shape[0], block_table.shape
+    if cu_tokens.shape[0] != S + 1 or len(table) != 2 or table[0] != S:
         raise ValueError("cu_tokens must be [sequences + 1], block_table [sequences, blocks]")
-    for t in scales:
-        if t.dtype != torch.float32 or not t.is_contiguous() or tuple(t.shape) != (num_blocks, H_kv):
-            raise TypeError("k_scale and v_scale must be contiguous float32 [num_blocks, H_kv] tensors")
+    held = [K, V, K_cache, V_cache, cu_tokens, context_lens, block_table]
+    ks = vs = ()
+    if scales:
+        for t in scales:
+            if t.dtype != f32 or not t.is_contiguous() or tuple(t.shape) != (num_blocks, H_kv):
+                raise TypeError("k_scale and v_scale must be contiguous float32 [num_blocks, H_kv] tensors")
+        held += scales
+        ks, vs = (scales[0].data_ptr(),), (scales[1].data_ptr(),)
     ldk, ldv = _rows(K, H_kv, D), _rows(V, H_kv, D)
-    H = ldq = ldqo = rotary = top = 0
-    held = [K, V, K_cache, V_cache, cu_tokens, context_lens, block_table, *scales]
+    H = ldq = ldqo = rotary = top = q = qo = c = s = 0
     if Q is not None:
         H = Q.shape[1]
         ldq = _rows(Q, H, D)
         if Q_out is None:
-            Q_out = torch.empty((T, H, D), dtype=bf16, device=Q.device)
+            Q_out = Q.new_empty((T, H, D))
+            ldqo = H * D
         elif Q_out.dtype != bf16 or Q_out.shape != Q.shape:
             raise ValueError("Q_out must be bfloat16 of Q's shape")
-        ldqo = _rows(Q_out, H, D)
-        held += [Q, Q_out]
+        else:
+            ldqo = _rows(Q_out, H, D)
+        held += (Q, Q_out)
+        q, qo = Q.data_ptr(), Q_out.data_ptr()
     if (cos is None) != (sin is None):
         raise ValueError("cos and sin come together")
     if cos is not None:
-        if cos.dtype != torch.float32 or sin.dtype != torch.float32 or not cos.is_contiguous() or not sin.is_contiguous():
+        if cos.dtype != f32 or sin.dtype != f32 or not cos.is_contiguous() or not sin.is_contiguous():
             raise TypeError("cos and sin must be contiguous float32 tensors")
-        if cos.dim() != 2 or cos.shape != sin.shape:
+        if cos.shape != sin.shape or cos.dim() != 2:
             raise ValueError("cos and sin must be [positions, rotary_dim / 2]")
-        top, rotary = cos.shape[0], 2 * cos.shape[1]
-        held += [cos, sin]
-
-    def ptr(t):
-        return t.data_ptr() if t is not None else 0
-
-    raw = kv_append_f8_raw if scales else kv_append_raw
-    rc = _on_device(held, stream, lambda st: raw(
-        ptr(Q), K.data_ptr(), V.data_ptr(), ptr(cos), ptr(sin), cu_tokens.data_ptr(), context_lens.data_ptr(), block_table.data_ptr(),
-        ptr(Q_out) if Q is not None else 0, K_cache.data_ptr(), V_cache.data_ptr(), *[t.data_ptr() for t in scales], T, S, H, H_kv, D, rotary,
-        int(bool(interleaved)), block_size, block_table.shape[1], num_blocks, top, ldq, ldk, ldv, ldqo, st))
-    if rc != MLT_OK:
-        raise MltError(rc, name)
+        top, rotary = cos.shape
+        rotary *= 2
+        held += (cos, sin)
+        c, s = cos.data_ptr(), sin.data_ptr()
+    _call(name, load().mlt_kv_append_f8 if scales else load().mlt_kv_append, held,
+          (q, K.data_ptr(), V.data_ptr(), c, s, cu_tokens.data_ptr(), context_lens.data_ptr(), block_table.data_ptr(), qo, K_cache.data_ptr(),
+           V_cache.data_ptr(), *ks, *vs, T, S, H, H_kv, D, rotary, 1 if interleaved else 0, block_size, table[1], num_blocks, top, ldq, ldk, ldv,
+           ldqo), stream)
     return Q_out if Q is not None else None
 
 
@@ -515,15 +545,18 @@ def paged_attn_decode_f8(Q, K_cache, V_cache, k_scale, v_scale, block_table, seq
     elif O.dtype != torch.bfloat16 or O.shape != Q.shape or not O.is_contiguous():
         raise ValueError("O must be contiguous bfloat16 of Q's shape")
     if LSE is None and return_lse:
-        LSE = torch.empty((S, H), dtype=torch.float32, device=Q.device)
+        LSE = Q.new_empty((S, H), dtype=torch.float32)
     elif LSE is not None and (LSE.dtype != torch.float32 or tuple(LSE.shape) != (S, H) or not LSE.is_contiguous()):
         raise ValueError("LSE must be contiguous float32 [S, H]")
     held = [Q, K_cache, V_cache, k_scale, v_scale, block_table, seq_lens, O]
-    held += [t for t in (LSE, workspace) if t is not None]
-    rc = _on_device(held, stream, lambda st: paged_attn_decode_f8_raw(
-        Q.data_ptr(), K_cache.data_ptr(), V_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), block_table.data_ptr(),
-        seq_lens.data_ptr(), O.data_ptr(), LSE.data_ptr() if LSE is not None else 0, S, H, H_kv, D, bs, block_table.shape[1], NB, float(scale),
-        workspace.data_ptr() if workspace is not None else 0, workspace.numel() * workspace.element_size() if workspace is not None else 0, st))
-    if rc != MLT_OK:
-        raise MltError(rc, "mlt_paged_attn_decode_f8")
+    lse = ws = ws_bytes = 0
+    if LSE is not None:
+        held.append(LSE)
+        lse = LSE.data_ptr()
+    if workspace is not None:
+        held.append(workspace)
+        ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    _call("mlt_paged_attn_decode_f8", load().mlt_paged_attn_decode_f8, held,
+          (Q.data_ptr(), K_cache.data_ptr(), V_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), block_table.data_ptr(),
+           seq_lens.data_ptr(), O.data_ptr(), lse, S, H, H_kv, D, bs, block_table.shape[1], NB, float(scale), ws, ws_bytes), stream)
     return O, LSE
