@@ -3,7 +3,9 @@
 //
 // Bound by HBM: 2 * len * D bytes per (sequence, KV head), half of the BF16 cache's.  At the copy bandwidth an SM gets
 // about 23 cache elements per clock, too many for the FP32 pipe (convert, multiply, add for each query head), so both
-// products run on warp-level tensor-core MMAs (m16n8k16, FP16) for every group size, with the group's query heads as rows.
+// products run on warp-level tensor-core MMAs (m16n8k16, FP16) for every group size: S^T = K Q^T with 16 tokens as rows and
+// the group's query heads as the 8 columns, O^T = V^T P^T with 16 elements of D as rows.  (Heads as rows would leave half of
+// every MMA empty, and of the accumulators: 64 MMAs of 8 clocks per 32 tokens instead of 32 kept the streams waiting.)
 // E4M3 to FP16 is exact (one conversion instruction per two elements).
 //   * Q is scaled by a power of two per row into FP16's range (its 8 significant bits fit), exact but for elements more
 //     than 2^28 below the row's largest.
@@ -51,10 +53,15 @@ constexpr int paged_f8_smem_bytes() {
     return kPagedWarps * kPagedRing * 2 * kPagedF8Unit * D + 1024;
 }
 
-__device__ __forceinline__ void mma_f16_16816(float (&c)[4], uint32_t a0, uint32_t a2, uint32_t b0, uint32_t b1) {  // rows 8..15 of A are zero
+__device__ __forceinline__ void mma_f16_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                 : "r"(a0), "r"(0u), "r"(a2), "r"(0u), "r"(b0), "r"(b1));
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t v) {  // lane (g, tg): row g, columns 2 tg, 2 tg + 1 -> the same of the transpose
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
 }
 __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
     uint32_t r;
@@ -71,6 +78,12 @@ __device__ __forceinline__ int paged_f8_chunks(const PagedF8Params& p, int s, in
 // chunks per CTA
 __device__ __forceinline__ long long paged_f8_quota(long long n, int ctas) { return max(1ll, (n + ctas - 1) / ctas); }
 
+// Every thread of the grid asks for its share of the lines of [base, base + bytes).
+__device__ __forceinline__ void l2_prefetch(const void* base, int64_t bytes) {
+    for (int64_t at = (static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x) * 128; at < bytes; at += static_cast<int64_t>(gridDim.x) * blockDim.x * 128)
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const char*>(base) + at));
+}
+
 template <int D, int G, int BS>
 __global__ void __launch_bounds__(kPagedThreads, kPagedF8CtasPerSm)
 paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const PagedF8Params p) {
@@ -78,7 +91,7 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
     static_assert(kPagedRing == 2, "the loop below keeps one unit in use and one in flight");
     constexpr int U = kPagedF8Unit;
     constexpr int PP = D / 64;       // 16-byte pieces of a token's K per lane
-    constexpr int NT = D / 8;        // column tiles of the output
+    constexpr int MT = D / 16;       // row tiles of the output
     constexpr int NB = U / BS;       // cache blocks per unit
     constexpr int kUnitBytes = 2 * U * D;
     __shared__ float2 sm_ml[kPagedWarps][G];
@@ -101,6 +114,11 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
         prefetch_tensormap(&tmap_v);
     }
 
+    // The lengths, the table entries they lead to and the cache those point at are three memory latencies in a row: while the
+    // first is under way, the CTAs together bring the table and the queries into L2.
+    l2_prefetch(p.block_table, static_cast<int64_t>(p.num_seqs) * p.max_blocks * 4);
+    l2_prefetch(p.Q, static_cast<int64_t>(p.num_seqs) * p.H * D * 2);
+
     // ---- which segments (row, token range) this CTA works on ----
     int seg_s, seg_kvh = 0, seg_tok_begin = 0, seg_tok_end = 0;
     bool seg_whole = true;  // the row lies inside this CTA's share
@@ -115,7 +133,11 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
         const int per = (S + kPagedThreads - 1) / kPagedThreads;
         const int s_lo = min(S, static_cast<int>(threadIdx.x) * per), s_hi = min(S, s_lo + per);
         int sum = 0;
-        for (int s2 = s_lo; s2 < s_hi; ++s2) sum += paged_f8_chunks(p, s2, BS);
+        for (int s2 = s_lo; s2 < s_hi; ++s2) {
+            const int c = paged_f8_chunks(p, s2, BS);
+            sm_pre[s2 + 1] = c;
+            sum += c;
+        }
         int incl = sum;
 #pragma unroll
         for (int w = 1; w < 32; w <<= 1) {
@@ -131,10 +153,7 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
             total += sm_red[w];
         }
         if (threadIdx.x == 0) sm_pre[0] = 0;
-        for (int s2 = s_lo; s2 < s_hi; ++s2) {
-            before += paged_f8_chunks(p, s2, BS);
-            sm_pre[s2 + 1] = before;
-        }
+        for (int s2 = s_lo; s2 < s_hi; ++s2) sm_pre[s2 + 1] = before += sm_pre[s2 + 1];
         __syncthreads();
         const long long n = static_cast<long long>(total) * p.H_kv;
         bal_q = paged_f8_quota(n, p.ctas);
@@ -172,44 +191,20 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
     const int s = seg_s, kvh = seg_kvh, tok_begin = seg_tok_begin, tok_end = seg_tok_end;
     const int head0 = kvh * G;
 
-    // Q as A fragments in FP16: lane (g, tg) holds elements tg * D / 4 .. of head g, scaled by 2^-qexp
-    uint32_t qa[PP][4][2];
-    float c_row;  // scores of row g in log2 units, before K's scale
-    {
-        uint4 v[2 * PP];
+    uint4 q_raw[2 * PP];  // lane (g, tg): elements tg * D / 4 .. of head g
 #pragma unroll
-        for (int i = 0; i < 2 * PP; ++i) {
-            v[i] = make_uint4(0u, 0u, 0u, 0u);
-            if (g < G) v[i] = *reinterpret_cast<const uint4*>(p.Q + (static_cast<int64_t>(s) * p.H + head0 + g) * D + tg * (D / 4) + i * 8);
-        }
-        float amax = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 2 * PP; ++i) {
-            float f[8];
-            bf16x8_to_f32(v[i], f);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) amax = fmaxf(amax, abs_if_finite(f[e]));
-        }
-        amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-        amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-        const int qexp = max(-100, static_cast<int>(__float_as_uint(amax) >> 23) - 127 - 14);  // the largest element becomes 2^14 .. 2^15
-        const float down = pow2f(-qexp);
-        c_row = p.scale_log2e * pow2f(qexp);
-#pragma unroll
-        for (int i = 0; i < 2 * PP; ++i) {
-            float f[8];
-            bf16x8_to_f32(v[i], f);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) qa[i >> 1][(i & 1) * 2 + (e >> 1)][e & 1] = pack_f16x2(f[2 * e] * down, f[2 * e + 1] * down);
-        }
+    for (int i = 0; i < 2 * PP; ++i) {
+        q_raw[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (g < G) q_raw[i] = *reinterpret_cast<const uint4*>(p.Q + (static_cast<int64_t>(s) * p.H + head0 + g) * D + tg * (D / 4) + i * 8);
     }
-    float oacc[NT][4];
+    float oacc[MT][4];  // elements g * MT * 2 + 2 mt (0, 1) and + 1 (2, 3) of D for heads 2 tg (0, 2) and 2 tg + 1 (1, 3)
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+    for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) oacc[nt][i] = 0.0f;
-    float m_run = -INFINITY, l_part = 0.0f;  // head g: running max (log2 units), this lane's share of the sum (times 2^14)
-    float v_ref = 0.0f;                      // the accumulators hold sums of p * 2^14 * vs / v_ref * V
+        for (int i = 0; i < 4; ++i) oacc[mt][i] = 0.0f;
+    float m_run[2] = {-INFINITY, -INFINITY};  // of the two heads: running max (log2 units, the same in all lanes of a tg)
+    float l_part[2] = {0.0f, 0.0f};           // ... this lane's share of the sum (times 2^14)
+    float v_ref = 0.0f;                       // the accumulators hold sums of p * 2^14 * vs / v_ref * V
 
     const int* table = p.block_table + static_cast<int64_t>(s) * p.max_blocks;
     struct Meta {  // of a unit whose copies are under way: which of its tokens count, and its blocks' scales
@@ -224,20 +219,15 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
     int tab[NB];
     float tks[NB], tvs[NB];
     int tab_base = -64;
-    auto issue_unit = [&](Meta& meta, int stage, int k) {
+    auto issue_unit = [&](Meta& meta, int stage, int k) {  // (take_scales fills in the scales)
         const int u0 = first + k * kStep;
+        bool fresh = false;
         if (k >= tab_base + 32) {
             tab_base = k;
             const int n = k + lane < n_units ? tok_end - (first + (k + lane) * kStep) : 0;  // tokens of unit k + lane and beyond
 #pragma unroll
             for (int i = 0; i < NB; ++i) tab[i] = i * BS < n ? table[(first + (k + lane) * kStep) / BS + i] : 0;
-#pragma unroll
-            for (int i = 0; i < NB; ++i) {
-                const bool there = i * BS < n && tab[i] >= 0 && tab[i] < p.num_blocks;
-                const int64_t at = static_cast<int64_t>(tab[i]) * p.H_kv + kvh;
-                tks[i] = there ? __ldg(p.ks + at) : 0.0f;
-                tvs[i] = there ? __ldg(p.vs + at) : 0.0f;
-            }
+            fresh = true;
         }
         const int left = tok_end - u0;
         meta.vis = left >= U ? 0xFFFFFFFFu : (1u << left) - 1u;
@@ -271,74 +261,143 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                     tma_load_3d(dst + (lane & 1) * (U * D) + i * BS * D, (lane & 1) ? &tmap_v : &tmap_k, bar, 0, 0, phys[i] * p.H_kv + kvh);
             __syncwarp();
         }
+        if (fresh) {  // (behind the copies: the scales are only needed when the unit is used)
+            const int n = k + lane < n_units ? tok_end - (first + (k + lane) * kStep) : 0;
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+                const bool there = i * BS < n && tab[i] >= 0 && tab[i] < p.num_blocks;
+                const int64_t at = static_cast<int64_t>(tab[i]) * p.H_kv + kvh;
+                tks[i] = there ? __ldg(p.ks + at) : 0.0f;
+                tvs[i] = there ? __ldg(p.vs + at) : 0.0f;
+            }
+        }
+    };
+    auto take_scales = [&](Meta& meta, int k) {  // of unit k, while the lanes hold its batch
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
             meta.ks[i] = __shfl_sync(0xffffffffu, tks[i], k - tab_base);
             meta.vs[i] = __shfl_sync(0xffffffffu, tvs[i], k - tab_base);
         }
     };
+    Meta cur, next;
+    cur.vis = next.vis = 0;
+    if (n_units > 0) issue_unit(cur, kbase & 1, 0);  // the first copies are under way before the queries are read
+
+    // Q^T as B fragments in FP16: lane (g, tg) holds elements tg * D / 4 .. of head g, scaled by 2^-qexp
+    uint32_t qb[PP][4][2];
+    float c_head[2];  // of heads 2 tg, 2 tg + 1: scores to log2 units, before K's scale
+    {
+        const uint4 (&v)[2 * PP] = q_raw;
+        float amax = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 2 * PP; ++i) {
+            float f[8];
+            bf16x8_to_f32(v[i], f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) amax = fmaxf(amax, abs_if_finite(f[e]));
+        }
+        amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+        amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+        const int qexp = max(-100, static_cast<int>(__float_as_uint(amax) >> 23) - 127 - 14);  // the largest element becomes 2^14 .. 2^15
+        const float down = pow2f(-qexp);
+        const float c_row = p.scale_log2e * pow2f(qexp);
+        c_head[0] = __shfl_sync(0xffffffffu, c_row, 8 * tg);
+        c_head[1] = __shfl_sync(0xffffffffu, c_row, 8 * tg + 4);
+#pragma unroll
+        for (int i = 0; i < 2 * PP; ++i) {
+            float f[8];
+            bf16x8_to_f32(v[i], f);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) qb[i >> 1][(i & 1) * 2 + (e >> 1)][e & 1] = pack_f16x2(f[2 * e] * down, f[2 * e + 1] * down);
+        }
+    }
     // byte offset of 16-byte piece c of token row r in a swizzled [tokens][D] tile
     auto at16 = [](int r, int c) { return D == 128 ? r * 128 + ((c ^ (r & 7)) << 4) : r * 64 + ((c ^ ((r >> 1) & 3)) << 4); };
     auto compute_unit = [&](const Meta& meta, int stage) {
         const uint8_t* ku = my_ring + stage * kUnitBytes;
         const uint8_t* vu = ku + U * D;
-        // ---- scores of head g for tokens 8 e + 2 tg, + 1 ----
+        // ---- scores of tokens 8 e + g for heads 2 tg, 2 tg + 1 ----
         float x[U / 8][2];
 #pragma unroll
-        for (int e = 0; e < U / 8; ++e) {
+        for (int h = 0; h < U / 16; ++h) {
             float sc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int pp = 0; pp < PP; ++pp) {
-                const uint4 w = *reinterpret_cast<const uint4*>(ku + at16(8 * e + g, PP * tg + pp));
-                const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+                const uint4 lo = *reinterpret_cast<const uint4*>(ku + at16(16 * h + g, PP * tg + pp));
+                const uint4 hi = *reinterpret_cast<const uint4*>(ku + at16(16 * h + 8 + g, PP * tg + pp));
+                const uint32_t wl[4] = {lo.x, lo.y, lo.z, lo.w}, wh[4] = {hi.x, hi.y, hi.z, hi.w};
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    uint32_t b0, b1;
-                    f16x2_from_f8x4(ww[j], b0, b1);
-                    mma_f16_16816(sc, qa[pp][j][0], qa[pp][j][1], b0, b1);
+                    uint32_t a0, a1, a2, a3;
+                    f16x2_from_f8x4(wl[j], a0, a2);
+                    f16x2_from_f8x4(wh[j], a1, a3);
+                    mma_f16_16816(sc, a0, a1, a2, a3, qb[pp][j][0], qb[pp][j][1]);
                 }
             }
-            const float f = c_row * meta.ks[8 * e / BS];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) x[e][i] = (meta.vis >> (8 * e + 2 * tg + i)) & 1u ? sc[i] * f : -INFINITY;
+            for (int i = 0; i < 2; ++i) {  // tiles e = 2 h + i, each inside one cache block
+                const int e = 2 * h + i;
+                const float ks = meta.ks[8 * e / BS];
+                x[e][0] = sc[2 * i] * (c_head[0] * ks);
+                x[e][1] = sc[2 * i + 1] * (c_head[1] * ks);
+            }
         }
-        float mb = fmaxf(x[0][0], x[0][1]);
+        if (meta.vis != 0xFFFFFFFFu) {
 #pragma unroll
-        for (int e = 1; e < U / 8; ++e) mb = fmaxf(mb, fmaxf(x[e][0], x[e][1]));
-        mb = fmaxf(mb, __shfl_xor_sync(0xffffffffu, mb, 1));
-        mb = fmaxf(mb, __shfl_xor_sync(0xffffffffu, mb, 2));
-        const float mn = fmaxf(m_run, mb);
-        const float ref = mn == -INFINITY ? 0.0f : mn;
-        const float alpha = fast_exp2(m_run - ref);  // 0 while m_run = -inf
+            for (int e = 0; e < U / 8; ++e)
+                if (!((meta.vis >> (8 * e + g)) & 1u)) x[e][0] = x[e][1] = -INFINITY;
+        }
+        float ref[2], alpha[2];
+        bool moved = false;
+        float m_new[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            float mb = x[0][i];
+#pragma unroll
+            for (int e = 1; e < U / 8; ++e) mb = fmaxf(mb, x[e][i]);
+#pragma unroll
+            for (int w = 4; w < 32; w <<= 1) mb = fmaxf(mb, __shfl_xor_sync(0xffffffffu, mb, w));
+            m_new[i] = fmaxf(m_run[i], mb);
+            moved |= m_new[i] != m_run[i];
+            ref[i] = m_new[i] == -INFINITY ? 0.0f : m_new[i];
+            alpha[i] = fast_exp2(m_run[i] - ref[i]);  // 0 while m_run = -inf
+        }
         float vm = v_ref;
 #pragma unroll
         for (int i = 0; i < NB; ++i) vm = fmaxf(vm, fabsf(meta.vs[i]));
-        if (__any_sync(0xffffffffu, mn != m_run) || vm != v_ref) {
-            const float f = vm > v_ref ? alpha * (v_ref / vm) : alpha;
+        if (__any_sync(0xffffffffu, moved) || vm != v_ref) {
+            const float shrink = vm > v_ref ? v_ref / vm : 1.0f;
+            const float f0 = alpha[0] * shrink, f1 = alpha[1] * shrink;
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                oacc[nt][0] *= f;
-                oacc[nt][1] *= f;
+            for (int mt = 0; mt < MT; ++mt) {
+                oacc[mt][0] *= f0;
+                oacc[mt][1] *= f1;
+                oacc[mt][2] *= f0;
+                oacc[mt][3] *= f1;
             }
-            l_part *= alpha;
-            m_run = mn;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                l_part[i] *= alpha[i];
+                m_run[i] = m_new[i];
+            }
             v_ref = vm;
         }
         float vw[NB];
 #pragma unroll
         for (int i = 0; i < NB; ++i) vw[i] = v_ref > 0.0f ? meta.vs[i] / v_ref : 0.0f;
-        uint32_t pa[U / 8];
+        uint32_t pb[U / 8];  // P^T as B fragments: lane (g, tg) holds tokens 8 e + 2 tg, + 1 of head g
 #pragma unroll
         for (int e = 0; e < U / 8; ++e) {
-            const float p0 = fast_exp2(x[e][0] - ref + 14.0f), p1 = fast_exp2(x[e][1] - ref + 14.0f);
-            l_part += p0 + p1;
+            const float p0 = fast_exp2(x[e][0] - ref[0] + 14.0f), p1 = fast_exp2(x[e][1] - ref[1] + 14.0f);
+            l_part[0] += p0;
+            l_part[1] += p1;
             const float w = vw[8 * e / BS];
-            pa[e] = pack_f16x2(p0 * w, p1 * w);
+            pb[e] = transpose_8x8(pack_f16x2(p0 * w, p1 * w));
         }
-        // ---- O += P V: column n = g of tile nt is element g * NT + nt of D ----
+        // ---- O^T += V^T P^T: row g of tile mt is element g * 2 MT + 2 mt, row g + 8 the one after it ----
 #pragma unroll
         for (int h = 0; h < U / 16; ++h) {
-            uint32_t w[4][NT / 4];  // tokens 16 h + {2 tg, 2 tg + 1, 2 tg + 8, 2 tg + 9}
+            uint32_t w[4][D / 32];  // tokens 16 h + {2 tg, 2 tg + 1, 2 tg + 8, 2 tg + 9}
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int t = 16 * h + 2 * tg + (i & 1) + (i >> 1) * 8;
@@ -349,31 +408,34 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                     const uint2 q = *reinterpret_cast<const uint2*>(vu + at16(t, g >> 1) + (g & 1) * 8);
                     w[i][0] = q.x; w[i][1] = q.y;
                 }
-                if (meta.vis != 0xFFFFFFFFu && !((meta.vis >> t) & 1u)) {  // whatever lies there, weight 0 must not meet a NaN
+            }
+            if (meta.vis != 0xFFFFFFFFu) {  // whatever lies there, weight 0 must not meet a NaN
 #pragma unroll
-                    for (int j = 0; j < NT / 4; ++j) w[i][j] = 0u;
-                }
+                for (int i = 0; i < 4; ++i)
+                    if (!((meta.vis >> (16 * h + 2 * tg + (i & 1) + (i >> 1) * 8)) & 1u)) {
+#pragma unroll
+                        for (int j = 0; j < D / 32; ++j) w[i][j] = 0u;
+                    }
             }
 #pragma unroll
-            for (int j = 0; j < NT / 4; ++j) {
+            for (int j = 0; j < D / 32; ++j) {
 #pragma unroll
                 for (int q = 0; q < 2; ++q) {  // elements 4 j + 2 q, + 1 of two tokens each
                     const uint32_t sel = q ? 0x7362u : 0x5140u;
-                    uint32_t a0, a1, b0, b1;
+                    uint32_t a0, a1, a2, a3;
                     f16x2_from_f8x4(__byte_perm(w[0][j], w[1][j], sel), a0, a1);
-                    f16x2_from_f8x4(__byte_perm(w[2][j], w[3][j], sel), b0, b1);
-                    mma_f16_16816(oacc[4 * j + 2 * q], pa[2 * h], pa[2 * h + 1], a0, b0);
-                    mma_f16_16816(oacc[4 * j + 2 * q + 1], pa[2 * h], pa[2 * h + 1], a1, b1);
+                    f16x2_from_f8x4(__byte_perm(w[2][j], w[3][j], sel), a2, a3);
+                    mma_f16_16816(oacc[2 * j + q], a0, a1, a2, a3, pb[2 * h], pb[2 * h + 1]);
                 }
             }
         }
     };
-    Meta cur, next;
-    cur.vis = next.vis = 0;
-    if (n_units > 0) issue_unit(cur, kbase & 1, 0);
     for (int k = 0; k < n_units && ok; ++k) {
         const uint32_t st = (kbase + k) & 1;
+        const bool refill = k + 1 == tab_base + 32;  // the next unit's entries replace this one's batch
+        if (refill) take_scales(cur, k);
         if (k + 1 < n_units) issue_unit(next, st ^ 1, k + 1);
+        if (!refill) take_scales(cur, k);  // (the first time, the scales are still on their way)
         if (cur.vis != 0) {  // (a unit all of whose blocks are bad has no copies and does not use its stage)
             ok = __all_sync(0xffffffffu, mbar_wait(&ring_bar[warp][st], (ring_parity >> st) & 1, &ring_abort, 0x600 + warp)) != 0;
             if (!ok) break;
@@ -386,43 +448,66 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
 
     // ---- the warps' results meet in shared memory, where the ring was (all copies have landed and been read) ----
     __syncthreads();
-    float (*sm_o)[G][D] = reinterpret_cast<float (*)[G][D]>(ring_base);
-    static_assert(sizeof(float) * kPagedWarps * G * D <= kPagedWarps * kPagedRing * kUnitBytes, "partials fit the ring");
-    l_part += __shfl_xor_sync(0xffffffffu, l_part, 1);
-    l_part += __shfl_xor_sync(0xffffffffu, l_part, 2);
-    if (g < G) {
+    constexpr int kRow = D + 2;  // (the lanes' pairs meet two-way bank conflicts, with D they would meet eight-way ones)
+    float (*sm_o)[8][kRow] = reinterpret_cast<float (*)[8][kRow]>(ring_base);
+    static_assert(sizeof(float) * kPagedWarps * 8 * kRow <= kPagedWarps * kPagedRing * kUnitBytes, "partials fit the ring");
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int w = 4; w < 32; w <<= 1) l_part[i] += __shfl_xor_sync(0xffffffffu, l_part[i], w);
+    {
         const float unit = v_ref * (1.0f / 16384.0f);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            sm_o[warp][g][(2 * tg) * NT + nt] = oacc[nt][0] * unit;
-            sm_o[warp][g][(2 * tg + 1) * NT + nt] = oacc[nt][1] * unit;
+        for (int i = 0; i < 2; ++i) {
+            if (2 * tg + i < G) {
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+                    *reinterpret_cast<float2*>(&sm_o[warp][2 * tg + i][g * 2 * MT + 2 * mt]) = make_float2(oacc[mt][i] * unit, oacc[mt][2 + i] * unit);
+                if (g == 0) sm_ml[warp][2 * tg + i] = make_float2(m_run[i], l_part[i] * (1.0f / 16384.0f));
+            }
         }
-        if (tg == 0) sm_ml[warp][g] = make_float2(m_run, l_part * (1.0f / 16384.0f));
     }
     __syncthreads();
-    for (int idx = threadIdx.x; idx < G * D; idx += kPagedThreads) {
-        const int gg = idx / D, d = idx % D;
-        float mt = -INFINITY;
+    // all loads of a thread's places before the first use: one round trip instead of one per place
+    constexpr int kPlaces = (G * D + kPagedThreads - 1) / kPagedThreads;
+    float ot[kPlaces], lt[kPlaces], mt[kPlaces];
 #pragma unroll
-        for (int w = 0; w < kPagedWarps; ++w) mt = fmaxf(mt, sm_ml[w][gg].x);
-        float lt = 0.0f, ot = 0.0f;
+    for (int it = 0; it < kPlaces; ++it) {
+        const int idx = threadIdx.x + it * kPagedThreads;
+        const int gg = idx / D < G ? idx / D : 0, at = idx % D;
+        float2 ml[kPagedWarps];
+        float o[kPagedWarps];
 #pragma unroll
         for (int w = 0; w < kPagedWarps; ++w) {
-            const float2 ml = sm_ml[w][gg];
-            const float sw = (ml.x == -INFINITY) ? 0.0f : fast_exp2(ml.x - mt);
-            lt += ml.y * sw;
-            ot += sm_o[w][gg][d] * sw;
+            ml[w] = sm_ml[w][gg];
+            o[w] = sm_o[w][gg][at];
         }
-        if (seg_whole) {
-            const int64_t row = static_cast<int64_t>(s) * p.H + head0 + gg;
-            p.O[row * D + d] = __float2bfloat16(lt == 0.0f ? 0.0f : ot / lt);
-            if (d == 0 && p.LSE) p.LSE[row] = lt == 0.0f ? -INFINITY : (mt + log2f(lt)) * 0.6931471805599453f;
-        } else {
-            const int64_t slot = (static_cast<int64_t>(s) * p.H_kv + kvh + blockIdx.x) * G + gg;
-            p.part_o[slot * D + d] = ot;
-            if (d == 0) p.part_ml[slot] = make_float2(mt, lt);
+        mt[it] = fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x));
+        lt[it] = ot[it] = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kPagedWarps; ++w) {
+            const float sw = (ml[w].x == -INFINITY) ? 0.0f : fast_exp2(ml[w].x - mt[it]);
+            lt[it] += ml[w].y * sw;
+            ot[it] += o[w] * sw;
         }
     }
+#pragma unroll
+    for (int it = 0; it < kPlaces; ++it) {
+        const int idx = threadIdx.x + it * kPagedThreads;
+        const int gg = idx / D, at = idx % D;
+        if (gg < G) {
+            if (seg_whole) {
+                const int64_t row = static_cast<int64_t>(s) * p.H + head0 + gg;
+                p.O[row * D + at] = __float2bfloat16(lt[it] == 0.0f ? 0.0f : ot[it] / lt[it]);
+                if (at == 0 && p.LSE) p.LSE[row] = lt[it] == 0.0f ? -INFINITY : (mt[it] + log2f(lt[it])) * 0.6931471805599453f;
+            } else {
+                const int64_t slot = (static_cast<int64_t>(s) * p.H_kv + kvh + blockIdx.x) * G + gg;
+                p.part_o[slot * D + at] = ot[it];
+                if (at == 0) p.part_ml[slot] = make_float2(mt[it], lt[it]);
+            }
+        }
+    }
+    static_assert(kPagedWarps == 4, "the maximum above is over four warps");
     if (p.ctas == 0 || !ok) break;
     fence_proxy_async_smem();
     __syncthreads();  // the results have left shared memory: copies may fill the ring again
