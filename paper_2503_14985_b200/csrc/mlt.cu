@@ -1163,7 +1163,7 @@ int mlt_paged_attn_decode_f8(const void* Q, const void* K_cache, const void* V_c
         const uint64_t dims[3] = {static_cast<uint64_t>(D), static_cast<uint64_t>(block_size),
                                   std::max<uint64_t>(1, static_cast<uint64_t>(num_blocks) * H_kv)};
         const uint64_t strides[2] = {static_cast<uint64_t>(D), static_cast<uint64_t>(D) * block_size};
-        const uint32_t box[3] = {static_cast<uint32_t>(D), static_cast<uint32_t>(block_size), 1};
+        const uint32_t box[3] = {static_cast<uint32_t>(D), static_cast<uint32_t>(std::min(block_size, kPagedF8Unit)), 1};
         rc = encode_bf16(&tk, K_cache, 3, dims, strides, box, 3, D == 64);
         if (rc != MLT_OK) return rc;
         rc = encode_bf16(&tv, V_cache, 3, dims, strides, box, 3, D == 64);

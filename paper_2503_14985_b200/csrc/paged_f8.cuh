@@ -45,12 +45,13 @@ struct PagedF8Params {
 };
 
 constexpr int kPagedF8Unit = 32;   // tokens per warp and ring stage
-constexpr int kPagedF8CtasPerSm = 3;
+constexpr int kPagedF8Ring = 3;    // stages: one in use, the others on their way
+constexpr int kPagedF8CtasPerSm = 2;
 constexpr int kPagedF8MaxCtas = 1024;  // bound on the balanced split's CTAs that the workspace formula uses
 
 template <int D>
 constexpr int paged_f8_smem_bytes() {
-    return kPagedWarps * kPagedRing * 2 * kPagedF8Unit * D + 1024;
+    return kPagedWarps * kPagedF8Ring * 2 * kPagedF8Unit * D + 1024;
 }
 
 __device__ __forceinline__ void mma_f16_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -88,26 +89,27 @@ template <int D, int G, int BS>
 __global__ void __launch_bounds__(kPagedThreads, kPagedF8CtasPerSm)
 paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const PagedF8Params p) {
     pdl_launch_dependents();
-    static_assert(kPagedRing == 2, "the loop below keeps one unit in use and one in flight");
     constexpr int U = kPagedF8Unit;
     constexpr int PP = D / 64;       // 16-byte pieces of a token's K per lane
     constexpr int MT = D / 16;       // row tiles of the output
-    constexpr int NB = U / BS;       // cache blocks per unit
+    constexpr int kPiece = BS < U ? BS : U;  // tokens per tensor copy: a cache block, or the part of one that the unit covers
+    constexpr int NB = U / kPiece;   // cache blocks per unit
+    constexpr uint32_t kFull = U == 32 ? 0xFFFFFFFFu : (1u << (U & 31)) - 1u;  // all tokens of a unit
     constexpr int kUnitBytes = 2 * U * D;
     __shared__ float2 sm_ml[kPagedWarps][G];
     __shared__ int sm_pre[kPagedBalanceMaxSeqs + 1];
     __shared__ int sm_red[kPagedWarps];
-    __shared__ uint64_t ring_bar[kPagedWarps][kPagedRing];
+    __shared__ uint64_t ring_bar[kPagedWarps][kPagedF8Ring];
     __shared__ uint32_t ring_abort;
     extern __shared__ uint8_t ring_raw[];
     uint8_t* ring_base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(ring_raw) + 1023) & ~uintptr_t(1023));
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int g = lane >> 2, tg = lane & 3;
-    uint8_t* my_ring = ring_base + warp * kPagedRing * kUnitBytes;
+    uint8_t* my_ring = ring_base + warp * kPagedF8Ring * kUnitBytes;
     if (lane == 0) {
 #pragma unroll
-        for (int i = 0; i < kPagedRing; ++i) mbar_init(&ring_bar[warp][i], 1);
+        for (int i = 0; i < kPagedF8Ring; ++i) mbar_init(&ring_bar[warp][i], 1);
         if (warp == 0) ring_abort = 0;
         fence_mbar_init();
         prefetch_tensormap(&tmap_k);
@@ -226,16 +228,16 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
             tab_base = k;
             const int n = k + lane < n_units ? tok_end - (first + (k + lane) * kStep) : 0;  // tokens of unit k + lane and beyond
 #pragma unroll
-            for (int i = 0; i < NB; ++i) tab[i] = i * BS < n ? table[(first + (k + lane) * kStep) / BS + i] : 0;
+            for (int i = 0; i < NB; ++i) tab[i] = i * kPiece < n ? table[(first + (k + lane) * kStep) / BS + i] : 0;
             fresh = true;
         }
         const int left = tok_end - u0;
-        meta.vis = left >= U ? 0xFFFFFFFFu : (1u << left) - 1u;
+        meta.vis = left >= U ? kFull : (1u << left) - 1u;
         int phys[NB], blocks = 0;
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
             phys[i] = __shfl_sync(0xffffffffu, tab[i], k - tab_base);
-            if (i * BS >= left) {
+            if (i * kPiece >= left) {
                 phys[i] = -1;
             } else if (phys[i] < 0 || phys[i] >= p.num_blocks) {  // never dereference a bad table entry: report, leave its tokens out
                 if (lane == 0 && atomicCAS(&g_status[0], 0u, kStatusBadBlock) == 0u) {
@@ -244,7 +246,7 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                     g_status[3] = static_cast<unsigned int>(phys[i]);
                 }
                 phys[i] = -1;
-                meta.vis &= ~((BS == 32 ? 0xFFFFFFFFu : (1u << (BS & 31)) - 1u) << (i * BS));
+                meta.vis &= ~((kPiece == 32 ? 0xFFFFFFFFu : (1u << (kPiece & 31)) - 1u) << (i * kPiece));
             } else {
                 ++blocks;
             }
@@ -252,20 +254,20 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
         if (blocks > 0) {
             __syncwarp();  // every lane is done reading the stage's previous contents
             uint64_t* bar = &ring_bar[warp][stage];
-            if (lane == 0) mbar_arrive_expect_tx(bar, 2u * blocks * BS * D);
+            if (lane == 0) mbar_arrive_expect_tx(bar, 2u * blocks * kPiece * D);
             __syncwarp();
             uint8_t* dst = my_ring + stage * kUnitBytes;
 #pragma unroll
             for (int i = 0; i < NB; ++i)
                 if (phys[i] >= 0 && (lane >> 1) == i)
-                    tma_load_3d(dst + (lane & 1) * (U * D) + i * BS * D, (lane & 1) ? &tmap_v : &tmap_k, bar, 0, 0, phys[i] * p.H_kv + kvh);
+                    tma_load_3d(dst + (lane & 1) * (U * D) + i * kPiece * D, (lane & 1) ? &tmap_v : &tmap_k, bar, 0, u0 % BS / kPiece * kPiece, phys[i] * p.H_kv + kvh);
             __syncwarp();
         }
         if (fresh) {  // (behind the copies: the scales are only needed when the unit is used)
             const int n = k + lane < n_units ? tok_end - (first + (k + lane) * kStep) : 0;
 #pragma unroll
             for (int i = 0; i < NB; ++i) {
-                const bool there = i * BS < n && tab[i] >= 0 && tab[i] < p.num_blocks;
+                const bool there = i * kPiece < n && tab[i] >= 0 && tab[i] < p.num_blocks;
                 const int64_t at = static_cast<int64_t>(tab[i]) * p.H_kv + kvh;
                 tks[i] = there ? __ldg(p.ks + at) : 0.0f;
                 tvs[i] = there ? __ldg(p.vs + at) : 0.0f;
@@ -279,9 +281,10 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
             meta.vs[i] = __shfl_sync(0xffffffffu, tvs[i], k - tab_base);
         }
     };
-    Meta cur, next;
-    cur.vis = next.vis = 0;
-    if (n_units > 0) issue_unit(cur, kbase & 1, 0);  // the first copies are under way before the queries are read
+    Meta ahead[kPagedF8Ring];  // units k, k + 1, ..: ahead[0] is the one in use
+#pragma unroll
+    for (int i = 0; i < kPagedF8Ring - 1; ++i)
+        if (i < n_units) issue_unit(ahead[i], (kbase + i) % kPagedF8Ring, i);  // under way before the queries are converted
 
     // Q^T as B fragments in FP16: lane (g, tg) holds elements tg * D / 4 .. of head g, scaled by 2^-qexp
     uint32_t qb[PP][4][2];
@@ -337,12 +340,12 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
 #pragma unroll
             for (int i = 0; i < 2; ++i) {  // tiles e = 2 h + i, each inside one cache block
                 const int e = 2 * h + i;
-                const float ks = meta.ks[8 * e / BS];
+                const float ks = meta.ks[8 * e / kPiece];
                 x[e][0] = sc[2 * i] * (c_head[0] * ks);
                 x[e][1] = sc[2 * i + 1] * (c_head[1] * ks);
             }
         }
-        if (meta.vis != 0xFFFFFFFFu) {
+        if (meta.vis != kFull) {
 #pragma unroll
             for (int e = 0; e < U / 8; ++e)
                 if (!((meta.vis >> (8 * e + g)) & 1u)) x[e][0] = x[e][1] = -INFINITY;
@@ -385,13 +388,14 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
         float vw[NB];
 #pragma unroll
         for (int i = 0; i < NB; ++i) vw[i] = v_ref > 0.0f ? meta.vs[i] / v_ref : 0.0f;
+        const float low[2] = {ref[0] - 14.0f, ref[1] - 14.0f};
         uint32_t pb[U / 8];  // P^T as B fragments: lane (g, tg) holds tokens 8 e + 2 tg, + 1 of head g
 #pragma unroll
         for (int e = 0; e < U / 8; ++e) {
-            const float p0 = fast_exp2(x[e][0] - ref[0] + 14.0f), p1 = fast_exp2(x[e][1] - ref[1] + 14.0f);
+            const float p0 = fast_exp2(x[e][0] - low[0]), p1 = fast_exp2(x[e][1] - low[1]);
             l_part[0] += p0;
             l_part[1] += p1;
-            const float w = vw[8 * e / BS];
+            const float w = vw[8 * e / kPiece];
             pb[e] = transpose_8x8(pack_f16x2(p0 * w, p1 * w));
         }
         // ---- O^T += V^T P^T: row g of tile mt is element g * 2 MT + 2 mt, row g + 8 the one after it ----
@@ -409,7 +413,7 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                     w[i][0] = q.x; w[i][1] = q.y;
                 }
             }
-            if (meta.vis != 0xFFFFFFFFu) {  // whatever lies there, weight 0 must not meet a NaN
+            if (meta.vis != kFull) {  // whatever lies there, weight 0 must not meet a NaN
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     if (!((meta.vis >> (16 * h + 2 * tg + (i & 1) + (i >> 1) * 8)) & 1u)) {
@@ -431,18 +435,23 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
         }
     };
     for (int k = 0; k < n_units && ok; ++k) {
-        const uint32_t st = (kbase + k) & 1;
-        const bool refill = k + 1 == tab_base + 32;  // the next unit's entries replace this one's batch
-        if (refill) take_scales(cur, k);
-        if (k + 1 < n_units) issue_unit(next, st ^ 1, k + 1);
-        if (!refill) take_scales(cur, k);  // (the first time, the scales are still on their way)
-        if (cur.vis != 0) {  // (a unit all of whose blocks are bad has no copies and does not use its stage)
+        const uint32_t st = (kbase + k) % kPagedF8Ring;
+        const int kk = k + kPagedF8Ring - 1;
+        if (kk == tab_base + 32) {  // that unit's entries will replace those of the units before it
+#pragma unroll
+            for (int i = 0; i < kPagedF8Ring - 1; ++i)
+                if (k + i >= tab_base) take_scales(ahead[i], k + i);
+        }
+        if (kk < n_units) issue_unit(ahead[kPagedF8Ring - 1], (kbase + kk) % kPagedF8Ring, kk);
+        if (k >= tab_base) take_scales(ahead[0], k);  // (the first time they are still on their way)
+        if (ahead[0].vis != 0) {  // (a unit all of whose blocks are bad has no copies and does not use its stage)
             ok = __all_sync(0xffffffffu, mbar_wait(&ring_bar[warp][st], (ring_parity >> st) & 1, &ring_abort, 0x600 + warp)) != 0;
             if (!ok) break;
             ring_parity ^= 1u << st;
-            compute_unit(cur, st);
+            compute_unit(ahead[0], st);
         }
-        cur = next;
+#pragma unroll
+        for (int i = 0; i < kPagedF8Ring - 1; ++i) ahead[i] = ahead[i + 1];
     }
     kbase += n_units;
 
@@ -450,7 +459,7 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
     __syncthreads();
     constexpr int kRow = D + 2;  // (the lanes' pairs meet two-way bank conflicts, with D they would meet eight-way ones)
     float (*sm_o)[8][kRow] = reinterpret_cast<float (*)[8][kRow]>(ring_base);
-    static_assert(sizeof(float) * kPagedWarps * 8 * kRow <= kPagedWarps * kPagedRing * kUnitBytes, "partials fit the ring");
+    static_assert(sizeof(float) * kPagedWarps * 8 * kRow <= kPagedWarps * kPagedF8Ring * kUnitBytes, "partials fit the ring");
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -515,20 +524,23 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
     }  // segments
 }
 
-// Rows that several CTAs worked on: sum of their partials, rescaled to the common maximum.  One CTA per (sequence, head),
-// blockDim.x / D groups of threads that take every blockDim.x / D-th partial.  Also writes the rows of empty sequences.
-constexpr int kPagedF8CombineBatch = 512;  // partials whose weights are in shared memory at a time
-template <int D, int BS>
-__global__ void paged_f8_combine_kernel(const PagedF8Params p) {
-    __shared__ float sm_w[kPagedF8CombineBatch];
-    __shared__ float sm_o[1024];
-    __shared__ int sm_i[2][32];
-    __shared__ float sm_f[2][32];
-    const int G = p.H / p.H_kv;
-    const int s = blockIdx.x / p.H, h = blockIdx.x % p.H, kvh = h / G, gg = h % G;
-    const int tid = threadIdx.x, lane = tid & 31, warps = blockDim.x >> 5;
+// Rows that several CTAs worked on: sum of their partials, rescaled to the common maximum.  One CTA per (sequence, KV head):
+// a thread owns four neighbouring outputs of one head and every `splits`-th partial, so that a row with many partials
+// uses all threads too.  Also writes the rows of empty sequences.
+constexpr int kPagedF8CombineThreads = 256;
+template <int D, int G, int BS>
+__global__ void __launch_bounds__(kPagedF8CombineThreads) paged_f8_combine_kernel(const PagedF8Params p) {
+    constexpr int kWarps = kPagedF8CombineThreads / 32;
+    constexpr int kVec = G * D / 4, kSplits = kPagedF8CombineThreads / kVec;
+    static_assert(kSplits >= 1 && kSplits * kVec == kPagedF8CombineThreads, "whole splits");
+    __shared__ int sm_i[2][kWarps];
+    __shared__ float sm_m[kWarps][G];
+    __shared__ float4 sm_o[kPagedF8CombineThreads];
+    __shared__ float sm_l[kPagedF8CombineThreads];
+    const int s = blockIdx.x / p.H_kv, kvh = blockIdx.x % p.H_kv;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int below = 0, total = 0;
-    for (int s2 = tid; s2 < p.num_seqs; s2 += blockDim.x) {
+    for (int s2 = tid; s2 < p.num_seqs; s2 += kPagedF8CombineThreads) {
         const int c = paged_f8_chunks(p, s2, BS);
         total += c;
         if (s2 < s) below += c;
@@ -538,16 +550,18 @@ __global__ void paged_f8_combine_kernel(const PagedF8Params p) {
         below += __shfl_xor_sync(0xffffffffu, below, w);
         total += __shfl_xor_sync(0xffffffffu, total, w);
     }
-    if (lane == 0) { sm_i[0][tid >> 5] = below; sm_i[1][tid >> 5] = total; }
+    if (lane == 0) { sm_i[0][warp] = below; sm_i[1][warp] = total; }
     __syncthreads();
     below = total = 0;
-    for (int w = 0; w < warps; ++w) { below += sm_i[0][w]; total += sm_i[1][w]; }
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) { below += sm_i[0][w]; total += sm_i[1][w]; }
     const int n_s = paged_f8_chunks(p, s, BS);
-    const int64_t row = static_cast<int64_t>(s) * p.H + h;
+    const int64_t row0 = static_cast<int64_t>(s) * p.H + kvh * G;  // of the group's first head
     cudaGridDependencySynchronize();  // (what was read so far are inputs)
+    const int v = tid % kVec, split = tid / kVec, gg = v * 4 / D;
     if (n_s == 0) {  // nothing to see: O = 0, LSE = -inf
-        if (tid < D) p.O[row * D + tid] = __float2bfloat16(0.0f);
-        if (tid == 0 && p.LSE) p.LSE[row] = -INFINITY;
+        if (split == 0) *reinterpret_cast<uint2*>(p.O + row0 * D + v * 4) = make_uint2(0u, 0u);
+        if (tid < G && p.LSE) p.LSE[row0 + tid] = -INFINITY;
         return;
     }
     const long long q = paged_f8_quota(static_cast<long long>(total) * p.H_kv, p.ctas);
@@ -555,52 +569,53 @@ __global__ void paged_f8_combine_kernel(const PagedF8Params p) {
     const int c0 = static_cast<int>(start / q), used = static_cast<int>((start + n_s - 1) / q) - c0 + 1;
     if (used == 1) return;  // one CTA had the whole row and finished it
     const int64_t slot0 = static_cast<int64_t>(s) * p.H_kv + kvh + c0;
-    const float2* ml = p.part_ml + slot0 * G + gg;
-    const float* po = p.part_o + (slot0 * G + gg) * D;
+    const float2* ml = p.part_ml + slot0 * G;
+    const float4* po = reinterpret_cast<const float4*>(p.part_o + slot0 * G * D) + v;
+    constexpr int kFirst = 4;  // requested before the maximum is known
+    float4 first[kFirst];
+#pragma unroll
+    for (int i = 0; i < kFirst; ++i)
+        first[i] = split + i * kSplits < used ? po[static_cast<int64_t>(split + i * kSplits) * kVec] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     float mt = -INFINITY;
-    for (int i = tid; i < used; i += blockDim.x) mt = fmaxf(mt, ml[static_cast<int64_t>(i) * G].x);
+    for (int i = tid; i < used * G; i += kPagedF8CombineThreads) mt = fmaxf(mt, ml[i].x);  // head tid % G (G divides the stride)
 #pragma unroll
-    for (int w = 16; w > 0; w >>= 1) mt = fmaxf(mt, __shfl_xor_sync(0xffffffffu, mt, w));
-    if (lane == 0) sm_f[0][tid >> 5] = mt;
+    for (int w = 16; w >= G; w >>= 1) mt = fmaxf(mt, __shfl_xor_sync(0xffffffffu, mt, w));
+    if (lane < G) sm_m[warp][lane] = mt;
     __syncthreads();
-    mt = -INFINITY;
-    for (int w = 0; w < warps; ++w) mt = fmaxf(mt, sm_f[0][w]);
-    const int d = tid % D, grp = tid / D, groups = blockDim.x / D;
-    float ot = 0.0f, lt = 0.0f;
-    for (int base = 0; base < used; base += kPagedF8CombineBatch) {
-        const int n = min(kPagedF8CombineBatch, used - base);
+    mt = sm_m[0][gg];
+#pragma unroll
+    for (int w = 1; w < kWarps; ++w) mt = fmaxf(mt, sm_m[w][gg]);
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    float lt = 0.0f;
+    auto add = [&](int i, const float4& x) {
+        const float2 a = ml[static_cast<int64_t>(i) * G + gg];
+        const float w = a.x == -INFINITY ? 0.0f : fast_exp2(a.x - mt);
+        lt += a.y * w;
+        o.x = fmaf(x.x, w, o.x);
+        o.y = fmaf(x.y, w, o.y);
+        o.z = fmaf(x.z, w, o.z);
+        o.w = fmaf(x.w, w, o.w);
+    };
+#pragma unroll
+    for (int i = 0; i < kFirst; ++i)
+        if (split + i * kSplits < used) add(split + i * kSplits, first[i]);
+#pragma unroll 4
+    for (int i = split + kFirst * kSplits; i < used; i += kSplits) add(i, po[static_cast<int64_t>(i) * kVec]);
+    if constexpr (kSplits > 1) {
+        sm_o[tid] = o;
+        sm_l[tid] = lt;
         __syncthreads();
-        for (int i = tid; i < n; i += blockDim.x) {
-            const float2 v = ml[static_cast<int64_t>(base + i) * G];
-            const float w = v.x == -INFINITY ? 0.0f : fast_exp2(v.x - mt);
-            sm_w[i] = w;
-            lt += v.y * w;
+        if (split != 0) return;
+#pragma unroll
+        for (int k = 1; k < kSplits; ++k) {
+            const float4 x = sm_o[k * kVec + v];
+            o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
+            lt += sm_l[k * kVec + v];
         }
-        __syncthreads();
-        const float* src = po + static_cast<int64_t>(base) * G * D + d;
-        int i = grp;
-        for (; i + 3 * groups < n; i += 4 * groups) {
-            float v[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) v[u] = src[static_cast<int64_t>(i + u * groups) * G * D];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) ot = fmaf(v[u], sm_w[i + u * groups], ot);
-        }
-        for (; i < n; i += groups) ot = fmaf(src[static_cast<int64_t>(i) * G * D], sm_w[i], ot);
     }
-#pragma unroll
-    for (int w = 16; w > 0; w >>= 1) lt += __shfl_xor_sync(0xffffffffu, lt, w);
-    if (lane == 0) sm_f[1][tid >> 5] = lt;
-    sm_o[tid] = ot;
-    __syncthreads();
-    if (tid < D) {
-        lt = 0.0f;
-        for (int w = 0; w < warps; ++w) lt += sm_f[1][w];
-        ot = 0.0f;
-        for (int k = 0; k < groups; ++k) ot += sm_o[k * D + tid];
-        p.O[row * D + tid] = __float2bfloat16(lt == 0.0f ? 0.0f : ot / lt);
-        if (tid == 0 && p.LSE) p.LSE[row] = lt == 0.0f ? -INFINITY : (mt + log2f(lt)) * 0.6931471805599453f;
-    }
+    const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
+    *reinterpret_cast<uint2*>(p.O + row0 * D + v * 4) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+    if (v * 4 % D == 0 && p.LSE) p.LSE[row0 + gg] = lt == 0.0f ? -INFINITY : (mt + log2f(lt)) * 0.6931471805599453f;
 }
 
 inline size_t paged_f8_slot_bytes(int G, int D) { return static_cast<size_t>(G) * (static_cast<size_t>(D) * 4 + 8); }
@@ -612,19 +627,16 @@ int paged_f8_launch_one(const CUtensorMap& tk, const CUtensorMap& tv, const Page
     paged_f8_decode_kernel<D, G, BS><<<static_cast<unsigned>(grid), kPagedThreads, paged_f8_smem_bytes<D>(), st>>>(tk, tv, p);
     if (cudaGetLastError() != cudaSuccess) return 4;
     if (p.ctas == 0) return 0;
-    const int64_t rows = static_cast<int64_t>(p.num_seqs) * p.H_kv;
-    int groups = 1;  // about four partials per thread where a row meets many CTAs
-    while (groups * D < 1024 && rows * groups * 4 < p.ctas) groups *= 2;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(p.num_seqs * p.H));
-    cfg.blockDim = dim3(static_cast<unsigned>(groups * D));
+    cfg.gridDim = dim3(static_cast<unsigned>(p.num_seqs * p.H_kv));
+    cfg.blockDim = dim3(kPagedF8CombineThreads);
     cfg.stream = st;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr.val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, paged_f8_combine_kernel<D, BS>, p) == cudaSuccess ? 0 : 4;
+    return cudaLaunchKernelEx(&cfg, paged_f8_combine_kernel<D, G, BS>, p) == cudaSuccess ? 0 : 4;
 }
 template <int D, int G>
 int paged_f8_launch_bs(const CUtensorMap& tk, const CUtensorMap& tv, const PagedF8Params& p, int block_size, cudaStream_t st) {
