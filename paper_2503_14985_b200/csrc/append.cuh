@@ -13,10 +13,12 @@
 // power-of-two scale of the new tokens' largest finite magnitude).  If that is larger than before, the tokens already
 // there are moved to it: q' = round(q * old / new), exact for powers of two unless a value underflows.
 //
-// Bound by HBM for prompts and by latency for single tokens: every input is read once, every output written once.  One
-// warp owns one head of the (at most BS) new tokens of one cache block, because the 8-bit block scale needs them
-// together; a lane owns two 8-element chunks of a token that hold both partners of its rotation pairs, so no exchange
-// between lanes is needed but the maximum.
+// Bound by HBM for prompts and by latency for single tokens: every input is read once, every output written once.
+//   keys, values  one warp owns one head of the (at most BS) new tokens of one cache block, because the 8-bit block scale needs
+//                 them together
+//   queries       one warp owns a token, whose heads lie side by side: the angles are read once for all of them
+// A lane owns two 8-element chunks of a head that hold both partners of its rotation pairs, so no exchange between lanes is
+// needed but the maximum.
 //
 // Which cache block a warp works on: the host does not know the lengths, so blocks are numbered with gaps: sequence s
 // has the slots cu[s] / BS + 2 s onwards.  n new tokens touch at most n / BS + 2 - 2 / BS blocks, and there are at least
@@ -42,14 +44,14 @@ struct AppendParams {
 
 constexpr int kAppendWarps = 4;
 
-// The last s with slot_of(s) <= slot, slot_of(s) = cu[s] / BS + 2 s (increasing); whole warp.
-template <int BS>
-__device__ __forceinline__ int append_find_seq(const int* cu, int S, int slot, int lane) {
+// The last s with at(s) <= x for an increasing at; whole warp.
+template <class F>
+__device__ __forceinline__ int append_find_seq(int S, int x, int lane, F at) {
     int lo = 0, hi = S;
     while (hi - lo > 1) {
         const int step = (hi - lo + 31) / 32;
         const int i = lo + lane * step;
-        const bool le = i < hi && cu[i] / BS + 2 * i <= slot;
+        const bool le = i < hi && at(i) <= x;
         const int n = max(1, __popc(__ballot_sync(0xffffffffu, le)));
         lo += (n - 1) * step;
         hi = min(hi, lo + step);
@@ -82,27 +84,97 @@ __device__ __forceinline__ void rotate_pair(float& a, float& b, float c, float s
     a = x;
 }
 
+// Whether sequence s lies inside the call's tokens and the tables' positions; reported where it does not (nothing of such a
+// sequence is read or written).
+__device__ __forceinline__ bool append_in_range(const AppendParams& p, int s, int t_begin, int t_end, int ctx, int lane) {
+    const bool ok = t_begin >= 0 && t_end <= p.T && ctx >= 0 && (p.R == 0 || static_cast<int64_t>(ctx) + (t_end - t_begin) <= p.max_pos);
+    if (!ok && lane == 0) append_report(kStatusBadPosition, s, t_begin, ctx);
+    return ok;
+}
+// cos (first half) and sin of the 8 pairs of lane position j at position pos
+__device__ __forceinline__ void append_angles(const AppendParams& p, int64_t pos, int j, float (&a)[16]) {
+    const int64_t at = pos * (p.R / 2) + j * 8;
+    *reinterpret_cast<float4*>(a) = __ldg(reinterpret_cast<const float4*>(p.cosv + at));
+    *reinterpret_cast<float4*>(a + 4) = __ldg(reinterpret_cast<const float4*>(p.cosv + at + 4));
+    *reinterpret_cast<float4*>(a + 8) = __ldg(reinterpret_cast<const float4*>(p.sinv + at));
+    *reinterpret_cast<float4*>(a + 12) = __ldg(reinterpret_cast<const float4*>(p.sinv + at + 4));
+}
+template <bool kInterleaved>
+__device__ __forceinline__ void append_rotate(float (&a)[8], float (&b)[8], const float (&cs)[16]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        if (kInterleaved) {
+            float* f = e < 4 ? a : b;
+            rotate_pair(f[2 * (e & 3)], f[2 * (e & 3) + 1], cs[e], cs[8 + e]);
+        } else {
+            rotate_pair(a[e], b[e], cs[e], cs[8 + e]);
+        }
+    }
+}
+
+// One token's queries: kUnroll steps of 32 / LPT heads on their way at a time.
+template <int D, bool kInterleaved>
+__device__ __forceinline__ void append_queries(const AppendParams& p, int t, int lane) {
+    constexpr int LPT = D / 16, HPS = 32 / LPT, kUnroll = 4;
+    const int j = lane % LPT, grp = lane / LPT;
+    const bool rot = j * 16 < p.R;
+    const int ca = !kInterleaved && rot ? j : 2 * j, cb = !kInterleaved && rot ? j + p.R / 16 : 2 * j + 1;
+    const __nv_bfloat16* src = p.Q + static_cast<int64_t>(t) * p.ldq + grp * D;
+    __nv_bfloat16* dst = p.Qo + static_cast<int64_t>(t) * p.ldqo + grp * D;
+    uint4 va[kUnroll], vb[kUnroll];
+    auto load = [&](int h0) {
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+            if (h0 + u * HPS + grp < p.H) {
+                va[u] = *reinterpret_cast<const uint4*>(src + static_cast<int64_t>(h0 + u * HPS) * D + ca * 8);
+                vb[u] = *reinterpret_cast<const uint4*>(src + static_cast<int64_t>(h0 + u * HPS) * D + cb * 8);
+            }
+    };
+    load(0);  // (the queries do not depend on the sequence: they are on their way before it is looked up)
+    const int s = append_find_seq(p.S, t, lane, [&](int i) { return p.cu[i]; });
+    const int t_begin = p.cu[s], t_end = p.cu[s + 1], ctx = p.ctx[s];
+    if (t < t_begin || t >= t_end || !append_in_range(p, s, t_begin, t_end, ctx, lane)) return;
+    float cs[16];
+    if (rot) append_angles(p, static_cast<int64_t>(ctx) + (t - t_begin), j, cs);
+    for (int h0 = 0; h0 < p.H; h0 += kUnroll * HPS) {
+        if (h0 > 0) load(h0);
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            if (h0 + u * HPS + grp < p.H) {
+                float a[8], b[8];
+                bf16x8_unpack(va[u], a);
+                bf16x8_unpack(vb[u], b);
+                if (rot) append_rotate<kInterleaved>(a, b, cs);
+                *reinterpret_cast<uint4*>(dst + static_cast<int64_t>(h0 + u * HPS) * D + ca * 8) = bf16x8_pack(a);
+                *reinterpret_cast<uint4*>(dst + static_cast<int64_t>(h0 + u * HPS) * D + cb * 8) = bf16x8_pack(b);
+            }
+        }
+    }
+}
+
 template <int D, int BS, bool kF8, bool kInterleaved>
-__global__ void __launch_bounds__(kAppendWarps * 32) kv_append_kernel(const AppendParams p) {
+__global__ void __launch_bounds__(kAppendWarps * 32) kv_append_kernel(const AppendParams p, int kv_ctas_per_slot, int q_ctas) {
     constexpr int LPT = D / 16;      // lanes per token: each owns two chunks of 8 elements
     constexpr int TPS = 32 / LPT;    // tokens per step of a warp
     constexpr int STEPS = BS / TPS;
     static_assert(BS % TPS == 0, "whole steps per block");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int task = blockIdx.y * kAppendWarps + warp;  // K heads, then V heads, then Q heads
-    if (task >= 2 * p.H_kv + (p.Q ? p.H : 0)) return;
-    const int slot = blockIdx.x;
-    const int s = append_find_seq<BS>(p.cu, p.S, slot, lane);
+    if (static_cast<int>(blockIdx.x) < q_ctas) {
+        const int t = blockIdx.x * kAppendWarps + warp;
+        if (t < p.T) append_queries<D, kInterleaved>(p, t, lane);
+        return;
+    }
+    const int kv = blockIdx.x - q_ctas;
+    const int slot = kv / kv_ctas_per_slot;
+    const int task = kv % kv_ctas_per_slot * kAppendWarps + warp;  // K heads, then V heads
+    if (task >= 2 * p.H_kv) return;
+    const bool is_v = task >= p.H_kv;
+    const int head = is_v ? task - p.H_kv : task;
+    const int s = append_find_seq(p.S, slot, lane, [&](int i) { return p.cu[i] / BS + 2 * i; });
     const int t_begin = p.cu[s], t_end = p.cu[s + 1], ctx = p.ctx[s];
     if (t_end <= t_begin) return;
     const int rel = slot - (t_begin / BS + 2 * s);
-    if (rel < 0) return;
-    const bool in_range = t_begin >= 0 && t_end <= p.T && ctx >= 0 &&
-                          (p.R == 0 || static_cast<int64_t>(ctx) + (t_end - t_begin) <= p.max_pos);
-    if (!in_range) {  // nothing of such a sequence is read or written
-        if (lane == 0) append_report(kStatusBadPosition, s, t_begin, ctx);
-        return;
-    }
+    if (rel < 0 || !append_in_range(p, s, t_begin, t_end, ctx, lane)) return;
     const int64_t blk64 = static_cast<int64_t>(ctx / BS) + rel;
     const int64_t end64 = static_cast<int64_t>(ctx) + (t_end - t_begin);
     if (blk64 * BS >= end64) return;
@@ -110,17 +182,6 @@ __global__ void __launch_bounds__(kAppendWarps * 32) kv_append_kernel(const Appe
     const int off0 = max(0, static_cast<int>(ctx - blk64 * BS));                  // new tokens sit at offsets off0 .. off1 - 1 of it
     const int off1 = static_cast<int>(min(static_cast<int64_t>(BS), end64 - blk64 * BS));
     const int tok0 = t_begin + static_cast<int>(blk64 * BS - ctx);                // token of offset 0 (may lie before the sequence's first)
-
-    const bool is_q = task >= 2 * p.H_kv, is_v = !is_q && task >= p.H_kv;
-    const int head = is_q ? task - 2 * p.H_kv : (is_v ? task - p.H_kv : task);
-    int phys = 0;
-    if (!is_q) {
-        phys = blk < p.max_blocks ? p.table[static_cast<int64_t>(s) * p.max_blocks + blk] : -1;
-        if (phys < 0 || phys >= p.num_blocks) {  // never write through a bad table entry: report and leave the block out
-            if (lane == 0) append_report(7u /* bad block */, blk, s, phys);
-            return;
-        }
-    }
 
     // this lane's two chunks: partners of the rotation inside the first R elements, neighbours elsewhere
     const int j = lane % LPT, grp = lane / LPT;
@@ -130,8 +191,8 @@ __global__ void __launch_bounds__(kAppendWarps * 32) kv_append_kernel(const Appe
         ca = j;
         cb = j + p.R / 16;
     }
-    const __nv_bfloat16* src = (is_q ? p.Q : is_v ? p.V : p.K) + static_cast<int64_t>(head) * D;
-    const int64_t ld = is_q ? p.ldq : is_v ? p.ldv : p.ldk;
+    const __nv_bfloat16* src = (is_v ? p.V : p.K) + static_cast<int64_t>(head) * D;
+    const int64_t ld = is_v ? p.ldv : p.ldk;
 
     float fa[STEPS][8], fb[STEPS][8];
 #pragma unroll
@@ -151,41 +212,27 @@ __global__ void __launch_bounds__(kAppendWarps * 32) kv_append_kernel(const Appe
         for (int i = 0; i < STEPS; ++i) {
             const int off = i * TPS + grp;
             if (off >= off0 && off < off1) {
-                const int64_t at = (blk64 * BS + off) * (p.R / 2) + j * 8;
-                float c[8], sn[8];
-                *reinterpret_cast<float4*>(c) = __ldg(reinterpret_cast<const float4*>(p.cosv + at));
-                *reinterpret_cast<float4*>(c + 4) = __ldg(reinterpret_cast<const float4*>(p.cosv + at + 4));
-                *reinterpret_cast<float4*>(sn) = __ldg(reinterpret_cast<const float4*>(p.sinv + at));
-                *reinterpret_cast<float4*>(sn + 4) = __ldg(reinterpret_cast<const float4*>(p.sinv + at + 4));
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    if (kInterleaved) {
-                        float* f = e < 4 ? fa[i] : fb[i];
-                        rotate_pair(f[2 * (e & 3)], f[2 * (e & 3) + 1], c[e], sn[e]);
-                    } else {
-                        rotate_pair(fa[i][e], fb[i][e], c[e], sn[e]);
-                    }
-                }
+                float cs[16];
+                append_angles(p, blk64 * BS + off, j, cs);
+                append_rotate<kInterleaved>(fa[i], fb[i], cs);
             }
         }
     }
+    // (the elements are on their way while the table is read)
+    const int phys = blk < p.max_blocks ? p.table[static_cast<int64_t>(s) * p.max_blocks + blk] : -1;
+    if (phys < 0 || phys >= p.num_blocks) {  // never write through a bad table entry: report and leave the block out
+        if (lane == 0) append_report(7u /* bad block */, blk, s, phys);
+        return;
+    }
 
-    if (!kF8 || is_q) {
-        __nv_bfloat16* dst;
-        int64_t pitch;
-        if (is_q) {
-            dst = p.Qo + static_cast<int64_t>(tok0) * p.ldqo + static_cast<int64_t>(head) * D;
-            pitch = p.ldqo;
-        } else {
-            dst = static_cast<__nv_bfloat16*>(is_v ? p.Vc : p.Kc) + (static_cast<int64_t>(phys) * p.H_kv + head) * BS * D;
-            pitch = D;
-        }
+    if (!kF8) {
+        __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(is_v ? p.Vc : p.Kc) + (static_cast<int64_t>(phys) * p.H_kv + head) * BS * D;
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
             const int off = i * TPS + grp;
             if (off >= off0 && off < off1) {
-                *reinterpret_cast<uint4*>(dst + off * pitch + ca * 8) = bf16x8_pack(fa[i]);
-                *reinterpret_cast<uint4*>(dst + off * pitch + cb * 8) = bf16x8_pack(fb[i]);
+                *reinterpret_cast<uint4*>(dst + off * D + ca * 8) = bf16x8_pack(fa[i]);
+                *reinterpret_cast<uint4*>(dst + off * D + cb * 8) = bf16x8_pack(fb[i]);
             }
         }
         return;
@@ -252,12 +299,13 @@ __global__ void __launch_bounds__(kAppendWarps * 32) kv_append_kernel(const Appe
 
 template <int D, int BS, bool kF8>
 int append_launch_r(const AppendParams& p, bool interleaved, cudaStream_t st) {
-    const int tasks = 2 * p.H_kv + (p.Q ? p.H : 0);
-    const dim3 grid(static_cast<unsigned>(p.T / BS + 2 * p.S), static_cast<unsigned>((tasks + kAppendWarps - 1) / kAppendWarps));
+    const int per_slot = (2 * p.H_kv + kAppendWarps - 1) / kAppendWarps, q_ctas = p.Q ? (p.T + kAppendWarps - 1) / kAppendWarps : 0;
+    const int64_t ctas = q_ctas + (p.T / BS + 2ll * p.S) * per_slot;
+    if (ctas > INT32_MAX) return 2;
     if (interleaved)
-        kv_append_kernel<D, BS, kF8, true><<<grid, kAppendWarps * 32, 0, st>>>(p);
+        kv_append_kernel<D, BS, kF8, true><<<static_cast<unsigned>(ctas), kAppendWarps * 32, 0, st>>>(p, per_slot, q_ctas);
     else
-        kv_append_kernel<D, BS, kF8, false><<<grid, kAppendWarps * 32, 0, st>>>(p);
+        kv_append_kernel<D, BS, kF8, false><<<static_cast<unsigned>(ctas), kAppendWarps * 32, 0, st>>>(p, per_slot, q_ctas);
     return cudaGetLastError() == cudaSuccess ? 0 : 4;
 }
 template <int D, bool kF8>

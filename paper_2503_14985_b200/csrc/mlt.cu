@@ -1077,8 +1077,8 @@ int append_run(const void* Q, const void* K, const void* V, const float* cosv, c
     if (!aligned16(K) || !aligned16(V) || !aligned16(K_cache) || !aligned16(V_cache) || ldk % 8 != 0 || ldv % 8 != 0) return MLT_ERR_ALIGNMENT;
     if (Q && (!aligned16(Q) || !aligned16(Q_out) || ldq % 8 != 0 || ldqo % 8 != 0)) return MLT_ERR_ALIGNMENT;
     if (rotary_dim > 0 && (!aligned16(cosv) || !aligned16(sinv))) return MLT_ERR_ALIGNMENT;
-    const int64_t tasks = 2ll * H_kv + (Q ? H : 0);
-    if (num_tokens / block_size + 2ll * num_seqs > INT32_MAX || tasks > 65535) return MLT_ERR_UNSUPPORTED;
+    if (H_kv > 65535 || H > 65535 || num_tokens / 4 + (num_tokens / block_size + 2ll * num_seqs) * ((H_kv + 1) / 2) > INT32_MAX - 1)
+        return MLT_ERR_UNSUPPORTED;  // grid size
     DeviceInfo dev;
     const int rc = get_device(&dev);
     if (rc != MLT_OK) return rc;

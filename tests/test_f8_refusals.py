@@ -63,7 +63,7 @@ def test_append_statuses(f8):
         assert append(f8, **{name: 0}) == INVALID
     assert append(f8, H_kv=0) == INVALID and append(f8, H=0) == INVALID and append(f8, rotary_dim=80) == INVALID
     assert append(f8, D=96) == UNSUPPORTED and append(f8, block_size=64) == UNSUPPORTED and append(f8, rotary_dim=24) == UNSUPPORTED
-    assert append(f8, H=65534, ldq=65534 * 64, ldqo=65534 * 64) == UNSUPPORTED and append(f8, num_seqs=2 ** 30) == UNSUPPORTED
+    assert append(f8, H=65536, ldq=65536 * 64, ldqo=65536 * 64) == UNSUPPORTED and append(f8, num_seqs=2 ** 30) == UNSUPPORTED
     assert append(f8, ldk=120) == INVALID and append(f8, ldv=120) == INVALID and append(f8, ldq=504) == INVALID and append(f8, ldqo=504) == INVALID
     assert append(f8, ldk=132) == ALIGNMENT and append(f8, ldv=132) == ALIGNMENT and append(f8, ldq=516) == ALIGNMENT and append(f8, ldqo=516) == ALIGNMENT
     for name in ("Q", "K", "V", "Q_out", "K_cache", "V_cache", "cos", "sin"):
