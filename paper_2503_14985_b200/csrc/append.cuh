@@ -158,6 +158,7 @@ __global__ void __launch_bounds__(kAppendWarps * 32) kv_append_kernel(const Appe
     constexpr int TPS = 32 / LPT;    // tokens per step of a warp
     constexpr int STEPS = BS / TPS;
     static_assert(BS % TPS == 0, "whole steps per block");
+    pdl_begin();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (static_cast<int>(blockIdx.x) < q_ctas) {
         const int t = blockIdx.x * kAppendWarps + warp;
@@ -302,11 +303,10 @@ int append_launch_r(const AppendParams& p, bool interleaved, cudaStream_t st) {
     const int per_slot = (2 * p.H_kv + kAppendWarps - 1) / kAppendWarps, q_ctas = p.Q ? (p.T + kAppendWarps - 1) / kAppendWarps : 0;
     const int64_t ctas = q_ctas + (p.T / BS + 2ll * p.S) * per_slot;
     if (ctas > INT32_MAX) return 2;
-    if (interleaved)
-        kv_append_kernel<D, BS, kF8, true><<<static_cast<unsigned>(ctas), kAppendWarps * 32, 0, st>>>(p, per_slot, q_ctas);
-    else
-        kv_append_kernel<D, BS, kF8, false><<<static_cast<unsigned>(ctas), kAppendWarps * 32, 0, st>>>(p, per_slot, q_ctas);
-    return cudaGetLastError() == cudaSuccess ? 0 : 4;
+    const dim3 grid(static_cast<unsigned>(ctas)), block(kAppendWarps * 32);
+    const cudaError_t e = interleaved ? pdl_launch(kv_append_kernel<D, BS, kF8, true>, grid, block, 0, st, 0, p, per_slot, q_ctas)
+                                      : pdl_launch(kv_append_kernel<D, BS, kF8, false>, grid, block, 0, st, 0, p, per_slot, q_ctas);
+    return e == cudaSuccess ? 0 : 4;
 }
 template <int D, bool kF8>
 int append_launch_bs(const AppendParams& p, int block_size, bool interleaved, cudaStream_t st) {

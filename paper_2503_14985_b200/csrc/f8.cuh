@@ -12,6 +12,33 @@ namespace mlt {
 
 constexpr int kF8MinExp = -64;
 
+// The kernels of the 8-bit path follow one another in short calls, so they are launched with programmatic stream
+// serialisation: a kernel's blocks may be placed while the one before it in the stream drains, and wait there
+// (pdl_begin, before the first access to memory and before any tensor memory is allocated) until that one has completed and
+// its writes are visible.  Every block executes pdl_begin, so a kernel's completion implies its predecessors'.
+// Measured back to back: 1 to 2 us per call.
+__device__ __forceinline__ void pdl_begin() {
+    pdl_launch_dependents();
+    cudaGridDependencySynchronize();
+}
+template <class... Params, class... Args>
+cudaError_t pdl_launch(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, int cluster, Args... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attrs[2];
+    attrs[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attrs[0].val.programmaticStreamSerializationAllowed = 1;
+    attrs[1].id = cudaLaunchAttributeClusterDimension;
+    attrs[1].val.clusterDim.x = static_cast<unsigned>(cluster);
+    attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
+    cfg.attrs = attrs;
+    cfg.numAttrs = cluster > 0 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
 // {hi, lo} -> two E4M3 codes, round to nearest even; magnitudes beyond 448 (infinities too) become 448, NaN stays NaN
 __device__ __forceinline__ uint32_t f8x2_from_f32(float lo, float hi) {
     uint16_t r;

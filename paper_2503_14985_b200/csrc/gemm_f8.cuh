@@ -158,6 +158,7 @@ gemm_f8_split_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_co
         prefetch_tensormap(&tmap_a);
         prefetch_tensormap(&tmap_b);
     }
+    pdl_begin();
     if (warp == 1) {
         tmem_alloc(&tmem_base_slot, 512);
         tmem_relinquish();
@@ -391,6 +392,7 @@ gemm_f8_big_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
         prefetch_tensormap(&tmap_b);
         prefetch_tensormap(&tmap_c);
     }
+    pdl_begin();
     if (warp == 1) {
         if constexpr (kPair) {
             tmem_alloc_pair(tmem_base_slot, 512);

@@ -1018,40 +1018,16 @@ int mlt_gemm_f8(const void* A, const float* scale_a, const void* B, const float*
         if (rc != MLT_OK) return rc;
         p.group_m = tiles_n >= 32 && plan.big == 2 ? 16 : 8;
         const int tiles = static_cast<int>(tiles_m * tiles_n);
-        cudaLaunchConfig_t big = {};
-        big.blockDim = dim3(kF8BigThreads);
-        big.stream = st;
-        cudaLaunchAttribute pair;
-        pair.id = cudaLaunchAttributeClusterDimension;
-        pair.val.clusterDim.x = plan.big;
-        pair.val.clusterDim.y = pair.val.clusterDim.z = 1;
-        big.attrs = &pair;
-        big.numAttrs = 1;
-        cudaError_t e;
-        if (plan.big == 2) {
-            big.gridDim = dim3(2 * std::min(tiles, dev.sm_count / 2));
-            big.dynamicSmemBytes = GemmF8BigSmem<true>::kTotal;
-            e = cudaLaunchKernelEx(&big, gemm_f8_big_kernel<true>, ta, tb, tc, p);
-        } else {
-            big.gridDim = dim3(std::min(tiles, dev.sm_count));
-            big.dynamicSmemBytes = GemmF8BigSmem<false>::kTotal;
-            e = cudaLaunchKernelEx(&big, gemm_f8_big_kernel<false>, ta, tb, tc, p);
-        }
-        return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? MLT_OK : MLT_ERR_CUDA;
+        const cudaError_t e =
+            plan.big == 2 ? pdl_launch(gemm_f8_big_kernel<true>, dim3(2 * std::min(tiles, dev.sm_count / 2)), dim3(kF8BigThreads),
+                                       GemmF8BigSmem<true>::kTotal, st, 2, ta, tb, tc, p)
+                          : pdl_launch(gemm_f8_big_kernel<false>, dim3(std::min(tiles, dev.sm_count)), dim3(kF8BigThreads),
+                                       GemmF8BigSmem<false>::kTotal, st, 1, ta, tb, tc, p);
+        return e == cudaSuccess ? MLT_OK : MLT_ERR_CUDA;
     }
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(tiles_m * tiles_n * plan.cluster));
-    cfg.blockDim = dim3(kF8Threads);
-    cfg.dynamicSmemBytes = gemm_f8_split_smem(bn, plan.a_rows, plan.stages);
-    cfg.stream = st;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = static_cast<unsigned>(plan.cluster);
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, gemm_f8_split_kernel, ta, tb, p);
-    return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? MLT_OK : MLT_ERR_CUDA;
+    const cudaError_t e = pdl_launch(gemm_f8_split_kernel, dim3(static_cast<unsigned>(tiles_m * tiles_n * plan.cluster)), dim3(kF8Threads),
+                                     gemm_f8_split_smem(bn, plan.a_rows, plan.stages), st, plan.cluster, ta, tb, p);
+    return e == cudaSuccess ? MLT_OK : MLT_ERR_CUDA;
 }
 
 }  // extern "C"

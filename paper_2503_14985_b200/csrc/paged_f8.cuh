@@ -88,7 +88,6 @@ __device__ __forceinline__ void l2_prefetch(const void* base, int64_t bytes) {
 template <int D, int G, int BS>
 __global__ void __launch_bounds__(kPagedThreads, kPagedF8CtasPerSm)
 paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const PagedF8Params p) {
-    pdl_launch_dependents();
     constexpr int U = kPagedF8Unit;
     constexpr int PP = D / 64;       // 16-byte pieces of a token's K per lane
     constexpr int MT = D / 16;       // row tiles of the output
@@ -116,6 +115,7 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
         prefetch_tensormap(&tmap_v);
     }
 
+    pdl_begin();
     // The lengths, the table entries they lead to and the cache those point at are three memory latencies in a row: while the
     // first is under way, the CTAs together bring the table and the queries into L2.
     l2_prefetch(p.block_table, static_cast<int64_t>(p.num_seqs) * p.max_blocks * 4);
@@ -537,6 +537,7 @@ __global__ void __launch_bounds__(kPagedF8CombineThreads) paged_f8_combine_kerne
     __shared__ float sm_m[kWarps][G];
     __shared__ float4 sm_o[kPagedF8CombineThreads];
     __shared__ float sm_l[kPagedF8CombineThreads];
+    pdl_launch_dependents();
     const int s = blockIdx.x / p.H_kv, kvh = blockIdx.x % p.H_kv;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int below = 0, total = 0;
@@ -624,19 +625,10 @@ template <int D, int G, int BS>
 int paged_f8_launch_one(const CUtensorMap& tk, const CUtensorMap& tv, const PagedF8Params& p, cudaStream_t st) {
     const int64_t grid = p.ctas ? p.ctas : static_cast<int64_t>(p.num_seqs) * p.H_kv;
     if (grid > INT32_MAX || static_cast<int64_t>(p.num_seqs) * p.H > INT32_MAX) return 2;
-    paged_f8_decode_kernel<D, G, BS><<<static_cast<unsigned>(grid), kPagedThreads, paged_f8_smem_bytes<D>(), st>>>(tk, tv, p);
-    if (cudaGetLastError() != cudaSuccess) return 4;
+    if (pdl_launch(paged_f8_decode_kernel<D, G, BS>, dim3(static_cast<unsigned>(grid)), dim3(kPagedThreads), paged_f8_smem_bytes<D>(), st, 0, tk, tv, p) != cudaSuccess)
+        return 4;
     if (p.ctas == 0) return 0;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(p.num_seqs * p.H_kv));
-    cfg.blockDim = dim3(kPagedF8CombineThreads);
-    cfg.stream = st;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, paged_f8_combine_kernel<D, G, BS>, p) == cudaSuccess ? 0 : 4;
+    return pdl_launch(paged_f8_combine_kernel<D, G, BS>, dim3(static_cast<unsigned>(p.num_seqs * p.H_kv)), dim3(kPagedF8CombineThreads), 0, st, 0, p) == cudaSuccess ? 0 : 4;
 }
 template <int D, int G>
 int paged_f8_launch_bs(const CUtensorMap& tk, const CUtensorMap& tv, const PagedF8Params& p, int block_size, cudaStream_t st) {

@@ -73,6 +73,7 @@ constexpr int kQuantizeThreads = 128;
 template <int kRows>
 __global__ void __launch_bounds__(kQuantizeThreads) quantize_rows_kernel(const QuantizeParams p) {
     static_assert(kRows <= 16, "one lane of a half warp per row stores its scale");
+    pdl_begin();
     const int lane = threadIdx.x & 31;
     const int col_tiles = (p.K + 255) / 256;
     const int64_t tile = static_cast<int64_t>(blockIdx.x) * (kQuantizeThreads / 32) + (threadIdx.x >> 5);
@@ -110,6 +111,7 @@ __global__ void __launch_bounds__(kQuantizeThreads) quantize_rows_kernel(const Q
 constexpr int kQuantizeBlockThreads = 256;
 __global__ void __launch_bounds__(kQuantizeBlockThreads) quantize_blocks_kernel(const QuantizeParams p) {
     __shared__ uint32_t sm[kQuantizeBlockThreads / 32];
+    pdl_begin();
     const int kbs = (p.K + 127) / 128;
     const int rb = static_cast<int>(blockIdx.x / kbs), kb = static_cast<int>(blockIdx.x % kbs);
     const int c0 = kb * 128 + (threadIdx.x & 15) * 8, r0 = rb * 128 + (threadIdx.x >> 4);
@@ -148,13 +150,11 @@ inline int quantize_launch(const QuantizeParams& p, int block_rows, cudaStream_t
         const int64_t tiles = static_cast<int64_t>((p.M + kRows - 1) / kRows) * ((p.K + 255) / 256);
         const int64_t ctas = (tiles + kQuantizeThreads / 32 - 1) / (kQuantizeThreads / 32);
         if (ctas > INT32_MAX) return 2;
-        quantize_rows_kernel<kRows><<<static_cast<unsigned>(ctas), kQuantizeThreads, 0, st>>>(p);
-    } else {
-        const int64_t ctas = static_cast<int64_t>((p.M + 127) / 128) * ((p.K + 127) / 128);
-        if (ctas > INT32_MAX) return 2;
-        quantize_blocks_kernel<<<static_cast<unsigned>(ctas), kQuantizeBlockThreads, 0, st>>>(p);
+        return pdl_launch(quantize_rows_kernel<kRows>, dim3(static_cast<unsigned>(ctas)), dim3(kQuantizeThreads), 0, st, 0, p) == cudaSuccess ? 0 : 4;
     }
-    return cudaGetLastError() == cudaSuccess ? 0 : 4;
+    const int64_t ctas = static_cast<int64_t>((p.M + 127) / 128) * ((p.K + 127) / 128);
+    if (ctas > INT32_MAX) return 2;
+    return pdl_launch(quantize_blocks_kernel, dim3(static_cast<unsigned>(ctas)), dim3(kQuantizeBlockThreads), 0, st, 0, p) == cudaSuccess ? 0 : 4;
 }
 
 }  // namespace mlt
