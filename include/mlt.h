@@ -179,6 +179,9 @@ int mlt_paged_attn_decode_static(const void* Q, const void* K_cache, const void*
 /*
  * ---- The 8-bit serving path (library additions; the paper's workloads have no 8-bit form) ----
  *
+ * These calls are launched so that a kernel's blocks may be placed while the kernel before it in the stream drains; they
+ * wait for its completion before they touch memory, so nothing changes for the caller.
+ *
  * E4M3 values are passed as bytes.  A decoding step runs them in this order: mlt_quantize_f8 (activations) ->
  * mlt_gemm_f8 (projections) -> mlt_kv_append_f8 -> mlt_paged_attn_decode_f8 -> mlt_quantize_f8 -> mlt_gemm_f8.
  *
@@ -232,9 +235,9 @@ int mlt_gemm_f8(const void* A, const float* scale_a, const void* B, const float*
  *                Pair i is (i, i + rotary_dim / 2), or with `interleaved` (2 i, 2 i + 1); (a, b) becomes
  *                (a cos_i - b sin_i, b cos_i + a sin_i).  The other elements pass through.
  *   cu_tokens    device, int32, [num_seqs + 1], ascending from 0;  context_lens device, int32, [num_seqs]
- *   block_table  device, int32, [num_seqs, max_blocks_per_seq].  The blocks that one call writes must differ between
- *                sequences (a shared block is copied before a sequence appends to it); where two share one all the
- *                same, what its tokens hold afterwards is undefined.
+ *   block_table  device, int32, [num_seqs, max_blocks_per_seq].  The entries that one call writes through must all differ,
+ *                within a sequence and between sequences (a shared block is copied before a sequence appends to it);
+ *                where two are equal all the same, what that block's tokens and scales hold afterwards is undefined.
  *   Q_out        device, BF16 out, pitch ldqo; may be Q itself with the same pitch
  *   K_cache, V_cache  device, [num_blocks, H_kv, block_size, D]
  *   k_scale, v_scale  device, FP32, [num_blocks, H_kv] (E4M3 cache).  A block's scale becomes the larger of the scale it

@@ -221,6 +221,31 @@ def test_many_sequences(S):
     assert (got.transpose(0, 2, 1, 3)[~touched] == SENTINEL).all()
 
 
+@pytest.mark.parametrize("cache8", [False, True])
+def test_no_tokens_and_no_sequences(cache8):
+    call = mlt.kv_append_f8 if cache8 else mlt.kv_append
+    kinds = dict(device="cuda", dtype=torch.int32)
+    caches = [torch.ones(3, 2, 16, 64, device="cuda").to(torch.float8_e4m3fn if cache8 else torch.bfloat16) for _ in range(2)]
+    scales = [torch.ones(3, 2, device="cuda") for _ in range(2)] if cache8 else []
+    q, k = torch.zeros(0, 4, 64, device="cuda", dtype=torch.bfloat16), torch.zeros(0, 2, 64, device="cuda", dtype=torch.bfloat16)
+    assert call(q, k, k, None, None, torch.zeros(3, **kinds), torch.zeros(2, **kinds), torch.zeros(2, 2, **kinds), *caches, *scales).shape == (0, 4, 64)
+    q, k = (torch.ones(5, h, 64, device="cuda", dtype=torch.bfloat16) for h in (4, 2))  # a batch of padding alone
+    out = torch.full_like(q, 3.0)
+    call(q, k, k, None, None, torch.zeros(3, **kinds), torch.zeros(2, **kinds), torch.zeros(2, 2, **kinds), *caches, *scales, Q_out=out)
+    call(q, k, k, None, None, torch.zeros(1, **kinds), torch.zeros(0, **kinds), torch.zeros(0, 2, **kinds), *caches, *scales, Q_out=out)
+    assert_device_healthy()
+    assert (out == 3).all() and all((c.float() == 1).all() for c in caches + scales)
+
+
+def test_many_query_heads_and_few():
+    # 71 heads do not fill the steps of a warp; the angles are shared by all of them
+    for H, Hkv, D in ((71, 1, 64), (40, 5, 128), (1, 1, 128)):
+        c = case([37, 2], [5, 40], H, Hkv, D, D, 16, False, seed=H)
+        Kc, Vc = (torch.zeros(c["blocks"], Hkv, 16, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        check_q(c, mlt.kv_append(c["q"], c["k"], c["v"], *dev_args(c), Kc, Vc), 39)
+    assert_device_healthy()
+
+
 def test_queries_in_place_and_without_queries():
     c = case([19, 30], [3, 0], 4, 2, 128, 128, 16, False, seed=30)
     args = dev_args(c)

@@ -110,3 +110,40 @@ def test_prompt_then_decoding_steps_and_the_captured_step():
         ctx += 1
         lens += 1
     assert_device_healthy()
+
+
+def test_dependent_calls_back_to_back_and_one_by_one_give_the_same_bits():
+    # the launches overlap the drain of the kernel before them: a call that read its inputs too early, or wrote before an earlier
+    # call had read, would differ from the same chain with a synchronisation after every call
+    g = torch.Generator().manual_seed(3)
+    w = [mlt.quantize_f8((torch.randn(512, 512, generator=g) * 512 ** -0.5).to(torch.bfloat16).cuda(), block_rows=128) for _ in range(2)]
+    x0 = torch.randn(48, 512, generator=g).to(torch.bfloat16).cuda()
+    cu = torch.arange(49, dtype=torch.int32, device="cuda")
+    cos, sin = (torch.randn(64, 32, generator=g).cuda() for _ in range(2))
+    table = torch.randperm(48 * 4, generator=g).to(torch.int32).view(48, 4).cuda()
+    ws = torch.empty(mlt.paged_attn_f8_workspace_bytes(48, 8, 2, 64), dtype=torch.uint8, device="cuda")
+    q8, sq = torch.empty(48, 512, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn), torch.empty(4, 48, device="cuda")
+    h = torch.empty(48, 512, dtype=torch.bfloat16, device="cuda")
+
+    def chain(after):
+        kc, vc = (torch.zeros(192, 2, 16, 64, device="cuda").to(torch.float8_e4m3fn) for _ in range(2))
+        ks, vs = (torch.ones(192, 2, device="cuda") for _ in range(2))
+        x, ctx = x0.clone(), torch.zeros(48, dtype=torch.int32, device="cuda")
+        seen = []
+        for step in range(40):
+            mlt.quantize_f8(x, Q=q8, scales=sq); after()                      # buffers are written again while the call before
+            mlt.gemm_f8(q8, sq, *w[step % 2], h); after()                     # may still be draining
+            kv = h.view(48, 8, 64)
+            mlt.kv_append_f8(kv, kv[:, 2:4], kv[:, 4:6], cos, sin, cu, ctx, table, kc, vc, ks, vs, Q_out=x.view(48, 8, 64)); after()
+            ctx += 1; after()
+            o, lse = mlt.paged_attn_decode_f8(x.view(48, 8, 64), kc, vc, ks, vs, table, ctx, scale=0.125, workspace=ws); after()
+            x = o.view(48, 512)
+            seen += [x, lse]
+        torch.cuda.synchronize()
+        return seen + [t.float() for t in (kc, vc, ks, vs)]
+
+    one_by_one = chain(torch.cuda.synchronize)
+    for _ in range(3):
+        for a, b in zip(chain(lambda: None), one_by_one):
+            assert torch.equal(a, b)
+    assert_device_healthy()

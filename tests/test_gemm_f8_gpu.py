@@ -62,6 +62,47 @@ def test_parity(M, N, K):
     check(run(M, N, K, a, sa, b, sb), ref, mag, K)
 
 
+# (M, N, K): which kernel; ragged in every direction, a pair whose second CTA has no rows (M mod 256 <= 128), right edges that
+# are no multiple of 8 columns, more tiles than SMs
+BY_KERNEL = {(4930, 261, 3931): 2, (5249, 333, 3500): 2, (3176, 546, 3552): 2, (4100, 4100, 2050): 2, (128, 20000, 300): 1, (64, 40000, 300): 1,
+             (300, 39999, 200): 1, (2600, 5101, 1000): 1, (100, 20003, 600): 0, (16, 28671, 1030): 0}
+
+
+@pytest.mark.parametrize("M,N,K", BY_KERNEL)
+def test_every_kernel(M, N, K):
+    assert mlt.gemm_f8_plan(M, N, K, sm_count=0)["kernel"] == BY_KERNEL[M, N, K]
+    a, sa, b, sb = operands(M, N, K, seed=M + N + K)
+    got = run(M, N, K, a, sa, b, sb)
+    rows = np.unique(np.concatenate([np.arange(min(M, 40)), np.arange(max(0, M - 150), M), np.random.RandomState(0).randint(0, M, 200)]))
+    ref, mag = f8.gemm(a[rows][:, :K], sa[:, rows], b[:, :K], sb)
+    check(got[rows], ref, mag, K)
+
+
+def test_padded_scale_pitches():
+    M, N, K = 150, 300, 500
+    a, sa, b, sb = operands(M, N, K, seed=2)
+    ref, mag = f8.gemm(a[:, :K], sa, b[:, :K], sb)
+    wide_a, wide_b = torch.full((4, M + 5), float("nan"), device="cuda"), torch.full((3, 4 + 3), float("nan"), device="cuda")
+    wide_a[:, 1:M + 1], wide_b[:, 2:6] = torch.from_numpy(sa), torch.from_numpy(sb)
+    got = to_f64(mlt.gemm_f8(dev8(a, K), wide_a[:, 1:M + 1], dev8(b, K), wide_b[:, 2:6]))
+    check(got, ref, mag, K)
+
+
+def test_output_beyond_32_bit_offsets():
+    # 2.3 G results (4.6 GB): the last rows lie beyond 2^31 elements; every row of A is the same but the last three
+    M, N, K = 80000, 28680, 128
+    a, sa, b, sb = operands(4, N, K, seed=6)
+    A = dev8(a, K)[:1].view(torch.uint8).expand(M, K).contiguous()
+    A[-3:] = dev8(a, K)[1:].view(torch.uint8)
+    s = torch.full((1, M), float(sa[0, 0]), device="cuda")
+    s[0, -3:] = torch.from_numpy(sa[0, 1:]).cuda()
+    C = mlt.gemm_f8(A.view(torch.float8_e4m3fn), s, dev8(b, K), torch.from_numpy(sb).cuda())
+    ref, mag = f8.gemm(a[:, :K], sa, b[:, :K], sb)
+    check(to_f64(C[-4:]), ref, mag, K)
+    assert torch.equal(C[:-3].min(0).values, C[0]) and torch.equal(C[:-3].max(0).values, C[0])
+    assert_device_healthy()
+
+
 @pytest.mark.parametrize("seed", range(24))
 def test_random_shapes(seed):
     rng = np.random.RandomState(900 + seed)

@@ -133,6 +133,15 @@ def test_more_sequences_than_the_scan_table():
     assert_device_healthy()
 
 
+def test_more_units_than_one_batch_of_table_entries():
+    # a warp reads the entries and scales of 32 of its units (4096 tokens) at a time; without scratch one CTA walks the whole row
+    for bs in (8, 16, 32):
+        c = Case([20000, 8191, 4097], 2, 1, 64, bs, seed=20 + bs)
+        for ws in ("full", 0):
+            c.check(*c.run(ws))
+    assert_device_healthy()
+
+
 def test_block_scales_of_very_different_size():
     # powers of two from 2^-40 to 2^15 from block to block: V's scale is applied relative to the largest met so far
     c = Case([400, 333], 8, 2, 128, 8, seed=4)
