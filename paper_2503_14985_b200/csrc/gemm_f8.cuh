@@ -137,22 +137,23 @@ gemm_f8_split_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_co
     const int cols0 = (bn / 16 + 1) / 2 * 16;  // columns of the first four promotion warps; the others have the rest
     const int quarters = (rows + 31) / 32, halves = bn > cols0 ? 2 : 1;  // promotion warps with something to do
 
-    if (threadIdx.x == 0) {
-        for (int s = 0; s < p.stages; ++s) {
-            mbar_init(&full[s], 1);
-            mbar_init(&empty[s], 1);
+    // one barrier per thread (one thread would take a microsecond for all of them)
+    if (threadIdx.x < kF8MaxStages) {
+        mbar_init(&full[threadIdx.x], 1);
+        mbar_init(&empty[threadIdx.x], 1);
+        if (threadIdx.x < 4) {
+            mbar_init(&acc_full[threadIdx.x], 1);
+            mbar_init(&acc_empty[threadIdx.x], quarters * halves);
         }
-        for (int a = 0; a < bufs; ++a) {
-            mbar_init(&acc_full[a], 1);
-            mbar_init(&acc_empty[a], quarters * halves);
+        if (threadIdx.x < kF8ScaleSlots) {
+            mbar_init(&scale_full[threadIdx.x], 32);
+            mbar_init(&scale_empty[threadIdx.x], quarters * halves);
         }
-        for (int a = 0; a < kF8ScaleSlots; ++a) {
-            mbar_init(&scale_full[a], 32);
-            mbar_init(&scale_empty[a], quarters * halves);
+        if (threadIdx.x == 0) {
+            abort_word = 0;
+            if (blockIdx.x == 0) clock_probe(0, 0);
         }
-        abort_word = 0;
         fence_mbar_init();
-        if (blockIdx.x == 0) clock_probe(0, 0);
     }
     if (warp == 0 && lane == 0) {
         prefetch_tensormap(&tmap_a);
@@ -285,23 +286,51 @@ gemm_f8_split_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_co
         tc_fence_before();
         cluster_sync_all();
         const int g0 = bn / 4 * slice / S, groups = bn / 4 * (slice + 1) / S - g0;  // groups of four columns
+        const int per_row = groups > 16 ? 32 : groups > 8 ? 16 : groups > 4 ? 8 : 4;  // lanes to a row
+        const int rows_at_once = 32 / per_row * 8;                                       // of the eight warps
         const uint32_t part_addr = smem_u32(part);
-        for (int idx = threadIdx.x - 128; idx < rows * groups; idx += kF8Threads - 128) {
-            const int row = idx / groups, c = (g0 + idx % groups) * 4;
-            float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            for (int s2 = 0; s2 < S; ++s2) {
-                const float4 v = ld_shared_cluster_f32x4(map_to_cta(part_addr + (row * part_pitch + c) * 4, s2));
-                sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
+        // four rows at a time, whose loads do not wait for one another; the CTA's own tile by plain loads
+        auto finish = [&](auto alone) {
+            for (int c = g0 + lane % per_row; c < g0 + groups; c += per_row) {
+                const int out = n0 + c * 4;
+                for (int row = (warp - 4) * (32 / per_row) + lane / per_row; row < rows; row += 4 * rows_at_once) {
+                    float4 sum[4];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) sum[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    if constexpr (decltype(alone)::value) {
+#pragma unroll
+                        for (int u = 0; u < 4; ++u)
+                            if (row + u * rows_at_once < rows) sum[u] = *reinterpret_cast<const float4*>(part + (row + u * rows_at_once) * part_pitch + c * 4);
+                    } else {
+                        for (int s2 = 0; s2 < S; ++s2) {
+                            const uint32_t peer = map_to_cta(part_addr + (row * part_pitch + c * 4) * 4, s2);
+                            float4 v[4];
+#pragma unroll
+                            for (int u = 0; u < 4; ++u)
+                                if (row + u * rows_at_once < rows) v[u] = ld_shared_cluster_f32x4(peer + u * rows_at_once * part_pitch * 4);
+#pragma unroll
+                            for (int u = 0; u < 4; ++u)
+                                if (row + u * rows_at_once < rows) {
+                                    sum[u].x += v[u].x; sum[u].y += v[u].y; sum[u].z += v[u].z; sum[u].w += v[u].w;
+                                }
+                        }
+                    }
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        if (row + u * rows_at_once < rows) {
+                            __nv_bfloat16* dst = p.C + static_cast<int64_t>(m0 + row + u * rows_at_once) * p.ldc + out;
+                            if (out + 4 <= p.N) {
+                                *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(sum[u].x, sum[u].y), pack_bf16x2(sum[u].z, sum[u].w));
+                            } else {
+                                const float a[4] = {sum[u].x, sum[u].y, sum[u].z, sum[u].w};
+                                for (int k = 0; k < 4 && out + k < p.N; ++k) dst[k] = __float2bfloat16(a[k]);
+                            }
+                        }
+                    }
+                }
             }
-            const int out = n0 + c;
-            __nv_bfloat16* dst = p.C + static_cast<int64_t>(m0 + row) * p.ldc + out;
-            if (out + 4 <= p.N) {
-                *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(sum.x, sum.y), pack_bf16x2(sum.z, sum.w));
-            } else {
-                const float a[4] = {sum.x, sum.y, sum.z, sum.w};
-                for (int j = 0; j < 4 && out + j < p.N; ++j) dst[j] = __float2bfloat16(a[j]);
-            }
-        }
+        };
+        if (S == 1) finish(std::true_type()); else finish(std::false_type());
         __syncwarp();
     }
 
@@ -375,16 +404,14 @@ gemm_f8_big_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
         n0 = r / rows * 256;
     };
 
-    if (threadIdx.x == 0) {
-        for (int s = 0; s < kStages; ++s) {
-            mbar_init(&full[s], 1);
-            mbar_init(&empty[s], 1);
+    if (threadIdx.x < kStages) {  // one barrier per thread
+        mbar_init(&full[threadIdx.x], 1);
+        mbar_init(&empty[threadIdx.x], 1);
+        if (threadIdx.x < 2) {
+            mbar_init(&acc_full[threadIdx.x], 1);
+            mbar_init(&acc_empty[threadIdx.x], kPair ? 16 : 8);  // every promotion warp
         }
-        for (int a = 0; a < 2; ++a) {
-            mbar_init(&acc_full[a], 1);
-            mbar_init(&acc_empty[a], kPair ? 16 : 8);  // every promotion warp
-        }
-        *abort_flag = 0;
+        if (threadIdx.x == 0) *abort_flag = 0;
         fence_mbar_init();
     }
     if (warp == 0 && lane == 0) {
