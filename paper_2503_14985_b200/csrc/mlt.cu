@@ -866,8 +866,11 @@ struct GemmF8Plan {
 //   5 us of launch, fill and drain per round of tiles; one K block takes 500 (pairs) or 520 ns (128 x 256 tiles; 680 with a
 //   single tile row, whose scales come from HBM), 200 + 1.6 bn + 2 a_rows in the split kernel, whose reduction over a cluster
 //   adds 0.7 us; and never less than the operands at the copy bandwidth.
-// Measured where they part: 16 x 28672 x 4096 split kernel 26 us, 128 x 256 tiles 45; 128 x 28672 x 4096 33 against 27;
-// 200 x 5000 x 4200 18 against 26; 512 x 4096 x 4096 21 against 20; 4096^3 122, 128 x 256 tiles 72, pairs 69.
+// Measured where they part (us: split kernel, 128 x 256 tiles, pairs):
+//   16 x 28672 x 4096   25  30  36      128 x 28672 x 4096  28  26  35      200 x 28672 x 4096  47  38  36
+//   512 x 5000 x 4200   23  24  21      777 x 5000 x 4200   28  25  36      512 x 4096 x 4096   18  20  19
+//   1024 x 4096 x 4096  26  20  20      2048 x 4096 x 4096  51  36  35      4096^3             100  69  65
+// Over 91 problems the pick was at most 7 % behind the fastest, with operands off the 128-byte grid 12 %.
 // cluster_slots: resident CTAs in clusters of 2, 4, 8 as the device reports them, or null for the SM count rounded down.
 GemmF8Plan gemm_f8_plan(int64_t M, int64_t N, int64_t K, int sm_count, const int* cluster_slots) {
     const int num_kb = static_cast<int>((K + kF8BK - 1) / kF8BK);

@@ -15,7 +15,7 @@
 //     are held times 2^14, so that weights down to 2^-28 of the largest keep FP16's full precision.
 //   * Scores, maxima, sums and outputs are FP32; the sum takes the probabilities before their rounding to FP16.
 //
-// Data path: tensor copies (TMA) of whole (block, head) pieces into a two-deep ring of 32-token units per warp, swizzled so
+// Data path: tensor copies (TMA) of whole (block, head) pieces into a three-deep ring of 32-token units per warp, swizzled so
 // that the fragment loads meet no bank conflict at D = 128 (a lane's 16 bytes of K cover 16 elements of one token: the
 // order of an MMA's summation index is free as long as both operands agree, as is the order of its output columns).
 //
@@ -24,6 +24,11 @@
 // share is finished by its CTA; otherwise each CTA that meets row r writes an unnormalised partial into slot
 // r + (its own index) -- strictly increasing along the line, so rows + CTAs slots are enough -- and a second kernel
 // combines them in ascending order.  Without scratch, or beyond 1024 sequences, one CTA works on each row.
+//
+// Measured, both kernels: 32 sequences of 2k to 4k tokens, 32 heads over 4, 29 us (3.5 TB/s), 2 of 32k with 8 heads 30 us
+// (4.3 TB/s).  The streams run at the copy's rate; around them lie 6 us of dependent latencies (lengths, table, first data)
+// and 2.4 us of the combine kernel.  Alternatives: heads as rows 37 and 37, units of 16 tokens 31 to 33, two stages and three
+// CTAs per SM 30 and 32.5, copies issued ahead into the CTA's next row 30 and 32 (longer loop).
 #pragma once
 
 #include "f8.cuh"
@@ -526,7 +531,7 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
 
 // Rows that several CTAs worked on: sum of their partials, rescaled to the common maximum.  One CTA per (sequence, KV head):
 // a thread owns four neighbouring outputs of one head and every `splits`-th partial, so that a row with many partials
-// uses all threads too.  Also writes the rows of empty sequences.
+// uses all threads too.  Also writes the rows of empty sequences.  2.4 us at 128 and 16 KV rows (5.7 with a CTA per query head).
 constexpr int kPagedF8CombineThreads = 256;
 template <int D, int G, int BS>
 __global__ void __launch_bounds__(kPagedF8CombineThreads) paged_f8_combine_kernel(const PagedF8Params p) {
