@@ -351,6 +351,19 @@ def _call(name, fn, tensors, args, stream):
         raise MltError(rc, name)
 
 
+def _new(t, shape, dtype, stream):
+    """An output on t's device.  Its memory belongs to the stream that the call runs on: the allocator's blocks of another
+    stream may still be in use by what that stream has under way."""
+    if stream is None or not t.is_cuda:
+        return t.new_empty(shape, dtype=dtype)
+    import torch
+    if not isinstance(stream, torch.cuda.Stream):
+        address = _stream(stream)
+        stream = torch.cuda.ExternalStream(address, device=t.device) if address else torch.cuda.default_stream(t.device)
+    with torch.cuda.stream(stream):
+        return t.new_empty(shape, dtype=dtype)
+
+
 def _pitch(t, width):
     """Row pitch of a 2-D tensor with unit inner stride (of a single row: any pitch serves)."""
     st = t.stride()
@@ -377,7 +390,7 @@ def quantize_f8(X, *, block_rows: int = 1, Q=None, scales=None, stream=None):
     shape = (kb, M) if block_rows == 1 else ((M + 127) // 128, kb)
     ldx = _pitch(X, (K + 7) // 8 * 8)
     if Q is None:
-        Q = X.new_empty((M, up16), dtype=_f8())
+        Q = _new(X, (M, up16), _f8(), stream)
         if up16 != K:
             Q = Q[:, :K]
         ldq = up16
@@ -388,7 +401,7 @@ def quantize_f8(X, *, block_rows: int = 1, Q=None, scales=None, stream=None):
     else:
         ldq = _pitch(Q, up16)
     if scales is None:
-        scales = X.new_empty(shape, dtype=torch.float32)
+        scales = _new(X, shape, torch.float32, stream)
         lds = shape[1]
     elif scales.dtype != torch.float32:
         raise TypeError("scales must be float32")
@@ -417,7 +430,7 @@ def gemm_f8(A, scale_a, B, scale_b, C=None, *, stream=None):
         raise ValueError("shape mismatch")
     up8, up16 = (N + 7) // 8 * 8, (K + 15) // 16 * 16
     if C is None:
-        C = A.new_empty((M, up8), dtype=torch.bfloat16)
+        C = _new(A, (M, up8), torch.bfloat16, stream)
         if up8 != N:
             C = C[:, :N]
         ldc = up8
@@ -471,7 +484,7 @@ def _kv_append(name, Q, K, V, cos, sin, cu_tokens, context_lens, block_table, K_
         H = Q.shape[1]
         ldq = _rows(Q, H, D)
         if Q_out is None:
-            Q_out = Q.new_empty((T, H, D))
+            Q_out = _new(Q, (T, H, D), bf16, stream)
             ldqo = H * D
         elif Q_out.dtype != bf16 or Q_out.shape != Q.shape:
             raise ValueError("Q_out must be bfloat16 of Q's shape")
@@ -541,11 +554,11 @@ def paged_attn_decode_f8(Q, K_cache, V_cache, k_scale, v_scale, block_table, seq
     if V_cache.shape != K_cache.shape or K_cache.shape[3] != D or seq_lens.shape[0] != S or block_table.dim() != 2 or block_table.shape[0] != S:
         raise ValueError("shape mismatch")
     if O is None:
-        O = torch.empty_like(Q)
+        O = _new(Q, Q.shape, torch.bfloat16, stream)
     elif O.dtype != torch.bfloat16 or O.shape != Q.shape or not O.is_contiguous():
         raise ValueError("O must be contiguous bfloat16 of Q's shape")
     if LSE is None and return_lse:
-        LSE = Q.new_empty((S, H), dtype=torch.float32)
+        LSE = _new(Q, (S, H), torch.float32, stream)
     elif LSE is not None and (LSE.dtype != torch.float32 or tuple(LSE.shape) != (S, H) or not LSE.is_contiguous()):
         raise ValueError("LSE must be contiguous float32 [S, H]")
     held = [Q, K_cache, V_cache, k_scale, v_scale, block_table, seq_lens, O]

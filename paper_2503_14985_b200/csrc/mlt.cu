@@ -1168,9 +1168,9 @@ int mlt_paged_attn_decode_f8(const void* Q, const void* K_cache, const void* V_c
     const int64_t rows = static_cast<int64_t>(num_seqs) * H_kv;
     if (workspace && num_seqs <= kPagedBalanceMaxSeqs) {
         const int64_t slots = static_cast<int64_t>(workspace_bytes / paged_f8_slot_bytes(G, D));
-        const int64_t chunks = rows * ((static_cast<int64_t>(max_blocks_per_seq) * block_size + kPagedChunkTokens - 1) / kPagedChunkTokens);
-        const int64_t ctas = std::min<int64_t>({static_cast<int64_t>(kPagedF8CtasPerSm) * dev.sm_count, kPagedF8MaxCtas, chunks, slots - rows});
-        if (ctas > 1) {
+        const int64_t chunks = num_seqs * ((static_cast<int64_t>(max_blocks_per_seq) * block_size + kPagedChunkTokens - 1) / kPagedChunkTokens);
+        const int64_t ctas = std::min<int64_t>({static_cast<int64_t>(kPagedF8CtasPerSm) * dev.sm_count, kPagedF8MaxCtas, chunks * H_kv, slots - rows});
+        if (ctas > 1 && chunks <= INT32_MAX) {  // (the kernels count a head's chunks in 32 bits)
             p.ctas = static_cast<int>(ctas);
             p.part_o = static_cast<float*>(workspace);
             p.part_ml = reinterpret_cast<float2*>(p.part_o + static_cast<size_t>(rows + ctas) * G * D);

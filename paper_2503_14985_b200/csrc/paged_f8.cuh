@@ -79,7 +79,8 @@ __device__ __forceinline__ int paged_f8_len(const PagedF8Params& p, int s, int b
     return static_cast<int>(max(0ll, min(static_cast<long long>(p.seq_lens[s]), static_cast<long long>(p.max_blocks) * bs)));
 }
 __device__ __forceinline__ int paged_f8_chunks(const PagedF8Params& p, int s, int bs) {
-    return (paged_f8_len(p, s, bs) + kPagedChunkTokens - 1) / kPagedChunkTokens;
+    const int len = paged_f8_len(p, s, bs);
+    return len / kPagedChunkTokens + (len % kPagedChunkTokens != 0);
 }
 // chunks per CTA
 __device__ __forceinline__ long long paged_f8_quota(long long n, int ctas) { return max(1ll, (n + ctas - 1) / ctas); }
@@ -183,7 +184,7 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
         const int ch0 = static_cast<int>(r % n_s);
         const int ch1 = static_cast<int>(min(static_cast<long long>(n_s), ch0 + (bal_hi - bal_i)));
         seg_tok_begin = ch0 * kPagedChunkTokens;
-        seg_tok_end = min(paged_f8_len(p, seg_s, BS), ch1 * kPagedChunkTokens);
+        seg_tok_end = ch1 == n_s ? paged_f8_len(p, seg_s, BS) : ch1 * kPagedChunkTokens;
         seg_whole = ch0 == 0 && ch1 == n_s;
         bal_i += ch1 - ch0;
         return true;
@@ -222,7 +223,7 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
     // read by one lane each and handed out by shuffles.
     constexpr int kStep = kPagedWarps * U;
     const int first = tok_begin + warp * U;
-    const int n_units = first < tok_end ? (tok_end - first + kStep - 1) / kStep : 0;
+    const int n_units = first < tok_end ? (tok_end - first - 1) / kStep + 1 : 0;
     int tab[NB];
     float tks[NB], tvs[NB];
     int tab_base = -64;

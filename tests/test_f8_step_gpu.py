@@ -147,3 +147,36 @@ def test_dependent_calls_back_to_back_and_one_by_one_give_the_same_bits():
         for a, b in zip(chain(lambda: None), one_by_one):
             assert torch.equal(a, b)
     assert_device_healthy()
+
+
+@pytest.mark.parametrize("address", [False, True])
+@pytest.mark.parametrize("op", ["quantize", "product", "append", "attend"])
+def test_new_outputs_on_a_given_stream_are_not_memory_that_another_stream_still_writes(op, address):
+    # blocks of the outputs' sizes go back to the allocator while the current stream is still going to write them: outputs of a
+    # call on another stream must not lie there
+    b = Block()
+    g = torch.Generator().manual_seed(5)
+    x = torch.randn(64, WIDTH, generator=g).to(torch.bfloat16).cuda()
+    x8, sx = mlt.quantize_f8(x)
+    cu = torch.tensor([0, 40, 57, 58], dtype=torch.int32, device="cuda")
+    ctx = torch.zeros(S, dtype=torch.int32, device="cuda")
+    lens = torch.tensor([40, 17, 1], dtype=torch.int32, device="cuda")
+    q, k, v = (torch.randn(58, h, D, generator=g).to(torch.bfloat16).cuda() for h in (H, HKV, HKV))
+    caches = b.kc, b.vc, b.ks, b.vs
+    mlt.kv_append_f8(q, k, v, b.cos, b.sin, cu, ctx, b.table, *caches)
+    run = {"quantize": lambda **kw: mlt.quantize_f8(x, **kw),
+           "product": lambda **kw: (mlt.gemm_f8(x8, sx, *b.w[0], **kw),),
+           "append": lambda **kw: (mlt.kv_append_f8(q, k, v, b.cos, b.sin, cu, ctx, b.table, *caches, **kw),),
+           "attend": lambda **kw: mlt.paged_attn_decode_f8(q[:S].contiguous(), *caches, b.table, lens, scale=0.125, workspace=b.ws, **kw)}[op]
+    want = [t.view(torch.uint8).clone() for t in run()]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    junk = [torch.empty_like(t) for t in want]
+    torch.cuda._sleep(20_000_000)
+    for t in junk:
+        t.fill_(1)
+    del junk, t
+    got = run(stream=side.cuda_stream if address else side)
+    torch.cuda.synchronize()
+    assert [torch.equal(a.view(torch.uint8), w) for a, w in zip(got, want)] == [True] * len(want)
+    assert_device_healthy()
