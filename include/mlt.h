@@ -270,7 +270,7 @@ int mlt_kv_append_f8(const void* Q, const void* K, const void* V, const float* c
  *   K_cache, V_cache  device, E4M3, [num_blocks, H_kv, block_size, D];  k_scale, v_scale  device, FP32, [num_blocks, H_kv]
  *   workspace    device scratch, 16-byte aligned; mlt_paged_attn_f8_workspace_bytes is always enough.  With less the
  *                work is cut into fewer shares, with NULL (or less than num_seqs * H_kv + 2 partials of
- *                (H / H_kv) * (4 D + 8) bytes) one CTA works on each (sequence, KV head).  Calls that overlap on the
+ *                (H / H_kv) * (4 D + 8) + 8 bytes) one CTA works on each (sequence, KV head).  Calls that overlap on the
  *                GPU must not share it.
  * num_blocks * H_kv must be below 2^31.  The tokens of a bad block-table entry are left out and reported.  The maximum, the
  * sum and the output accumulate in FP32; the probabilities are rounded to FP16 for the second product.

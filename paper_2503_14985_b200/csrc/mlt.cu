@@ -1115,7 +1115,7 @@ int mlt_kv_append_f8(const void* Q, const void* K, const void* V, const float* c
 
 size_t mlt_paged_attn_f8_workspace_bytes(int num_seqs, int H, int H_kv, int D) {
     if (num_seqs <= 0 || H <= 0 || H_kv <= 0 || D <= 0 || H % H_kv != 0) return 0;
-    return (static_cast<size_t>(num_seqs) * H_kv + kPagedF8MaxCtas) * paged_f8_slot_bytes(H / H_kv, D);
+    return (static_cast<size_t>(num_seqs) * H_kv + kPagedF8MaxShares) * paged_f8_slot_bytes(H / H_kv, D);
 }
 
 int mlt_paged_attn_decode_f8(const void* Q, const void* K_cache, const void* V_cache, const float* k_scale, const float* v_scale,
@@ -1164,16 +1164,21 @@ int mlt_paged_attn_decode_f8(const void* Q, const void* K_cache, const void* V_c
     p.scale_log2e = scale * 1.4426950408889634f;
     p.part_o = nullptr;
     p.part_ml = nullptr;
-    p.ctas = 0;
+    p.splits = nullptr;
+    p.by_row = false;
+    p.shares = 0;
     const int64_t rows = static_cast<int64_t>(num_seqs) * H_kv;
     if (workspace && num_seqs <= kPagedBalanceMaxSeqs) {
         const int64_t slots = static_cast<int64_t>(workspace_bytes / paged_f8_slot_bytes(G, D));
-        const int64_t chunks = num_seqs * ((static_cast<int64_t>(max_blocks_per_seq) * block_size + kPagedChunkTokens - 1) / kPagedChunkTokens);
-        const int64_t ctas = std::min<int64_t>({static_cast<int64_t>(kPagedF8CtasPerSm) * dev.sm_count, kPagedF8MaxCtas, chunks * H_kv, slots - rows});
-        if (ctas > 1 && chunks <= INT32_MAX) {  // (the kernels count a head's chunks in 32 bits)
-            p.ctas = static_cast<int>(ctas);
+        const int64_t units = num_seqs * ((static_cast<int64_t>(max_blocks_per_seq) * block_size + kPagedF8Unit - 1) / kPagedF8Unit);
+        const int64_t shares = std::min<int64_t>({static_cast<int64_t>(kPagedF8CtasPerSm) * dev.sm_count * kPagedWarps, kPagedF8MaxShares,
+                                                  units * H_kv / kPagedF8MinShare, slots - rows});
+        if (shares > 1 && units <= INT32_MAX) {  // (the kernels count a head's units in 32 bits)
+            p.shares = static_cast<int>(shares);
             p.part_o = static_cast<float*>(workspace);
-            p.part_ml = reinterpret_cast<float2*>(p.part_o + static_cast<size_t>(rows + ctas) * G * D);
+            p.part_ml = reinterpret_cast<float2*>(p.part_o + static_cast<size_t>(rows + shares) * G * D);
+            p.splits = reinterpret_cast<int2*>(p.part_ml + static_cast<size_t>(rows + shares) * G);
+            p.by_row = rows <= shares;
         }
     }
     return D == 64 ? paged_f8_launch<64>(tk, tv, p, block_size, static_cast<cudaStream_t>(stream))

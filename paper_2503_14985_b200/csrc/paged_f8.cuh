@@ -42,17 +42,20 @@ struct PagedF8Params {
     const int *block_table, *seq_lens;
     __nv_bfloat16* O;        // [num_seqs, H, D]
     float* LSE;              // [num_seqs, H] or null
-    float* part_o;           // [num_seqs * H_kv + ctas][G][D]
-    float2* part_ml;         // [num_seqs * H_kv + ctas][G] {m in log2 units, l}
+    float* part_o;           // [num_seqs * H_kv + shares][G][D]
+    float2* part_ml;         // [num_seqs * H_kv + shares][G] {m in log2 units, l}
+    int2* splits;            // what to combine: [row] {first share, shares it lies in}, or [share] {row that begins in it and goes on, ...}
+    bool by_row;             // which of the two (the shorter)
     int num_seqs, H, H_kv, max_blocks, num_blocks;
-    int ctas;                // CTAs of the balanced split; 0: one CTA per row
+    int shares;              // warps that the live units are dealt to; 0: one CTA per row
     float scale_log2e;
 };
 
 constexpr int kPagedF8Unit = 32;   // tokens per warp and ring stage
 constexpr int kPagedF8Ring = 3;    // stages: one in use, the others on their way
 constexpr int kPagedF8CtasPerSm = 2;
-constexpr int kPagedF8MaxCtas = 1024;  // bound on the balanced split's CTAs that the workspace formula uses
+constexpr int kPagedF8MaxShares = 2048;  // bound on the shares that the workspace formula uses
+constexpr int kPagedF8MinShare = 2;    // units: a shorter share is not worth its partial
 
 template <int D>
 constexpr int paged_f8_smem_bytes() {
@@ -78,12 +81,15 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
 __device__ __forceinline__ int paged_f8_len(const PagedF8Params& p, int s, int bs) {  // cut at the table's end
     return static_cast<int>(max(0ll, min(static_cast<long long>(p.seq_lens[s]), static_cast<long long>(p.max_blocks) * bs)));
 }
-__device__ __forceinline__ int paged_f8_chunks(const PagedF8Params& p, int s, int bs) {
+__device__ __forceinline__ int paged_f8_units(const PagedF8Params& p, int s, int bs) {
     const int len = paged_f8_len(p, s, bs);
-    return len / kPagedChunkTokens + (len % kPagedChunkTokens != 0);
+    return len / kPagedF8Unit + (len % kPagedF8Unit != 0);
 }
-// chunks per CTA
-__device__ __forceinline__ long long paged_f8_quota(long long n, int ctas) { return max(1ll, (n + ctas - 1) / ctas); }
+// n units are dealt to min(shares, n / kPagedF8MinShare) shares: share c has the units c n / shares .. (c + 1) n / shares - 1,
+// and unit x lies in share ((x + 1) shares - 1) / n.
+__device__ __forceinline__ long long paged_f8_shares(long long n, int shares) {
+    return max(1ll, min(static_cast<long long>(shares), n / kPagedF8MinShare));
+}
 
 // Every thread of the grid asks for its share of the lines of [base, base + bytes).
 __device__ __forceinline__ void l2_prefetch(const void* base, int64_t bytes) {
@@ -122,16 +128,14 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
     }
 
     pdl_begin();
-    // The lengths, the table entries they lead to and the cache those point at are three memory latencies in a row: while the
-    // first is under way, the CTAs together bring the table and the queries into L2.
-    l2_prefetch(p.block_table, static_cast<int64_t>(p.num_seqs) * p.max_blocks * 4);
-    l2_prefetch(p.Q, static_cast<int64_t>(p.num_seqs) * p.H * D * 2);
+    l2_prefetch(p.Q, static_cast<int64_t>(p.num_seqs) * p.H * D * 2);  // (while the lengths are on their way)
 
-    // ---- which segments (row, token range) this CTA works on ----
+    // ---- which segments (row, token range) this warp works on (with its CTA's others, where there is no scratch) ----
     int seg_s, seg_kvh = 0, seg_tok_begin = 0, seg_tok_end = 0;
-    bool seg_whole = true;  // the row lies inside this CTA's share
-    long long bal_i = 0, bal_hi = 0, bal_q = 1;
-    if (p.ctas == 0) {
+    bool seg_whole = true;  // the row lies inside this warp's share
+    long long bal_i = 0, bal_hi = 0, bal_n = 0, bal_shares = 0;
+    const int share = warp * gridDim.x + blockIdx.x;  // (neighbouring shares on different SMs: few shares spread over all)
+    if (p.shares == 0) {
         seg_s = blockIdx.x / p.H_kv;
         seg_kvh = blockIdx.x % p.H_kv;
         seg_tok_end = paged_f8_len(p, seg_s, BS);
@@ -142,7 +146,7 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
         const int s_lo = min(S, static_cast<int>(threadIdx.x) * per), s_hi = min(S, s_lo + per);
         int sum = 0;
         for (int s2 = s_lo; s2 < s_hi; ++s2) {
-            const int c = paged_f8_chunks(p, s2, BS);
+            const int c = paged_f8_units(p, s2, BS);
             sm_pre[s2 + 1] = c;
             sum += c;
         }
@@ -164,10 +168,23 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
         for (int s2 = s_lo; s2 < s_hi; ++s2) sm_pre[s2 + 1] = before += sm_pre[s2 + 1];
         __syncthreads();
         const long long n = static_cast<long long>(total) * p.H_kv;
-        bal_q = paged_f8_quota(n, p.ctas);
-        bal_i = blockIdx.x * bal_q;
-        bal_hi = min(n, bal_i + bal_q);
-        if (bal_i >= n) return;
+        const long long shares = paged_f8_shares(n, p.shares);
+        for (int s2 = blockIdx.x; s2 < S; s2 += gridDim.x) {
+            if (sm_pre[s2] != sm_pre[s2 + 1]) continue;
+            for (int i = threadIdx.x; i < p.H * D / 8; i += kPagedThreads) reinterpret_cast<uint4*>(p.O + static_cast<int64_t>(s2) * p.H * D)[i] = make_uint4(0u, 0u, 0u, 0u);
+            for (int i = threadIdx.x; i < p.H; i += kPagedThreads) {
+                if (p.LSE) p.LSE[static_cast<int64_t>(s2) * p.H + i] = -INFINITY;
+                if (p.by_row && i < p.H_kv) p.splits[static_cast<int64_t>(s2) * p.H_kv + i] = make_int2(0, 0);
+            }
+        }
+        if (share >= shares || n == 0) {  // (from here on no warp waits for another)
+            if (!p.by_row && share < p.shares && lane == 0) p.splits[share] = make_int2(0, 0);
+            return;
+        }
+        bal_n = n;
+        bal_shares = shares;
+        bal_i = share * n / shares;
+        bal_hi = (share + 1) * n / shares;
         int lo = 0, hi = S;  // H_kv * pre[lo] <= bal_i < H_kv * pre[hi]
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
@@ -183,13 +200,22 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
         seg_kvh = static_cast<int>(r / n_s);
         const int ch0 = static_cast<int>(r % n_s);
         const int ch1 = static_cast<int>(min(static_cast<long long>(n_s), ch0 + (bal_hi - bal_i)));
-        seg_tok_begin = ch0 * kPagedChunkTokens;
-        seg_tok_end = ch1 == n_s ? paged_f8_len(p, seg_s, BS) : ch1 * kPagedChunkTokens;
+        seg_tok_begin = ch0 * U;
+        seg_tok_end = ch1 == n_s ? paged_f8_len(p, seg_s, BS) : ch1 * U;
         seg_whole = ch0 == 0 && ch1 == n_s;
+        if (lane == 0) {  // the combine kernel's list
+            const int used = ch0 != 0 ? 0 : ch1 == n_s ? 1 : static_cast<int>(((bal_i + n_s) * bal_shares - 1) / bal_n) - share + 1;
+            const int row = seg_s * p.H_kv + seg_kvh;
+            if (p.by_row) {
+                if (ch0 == 0) p.splits[row] = make_int2(share, used);
+            } else if (bal_i + (ch1 - ch0) == bal_hi) {
+                p.splits[share] = make_int2(row, used);
+            }
+        }
         bal_i += ch1 - ch0;
         return true;
     };
-    if (p.ctas != 0 && !next_segment()) return;
+    if (p.shares != 0 && !next_segment()) return;
 
     uint32_t kbase = 0;        // units this warp has been through (the ring stage follows it)
     uint32_t ring_parity = 0;  // bit st: parity of the next completion of stage st's barrier
@@ -221,8 +247,8 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
     };
     // Unit k of this warp starts at token first + k * kStep.  The table entries and scales of 32 units at a time are
     // read by one lane each and handed out by shuffles.
-    constexpr int kStep = kPagedWarps * U;
-    const int first = tok_begin + warp * U;
+    const int kStep = p.shares ? U : kPagedWarps * U;
+    const int first = p.shares ? tok_begin : tok_begin + warp * U;
     const int n_units = first < tok_end ? (tok_end - first - 1) / kStep + 1 : 0;
     int tab[NB];
     float tks[NB], tvs[NB];
@@ -461,15 +487,48 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
     }
     kbase += n_units;
 
-    // ---- the warps' results meet in shared memory, where the ring was (all copies have landed and been read) ----
-    __syncthreads();
-    constexpr int kRow = D + 2;  // (the lanes' pairs meet two-way bank conflicts, with D they would meet eight-way ones)
-    float (*sm_o)[8][kRow] = reinterpret_cast<float (*)[8][kRow]>(ring_base);
-    static_assert(sizeof(float) * kPagedWarps * 8 * kRow <= kPagedWarps * kPagedF8Ring * kUnitBytes, "partials fit the ring");
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int w = 4; w < 32; w <<= 1) l_part[i] += __shfl_xor_sync(0xffffffffu, l_part[i], w);
+    if (p.shares) {  // lane (g, tg) has 2 MT neighbouring elements of heads 2 tg, 2 tg + 1
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int gg = 2 * tg + i;
+            if (gg < G) {
+                const float l = l_part[i] * (1.0f / 16384.0f);
+                if (seg_whole) {
+                    const float f = l == 0.0f ? 0.0f : v_ref * (1.0f / 16384.0f) / l;
+                    const int64_t row = static_cast<int64_t>(s) * p.H + head0 + gg;
+                    uint4* dst = reinterpret_cast<uint4*>(p.O + row * D + g * 2 * MT);
+#pragma unroll
+                    for (int q = 0; q < MT / 4; ++q) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) w[j] = pack_bf16x2(oacc[4 * q + j][i] * f, oacc[4 * q + j][2 + i] * f);
+                        dst[q] = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                    if (g == 0 && p.LSE) p.LSE[row] = l == 0.0f ? -INFINITY : (m_run[i] + log2f(l)) * 0.6931471805599453f;
+                } else {
+                    const float f = v_ref * (1.0f / 16384.0f);
+                    const int64_t slot = (static_cast<int64_t>(s) * p.H_kv + kvh + share) * G + gg;
+                    float4* dst = reinterpret_cast<float4*>(p.part_o + slot * D + g * 2 * MT);
+#pragma unroll
+                    for (int q = 0; q < MT / 2; ++q)
+                        dst[q] = make_float4(oacc[2 * q][i] * f, oacc[2 * q][2 + i] * f, oacc[2 * q + 1][i] * f, oacc[2 * q + 1][2 + i] * f);
+                    if (g == 0) p.part_ml[slot] = make_float2(m_run[i], l);
+                }
+            }
+        }
+        if (!ok || !next_segment()) return;
+        continue;
+    }
+
+    // ---- without shares: the warps' results meet in shared memory, where the ring was (all copies have landed and been read) ----
+    __syncthreads();
+    constexpr int kRow = D + 2;  // (the lanes' pairs meet two-way bank conflicts, with D they would meet eight-way ones)
+    float (*sm_o)[8][kRow] = reinterpret_cast<float (*)[8][kRow]>(ring_base);
+    static_assert(sizeof(float) * kPagedWarps * 8 * kRow <= kPagedWarps * kPagedF8Ring * kUnitBytes, "partials fit the ring");
     {
         const float unit = v_ref * (1.0f / 16384.0f);
 #pragma unroll
@@ -511,78 +570,47 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
         const int idx = threadIdx.x + it * kPagedThreads;
         const int gg = idx / D, at = idx % D;
         if (gg < G) {
-            if (seg_whole) {
-                const int64_t row = static_cast<int64_t>(s) * p.H + head0 + gg;
-                p.O[row * D + at] = __float2bfloat16(lt[it] == 0.0f ? 0.0f : ot[it] / lt[it]);
-                if (at == 0 && p.LSE) p.LSE[row] = lt[it] == 0.0f ? -INFINITY : (mt[it] + log2f(lt[it])) * 0.6931471805599453f;
-            } else {
-                const int64_t slot = (static_cast<int64_t>(s) * p.H_kv + kvh + blockIdx.x) * G + gg;
-                p.part_o[slot * D + at] = ot[it];
-                if (at == 0) p.part_ml[slot] = make_float2(mt[it], lt[it]);
-            }
+            const int64_t row = static_cast<int64_t>(s) * p.H + head0 + gg;
+            p.O[row * D + at] = __float2bfloat16(lt[it] == 0.0f ? 0.0f : ot[it] / lt[it]);
+            if (at == 0 && p.LSE) p.LSE[row] = lt[it] == 0.0f ? -INFINITY : (mt[it] + log2f(lt[it])) * 0.6931471805599453f;
         }
     }
     static_assert(kPagedWarps == 4, "the maximum above is over four warps");
-    if (p.ctas == 0 || !ok) break;
-    fence_proxy_async_smem();
-    __syncthreads();  // the results have left shared memory: copies may fill the ring again
-    if (!next_segment()) break;
+    break;
     }  // segments
 }
 
 // Rows that several CTAs worked on: sum of their partials, rescaled to the common maximum.  One CTA per (sequence, KV head):
 // a thread owns four neighbouring outputs of one head and every `splits`-th partial, so that a row with many partials
-// uses all threads too.  Also writes the rows of empty sequences.  2.4 us at 128 and 16 KV rows (5.7 with a CTA per query head).
+// uses all threads too.  2.4 us at 128 and 16 KV rows (5.7 with a CTA per query head).
 constexpr int kPagedF8CombineThreads = 256;
-template <int D, int G, int BS>
+template <int D, int G, int kVec>
 __global__ void __launch_bounds__(kPagedF8CombineThreads) paged_f8_combine_kernel(const PagedF8Params p) {
     constexpr int kWarps = kPagedF8CombineThreads / 32;
-    constexpr int kVec = G * D / 4, kSplits = kPagedF8CombineThreads / kVec;
+    constexpr int kSlices = G * D / 4 / kVec, kSplits = kPagedF8CombineThreads / kVec;
     static_assert(kSplits >= 1 && kSplits * kVec == kPagedF8CombineThreads, "whole splits");
-    __shared__ int sm_i[2][kWarps];
     __shared__ float sm_m[kWarps][G];
     __shared__ float4 sm_o[kPagedF8CombineThreads];
     __shared__ float sm_l[kPagedF8CombineThreads];
     pdl_launch_dependents();
-    const int s = blockIdx.x / p.H_kv, kvh = blockIdx.x % p.H_kv;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    int below = 0, total = 0;
-    for (int s2 = tid; s2 < p.num_seqs; s2 += kPagedF8CombineThreads) {
-        const int c = paged_f8_chunks(p, s2, BS);
-        total += c;
-        if (s2 < s) below += c;
-    }
-#pragma unroll
-    for (int w = 16; w > 0; w >>= 1) {
-        below += __shfl_xor_sync(0xffffffffu, below, w);
-        total += __shfl_xor_sync(0xffffffffu, total, w);
-    }
-    if (lane == 0) { sm_i[0][warp] = below; sm_i[1][warp] = total; }
-    __syncthreads();
-    below = total = 0;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) { below += sm_i[0][w]; total += sm_i[1][w]; }
-    const int n_s = paged_f8_chunks(p, s, BS);
-    const int64_t row0 = static_cast<int64_t>(s) * p.H + kvh * G;  // of the group's first head
-    cudaGridDependencySynchronize();  // (what was read so far are inputs)
-    const int v = tid % kVec, split = tid / kVec, gg = v * 4 / D;
-    if (n_s == 0) {  // nothing to see: O = 0, LSE = -inf
-        if (split == 0) *reinterpret_cast<uint2*>(p.O + row0 * D + v * 4) = make_uint2(0u, 0u);
-        if (tid < G && p.LSE) p.LSE[row0 + tid] = -INFINITY;
-        return;
-    }
-    const long long q = paged_f8_quota(static_cast<long long>(total) * p.H_kv, p.ctas);
-    const long long start = static_cast<long long>(below) * p.H_kv + static_cast<long long>(kvh) * n_s;
-    const int c0 = static_cast<int>(start / q), used = static_cast<int>((start + n_s - 1) / q) - c0 + 1;
-    if (used == 1) return;  // one CTA had the whole row and finished it
-    const int64_t slot0 = static_cast<int64_t>(s) * p.H_kv + kvh + c0;
+    const int v = blockIdx.x % kSlices * kVec + tid % kVec, split = tid / kVec, gg = v * 4 / D;  // column, of the group's outputs
+    const int item = blockIdx.x / kSlices;
+    cudaGridDependencySynchronize();
+    const int2 what = p.splits[item];
+    const int used = what.y;
+    if (used <= 1) return;  // one warp had the whole row and finished it, or there is none
+    const int row = p.by_row ? item : what.x, c0 = p.by_row ? what.x : item;
+    if (row < 0 || row >= p.num_seqs * p.H_kv || c0 < 0 || c0 >= p.shares || used > p.shares - c0) return;  // (after a wait that expired the list has gaps)
+    const int64_t row0 = static_cast<int64_t>(row) * G;  // of the group's first head
+    const int64_t slot0 = static_cast<int64_t>(row) + c0;
     const float2* ml = p.part_ml + slot0 * G;
     const float4* po = reinterpret_cast<const float4*>(p.part_o + slot0 * G * D) + v;
-    constexpr int kFirst = 4;  // requested before the maximum is known
+    constexpr int kFirst = 8;  // requested before the maximum is known
     float4 first[kFirst];
 #pragma unroll
     for (int i = 0; i < kFirst; ++i)
-        first[i] = split + i * kSplits < used ? po[static_cast<int64_t>(split + i * kSplits) * kVec] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        first[i] = split + i * kSplits < used ? po[static_cast<int64_t>(split + i * kSplits) * (G * D / 4)] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     float mt = -INFINITY;
     for (int i = tid; i < used * G; i += kPagedF8CombineThreads) mt = fmaxf(mt, ml[i].x);  // head tid % G (G divides the stride)
 #pragma unroll
@@ -607,7 +635,7 @@ __global__ void __launch_bounds__(kPagedF8CombineThreads) paged_f8_combine_kerne
     for (int i = 0; i < kFirst; ++i)
         if (split + i * kSplits < used) add(split + i * kSplits, first[i]);
 #pragma unroll 4
-    for (int i = split + kFirst * kSplits; i < used; i += kSplits) add(i, po[static_cast<int64_t>(i) * kVec]);
+    for (int i = split + kFirst * kSplits; i < used; i += kSplits) add(i, po[static_cast<int64_t>(i) * (G * D / 4)]);
     if constexpr (kSplits > 1) {
         sm_o[tid] = o;
         sm_l[tid] = lt;
@@ -615,9 +643,9 @@ __global__ void __launch_bounds__(kPagedF8CombineThreads) paged_f8_combine_kerne
         if (split != 0) return;
 #pragma unroll
         for (int k = 1; k < kSplits; ++k) {
-            const float4 x = sm_o[k * kVec + v];
+            const float4 x = sm_o[k * kVec + tid];
             o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
-            lt += sm_l[k * kVec + v];
+            lt += sm_l[k * kVec + tid];
         }
     }
     const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
@@ -625,16 +653,20 @@ __global__ void __launch_bounds__(kPagedF8CombineThreads) paged_f8_combine_kerne
     if (v * 4 % D == 0 && p.LSE) p.LSE[row0 + gg] = lt == 0.0f ? -INFINITY : (mt + log2f(lt)) * 0.6931471805599453f;
 }
 
-inline size_t paged_f8_slot_bytes(int G, int D) { return static_cast<size_t>(G) * (static_cast<size_t>(D) * 4 + 8); }
+inline size_t paged_f8_slot_bytes(int G, int D) { return static_cast<size_t>(G) * (static_cast<size_t>(D) * 4 + 8) + 8; }
 
 template <int D, int G, int BS>
 int paged_f8_launch_one(const CUtensorMap& tk, const CUtensorMap& tv, const PagedF8Params& p, cudaStream_t st) {
-    const int64_t grid = p.ctas ? p.ctas : static_cast<int64_t>(p.num_seqs) * p.H_kv;
+    const int64_t grid = p.shares ? (p.shares + kPagedWarps - 1) / kPagedWarps : static_cast<int64_t>(p.num_seqs) * p.H_kv;
     if (grid > INT32_MAX || static_cast<int64_t>(p.num_seqs) * p.H > INT32_MAX) return 2;
     if (pdl_launch(paged_f8_decode_kernel<D, G, BS>, dim3(static_cast<unsigned>(grid)), dim3(kPagedThreads), paged_f8_smem_bytes<D>(), st, 0, tk, tv, p) != cudaSuccess)
         return 4;
-    if (p.ctas == 0) return 0;
-    return pdl_launch(paged_f8_combine_kernel<D, G, BS>, dim3(static_cast<unsigned>(p.num_seqs * p.H_kv)), dim3(kPagedF8CombineThreads), 0, st, 0, p) == cudaSuccess ? 0 : 4;
+    if (p.shares == 0) return 0;
+    constexpr int kAll = G * D / 4, kFew = kAll < 32 ? kAll : 32;  // float4 columns per CTA
+    const int items = p.by_row ? p.num_seqs * p.H_kv : p.shares;
+    const bool few = items < 64;
+    return pdl_launch(few ? paged_f8_combine_kernel<D, G, kFew> : paged_f8_combine_kernel<D, G, kAll>,
+                      dim3(static_cast<unsigned>(items * (few ? kAll / kFew : 1))), dim3(kPagedF8CombineThreads), 0, st, 0, p) == cudaSuccess ? 0 : 4;
 }
 template <int D, int G>
 int paged_f8_launch_bs(const CUtensorMap& tk, const CUtensorMap& tv, const PagedF8Params& p, int block_size, cudaStream_t st) {

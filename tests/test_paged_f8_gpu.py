@@ -265,3 +265,18 @@ def test_cache_beyond_32_bit_byte_offsets():
     o, lse = mlt.paged_attn_decode_f8(args[0], kc.view(torch.float8_e4m3fn), vc.view(torch.float8_e4m3fn), ks, vs, table, args[6], scale=c.scale)
     c.check(to_f64(o), lse.cpu().numpy().astype(np.float64))
     assert_device_healthy()
+
+
+@pytest.mark.parametrize("H,Hkv,D,bs", [(4, 4, 64, 16), (32, 4, 128, 8), (8, 2, 64, 32)])
+def test_more_rows_than_shares(H, Hkv, D, bs):
+    # most rows lie inside one share, some cross a border, some are empty; a few long ones lie in many shares
+    rng = np.random.RandomState(H + D + bs)
+    lens = rng.randint(0, 90, 2600 // Hkv)
+    lens[rng.randint(0, len(lens), 40)] = 0
+    lens[-3:] = 0
+    lens[7] = 2500
+    assert len(lens) * Hkv > 2048
+    c = Case(lens, H, Hkv, D, bs, seed=9)
+    c.check(*c.run())
+    c.check(*c.run((len(lens) * Hkv + 9) * (H // Hkv * (4 * D + 8) + 8)))
+    assert_device_healthy()
