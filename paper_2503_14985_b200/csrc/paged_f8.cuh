@@ -19,16 +19,20 @@
 // that the fragment loads meet no bank conflict at D = 128 (a lane's 16 bytes of K cover 16 elements of one token: the
 // order of an MMA's summation index is free as long as both operands agree, as is the order of its output columns).
 //
-// Work split: the live chunks of 128 tokens of all (sequence, KV head) rows are numbered in row order and cut into equal
-// contiguous shares, one per CTA (the lengths are only known on the device: every CTA scans them).  A row inside one
-// share is finished by its CTA; otherwise each CTA that meets row r writes an unnormalised partial into slot
-// r + (its own index) -- strictly increasing along the line, so rows + CTAs slots are enough -- and a second kernel
-// combines them in ascending order.  Without scratch, or beyond 1024 sequences, one CTA works on each row.
+// Work split: the live units of 32 tokens of all (sequence, KV head) rows are numbered in row order and dealt in equal
+// contiguous shares, one per warp (the lengths are only known on the device: every CTA scans them).  From there on warps do not
+// wait for one another.  A row inside one share is finished by its warp; otherwise each warp that meets row r writes an
+// unnormalised partial into slot r + (its share) -- strictly increasing along the line, so rows + shares slots are enough -- and
+// a second kernel combines them in ascending order.  Which rows those are the first kernel writes down, so that the second need
+// not scan the lengths.  Without scratch, or beyond 1024 sequences, one CTA works on each row and its warps' results meet in
+// shared memory.
 //
 // Measured, both kernels: 32 sequences of 2k to 4k tokens, 32 heads over 4, 29 us (3.5 TB/s), 2 of 32k with 8 heads 30 us
-// (4.3 TB/s).  The streams run at the copy's rate; around them lie 6 us of dependent latencies (lengths, table, first data)
-// and 2.4 us of the combine kernel.  Alternatives: heads as rows 37 and 37, units of 16 tokens 31 to 33, two stages and three
-// CTAs per SM 30 and 32.5, copies issued ahead into the CTA's next row 30 and 32 (longer loop).
+// (4.3 TB/s); 256 of 500, 32 heads over 4, 35 us (3.7 TB/s), 1000 of 200 58 us (3.5 TB/s).  Around the streams lie 6 us of
+// dependent latencies (lengths, table, first data) and 2 to 3 us of the combine kernel.  Alternatives, in the same order: shares
+// of 128-token chunks per CTA with a merge in shared memory 28.5, 29.5, 44 and 107; the same with copies issued ahead into the
+// CTA's next row (longer loop) 30, 32, 47 and 116.  The first two cases at earlier stages: heads as rows 37 and 37 instead of 30
+// and 32, units of 16 tokens 31 to 33, two stages and three CTAs per SM 30 and 32.5 instead of 29 and 30.
 #pragma once
 
 #include "f8.cuh"
@@ -46,6 +50,7 @@ struct PagedF8Params {
     float2* part_ml;         // [num_seqs * H_kv + shares][G] {m in log2 units, l}
     int2* splits;            // what to combine: [row] {first share, shares it lies in}, or [share] {row that begins in it and goes on, ...}
     bool by_row;             // which of the two (the shorter)
+    int block_size;
     int num_seqs, H, H_kv, max_blocks, num_blocks;
     int shares;              // warps that the live units are dealt to; 0: one CTA per row
     float scale_log2e;
@@ -91,12 +96,6 @@ __device__ __forceinline__ long long paged_f8_shares(long long n, int shares) {
     return max(1ll, min(static_cast<long long>(shares), n / kPagedF8MinShare));
 }
 
-// Every thread of the grid asks for its share of the lines of [base, base + bytes).
-__device__ __forceinline__ void l2_prefetch(const void* base, int64_t bytes) {
-    for (int64_t at = (static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x) * 128; at < bytes; at += static_cast<int64_t>(gridDim.x) * blockDim.x * 128)
-        asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const char*>(base) + at));
-}
-
 template <int D, int G, int BS>
 __global__ void __launch_bounds__(kPagedThreads, kPagedF8CtasPerSm)
 paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const PagedF8Params p) {
@@ -128,7 +127,6 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
     }
 
     pdl_begin();
-    l2_prefetch(p.Q, static_cast<int64_t>(p.num_seqs) * p.H * D * 2);  // (while the lengths are on their way)
 
     // ---- which segments (row, token range) this warp works on (with its CTA's others, where there is no scratch) ----
     int seg_s, seg_kvh = 0, seg_tok_begin = 0, seg_tok_end = 0;
@@ -580,39 +578,59 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
     }  // segments
 }
 
-// Rows that several CTAs worked on: sum of their partials, rescaled to the common maximum.  One CTA per (sequence, KV head):
-// a thread owns four neighbouring outputs of one head and every `splits`-th partial, so that a row with many partials
-// uses all threads too.  2.4 us at 128 and 16 KV rows (5.7 with a CTA per query head).
-constexpr int kPagedF8CombineThreads = 256;
-template <int D, int G, int kVec>
-__global__ void __launch_bounds__(kPagedF8CombineThreads) paged_f8_combine_kernel(const PagedF8Params p) {
-    constexpr int kWarps = kPagedF8CombineThreads / 32;
-    constexpr int kSlices = G * D / 4 / kVec, kSplits = kPagedF8CombineThreads / kVec;
-    static_assert(kSplits >= 1 && kSplits * kVec == kPagedF8CombineThreads, "whole splits");
+// Rows that several warps worked on: sum of their partials, rescaled to the common maximum.  A CTA has kVec float4 columns of a
+// row's group of heads, a thread one of them and every kSplits-th partial.  Few rows have many partials each: below 64 rows
+// 512 threads with 32 columns (8 rows of 148 partials: 22 us in all, with all columns in a CTA of 256 threads 41), otherwise all
+// columns and 256 threads (1000 sequences of 200 tokens: 58 us in all, with 512 threads 63).
+template <int D, int G, int kVec, int kThreads>
+__global__ void __launch_bounds__(kThreads) paged_f8_combine_kernel(const PagedF8Params p) {
+    constexpr int kWarps = kThreads / 32;
+    constexpr int kSlices = G * D / 4 / kVec, kSplits = kThreads / kVec;
+    static_assert(kSplits >= 1 && kSplits * kVec == kThreads, "whole splits");
     __shared__ float sm_m[kWarps][G];
-    __shared__ float4 sm_o[kPagedF8CombineThreads];
-    __shared__ float sm_l[kPagedF8CombineThreads];
+    __shared__ float4 sm_o[kThreads];
+    __shared__ float sm_l[kThreads];
     pdl_launch_dependents();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int v = blockIdx.x % kSlices * kVec + tid % kVec, split = tid / kVec, gg = v * 4 / D;  // column, of the group's outputs
     const int item = blockIdx.x / kSlices;
-    cudaGridDependencySynchronize();
-    const int2 what = p.splits[item];
-    const int used = what.y;
+    int row = item, c0 = 0, used;
+    if (p.by_row && p.num_seqs <= 32) {  // few sequences: from their lengths, while the other kernel is still at work
+        const int units = lane < p.num_seqs ? paged_f8_units(p, lane, p.block_size) : 0, at = row / p.H_kv;
+        int total = units, below = lane < at ? units : 0;
+#pragma unroll
+        for (int w = 16; w > 0; w >>= 1) {
+            total += __shfl_xor_sync(0xffffffffu, total, w);
+            below += __shfl_xor_sync(0xffffffffu, below, w);
+        }
+        const long long n = static_cast<long long>(total) * p.H_kv, shares = paged_f8_shares(n, p.shares);
+        const long long n_s = __shfl_sync(0xffffffffu, units, at), start = static_cast<long long>(below) * p.H_kv + row % p.H_kv * n_s;
+        used = 0;
+        if (n_s > 0) {
+            c0 = static_cast<int>(((start + 1) * shares - 1) / n);
+            used = static_cast<int>(((start + n_s) * shares - 1) / n) - c0 + 1;
+        }
+        cudaGridDependencySynchronize();
+    } else {
+        cudaGridDependencySynchronize();
+        const int2 what = p.splits[item];
+        used = what.y;
+        if (p.by_row) c0 = what.x;
+        else row = what.x, c0 = item;
+    }
     if (used <= 1) return;  // one warp had the whole row and finished it, or there is none
-    const int row = p.by_row ? item : what.x, c0 = p.by_row ? what.x : item;
     if (row < 0 || row >= p.num_seqs * p.H_kv || c0 < 0 || c0 >= p.shares || used > p.shares - c0) return;  // (after a wait that expired the list has gaps)
     const int64_t row0 = static_cast<int64_t>(row) * G;  // of the group's first head
     const int64_t slot0 = static_cast<int64_t>(row) + c0;
     const float2* ml = p.part_ml + slot0 * G;
     const float4* po = reinterpret_cast<const float4*>(p.part_o + slot0 * G * D) + v;
-    constexpr int kFirst = 8;  // requested before the maximum is known
+    constexpr int kFirst = kThreads / 64;  // requested before the maximum is known
     float4 first[kFirst];
 #pragma unroll
     for (int i = 0; i < kFirst; ++i)
         first[i] = split + i * kSplits < used ? po[static_cast<int64_t>(split + i * kSplits) * (G * D / 4)] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     float mt = -INFINITY;
-    for (int i = tid; i < used * G; i += kPagedF8CombineThreads) mt = fmaxf(mt, ml[i].x);  // head tid % G (G divides the stride)
+    for (int i = tid; i < used * G; i += kThreads) mt = fmaxf(mt, ml[i].x);  // head tid % G (G divides the stride)
 #pragma unroll
     for (int w = 16; w >= G; w >>= 1) mt = fmaxf(mt, __shfl_xor_sync(0xffffffffu, mt, w));
     if (lane < G) sm_m[warp][lane] = mt;
@@ -665,8 +683,8 @@ int paged_f8_launch_one(const CUtensorMap& tk, const CUtensorMap& tv, const Page
     constexpr int kAll = G * D / 4, kFew = kAll < 32 ? kAll : 32;  // float4 columns per CTA
     const int items = p.by_row ? p.num_seqs * p.H_kv : p.shares;
     const bool few = items < 64;
-    return pdl_launch(few ? paged_f8_combine_kernel<D, G, kFew> : paged_f8_combine_kernel<D, G, kAll>,
-                      dim3(static_cast<unsigned>(items * (few ? kAll / kFew : 1))), dim3(kPagedF8CombineThreads), 0, st, 0, p) == cudaSuccess ? 0 : 4;
+    return pdl_launch(few ? paged_f8_combine_kernel<D, G, kFew, 512> : paged_f8_combine_kernel<D, G, kAll, 256>,
+                      dim3(static_cast<unsigned>(items * (few ? kAll / kFew : 1))), dim3(few ? 512 : 256), 0, st, 0, p) == cudaSuccess ? 0 : 4;
 }
 template <int D, int G>
 int paged_f8_launch_bs(const CUtensorMap& tk, const CUtensorMap& tv, const PagedF8Params& p, int block_size, cudaStream_t st) {
