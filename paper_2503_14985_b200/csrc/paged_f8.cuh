@@ -60,7 +60,7 @@ constexpr int kPagedF8Unit = 32;   // tokens per warp and ring stage
 constexpr int kPagedF8Ring = 3;    // stages: one in use, the others on their way
 constexpr int kPagedF8CtasPerSm = 2;
 constexpr int kPagedF8MaxShares = 2048;  // bound on the shares that the workspace formula uses
-constexpr int kPagedF8MinShare = 2;    // units: a shorter share is not worth its partial
+constexpr int kPagedF8MinShare = 2;  // units per share at least (128 sequences of 128 tokens, 4 KV heads: 11.7 us, with 1 14.2; 8 of 500: 10.4, 9.9, with 4 13.3)
 
 template <int D>
 constexpr int paged_f8_smem_bytes() {
