@@ -1166,7 +1166,6 @@ int mlt_paged_attn_decode_f8(const void* Q, const void* K_cache, const void* V_c
     p.part_ml = nullptr;
     p.splits = nullptr;
     p.by_row = false;
-    p.block_size = block_size;
     p.shares = 0;
     const int64_t rows = static_cast<int64_t>(num_seqs) * H_kv;
     if (workspace && num_seqs <= kPagedBalanceMaxSeqs) {

@@ -23,8 +23,8 @@
 // contiguous shares, one per warp (the lengths are only known on the device: every CTA scans them).  From there on warps do not
 // wait for one another.  A row inside one share is finished by its warp; otherwise each warp that meets row r writes an
 // unnormalised partial into slot r + (its share) -- strictly increasing along the line, so rows + shares slots are enough -- and
-// a second kernel combines them in ascending order.  Which rows those are the first kernel writes down, so that the second need
-// not scan the lengths.  Without scratch, or beyond 1024 sequences, one CTA works on each row and its warps' results meet in
+// a second kernel combines them in ascending order.  Which rows those are the first kernel writes down, so that the second does
+// not read the lengths at all.  Without scratch, or beyond 1024 sequences, one CTA works on each row and its warps' results meet in
 // shared memory.
 //
 // Measured, both kernels: 32 sequences of 2k to 4k tokens, 32 heads over 4, 29 us (3.5 TB/s), 2 of 32k with 8 heads 30 us
@@ -50,7 +50,6 @@ struct PagedF8Params {
     float2* part_ml;         // [num_seqs * H_kv + shares][G] {m in log2 units, l}
     int2* splits;            // what to combine: [row] {first share, shares it lies in}, or [share] {row that begins in it and goes on, ...}
     bool by_row;             // which of the two (the shorter)
-    int block_size;
     int num_seqs, H, H_kv, max_blocks, num_blocks;
     int shares;              // warps that the live units are dealt to; 0: one CTA per row
     float scale_log2e;
@@ -594,30 +593,11 @@ __global__ void __launch_bounds__(kThreads) paged_f8_combine_kernel(const PagedF
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int v = blockIdx.x % kSlices * kVec + tid % kVec, split = tid / kVec, gg = v * 4 / D;  // column, of the group's outputs
     const int item = blockIdx.x / kSlices;
-    int row = item, c0 = 0, used;
-    if (p.by_row && p.num_seqs <= 32) {  // few sequences: from their lengths, while the other kernel is still at work
-        const int units = lane < p.num_seqs ? paged_f8_units(p, lane, p.block_size) : 0, at = row / p.H_kv;
-        int total = units, below = lane < at ? units : 0;
-#pragma unroll
-        for (int w = 16; w > 0; w >>= 1) {
-            total += __shfl_xor_sync(0xffffffffu, total, w);
-            below += __shfl_xor_sync(0xffffffffu, below, w);
-        }
-        const long long n = static_cast<long long>(total) * p.H_kv, shares = paged_f8_shares(n, p.shares);
-        const long long n_s = __shfl_sync(0xffffffffu, units, at), start = static_cast<long long>(below) * p.H_kv + row % p.H_kv * n_s;
-        used = 0;
-        if (n_s > 0) {
-            c0 = static_cast<int>(((start + 1) * shares - 1) / n);
-            used = static_cast<int>(((start + n_s) * shares - 1) / n) - c0 + 1;
-        }
-        cudaGridDependencySynchronize();
-    } else {
-        cudaGridDependencySynchronize();
-        const int2 what = p.splits[item];
-        used = what.y;
-        if (p.by_row) c0 = what.x;
-        else row = what.x, c0 = item;
-    }
+    // Nothing before this wait: the decode kernel releases this launch before its own wait, so the kernel in front of it, which
+    // may be the one that writes the lengths, can still be at work here.
+    cudaGridDependencySynchronize();
+    const int2 what = p.splits[item];
+    const int row = p.by_row ? item : what.x, c0 = p.by_row ? what.x : item, used = what.y;
     if (used <= 1) return;  // one warp had the whole row and finished it, or there is none
     if (row < 0 || row >= p.num_seqs * p.H_kv || c0 < 0 || c0 >= p.shares || used > p.shares - c0) return;  // (after a wait that expired the list has gaps)
     const int64_t row0 = static_cast<int64_t>(row) * G;  // of the group's first head
