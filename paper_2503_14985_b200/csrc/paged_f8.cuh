@@ -10,10 +10,14 @@
 //   * Q is scaled by a power of two per row into FP16's range (its 8 significant bits fit), exact but for elements more
 //     than 2^28 below the row's largest.
 //   * K's scale multiplies the scores of its block's tokens.  A tile of 8 tokens lies in one block.
-//   * V's scale multiplies the probabilities before they become the FP16 operand, relative to the largest V scale the
-//     warp has met (v_ref, kept like a running maximum: the accumulators are rescaled when it grows).  Probabilities
-//     are held times 2^14, so that weights down to 2^-28 of the largest keep FP16's full precision.
-//   * Scores, maxima, sums and outputs are FP32; the sum takes the probabilities before their rounding to FP16.
+//   * The second product's FP16 operand is the weight w = p * vs.  The scales may be anything, so the most likely token need not
+//     have the largest weight: next to the running maximum m of the scores x (log2 units), which the sum l of the probabilities
+//     goes by, a head keeps d = max(x + e) - m with vs = (1 .. 2) * 2^e, and its weights and accumulators are held times 2^14
+//     relative to 2^(m + d).  The largest lies in 2^14 .. 2^15 whatever the scales are, and weights down to 2^-28 of it keep
+//     FP16's full precision.  Partial results are means (divided by l): a sum over many tokens may lie beyond FP32 where
+//     their mean does not.  That is a second exponential per score (16 MUFU cycles of the 350 that a unit's copies take) and
+//     no division.
+//   * Scores, maxima, sums and outputs are FP32; the sum takes the probabilities, which are not rounded to FP16.
 //
 // Data path: tensor copies (TMA) of whole (block, head) pieces into a three-deep ring of 32-token units per warp, swizzled so
 // that the fragment loads meet no bank conflict at D = 128 (a lane's 16 bytes of K cover 16 elements of one token: the
@@ -21,18 +25,21 @@
 //
 // Work split: the live units of 32 tokens of all (sequence, KV head) rows are numbered in row order and dealt in equal
 // contiguous shares, one per warp (the lengths are only known on the device: every CTA scans them).  From there on warps do not
-// wait for one another.  A row inside one share is finished by its warp; otherwise each warp that meets row r writes an
-// unnormalised partial into slot r + (its share) -- strictly increasing along the line, so rows + shares slots are enough -- and
+// wait for one another.  A row inside one share is finished by its warp; otherwise each warp that meets row r writes a
+// partial into slot r + (its share) -- strictly increasing along the line, so rows + shares slots are enough -- and
 // a second kernel combines them in ascending order.  Which rows those are the first kernel writes down, so that the second does
 // not read the lengths at all.  Without scratch, or beyond 1024 sequences, one CTA works on each row and its warps' results meet in
 // shared memory.
 //
-// Measured, both kernels: 32 sequences of 2k to 4k tokens, 32 heads over 4, 29 us (3.5 TB/s), 2 of 32k with 8 heads 30 us
-// (4.3 TB/s); 256 of 500, 32 heads over 4, 35 us (3.7 TB/s), 1000 of 200 58 us (3.5 TB/s).  Around the streams lie 6 us of
-// dependent latencies (lengths, table, first data) and 2 to 3 us of the combine kernel.  Alternatives, in the same order: shares
-// of 128-token chunks per CTA with a merge in shared memory 28.5, 29.5, 44 and 107; the same with copies issued ahead into the
-// CTA's next row (longer loop) 30, 32, 47 and 116.  The first two cases at earlier stages: heads as rows 37 and 37 instead of 30
-// and 32, units of 16 tokens 31 to 33, two stages and three CTAs per SM 30 and 32.5 instead of 29 and 30.
+// Measured, both kernels, device time in a captured graph: 32 sequences of 2k to 4k tokens, 32 heads over 4, 30 us (3.4 TB/s), 2
+// of 32k with 8 heads 32 us (4.1 TB/s); 256 of 500, 32 heads over 4, 37.5 us (3.6 TB/s), 1000 of 200 60 us (3.7 TB/s); 16 of 2k to 4k
+// with D = 64, 16 heads over 8, 22 us.  Around the streams lie 6 us of dependent latencies (lengths, table, first data) and 3 to 4 us of the
+// combine kernel.  Alternatives, in the order of the first four: weights relative to the largest V scale, which lost the output where that
+// scale's tokens were unlikely, 29, 30.5, 35.5 and 58 (D = 64: 23.5); on top of those, shares of 128-token chunks per CTA with a merge in
+// shared memory 28.5, 29.5, 44 and 107; the same with copies issued ahead into the CTA's next row (longer loop) 30, 32, 47 and 116.  The first
+// two cases at earlier stages: heads as rows 37 and 37 instead of 30 and 32, units of 16 tokens 31 to 33, two stages and three CTAs per SM 30
+// and 32.5 instead of 29 and 30.  For the maximum of x + e: next to that of x in one pass, with a branch for scores beyond 2^23, where x + e
+// loses e, 30, 32, 37.5 and 61.
 #pragma once
 
 #include "f8.cuh"
@@ -46,7 +53,7 @@ struct PagedF8Params {
     const int *block_table, *seq_lens;
     __nv_bfloat16* O;        // [num_seqs, H, D]
     float* LSE;              // [num_seqs, H] or null
-    float* part_o;           // [num_seqs * H_kv + shares][G][D]
+    float* part_o;           // [num_seqs * H_kv + shares][G][D], divided by l
     float2* part_ml;         // [num_seqs * H_kv + shares][G] {m in log2 units, l}
     int2* splits;            // what to combine: [row] {first share, shares it lies in}, or [share] {row that begins in it and goes on, ...}
     bool by_row;             // which of the two (the shorter)
@@ -81,6 +88,22 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
+
+// v = m * 2^e with 1 <= |m| < 2 (0: m = 0, e = -inf; infinities and NaN stay in m, with e = 0)
+__device__ __forceinline__ void split_scale(float v, float& m, float& e) {
+    const uint32_t b = __float_as_uint(v);
+    const int x = static_cast<int>(b >> 23 & 0xFFu);
+    m = __uint_as_float((b & 0x807FFFFFu) | 0x3F800000u);
+    e = static_cast<float>(x - 127);
+    if (x == 0 || x == 255) {
+        const uint32_t f = b & 0x7FFFFFu;
+        const int up = __clz(f) - 8;  // a subnormal is f * 2^-149
+        m = x == 255 ? v : f == 0u ? 0.0f : __uint_as_float((b & 0x80000000u) | 0x3F800000u | (f << up & 0x7FFFFFu));
+        e = x == 255 ? 0.0f : f == 0u ? -INFINITY : static_cast<float>(-126 - up);
+    }
+}
+
+__device__ __forceinline__ float finite_or_0(float x) { return x == -INFINITY ? 0.0f : x; }  // a reference where nothing was seen
 
 __device__ __forceinline__ int paged_f8_len(const PagedF8Params& p, int s, int bs) {  // cut at the table's end
     return static_cast<int>(max(0ll, min(static_cast<long long>(p.seq_lens[s]), static_cast<long long>(p.max_blocks) * bs)));
@@ -233,9 +256,9 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
         for (int i = 0; i < 4; ++i) oacc[mt][i] = 0.0f;
-    float m_run[2] = {-INFINITY, -INFINITY};  // of the two heads: running max (log2 units, the same in all lanes of a tg)
-    float l_part[2] = {0.0f, 0.0f};           // ... this lane's share of the sum (times 2^14)
-    float v_ref = 0.0f;                       // the accumulators hold sums of p * 2^14 * vs / v_ref * V
+    float m_run[2] = {-INFINITY, -INFINITY};  // of the two heads: running max of x (log2 units, the same in all lanes of a tg)
+    float d_run[2] = {-INFINITY, -INFINITY};  // ... running max of x + e, less m_run: the accumulators hold sums of 2^(x - m_run - d_run + 14) vs V
+    float l_part[2] = {0.0f, 0.0f};           // ... this lane's share of the sum
 
     const int* table = p.block_table + static_cast<int64_t>(s) * p.max_blocks;
     struct Meta {  // of a unit whose copies are under way: which of its tokens count, and its blocks' scales
@@ -379,9 +402,11 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
             for (int e = 0; e < U / 8; ++e)
                 if (!((meta.vis >> (8 * e + g)) & 1u)) x[e][0] = x[e][1] = -INFINITY;
         }
-        float ref[2], alpha[2];
+        float vm[NB], ve[NB];
+#pragma unroll
+        for (int i = 0; i < NB; ++i) split_scale(meta.vs[i], vm[i], ve[i]);
         bool moved = false;
-        float m_new[2];
+        float m_new[2], d_new[2], f_l[2], f_o[2], off[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             float mb = x[0][i];
@@ -390,42 +415,45 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
 #pragma unroll
             for (int w = 4; w < 32; w <<= 1) mb = fmaxf(mb, __shfl_xor_sync(0xffffffffu, mb, w));
             m_new[i] = fmaxf(m_run[i], mb);
-            moved |= m_new[i] != m_run[i];
-            ref[i] = m_new[i] == -INFINITY ? 0.0f : m_new[i];
-            alpha[i] = fast_exp2(m_run[i] - ref[i]);  // 0 while m_run = -inf
-        }
-        float vm = v_ref;
+            const float ref = finite_or_0(m_new[i]);
+            float db = -INFINITY;  // (of x - ref: e would be lost next to a large x)
 #pragma unroll
-        for (int i = 0; i < NB; ++i) vm = fmaxf(vm, fabsf(meta.vs[i]));
-        if (__any_sync(0xffffffffu, moved) || vm != v_ref) {
-            const float shrink = vm > v_ref ? v_ref / vm : 1.0f;
-            const float f0 = alpha[0] * shrink, f1 = alpha[1] * shrink;
+            for (int e = 0; e < U / 8; ++e) {
+                x[e][i] -= ref;
+                db = fmaxf(db, x[e][i] + ve[8 * e / kPiece]);
+            }
+#pragma unroll
+            for (int w = 4; w < 32; w <<= 1) db = fmaxf(db, __shfl_xor_sync(0xffffffffu, db, w));
+            const float fall = m_run[i] - ref;  // -inf the first time
+            d_new[i] = fmaxf(d_run[i] + fall, db);
+            const float d_ref = finite_or_0(d_new[i]);
+            moved |= m_new[i] != m_run[i] || d_new[i] != d_run[i];
+            f_l[i] = fast_exp2(fall);
+            f_o[i] = fast_exp2(fall + (d_run[i] - d_ref));
+            off[i] = 14.0f - d_ref;
+        }
+        if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
-                oacc[mt][0] *= f0;
-                oacc[mt][1] *= f1;
-                oacc[mt][2] *= f0;
-                oacc[mt][3] *= f1;
+                oacc[mt][0] *= f_o[0];
+                oacc[mt][1] *= f_o[1];
+                oacc[mt][2] *= f_o[0];
+                oacc[mt][3] *= f_o[1];
             }
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                l_part[i] *= alpha[i];
+                l_part[i] *= f_l[i];
                 m_run[i] = m_new[i];
+                d_run[i] = d_new[i];
             }
-            v_ref = vm;
         }
-        float vw[NB];
-#pragma unroll
-        for (int i = 0; i < NB; ++i) vw[i] = v_ref > 0.0f ? meta.vs[i] / v_ref : 0.0f;
-        const float low[2] = {ref[0] - 14.0f, ref[1] - 14.0f};
         uint32_t pb[U / 8];  // P^T as B fragments: lane (g, tg) holds tokens 8 e + 2 tg, + 1 of head g
 #pragma unroll
         for (int e = 0; e < U / 8; ++e) {
-            const float p0 = fast_exp2(x[e][0] - low[0]), p1 = fast_exp2(x[e][1] - low[1]);
-            l_part[0] += p0;
-            l_part[1] += p1;
-            const float w = vw[8 * e / kPiece];
-            pb[e] = transpose_8x8(pack_f16x2(p0 * w, p1 * w));
+            const int i = 8 * e / kPiece;
+            l_part[0] += fast_exp2(x[e][0]);
+            l_part[1] += fast_exp2(x[e][1]);
+            pb[e] = transpose_8x8(pack_f16x2(fast_exp2(x[e][0] + (ve[i] + off[0])) * vm[i], fast_exp2(x[e][1] + (ve[i] + off[1])) * vm[i]));
         }
         // ---- O^T += V^T P^T: row g of tile mt is element g * 2 MT + 2 mt, row g + 8 the one after it ----
 #pragma unroll
@@ -488,31 +516,36 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
     for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int w = 4; w < 32; w <<= 1) l_part[i] += __shfl_xor_sync(0xffffffffu, l_part[i], w);
+    // The accumulators become means by two factors (their product could lie outside FP32: d is -150 .. 128).
+    float mean1[2], mean2[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        mean1[i] = d_run[i] == -INFINITY ? 0.0f : fast_exp2(0.5f * d_run[i]);
+        mean2[i] = l_part[i] == 0.0f ? 0.0f : mean1[i] * (1.0f / 16384.0f) / l_part[i];
+    }
     if (p.shares) {  // lane (g, tg) has 2 MT neighbouring elements of heads 2 tg, 2 tg + 1
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int gg = 2 * tg + i;
             if (gg < G) {
-                const float l = l_part[i] * (1.0f / 16384.0f);
+                const float l = l_part[i], f1 = mean1[i], f2 = mean2[i];
                 if (seg_whole) {
-                    const float f = l == 0.0f ? 0.0f : v_ref * (1.0f / 16384.0f) / l;
                     const int64_t row = static_cast<int64_t>(s) * p.H + head0 + gg;
                     uint4* dst = reinterpret_cast<uint4*>(p.O + row * D + g * 2 * MT);
 #pragma unroll
                     for (int q = 0; q < MT / 4; ++q) {
                         uint32_t w[4];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) w[j] = pack_bf16x2(oacc[4 * q + j][i] * f, oacc[4 * q + j][2 + i] * f);
+                        for (int j = 0; j < 4; ++j) w[j] = pack_bf16x2(oacc[4 * q + j][i] * f2 * f1, oacc[4 * q + j][2 + i] * f2 * f1);
                         dst[q] = make_uint4(w[0], w[1], w[2], w[3]);
                     }
                     if (g == 0 && p.LSE) p.LSE[row] = l == 0.0f ? -INFINITY : (m_run[i] + log2f(l)) * 0.6931471805599453f;
                 } else {
-                    const float f = v_ref * (1.0f / 16384.0f);
                     const int64_t slot = (static_cast<int64_t>(s) * p.H_kv + kvh + share) * G + gg;
                     float4* dst = reinterpret_cast<float4*>(p.part_o + slot * D + g * 2 * MT);
 #pragma unroll
                     for (int q = 0; q < MT / 2; ++q)
-                        dst[q] = make_float4(oacc[2 * q][i] * f, oacc[2 * q][2 + i] * f, oacc[2 * q + 1][i] * f, oacc[2 * q + 1][2 + i] * f);
+                        dst[q] = make_float4(oacc[2 * q][i] * f2 * f1, oacc[2 * q][2 + i] * f2 * f1, oacc[2 * q + 1][i] * f2 * f1, oacc[2 * q + 1][2 + i] * f2 * f1);
                     if (g == 0) p.part_ml[slot] = make_float2(m_run[i], l);
                 }
             }
@@ -527,14 +560,13 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
     float (*sm_o)[8][kRow] = reinterpret_cast<float (*)[8][kRow]>(ring_base);
     static_assert(sizeof(float) * kPagedWarps * 8 * kRow <= kPagedWarps * kPagedF8Ring * kUnitBytes, "partials fit the ring");
     {
-        const float unit = v_ref * (1.0f / 16384.0f);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             if (2 * tg + i < G) {
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt)
-                    *reinterpret_cast<float2*>(&sm_o[warp][2 * tg + i][g * 2 * MT + 2 * mt]) = make_float2(oacc[mt][i] * unit, oacc[mt][2 + i] * unit);
-                if (g == 0) sm_ml[warp][2 * tg + i] = make_float2(m_run[i], l_part[i] * (1.0f / 16384.0f));
+                    *reinterpret_cast<float2*>(&sm_o[warp][2 * tg + i][g * 2 * MT + 2 * mt]) = make_float2(oacc[mt][i] * mean2[i] * mean1[i], oacc[mt][2 + i] * mean2[i] * mean1[i]);
+                if (g == 0) sm_ml[warp][2 * tg + i] = make_float2(m_run[i], l_part[i]);
             }
         }
     }
@@ -553,14 +585,17 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
             ml[w] = sm_ml[w][gg];
             o[w] = sm_o[w][gg][at];
         }
-        mt[it] = fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x));
+        mt[it] = finite_or_0(fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)));
         lt[it] = ot[it] = 0.0f;
+        float h[kPagedWarps];  // the weights' roots, as in the combine kernel
 #pragma unroll
         for (int w = 0; w < kPagedWarps; ++w) {
-            const float sw = (ml[w].x == -INFINITY) ? 0.0f : fast_exp2(ml[w].x - mt[it]);
-            lt[it] += ml[w].y * sw;
-            ot[it] += o[w] * sw;
+            h[w] = fast_exp2(0.5f * (ml[w].x - mt[it]));
+            lt[it] += ml[w].y * h[w] * h[w];
         }
+        const float inv = lt[it] == 0.0f ? 0.0f : 1.0f / lt[it];
+#pragma unroll
+        for (int w = 0; w < kPagedWarps; ++w) ot[it] += o[w] * h[w] * (ml[w].y * inv * h[w]);
     }
 #pragma unroll
     for (int it = 0; it < kPlaces; ++it) {
@@ -568,7 +603,7 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
         const int gg = idx / D, at = idx % D;
         if (gg < G) {
             const int64_t row = static_cast<int64_t>(s) * p.H + head0 + gg;
-            p.O[row * D + at] = __float2bfloat16(lt[it] == 0.0f ? 0.0f : ot[it] / lt[it]);
+            p.O[row * D + at] = __float2bfloat16(ot[it]);
             if (at == 0 && p.LSE) p.LSE[row] = lt[it] == 0.0f ? -INFINITY : (mt[it] + log2f(lt[it])) * 0.6931471805599453f;
         }
     }
@@ -580,13 +615,13 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
 // Rows that several warps worked on: sum of their partials, rescaled to the common maximum.  A CTA has kVec float4 columns of a
 // row's group of heads, a thread one of them and every kSplits-th partial.  Few rows have many partials each: below 64 rows
 // 512 threads with 32 columns (8 rows of 148 partials: 22 us in all, with all columns in a CTA of 256 threads 41), otherwise all
-// columns and 256 threads (1000 sequences of 200 tokens: 58 us in all, with 512 threads 63).
+// columns and 256 threads (1000 sequences of 200 tokens: 60 us in all, with 512 threads about 5 more).
 template <int D, int G, int kVec, int kThreads>
 __global__ void __launch_bounds__(kThreads) paged_f8_combine_kernel(const PagedF8Params p) {
     constexpr int kWarps = kThreads / 32;
     constexpr int kSlices = G * D / 4 / kVec, kSplits = kThreads / kVec;
     static_assert(kSplits >= 1 && kSplits * kVec == kThreads, "whole splits");
-    __shared__ float sm_m[kWarps][G];
+    __shared__ float2 sm_m[kWarps][G];
     __shared__ float4 sm_o[kThreads];
     __shared__ float sm_l[kThreads];
     pdl_launch_dependents();
@@ -609,25 +644,41 @@ __global__ void __launch_bounds__(kThreads) paged_f8_combine_kernel(const PagedF
 #pragma unroll
     for (int i = 0; i < kFirst; ++i)
         first[i] = split + i * kSplits < used ? po[static_cast<int64_t>(split + i * kSplits) * (G * D / 4)] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    float mt = -INFINITY;
-    for (int i = tid; i < used * G; i += kThreads) mt = fmaxf(mt, ml[i].x);  // head tid % G (G divides the stride)
+    float mt = -INFINITY, l_all = 0.0f;  // of all partials: the largest m, and the sum of l as if every m were that
+    for (int i = tid; i < used * G; i += kThreads) {  // head tid % G (G divides the stride)
+        const float2 a = ml[i];
+        mt = fmaxf(mt, a.x);
+        l_all += a.y;
+    }
 #pragma unroll
-    for (int w = 16; w >= G; w >>= 1) mt = fmaxf(mt, __shfl_xor_sync(0xffffffffu, mt, w));
-    if (lane < G) sm_m[warp][lane] = mt;
+    for (int w = 16; w >= G; w >>= 1) {
+        mt = fmaxf(mt, __shfl_xor_sync(0xffffffffu, mt, w));
+        l_all += __shfl_xor_sync(0xffffffffu, l_all, w);
+    }
+    if (lane < G) sm_m[warp][lane] = make_float2(mt, l_all);
     __syncthreads();
-    mt = sm_m[0][gg];
+    mt = -INFINITY;
+    l_all = 0.0f;
 #pragma unroll
-    for (int w = 1; w < kWarps; ++w) mt = fmaxf(mt, sm_m[w][gg]);
+    for (int w = 0; w < kWarps; ++w) {
+        const float2 a = sm_m[w][gg];
+        mt = fmaxf(mt, a.x);
+        l_all += a.y;
+    }
+    mt = finite_or_0(mt);
+    // The weights l 2^(m - mt) / l_all sum to 1 at most, so that no sum of means overflows.  They are applied by two factors of half the
+    // exponent: a weight of 2^-200 alone would vanish, but not its product with a mean of 2^100.
+    const float unit = l_all == 0.0f ? 0.0f : 1.0f / l_all;
     float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     float lt = 0.0f;
     auto add = [&](int i, const float4& x) {
         const float2 a = ml[static_cast<int64_t>(i) * G + gg];
-        const float w = a.x == -INFINITY ? 0.0f : fast_exp2(a.x - mt);
-        lt += a.y * w;
-        o.x = fmaf(x.x, w, o.x);
-        o.y = fmaf(x.y, w, o.y);
-        o.z = fmaf(x.z, w, o.z);
-        o.w = fmaf(x.w, w, o.w);
+        const float h = fast_exp2(0.5f * (a.x - mt)), w = a.y * unit * h;
+        lt = fmaf(w, h, lt);
+        o.x = fmaf(x.x * h, w, o.x);
+        o.y = fmaf(x.y * h, w, o.y);
+        o.z = fmaf(x.z * h, w, o.z);
+        o.w = fmaf(x.w * h, w, o.w);
     };
 #pragma unroll
     for (int i = 0; i < kFirst; ++i)
@@ -648,7 +699,7 @@ __global__ void __launch_bounds__(kThreads) paged_f8_combine_kernel(const PagedF
     }
     const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
     *reinterpret_cast<uint2*>(p.O + row0 * D + v * 4) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
-    if (v * 4 % D == 0 && p.LSE) p.LSE[row0 + gg] = lt == 0.0f ? -INFINITY : (mt + log2f(lt)) * 0.6931471805599453f;
+    if (v * 4 % D == 0 && p.LSE) p.LSE[row0 + gg] = lt == 0.0f ? -INFINITY : (mt + log2f(lt) + log2f(l_all)) * 0.6931471805599453f;
 }
 
 inline size_t paged_f8_slot_bytes(int G, int D) { return static_cast<size_t>(G) * (static_cast<size_t>(D) * 4 + 8) + 8; }
