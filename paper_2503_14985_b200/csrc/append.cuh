@@ -96,10 +96,10 @@ __device__ __forceinline__ bool append_in_range(const AppendParams& p, int s, in
 // cos (first half) and sin of the 8 pairs of lane position j at position pos
 __device__ __forceinline__ void append_angles(const AppendParams& p, int64_t pos, int j, float (&a)[16]) {
     const int64_t at = pos * (p.R / 2) + j * 8;
-    *reinterpret_cast<float4*>(a) = __ldg(reinterpret_cast<const float4*>(p.cosv + at));
-    *reinterpret_cast<float4*>(a + 4) = __ldg(reinterpret_cast<const float4*>(p.cosv + at + 4));
-    *reinterpret_cast<float4*>(a + 8) = __ldg(reinterpret_cast<const float4*>(p.sinv + at));
-    *reinterpret_cast<float4*>(a + 12) = __ldg(reinterpret_cast<const float4*>(p.sinv + at + 4));
+    *reinterpret_cast<float4*>(a) = *reinterpret_cast<const float4*>(p.cosv + at);
+    *reinterpret_cast<float4*>(a + 4) = *reinterpret_cast<const float4*>(p.cosv + at + 4);
+    *reinterpret_cast<float4*>(a + 8) = *reinterpret_cast<const float4*>(p.sinv + at);
+    *reinterpret_cast<float4*>(a + 12) = *reinterpret_cast<const float4*>(p.sinv + at + 4);
 }
 template <bool kInterleaved>
 __device__ __forceinline__ void append_rotate(float (&a)[8], float (&b)[8], const float (&cs)[16]) {

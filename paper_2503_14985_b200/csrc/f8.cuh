@@ -15,7 +15,9 @@ constexpr int kF8MinExp = -64;
 // The kernels of the 8-bit path follow one another in short calls, so they are launched with programmatic stream
 // serialisation: a kernel's blocks may be placed while the one before it in the stream drains, and wait there
 // (pdl_begin, before the first access to memory and before any tensor memory is allocated) until that one has completed and
-// its writes are visible.  Every block executes pdl_begin, so a kernel's completion implies its predecessors'.
+// its writes are visible.  No load is a non-coherent one (ld.global.nc, __ldg): that asks for memory that does not change while
+// the kernel is there, and it is there while the kernel before it still writes.  Every block executes pdl_begin, so a kernel's
+// completion implies its predecessors'.
 // Measured back to back: 1 to 2 us per call.
 __device__ __forceinline__ void pdl_begin() {
     pdl_launch_dependents();

@@ -350,7 +350,7 @@ gemm_f8_split_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_co
 // A load that stays where it is written (a prefetch that the compiler would move down to its use); 0 where `there` is false.
 __device__ __forceinline__ float ld_f32_if(const float* p, bool there) {
     float v;
-    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\tmov.f32 %0, 0f00000000;\n\t@q ld.global.nc.f32 %0, [%1];\n\t}"
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\tmov.f32 %0, 0f00000000;\n\t@q ld.global.f32 %0, [%1];\n\t}"
                  : "=f"(v)
                  : "l"(p), "r"(static_cast<int>(there)));
     return v;

@@ -321,8 +321,8 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
             for (int i = 0; i < NB; ++i) {
                 const bool there = i * kPiece < n && tab[i] >= 0 && tab[i] < p.num_blocks;
                 const int64_t at = static_cast<int64_t>(tab[i]) * p.H_kv + kvh;
-                tks[i] = there ? __ldg(p.ks + at) : 0.0f;
-                tvs[i] = there ? __ldg(p.vs + at) : 0.0f;
+                tks[i] = there ? p.ks[at] : 0.0f;
+                tvs[i] = there ? p.vs[at] : 0.0f;
             }
         }
     };

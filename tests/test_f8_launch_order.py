@@ -60,3 +60,10 @@ def test_nothing_is_read_before_the_wait(name, kernel, body):
     before = body[:wait.start()]
     assert not re.search(r"\bp\.(%s)\b" % "|".join(sorted(pointer_fields(name))), before), "a pointer of the parameters is used before the wait"
     assert not re.search(r"[(,]\s*p\s*[,)]", before), "the parameters go to a function before the wait"
+
+
+@pytest.mark.parametrize("name", FILES + ("f8.cuh",))
+def test_no_non_coherent_loads(name):
+    # such a load may only meet memory that nothing writes while the kernel is there, and these kernels are there while the one before
+    # them may still write their inputs (scales that the quantiser or the cache append has just made, say)
+    assert not re.search(r"\b__ldg\b|\bld\.global\.nc\b|\b__restrict__\b", source(name))
