@@ -152,10 +152,7 @@ gemm_f8_split_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_co
             mbar_init(&scale_full[threadIdx.x], 32);
             mbar_init(&scale_empty[threadIdx.x], quarters * halves);
         }
-        if (threadIdx.x == 0) {
-            abort_word = 0;
-            if (blockIdx.x == 0) clock_probe(0, 0);
-        }
+        if (threadIdx.x == 0) abort_word = 0;
         fence_mbar_init();
     }
     if (warp == 0 && lane == 0) {
@@ -163,6 +160,7 @@ gemm_f8_split_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_co
         prefetch_tensormap(&tmap_b);
     }
     pdl_begin();
+    if (blockIdx.x == 0 && threadIdx.x == 0) clock_probe(0, 0);
     if (warp == 1) {
         tmem_alloc(&tmem_base_slot, 512);
         tmem_relinquish();
@@ -397,7 +395,6 @@ gemm_f8_big_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
     volatile uint32_t* abort_flag = tmem_base_slot + 1;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    if (blockIdx.x == 0 && threadIdx.x == 0) clock_probe(0, 0);
     const int rank = kPair ? static_cast<int>(cluster_ctarank()) : 0;
     const int first = kPair ? blockIdx.x >> 1 : blockIdx.x, step = kPair ? gridDim.x >> 1 : gridDim.x;
     const int num_kb = (p.K + kF8BK - 1) / kF8BK;
@@ -442,6 +439,7 @@ gemm_f8_big_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
 
     if (warp == 0) {
         if (lane == 0) {
+            if (blockIdx.x == 0) clock_probe(0, 0);
             int stage = 0;
             uint32_t phase = 0;
             bool ok = true;

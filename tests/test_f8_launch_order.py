@@ -67,3 +67,10 @@ def test_no_non_coherent_loads(name):
     # such a load may only meet memory that nothing writes while the kernel is there, and these kernels are there while the one before
     # them may still write their inputs (scales that the quantiser or the cache append has just made, say)
     assert not re.search(r"\b__ldg\b|\bld\.global\.nc\b|\b__restrict__\b", source(name))
+
+
+@pytest.mark.parametrize("name,kernel,body", KERNELS, ids=[k for _, k, _ in KERNELS])
+def test_nothing_is_written_before_the_wait(name, kernel, body):
+    # the clock stamps in particular: taken before the wait they would count the predecessor's time as the kernel's
+    before = body[:WAIT.search(body).start()]
+    assert not re.search(r"\bclock_probe\b|\bg_status\b|\bappend_report\b|\bst\.global\b", before)
