@@ -11,7 +11,8 @@
 //
 // 8-bit cache: the block's scale becomes max(the scale it had, if the block already holds tokens of the sequence; the
 // power-of-two scale of the new tokens' largest finite magnitude).  If that is larger than before, the tokens already
-// there are moved to it: q' = round(q * old / new), exact for powers of two unless a value underflows.
+// there are moved to it: q' = round(q * old / new), exact for powers of two unless a value underflows.  Every value is rounded
+// once, also under a scale that is no power of two (set by someone else).
 //
 // Bound by HBM for prompts and by latency for single tokens: every input is read once, every output written once.
 //   keys, values  one warp owns one head of the (at most BS) new tokens of one cache block, because the 8-bit block scale needs
@@ -273,7 +274,7 @@ __global__ void __launch_bounds__(kAppendWarps * 32) kv_append_kernel(const Appe
                             uint32_t lo, hi;
                             f16x2_from_f8x4(u ? v.y : v.x, lo, hi);
                             const float2 x = f32x2_from_f16x2(lo), y = f32x2_from_f16x2(hi);
-                            o[u] = f8x4_from_f32(x.x * ratio, x.y * ratio, y.x * ratio, y.y * ratio);
+                            o[u] = f8x4_from_f32(mul_to_odd(x.x, ratio), mul_to_odd(x.y, ratio), mul_to_odd(y.x, ratio), mul_to_odd(y.y, ratio));
                         }
                         *q = make_uint2(o[0], o[1]);
                     }
@@ -283,7 +284,18 @@ __global__ void __launch_bounds__(kAppendWarps * 32) kv_append_kernel(const Appe
     }
     __syncwarp();  // every lane has read the old scale
     if (lane == 0) *scale_at = scale;
-    const float inv = 1.0f / scale;
+    // x / scale is exact for a power of two; a scale that came from elsewhere (and only such a block's) goes through divisions
+    float inv = 1.0f / scale;
+    if (!is_pow2(scale)) {
+        inv = 1.0f;
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                fa[i][e] = div_to_odd(fa[i][e], scale);
+                fb[i][e] = div_to_odd(fb[i][e], scale);
+            }
+    }
 #pragma unroll
     for (int i = 0; i < STEPS; ++i) {
         const int off = i * TPS + grp;

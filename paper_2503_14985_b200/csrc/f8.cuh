@@ -74,6 +74,24 @@ __device__ __forceinline__ int f8_scale_exp(float amax) {
 }
 __device__ __forceinline__ float pow2f(int e) { return __uint_as_float(static_cast<uint32_t>(e + 127) << 23); }  // -126 <= e <= 127
 
+__device__ __forceinline__ bool is_pow2(float s) { return (__float_as_uint(s) & 0x7FFFFFu) == 0u; }  // of a positive normal number
+
+// a * b and a / b rounded to odd: toward zero, with the last bit set where something was cut off.  A later rounding to E4M3's four
+// bits then gives what rounding the exact result gives (a rounding to nearest in between could land on the middle between two
+// values).  The remainders are exact, or far too small to matter where they underflow.
+__device__ __forceinline__ float to_odd(float cut, float rest) {
+    const bool odd = rest != 0.0f && fabsf(cut) <= 3.402823466e38f;  // (infinities and NaN as they are)
+    return __uint_as_float(__float_as_uint(cut) | (odd ? 1u : 0u));
+}
+__device__ __forceinline__ float mul_to_odd(float a, float b) {
+    const float r = __fmul_rz(a, b);
+    return to_odd(r, fmaf(a, b, -r));
+}
+__device__ __forceinline__ float div_to_odd(float a, float b) {
+    const float r = __fdiv_rz(a, b);
+    return to_odd(r, fmaf(-r, b, a));
+}
+
 __device__ __forceinline__ float abs_if_finite(float x) {
     const float a = fabsf(x);
     return a <= 3.402823466e38f ? a : 0.0f;  // infinities and NaN do not set a scale
