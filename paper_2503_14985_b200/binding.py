@@ -534,7 +534,7 @@ def paged_attn_decode_f8(Q, K_cache, V_cache, k_scale, v_scale, block_table, seq
                          LSE=None, return_lse: bool = True, stream=None):
     """paged_attn_decode over float8_e4m3fn caches with float32 scales k_scale, v_scale [num_blocks, H_kv].
 
-    `workspace` is an optional uint8 CUDA tensor (see paged_attn_f8_workspace_bytes).  Returns (O [S,H,D] bfloat16,
+    `workspace` is an optional contiguous uint8 CUDA tensor (see paged_attn_f8_workspace_bytes).  Returns (O [S,H,D] bfloat16,
     LSE [S,H] float32 or None).
     """
     import torch
@@ -567,6 +567,8 @@ def paged_attn_decode_f8(Q, K_cache, V_cache, k_scale, v_scale, block_table, seq
         held.append(LSE)
         lse = LSE.data_ptr()
     if workspace is not None:
+        if not workspace.is_contiguous():
+            raise TypeError("workspace must be contiguous")
         held.append(workspace)
         ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     _call("mlt_paged_attn_decode_f8", load().mlt_paged_attn_decode_f8, held,
