@@ -19,3 +19,30 @@ def test_workspace_that_is_not_contiguous(ws):
     # the call takes the address and as many bytes as the view has elements: it would write what lies between them, or behind them
     with pytest.raises(TypeError, match="workspace"):
         mlt.paged_attn_decode_f8(*decode_args(), scale=0.1, workspace=ws)
+
+
+@pytest.mark.parametrize("shape", [(2, 3), (2, 1, 1), (2, 0)])
+def test_lengths_that_are_not_a_vector(shape):
+    # [sequences, 3], say, would be read as if its first row held the lengths
+    args = decode_args()
+    args[6] = torch.zeros(shape, dtype=I32)
+    with pytest.raises(ValueError, match="seq_lens"):
+        mlt.paged_attn_decode_f8(*args, scale=0.1)
+    q, k, cache = torch.zeros(3, 4, 64, dtype=BF), torch.zeros(3, 2, 64, dtype=BF), torch.zeros(5, 2, 16, 64, dtype=BF)
+    cu, ctx, table = torch.zeros(3, dtype=I32), torch.zeros(2, dtype=I32), torch.zeros(2, 2, dtype=I32)
+    wide = torch.zeros((3,) + shape[1:], dtype=I32)
+    for c, x in ((wide, ctx), (cu, torch.zeros(shape, dtype=I32))):
+        with pytest.raises(ValueError, match="cu_tokens"):
+            mlt.kv_append(q, k, k, None, None, c, x, table, cache, cache)
+        with pytest.raises(ValueError, match="cu_tokens"):
+            mlt.kv_append_f8(q, k, k, None, None, c, x, table, cache.to(F8), cache.to(F8), torch.ones(5, 2), torch.ones(5, 2))
+
+
+def test_lengths_without_a_dimension():
+    args = decode_args()
+    args[6] = torch.tensor(2, dtype=I32)
+    with pytest.raises(ValueError, match="seq_lens"):
+        mlt.paged_attn_decode_f8(*args, scale=0.1)
+    k, cache = torch.zeros(3, 2, 64, dtype=BF), torch.zeros(5, 2, 16, 64, dtype=BF)
+    with pytest.raises(ValueError, match="cu_tokens"):
+        mlt.kv_append(None, k, k, None, None, torch.zeros(2, dtype=I32), torch.tensor(0, dtype=I32), torch.zeros(1, 2, dtype=I32), cache, cache)
