@@ -467,10 +467,9 @@ def _kv_append(name, Q, K, V, cos, sin, cu_tokens, context_lens, block_table, K_
     for t in (cu_tokens, context_lens, block_table):
         if t.dtype != i32 or not t.is_contiguous():
             raise TypeError("cu_tokens, context_lens and block_table must be contiguous int32 tensors")
-    cu, ctx, table = cu_tokens.shape, context_lens.shape, block_table.shape
-    if len(ctx) != 1 or len(cu) != 1 or cu[0] != ctx[0] + 1 or len(table) != 2 or table[0] != ctx[0]:
+    S, table = context_lens.numel(), block_table.shape  # (columns of one element serve as vectors)
+    if cu_tokens.numel() != S + 1 or len(table) != 2 or table[0] != S:
         raise ValueError("cu_tokens must be [sequences + 1], context_lens [sequences], block_table [sequences, blocks]")
-    S = ctx[0]
     held = [K, V, K_cache, V_cache, cu_tokens, context_lens, block_table]
     ks = vs = ()
     if scales:
@@ -552,7 +551,7 @@ def paged_attn_decode_f8(Q, K_cache, V_cache, k_scale, v_scale, block_table, seq
     for t in (k_scale, v_scale):
         if t.dtype != torch.float32 or not t.is_contiguous() or tuple(t.shape) != (NB, H_kv):
             raise TypeError("k_scale and v_scale must be contiguous float32 [num_blocks, H_kv] tensors")
-    if seq_lens.dim() != 1 or seq_lens.shape[0] != S or block_table.dim() != 2 or block_table.shape[0] != S:
+    if seq_lens.numel() != S or block_table.dim() != 2 or block_table.shape[0] != S:
         raise ValueError("seq_lens must be [sequences], block_table [sequences, blocks]")
     if V_cache.shape != K_cache.shape or K_cache.shape[3] != D:
         raise ValueError("shape mismatch")

@@ -21,7 +21,7 @@ def test_workspace_that_is_not_contiguous(ws):
         mlt.paged_attn_decode_f8(*decode_args(), scale=0.1, workspace=ws)
 
 
-@pytest.mark.parametrize("shape", [(2, 3), (2, 1, 1), (2, 0)])
+@pytest.mark.parametrize("shape", [(2, 3), (2, 1, 2), (2, 0)])
 def test_lengths_that_are_not_a_vector(shape):
     # [sequences, 3], say, would be read as if its first row held the lengths
     args = decode_args()
@@ -38,11 +38,11 @@ def test_lengths_that_are_not_a_vector(shape):
             mlt.kv_append_f8(q, k, k, None, None, c, x, table, cache.to(F8), cache.to(F8), torch.ones(5, 2), torch.ones(5, 2))
 
 
-def test_lengths_without_a_dimension():
+def test_columns_of_one_element_serve_as_vectors():
     args = decode_args()
-    args[6] = torch.tensor(2, dtype=I32)
-    with pytest.raises(ValueError, match="seq_lens"):
+    args[6] = args[6][:, None]
+    with pytest.raises(ValueError, match="CUDA"):               # the next check: the tensors are not on a GPU
         mlt.paged_attn_decode_f8(*args, scale=0.1)
     k, cache = torch.zeros(3, 2, 64, dtype=BF), torch.zeros(5, 2, 16, 64, dtype=BF)
-    with pytest.raises(ValueError, match="cu_tokens"):
-        mlt.kv_append(None, k, k, None, None, torch.zeros(2, dtype=I32), torch.tensor(0, dtype=I32), torch.zeros(1, 2, dtype=I32), cache, cache)
+    with pytest.raises(ValueError, match="CUDA"):
+        mlt.kv_append(None, k, k, None, None, torch.zeros(2, 1, dtype=I32), torch.zeros(1, 1, dtype=I32), torch.zeros(1, 2, dtype=I32), cache, cache)
