@@ -18,7 +18,8 @@ constexpr int kF8MinExp = -64;
 // its writes are visible.  No load is a non-coherent one (ld.global.nc, __ldg): that asks for memory that does not change while
 // the kernel is there, and it is there while the kernel before it still writes.  Every block executes pdl_begin, so a kernel's
 // completion implies its predecessors'.
-// Measured back to back: 1 to 2 us per call.
+// Measured in captured graphs of one call after the other, against plain launches: 0.1 to 0.3 us less per call for single tokens
+// (2.6 to 3.9 us), 0.4 to 0.8 for the next-token products, prompts and batches of decode, 1.3 for two long sequences, 1.9 for 777 x 5000 x 4200.
 __device__ __forceinline__ void pdl_begin() {
     pdl_launch_dependents();
     cudaGridDependencySynchronize();

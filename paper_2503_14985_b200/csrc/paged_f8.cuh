@@ -614,8 +614,9 @@ paged_f8_decode_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
 
 // Rows that several warps worked on: sum of their partials, rescaled to the common maximum.  A CTA has kVec float4 columns of a
 // row's group of heads, a thread one of them and every kSplits-th partial.  Few rows have many partials each: below 64 rows
-// 512 threads with 32 columns (8 rows of 148 partials: 22 us in all, with all columns in a CTA of 256 threads 41), otherwise all
-// columns and 256 threads (1000 sequences of 200 tokens: 60 us in all, with 512 threads about 5 more).
+// 512 threads with 32 columns, otherwise all columns and 256 threads.  Both sides measured, decode and combine together (us, the first
+// form and the second): 1 row of 32k tokens 15 and 101, 16 rows of 16k 23 and 35, 32 of 4k 15 and 21 (of 500 11.2 and 10.4), 64 of 4k 25.3 and
+// 25.5 (of 500 13.7 and 11.4), 128 of 3k 36 and 31.
 template <int D, int G, int kVec, int kThreads>
 __global__ void __launch_bounds__(kThreads) paged_f8_combine_kernel(const PagedF8Params p) {
     constexpr int kWarps = kThreads / 32;
