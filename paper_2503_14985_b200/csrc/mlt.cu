@@ -1007,7 +1007,7 @@ int mlt_gemm_f8(const void* A, const float* scale_a, const void* B, const float*
     p.K = static_cast<int>(K);
     p.tiles_m = static_cast<int>(tiles_m);
     p.tiles_n = static_cast<int>(tiles_n);
-    p.group_m = 8;  // (4, 8 and 16 over ten problems: within their noise; 8192 x 28672 x 4096 857-889, 902-926 and 915-948 us, 777 x 5000 x 4200 27 us)
+    p.group_m = 8;
     p.bn = bn;
     p.bufs = plan.bufs;
     p.a_rows = plan.a_rows;
@@ -1019,6 +1019,10 @@ int mlt_gemm_f8(const void* A, const float* scale_a, const void* B, const float*
         const uint32_t box[2] = {64, 32};
         rc = encode_bf16(&tc, C, 2, dims, strides, box);
         if (rc != MLT_OK) return rc;
+        // Tile rows per raster group: with 16 a wide pair problem reads B panels half as often, which shows under the power cap (8192 x 28672
+        // x 4096 call after call: 971 us, with 8 1009).  Elsewhere 8 and 16 are alike (777 x 5000 x 4200 27.0 and 27.2, 1024 x 28672 x 4096
+        // 120 and 122, 4096 x 8192 x 8192 298 and 299).
+        if (tiles_n >= 32 && plan.big == 2) p.group_m = 16;
         const int tiles = static_cast<int>(tiles_m * tiles_n);
         const cudaError_t e =
             plan.big == 2 ? pdl_launch(gemm_f8_big_kernel<true>, dim3(2 * std::min(tiles, dev.sm_count / 2)), dim3(kF8BigThreads),
