@@ -272,10 +272,11 @@ int mlt_kv_append_f8(const void* Q, const void* K, const void* V, const float* c
  *                work is cut into fewer shares, with NULL (or less than num_seqs * H_kv + 2 partials of
  *                (H / H_kv) * (4 D + 8) + 8 bytes) one CTA works on each (sequence, KV head).  Calls that overlap on the
  *                GPU must not share it.
- * num_blocks * H_kv must be below 2^31.  The tokens of a bad block-table entry are left out and reported.  The maximum, the
- * sum and the output accumulate in FP32.  Two operands are rounded to FP16: a token's weight p * |v_scale| for the second
- * product, under a power of two for the row's largest one, so that weights below 2^-28 of that lose bits and below 2^-39 are
- * zero; and the queries, under a power of two for each row's largest element, so that elements below 2^-28 of that lose bits.
+ * num_blocks * H_kv must be below 2^31.  The scales may be any FP32 values for which scores and outputs stay in FP32.
+ * The tokens of a bad block-table entry are left out and reported.  The maximum, the sum and the output accumulate in
+ * FP32.  Two operands are rounded to FP16: a token's weight p * |v_scale| for the second product, under a power of
+ * two for the row's largest one, so that weights below 2^-28 of that lose bits and below 2^-39 are zero; and the
+ * queries, under a power of two for each row's largest element, so that elements below 2^-28 of that lose bits.
  */
 size_t mlt_paged_attn_f8_workspace_bytes(int num_seqs, int H, int H_kv, int D);
 int mlt_paged_attn_decode_f8(const void* Q, const void* K_cache, const void* V_cache, const float* k_scale, const float* v_scale,

@@ -517,7 +517,8 @@ def kv_append(Q, K, V, cos, sin, cu_tokens, context_lens, block_table, K_cache, 
     Q [T, H, D] (or None: only the cache is written), K and V [T, H_kv, D] bfloat16, a token's heads side by side (views
     of one fused projection work); cos, sin [positions, rotary_dim / 2] float32 (both None: no rotation); cu_tokens
     [S + 1], context_lens [S], block_table [S, max_blocks] int32; caches [num_blocks, H_kv, block_size, D].  Tokens from
-    cu_tokens[S] on are left out.  Q_out may be Q.
+    cu_tokens[S] on (a padded batch) are left out: their rows of Q_out are not written, so those of a new Q_out hold
+    whatever its memory held.  Q_out may be Q.
     """
     return _kv_append("mlt_kv_append", Q, K, V, cos, sin, cu_tokens, context_lens, block_table, K_cache, V_cache, (),
                       interleaved, Q_out, stream)
@@ -534,8 +535,9 @@ def paged_attn_decode_f8(Q, K_cache, V_cache, k_scale, v_scale, block_table, seq
                          LSE=None, return_lse: bool = True, stream=None):
     """paged_attn_decode over float8_e4m3fn caches with float32 scales k_scale, v_scale [num_blocks, H_kv].
 
-    `workspace` is an optional contiguous uint8 CUDA tensor (see paged_attn_f8_workspace_bytes).  Returns (O [S,H,D] bfloat16,
-    LSE [S,H] float32 or None).
+    `workspace` is an optional contiguous uint8 CUDA tensor (see paged_attn_f8_workspace_bytes); without one a single CTA
+    works on each (sequence, KV head), which is slow for few or long sequences.  Returns (O [S,H,D] bfloat16, LSE [S,H]
+    float32 or None).
     """
     import torch
     if Q.dtype != torch.bfloat16 or not Q.is_contiguous() or Q.dim() != 3:

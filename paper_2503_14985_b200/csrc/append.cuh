@@ -18,8 +18,9 @@
 //   keys, values  one warp owns one head of the (at most BS) new tokens of one cache block, because the 8-bit block scale needs
 //                 them together
 //   queries       one warp owns a token, whose heads lie side by side: the angles are read once for all of them
-// Measured (32 query heads, 8 KV heads of 128): 8 prompts of 500 to 1500 tokens in 36 us (BF16 cache, 5.6 TB/s) or 35 us (E4M3,
-// 5.3 TB/s), 43 us with queries by head like the keys; 32 single tokens in 3.1 and 3.6 us, a chain of memory latencies.
+// Measured, device time in captured graphs (32 query heads, 8 KV heads of 128): 8 prompts of 500 to 1500 tokens in 36 us (BF16 cache, 5.6 TB/s)
+// or 35 us (E4M3, 5.3 TB/s), 43 us with queries by head like the keys; 32 single tokens in 3.1 and 3.6 us, a chain of memory
+// latencies (a call from Python takes 15 to 17 us of host time).
 // A lane owns two 8-element chunks of a head that hold both partners of its rotation pairs, so no exchange between lanes is
 // needed but the maximum.
 //

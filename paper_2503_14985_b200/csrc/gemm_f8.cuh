@@ -104,9 +104,12 @@ __device__ __forceinline__ void gemm_f8_promote(float2 (&acc)[kChunks * 8], uint
 // cut over the S CTAs of the cluster.  Such a problem is bound by how evenly the stream of B is spread over the SMs, so the
 // host picks bn and S together such that tiles x S comes close to the SM count from below.  The CTAs' FP32 tiles meet in
 // distributed shared memory (the stages are free by then) and are summed in ascending slice order (deterministic).
-// Bound by HBM.  Measured: 16 x 28672 x 4096 in 25 us (4.8 TB/s; 18 us at the copy's rate, 3.5 until the first data, 3 from the
-// last product to the last store), 16 x 4096 x 28672 in 28 us, 512 x 4096 x 4096 in 18 us.  Without setmaxnreg (spills) 45, with
-// a branch per 16 columns instead of the switch 33, without the scale warp 28.
+// Bound by HBM with many columns and short K; with few columns and long K by the promotion, of which a cluster's CTA does one K
+// block after the other (with 16 rows in two of the eight warps only).  Measured, device time in a captured graph (one call among other
+// passes takes about 3 us more): 16 x 28672 x 4096 in 25 us (4.7 TB/s; 18 us at the copy's rate, 3.5 until the first data, 3 from the last
+// product to the last store), 16 x 4096 x 28672 in 28 us (56 K blocks at about 440 ns by the launch plan's model, 24.5 us),
+// 512 x 4096 x 4096 in 18 us.  Without setmaxnreg 45, with a branch per 16 columns instead of the switch 33, without the scale warp 28.
+// (ptxas reports 32 bytes of spill stores and 260 of spill loads for the kernel as it is, 88 of stores for the one that took 45.)
 // ---------------------------------------------------------------------------------------------------------
 constexpr int kF8SplitSmem = 208 * 1024;
 // A stages | B stages.  The A descriptor always spans 128 rows, of which the first a_rows are loaded: the span may
@@ -363,9 +366,11 @@ __device__ __forceinline__ float ld_f32_if(const float* p, bool there) {
 // The two accumulators in tensor memory (2 x 256 columns) belong to alternate K blocks, across tile borders: while the
 // promotion warps round and store a tile, the tensor core is up to two K blocks into the next one.  Results leave through
 // 4 KB of shared memory per warp (32 rows x 64 columns, 128-byte swizzle) and TMA stores.
-// Bound by the power cap, and by the hand-over between tensor core and promotion warps.  Measured: 8192 x 28672 x 4096 in 946
-// us, 2.03 PFLOP/s at 1.4 GHz (671 without any promotion); 777 x 5000 x 4200 in 24 us, 4096^3 in 65.  Four accumulators of 128
-// columns 1048 (A is read twice), tcgen05.ld of 64 columns 1230, scales through a ring in shared memory 1060, setmaxnreg 1065.
+// Bound by the hand-over between tensor core and promotion warps: without any promotion the first case takes 671 us, at the same power
+// cap.  Measured, device time in captured graphs: 8192 x 28672 x 4096 in 950 to 975 us, 2.0 PFLOP/s at 1.4 GHz (one call among other
+// passes up to 1020; 850 to 900 in the first replays, before the clock comes down); 777 x 5000 x 4200 in 25 us, 4096^3 in 69 (84 call after
+// call).  Four accumulators of 128 columns 1048 (A is read twice), tcgen05.ld of 64 columns 1230, scales through a ring in shared memory
+// 1060, setmaxnreg 1065.
 // ---------------------------------------------------------------------------------------------------------
 constexpr int kF8BigThreads = 320;  // producer, issuer, eight promotion warps (168 registers per thread)
 template <bool kPair>

@@ -31,15 +31,17 @@
 // not read the lengths at all.  Without scratch, or beyond 1024 sequences, one CTA works on each row and its warps' results meet in
 // shared memory.
 //
-// Measured, both kernels, device time in a captured graph: 32 sequences of 2k to 4k tokens, 32 heads over 4, 30 us (3.4 TB/s), 2
-// of 32k with 8 heads 32 us (4.1 TB/s); 256 of 500, 32 heads over 4, 37.5 us (3.6 TB/s), 1000 of 200 60 us (3.7 TB/s); 16 of 2k to 4k
-// with D = 64, 16 heads over 8, 22 us.  Around the streams lie 6 us of dependent latencies (lengths, table, first data) and 3 to 4 us of the
-// combine kernel.  Alternatives, in the order of the first four: weights relative to the largest V scale, which lost the output where that
-// scale's tokens were unlikely, 29, 30.5, 35.5 and 58 (D = 64: 23.5); on top of those, shares of 128-token chunks per CTA with a merge in
-// shared memory 28.5, 29.5, 44 and 107; the same with copies issued ahead into the CTA's next row (longer loop) 30, 32, 47 and 116.  The first
-// two cases at earlier stages: heads as rows 37 and 37 instead of 30 and 32, units of 16 tokens 31 to 33, two stages and three CTAs per SM 30
-// and 32.5 instead of 29 and 30.  For the maximum of x + e: next to that of x in one pass, with a branch for scores beyond 2^23, where x + e
-// loses e, 30, 32, 37.5 and 61.
+// Measured, both kernels, device time in a captured graph: 32 sequences of 2k to 4k tokens, 32 heads over 4, 30 us (3.4
+// TB/s), 2 of 32k with 8 heads 32 us (4.1 TB/s); 256 of 500, 32 heads over 4, 37.5 us (3.6 TB/s), 1000 of 200 60 us (3.7
+// TB/s); 16 of 2k to 4k with D = 64, 16 heads over 8, 22 us.  Around the streams lie 6 us of dependent latencies (lengths,
+// table, first data) and 3 to 4 us of the combine kernel; that leaves 4 to 5 us of the first case not accounted for.
+// Without scratch, one CTA per row: 54, 324, 44 and 101. Beyond 1024 sequences likewise (1100 of 200 111).  Alternatives, in
+// the order of the first four: weights relative to the largest V scale, which lost the output where that scale's tokens were
+// unlikely, 29, 30.5, 35.5 and 58 (D = 64: 23.5); on top of those, shares of 128-token chunks per CTA with a merge in shared
+// memory 28.5, 29.5, 44 and 107; the same with copies issued ahead into the CTA's next row (longer loop) 30, 32, 47 and 116.
+// The first two cases at earlier stages: heads as rows 37 and 37 instead of 30 and 32, units of 16 tokens 31 to 33, two
+// stages and three CTAs per SM 30 and 32.5 instead of 29 and 30.  For the maximum of x + e: next to that of x in one pass,
+// with a branch for scores beyond 2^23, where x + e loses e, 30, 32, 37.5 and 61.
 #pragma once
 
 #include "f8.cuh"

@@ -69,8 +69,9 @@ __device__ __forceinline__ uint32_t max16lanes(uint32_t a) {
 
 // 1 x 128 blocks.  A warp owns kRows rows x 256 columns: kRows independent 16-byte loads per lane, and the scales of
 // kRows consecutive rows leave as one contiguous piece per K block.
-// Measured: 8192 x 28672 in 110 us, 6.4 TB/s (a copy: 6.45); 16 x 4096 in 2.6 us (latency).  4 or 16 rows per warp 116 to
-// 119 us, loads and stores marked as streaming 112 to 117.
+// Measured, device time in a captured graph: 8192 x 28672 in 110 us, 6.4 TB/s (a copy: 6.45); 16 x 4096 in 2.6 us (latency).  One call among
+// other passes on fresh buffers takes 111 to 125 us and 11 us.  4 or 16 rows per warp 116 to 119 us, loads and stores marked as
+// streaming 112 to 117.
 constexpr int kQuantizeThreads = 128;
 template <int kRows>
 __global__ void __launch_bounds__(kQuantizeThreads) quantize_rows_kernel(const QuantizeParams p) {
@@ -109,7 +110,8 @@ __global__ void __launch_bounds__(kQuantizeThreads) quantize_rows_kernel(const Q
     if ((lane & 15) < kRows && row0 + (lane & 15) < p.M && kb * 128 < p.K) p.S[kb * p.lds + row0 + (lane & 15)] = scale;
 }
 
-// 128 x 128 blocks: one CTA each, 16 rows at a time.  Measured: 28672 x 4096 in 54 us, 6.5 TB/s.
+// 128 x 128 blocks: one CTA each, 16 rows at a time.  Measured, device time in a captured graph: 28672 x 4096 and 4096 x 28672 in 54 us,
+// 6.5 TB/s.
 constexpr int kQuantizeBlockThreads = 256;
 __global__ void __launch_bounds__(kQuantizeBlockThreads) quantize_blocks_kernel(const QuantizeParams p) {
     __shared__ uint32_t sm[kQuantizeBlockThreads / 32];
