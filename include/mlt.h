@@ -31,7 +31,7 @@ typedef enum {
     MLT_ERR_TIMEOUT = 6,     /* a bounded device-side wait expired (reported by mlt_last_device_error) */
     MLT_ERR_BAD_BLOCK = 7,   /* a block-table entry outside [0, num_blocks) was met (reported by mlt_last_device_error) */
     MLT_ERR_SCRATCH_LIMIT = 8, /* mlt_paged_attn_decode_static: the call needs more than MLT_PAGED_STATIC_SCRATCH_BYTES */
-    MLT_ERR_BAD_POSITION = 9 /* mlt_kv_append*: a sequence's token offsets or positions lie outside the call's tokens or the
+    MLT_ERR_BAD_POSITION = 9 /* a sequence's token offsets or positions lie outside the call's tokens, keys, block table or
                                 cos / sin tables (reported by mlt_last_device_error) */
 } mlt_status;
 
@@ -285,6 +285,61 @@ int mlt_paged_attn_decode_f8(const void* Q, const void* K_cache, const void* V_c
                              int num_seqs, int H, int H_kv, int D,
                              int block_size, int max_blocks_per_seq, int num_blocks, float scale,
                              void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * ---- The BF16 serving path (library additions) ----
+ *
+ * Launched like the 8-bit path: a kernel's blocks may be placed while the kernel before it drains, and touch memory only
+ * after it has completed.
+ */
+
+/*
+ * mlt_mha_fwd for sequences of different lengths packed one behind another, with grouped heads.
+ *
+ *   Q       device, BF16; token t, head h, element d at t * ldq + h * D + d
+ *   K, V    device, BF16; key j, KV head at j * ldk + h * D + d (likewise ldv); query head h reads KV head h / (H / H_kv)
+ *   cu_q, cu_k  device, int32, [num_seqs + 1]: sequence s has the queries cu_q[s] .. cu_q[s + 1] - 1 and the keys
+ *           cu_k[s] .. cu_k[s + 1] - 1 (either may be none); they may be the same array
+ *   O       device, BF16 out, pitch ldo;  LSE  device, FP32 out, [num_q, H], or NULL
+ *   causal  non-zero: key j is visible to query i of the same sequence iff j <= i + (keys - queries) (bottom-right
+ *           aligned; queries beyond the keys see nothing)
+ * H / H_kv is any whole number up to 128.  D in {64, 128}; pitches in elements, multiples of 8.
+ * A query that sees no key gives O = 0 and LSE = -inf.  Rows of O and LSE that belong to no sequence (a padded batch) are
+ * left as they were.  What lies in K and V behind a sequence's last key (the next sequence, padding) never reaches its results, not
+ * even a NaN; inside a sequence a masked V must be finite (it may meet a weight of zero).
+ * A sequence whose offsets descend or reach outside num_q or num_k is left out and reported (MLT_ERR_BAD_POSITION,
+ * mlt_last_device_error).  num_q == 0 or num_seqs == 0: MLT_OK, nothing launched.
+ * P is rounded to BF16 for the second product; S, m, l and O accumulate in FP32.  With few queries behind many keys the key
+ * range is cut and the parts are joined in FP32.
+ *
+ *   workspace  device scratch, 16-byte aligned; mlt_mha_packed_workspace_bytes is always enough.  With less fewer parts are
+ *              made, with too little for the list of work items the call returns MLT_ERR_INVALID_ARG.  Its contents are scratch;
+ *              calls that overlap on the GPU must not share it.
+ */
+size_t mlt_mha_packed_workspace_bytes(int num_q, int num_seqs, int H, int H_kv, int D);
+int mlt_mha_packed_fwd(const void* Q, const void* K, const void* V, const int32_t* cu_q, const int32_t* cu_k, void* O, float* LSE,
+                       int num_q, int num_k, int num_seqs, int H, int H_kv, int D, int causal, float scale,
+                       int64_t ldq, int64_t ldk, int64_t ldv, int64_t ldo,
+                       void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Causal attention of new tokens (a prompt, a chunk of one, a few speculated tokens) over the paged cache of
+ * mlt_paged_attn_decode, which holds their own keys and values already: cu_tokens, context_lens and block_table are those of
+ * the mlt_kv_append call that put them there.
+ *
+ *   Q       device, BF16, pitch ldq, rotated;  K_cache, V_cache  device, BF16, [num_blocks, H_kv, block_size, D]
+ *   token t of sequence s sees the positions 0 .. context_lens[s] + t - cu_tokens[s] of its cache
+ *   O, LSE, workspace (mlt_mha_packed_workspace_bytes) and the rest as for mlt_mha_packed_fwd
+ * block_size in {8, 16, 32}; num_blocks * H_kv must be below 2^31.  A block-table entry outside [0, num_blocks) that a
+ * sequence reaches counts as a block of zeros and is reported (MLT_ERR_BAD_BLOCK).  A sequence whose offsets do not fit
+ * num_tokens, whose context is negative, or whose positions do not fit the table is left out and reported (MLT_ERR_BAD_POSITION).
+ */
+int mlt_paged_attn_prefill(const void* Q, const void* K_cache, const void* V_cache,
+                           const int32_t* cu_tokens, const int32_t* context_lens, const int32_t* block_table,
+                           void* O, float* LSE,
+                           int num_tokens, int num_seqs, int H, int H_kv, int D,
+                           int block_size, int max_blocks_per_seq, int num_blocks, float scale,
+                           int64_t ldq, int64_t ldo, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * The SM clock the last GEMM (which = 0) or attention (which = 1) launch on the current device really ran at, in

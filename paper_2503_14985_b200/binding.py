@@ -21,6 +21,7 @@ PAGED_STATIC_SCRATCH_BYTES = 16 * 1024 * 1024
 EXPORTS = ("mlt_gemm", "mlt_gemm_f16", "mlt_gemm_ex", "mlt_gemm_workspace_bytes", "mlt_mha_fwd", "mlt_paged_attn_decode", "mlt_paged_attn_decode_static",
            "mlt_paged_attn_workspace_bytes",
            "mlt_quantize_f8", "mlt_gemm_f8", "mlt_kv_append", "mlt_kv_append_f8", "mlt_paged_attn_decode_f8", "mlt_paged_attn_f8_workspace_bytes",
+           "mlt_mha_packed_fwd", "mlt_mha_packed_workspace_bytes", "mlt_paged_attn_prefill",
            "mlt_last_device_error", "mlt_debug_wait_timeout_selftest", "mlt_debug_last_clock_mhz", "mlt_debug_gemm_plan", "mlt_debug_gemm_f8_plan", "mlt_status_string",
            "mlt_version")
 
@@ -79,6 +80,12 @@ def load() -> ctypes.CDLL:
         lib.mlt_paged_attn_f8_workspace_bytes.restype = ctypes.c_size_t
         lib.mlt_paged_attn_decode_f8.argtypes = [p] * 9 + [i32] * 7 + [ctypes.c_float, p, ctypes.c_size_t, p]
         lib.mlt_paged_attn_decode_f8.restype = i32
+        lib.mlt_mha_packed_workspace_bytes.argtypes = [i32] * 5
+        lib.mlt_mha_packed_workspace_bytes.restype = ctypes.c_size_t
+        lib.mlt_mha_packed_fwd.argtypes = [p] * 7 + [i32] * 7 + [ctypes.c_float] + [i64] * 4 + [p, ctypes.c_size_t, p]
+        lib.mlt_mha_packed_fwd.restype = i32
+        lib.mlt_paged_attn_prefill.argtypes = [p] * 8 + [i32] * 8 + [ctypes.c_float] + [i64] * 2 + [p, ctypes.c_size_t, p]
+        lib.mlt_paged_attn_prefill.restype = i32
         lib.mlt_last_device_error.argtypes = [p]
         lib.mlt_last_device_error.restype = i32
         lib.mlt_status_string.argtypes = [i32]
@@ -193,6 +200,26 @@ def paged_attn_decode_f8_raw(Q: int, K_cache: int, V_cache: int, k_scale: int, v
     return load().mlt_paged_attn_decode_f8(Q, K_cache, V_cache, k_scale, v_scale, block_table, seq_lens, O, LSE, num_seqs, H,
                                            H_kv, D, block_size, max_blocks, num_blocks, scale, workspace, workspace_bytes,
                                            stream)
+
+
+def mha_packed_workspace_bytes(num_q: int, num_seqs: int, H: int, H_kv: int, D: int) -> int:
+    return int(load().mlt_mha_packed_workspace_bytes(num_q, num_seqs, H, H_kv, D))
+
+
+def mha_packed_fwd_raw(Q: int, K: int, V: int, cu_q: int, cu_k: int, O: int, LSE: int, num_q: int, num_k: int, num_seqs: int, H: int,
+                       H_kv: int, D: int, causal: int, scale: float, ldq: int, ldk: int, ldv: int, ldo: int, workspace: int,
+                       workspace_bytes: int, stream: int = 0) -> int:
+    """mlt_mha_packed_fwd with raw device addresses; returns the status code."""
+    return load().mlt_mha_packed_fwd(Q, K, V, cu_q, cu_k, O, LSE, num_q, num_k, num_seqs, H, H_kv, D, causal, scale, ldq, ldk, ldv, ldo,
+                                     workspace, workspace_bytes, stream)
+
+
+def paged_attn_prefill_raw(Q: int, K_cache: int, V_cache: int, cu_tokens: int, context_lens: int, block_table: int, O: int, LSE: int,
+                           num_tokens: int, num_seqs: int, H: int, H_kv: int, D: int, block_size: int, max_blocks: int, num_blocks: int,
+                           scale: float, ldq: int, ldo: int, workspace: int, workspace_bytes: int, stream: int = 0) -> int:
+    """mlt_paged_attn_prefill with raw device addresses; returns the status code."""
+    return load().mlt_paged_attn_prefill(Q, K_cache, V_cache, cu_tokens, context_lens, block_table, O, LSE, num_tokens, num_seqs, H, H_kv, D,
+                                         block_size, max_blocks, num_blocks, scale, ldq, ldo, workspace, workspace_bytes, stream)
 
 
 def last_device_error():
@@ -578,4 +605,111 @@ def paged_attn_decode_f8(Q, K_cache, V_cache, k_scale, v_scale, block_table, seq
     _call("mlt_paged_attn_decode_f8", load().mlt_paged_attn_decode_f8, held,
           (Q.data_ptr(), K_cache.data_ptr(), V_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), block_table.data_ptr(),
            seq_lens.data_ptr(), O.data_ptr(), lse, S, H, H_kv, D, bs, block_table.shape[1], NB, float(scale), ws, ws_bytes), stream)
+    return O, LSE
+
+
+def _out_rows(Q, O, LSE, return_lse, stream):
+    """O [T, H, D] with its token pitch, and LSE [T, H] or None: the caller's, checked, or new ones."""
+    import torch
+    T, H, D = Q.shape
+    if O is None:
+        O = _new(Q, (T, H, D), torch.bfloat16, stream)
+    elif O.dtype != torch.bfloat16 or O.shape != Q.shape:
+        raise ValueError("O must be bfloat16 of Q's shape")
+    if LSE is None and return_lse:
+        LSE = _new(Q, (T, H), torch.float32, stream)
+    elif LSE is not None and (LSE.dtype != torch.float32 or tuple(LSE.shape) != (T, H) or not LSE.is_contiguous()):
+        raise ValueError("LSE must be contiguous float32 [T, H]")
+    return O, _rows(O, H, D), LSE
+
+
+def _scratch(Q, workspace, need, stream):
+    """The caller's workspace, or a new one of the size that is always enough."""
+    import torch
+    if workspace is None:
+        return _new(Q, (need,), torch.uint8, stream)
+    if not workspace.is_contiguous():
+        raise TypeError("workspace must be contiguous")
+    return workspace
+
+
+def _vectors(*tensors):
+    import torch
+    for t in tensors:
+        if t.dtype != torch.int32 or not t.is_contiguous():
+            raise TypeError("token offsets, lengths and block tables must be contiguous int32 tensors")
+
+
+def mha_packed_fwd(Q, K, V, cu_q, cu_k=None, *, causal: bool, scale: float, O=None, LSE=None, return_lse: bool = True, workspace=None,
+                   stream=None):
+    """Attention forward over sequences packed one behind another, with grouped heads.
+
+    Q [T, H, D], K and V [T_k, H_kv, D] bfloat16, a token's heads side by side (views of one fused projection work); cu_q, cu_k
+    [S + 1] int32: sequence s has the queries cu_q[s] .. cu_q[s + 1] - 1 and the keys cu_k[s] .. cu_k[s + 1] - 1 (cu_k None: cu_q).
+    Causal masks are aligned bottom-right, as in mha_fwd; a query without a visible key gives O = 0 and LSE = -inf.  Rows of no
+    sequence are not written.  `workspace`: a contiguous uint8 CUDA tensor of mha_packed_workspace_bytes (a new one without).
+    Returns (O [T, H, D] bfloat16, LSE [T, H] float32 or None).
+    """
+    import torch
+    for t in (Q, K, V):
+        if t.dtype != torch.bfloat16 or t.dim() != 3:
+            raise TypeError("Q, K and V must be [tokens, heads, D] bfloat16 tensors")
+    if cu_k is None:
+        cu_k = cu_q
+    _vectors(cu_q, cu_k)
+    T, H, D = Q.shape
+    Tk, H_kv, _ = K.shape
+    if V.shape != K.shape or K.shape[2] != D:
+        raise ValueError("shape mismatch")
+    S = cu_q.numel() - 1
+    if S < 0 or cu_k.numel() != S + 1:
+        raise ValueError("cu_q and cu_k must be [sequences + 1]")
+    O, ldo, LSE = _out_rows(Q, O, LSE, return_lse, stream)
+    workspace = _scratch(Q, workspace, mha_packed_workspace_bytes(T, S, H, H_kv, D), stream)
+    held = [Q, K, V, cu_q, cu_k, O, workspace]
+    lse = 0
+    if LSE is not None:
+        held.append(LSE)
+        lse = LSE.data_ptr()
+    _call("mlt_mha_packed_fwd", load().mlt_mha_packed_fwd, held,
+          (Q.data_ptr(), K.data_ptr(), V.data_ptr(), cu_q.data_ptr(), cu_k.data_ptr(), O.data_ptr(), lse, T, Tk, S, H, H_kv, D,
+           1 if causal else 0, float(scale), _rows(Q, H, D), _rows(K, H_kv, D), _rows(V, H_kv, D), ldo, workspace.data_ptr(),
+           workspace.numel() * workspace.element_size()), stream)
+    return O, LSE
+
+
+def paged_attn_prefill(Q, K_cache, V_cache, cu_tokens, context_lens, block_table, *, scale: float, O=None, LSE=None,
+                       return_lse: bool = True, workspace=None, stream=None):
+    """Causal attention of new tokens over the paged cache, which holds their own keys and values already (see kv_append, whose
+    cu_tokens, context_lens and block_table these are).
+
+    Q [T, H, D] bfloat16 (rotated, a token's heads side by side); caches [num_blocks, H_kv, block_size, D] bfloat16.  Token t of
+    sequence s sees the cache positions 0 .. context_lens[s] + t - cu_tokens[s].  Rows of no sequence are not written.  `workspace`
+    as for mha_packed_fwd.  Returns (O [T, H, D] bfloat16, LSE [T, H] float32 or None).
+    """
+    import torch
+    if Q.dtype != torch.bfloat16 or Q.dim() != 3:
+        raise TypeError("Q must be a [tokens, heads, D] bfloat16 tensor")
+    for t in (K_cache, V_cache):
+        if t.dtype != torch.bfloat16 or not t.is_contiguous() or t.dim() != 4:
+            raise TypeError("the caches must be contiguous 4-D bfloat16 tensors")
+    _vectors(cu_tokens, context_lens, block_table)
+    T, H, D = Q.shape
+    num_blocks, H_kv, block_size, _ = K_cache.shape
+    if V_cache.shape != K_cache.shape or K_cache.shape[3] != D:
+        raise ValueError("shape mismatch")
+    S = context_lens.numel()
+    if cu_tokens.numel() != S + 1 or block_table.dim() != 2 or block_table.shape[0] != S:
+        raise ValueError("cu_tokens must be [sequences + 1], context_lens [sequences], block_table [sequences, blocks]")
+    O, ldo, LSE = _out_rows(Q, O, LSE, return_lse, stream)
+    workspace = _scratch(Q, workspace, mha_packed_workspace_bytes(T, S, H, H_kv, D), stream)
+    held = [Q, K_cache, V_cache, cu_tokens, context_lens, block_table, O, workspace]
+    lse = 0
+    if LSE is not None:
+        held.append(LSE)
+        lse = LSE.data_ptr()
+    _call("mlt_paged_attn_prefill", load().mlt_paged_attn_prefill, held,
+          (Q.data_ptr(), K_cache.data_ptr(), V_cache.data_ptr(), cu_tokens.data_ptr(), context_lens.data_ptr(), block_table.data_ptr(),
+           O.data_ptr(), lse, T, S, H, H_kv, D, block_size, block_table.shape[1], num_blocks, float(scale), _rows(Q, H, D), ldo,
+           workspace.data_ptr(), workspace.numel() * workspace.element_size()), stream)
     return O, LSE

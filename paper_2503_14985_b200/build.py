@@ -9,7 +9,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libmlt.so")
 SOURCES = ["mlt.cu"]
-HEADERS = ["ptx.cuh", "gemm.cuh", "mha.cuh", "paged.cuh", "f8.cuh", "quantize.cuh", "gemm_f8.cuh", "append.cuh", "paged_f8.cuh",
+HEADERS = ["ptx.cuh", "gemm.cuh", "mha.cuh", "mha_packed.cuh", "paged.cuh", "f8.cuh", "quantize.cuh", "gemm_f8.cuh", "append.cuh", "paged_f8.cuh",
            os.path.join("..", "..", "include", "mlt.h")]
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -23,14 +23,15 @@ def is_stale() -> bool:
     return any(os.path.getmtime(os.path.join(CSRC, f)) > t for f in SOURCES + HEADERS)
 
 
-# The attention kernel and the scaled GEMM's split kernel move registers between their warpgroups (setmaxnreg): 8 warps at 208
+# The attention kernels and the scaled GEMM's split kernel move registers between their warpgroups (setmaxnreg): 8 warps at 208
 # and 4 other warps at 88 must fit the launch allocation of 384 threads, i.e. ptxas has to assign at least this many per thread.
 MHA_MIN_REGISTERS = 168
+HAND_OVER_KERNELS = ("mha_fwd_kernel", "mha_packed_kernel", "gemm_f8_split_kernel")
 
 
 def check_mha_registers(ptxas_log: str) -> dict:
-    """Register counts of the mha_fwd_kernel and gemm_f8_split_kernel instantiations in a `-Xptxas -v` log; raises if one is below
-    the budget the in-kernel register hand-over needs (launching such a build would wait for registers that never come)."""
+    """Register counts of the HAND_OVER_KERNELS' instantiations in a `-Xptxas -v` log; raises if one is below the budget
+    the in-kernel register hand-over needs (launching such a build would wait for registers that never come)."""
     found = {}
     name = None
     for line in ptxas_log.splitlines():
@@ -38,7 +39,7 @@ def check_mha_registers(ptxas_log: str) -> dict:
         if m:
             name = m.group(1)
         m = re.search(r"Used (\d+) registers", line)
-        if m and name and ("mha_fwd_kernel" in name or "gemm_f8_split_kernel" in name):
+        if m and name and any(k in name for k in HAND_OVER_KERNELS):
             found[name] = int(m.group(1))
             name = None
     low = {k: v for k, v in found.items() if v < MHA_MIN_REGISTERS}
@@ -57,8 +58,8 @@ def build(force: bool = False, verbose: bool = False) -> str:
         if res.returncode != 0:
             raise RuntimeError("nvcc failed:\n" + res.stdout + res.stderr)
         found = check_mha_registers(res.stdout + res.stderr)
-        if not all(any(k in name for name in found) for k in ("mha_fwd_kernel", "gemm_f8_split_kernel")):
-            raise RuntimeError("no mha_fwd_kernel or gemm_f8_split_kernel entry in the ptxas log")
+        if not all(any(k in name for name in found) for k in HAND_OVER_KERNELS):
+            raise RuntimeError(f"an entry of {HAND_OVER_KERNELS} is missing in the ptxas log")
         os.replace(tmp, LIB)
         if verbose:
             print(res.stdout + res.stderr)

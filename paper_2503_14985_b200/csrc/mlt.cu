@@ -15,6 +15,7 @@
 #include "gemm.cuh"
 #include "gemm_f8.cuh"
 #include "mha.cuh"
+#include "mha_packed.cuh"
 #include "paged.cuh"
 #include "paged_f8.cuh"
 #include "quantize.cuh"
@@ -32,6 +33,7 @@ struct DeviceInfo {
     int cc_major = 0;
     bool configured = false;
     bool mha_ok = false;  // the attention kernels' compiled register count covers their in-kernel register hand-over
+    bool packed_ok = false;   // likewise for the packed attention kernels
     bool gemm_f8_ok = false;  // likewise for the scaled GEMM
     // CTAs that can be resident at once as clusters of 2, 4 and 8 of the K-cutting GEMM kernel (a cluster must fit
     // one GPC, so this can be less than the SM count rounded down to a multiple of the cluster size)
@@ -108,6 +110,9 @@ int get_device(DeviceInfo* out) {
         const int mha_rc = mha_configure();
         if (mha_rc == 1) return MLT_ERR_CUDA;
         d.mha_ok = mha_rc == 0;
+        const int packed_rc = packed_configure();
+        if (packed_rc == 1) return MLT_ERR_CUDA;
+        d.packed_ok = packed_rc == 0;
         d.configured = true;
     }
     *out = d;
@@ -1186,6 +1191,162 @@ int mlt_paged_attn_decode_f8(const void* Q, const void* K_cache, const void* V_c
     }
     return D == 64 ? paged_f8_launch<64>(tk, tv, p, block_size, static_cast<cudaStream_t>(stream))
                    : paged_f8_launch<128>(tk, tv, p, block_size, static_cast<cudaStream_t>(stream));
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------------------------------------
+// The BF16 serving path: attention of packed prompts, of new tokens over the paged cache, decode behind a shared prefix
+// ---------------------------------------------------------------------------------------------------------
+namespace {
+
+// Checks that the packed attention entry points share.  MLT_OK with *launch false: nothing to do.
+int packed_check(const void* Q, const void* K, const void* V, const void* O, int T, int S, int H, int H_kv, int D, float scale,
+                 int64_t ldq, int64_t ldo, const void* workspace, bool* launch) {
+    *launch = false;
+    if (T < 0 || S < 0 || H < 0 || H_kv < 0) return MLT_ERR_INVALID_ARG;
+    if (T == 0 || S == 0 || H == 0) return MLT_OK;
+    if (!Q || !K || !V || !O || !workspace || H_kv == 0 || H % H_kv != 0) return MLT_ERR_INVALID_ARG;
+    if (!(scale > 0.0f) || scale > 3.0e38f) return MLT_ERR_INVALID_ARG;
+    const int64_t width = static_cast<int64_t>(H) * D;
+    if (D != 64 && D != 128) return MLT_ERR_UNSUPPORTED;
+    if (ldq < width || ldo < width) return MLT_ERR_INVALID_ARG;
+    if (H / H_kv > kMhaBlock || H > 65536) return MLT_ERR_UNSUPPORTED;
+    if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(O) || !aligned16(workspace) || ldq % 8 != 0 || ldo % 8 != 0)
+        return MLT_ERR_ALIGNMENT;
+    // work items (tile pairs of all sequences x KV heads) are counted in 32 bits
+    if ((static_cast<int64_t>(T) / (2 * (kMhaBlock / (H / H_kv))) + S) * H_kv > INT32_MAX / 2) return MLT_ERR_UNSUPPORTED;
+    *launch = true;
+    return MLT_OK;
+}
+
+// Parameters that do not depend on where the keys come from, and the Q tensor map.
+int packed_fill(PackedParams* p, CUtensorMap* tq, const void* Q, void* O, float* LSE, int T, int S, int H, int H_kv, int D, float scale,
+                int64_t ldq, int64_t ldo, const PackedScratch& x, void* workspace, int64_t slots, int sm_count) {
+    *p = PackedParams{};
+    p->S = S;
+    p->T = T;
+    p->G = H / H_kv;
+    p->W = x.W;
+    p->H = H;
+    p->H_kv = H_kv;
+    p->scale = scale;
+    p->O = static_cast<__nv_bfloat16*>(O);
+    p->LSE = LSE;
+    p->ldo = ldo;
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    p->hdr = reinterpret_cast<PackedHeader*>(ws);
+    p->seqs = reinterpret_cast<int4*>(ws + x.seqs);
+    p->entries = reinterpret_cast<int4*>(ws + x.entries);
+    p->tile_first = reinterpret_cast<int*>(ws + x.tile_first);
+    p->max_tiles = x.max_tiles;
+    p->max_entries = x.max_entries;
+    p->slot_rows = x.slot_rows;
+    p->slots = static_cast<int>(slots);
+    p->part_o = reinterpret_cast<float*>(ws + x.lists);
+    p->part_ml = reinterpret_cast<float2*>(p->part_o + static_cast<size_t>(slots) * x.slot_rows * D);
+    p->sm_count = sm_count;
+    const uint64_t dims[3] = {static_cast<uint64_t>(D), static_cast<uint64_t>(H), static_cast<uint64_t>(T)};
+    const uint64_t strides[2] = {static_cast<uint64_t>(D) * 2, static_cast<uint64_t>(ldq) * 2};
+    const uint32_t box[3] = {64, static_cast<uint32_t>(p->G), static_cast<uint32_t>(p->W)};
+    return encode_bf16(tq, Q, 3, dims, strides, box);
+}
+
+// Parts of cut key ranges that pay: none when there are enough items for two rounds of the SMs as it is.
+int64_t packed_slots(const PackedScratch& x, int64_t T, int H_kv, size_t workspace_bytes, int sm_count) {
+    if ((T + 2 * x.W - 1) / (2 * x.W) * H_kv >= 2ll * sm_count) return 0;
+    return std::min<int64_t>(kPackedMaxSlots, static_cast<int64_t>((workspace_bytes - x.lists) / x.slot_bytes));
+}
+
+int packed_cache_maps(CUtensorMap* tk, CUtensorMap* tv, const void* K_cache, const void* V_cache, int num_blocks, int H_kv, int block_size, int D) {
+    const uint64_t dims[3] = {static_cast<uint64_t>(D), static_cast<uint64_t>(block_size),
+                              std::max<uint64_t>(1, static_cast<uint64_t>(num_blocks) * H_kv)};
+    const uint64_t strides[2] = {static_cast<uint64_t>(D) * 2, static_cast<uint64_t>(D) * 2 * block_size};
+    const uint32_t box[3] = {64, static_cast<uint32_t>(block_size), 1};
+    const int rc = encode_bf16(tk, K_cache, 3, dims, strides, box);
+    return rc != MLT_OK ? rc : encode_bf16(tv, V_cache, 3, dims, strides, box);
+}
+
+int packed_run(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const PackedParams& p, int D, void* stream) {
+    return D == 64 ? packed_launch<64>(tq, tk, tv, p, static_cast<cudaStream_t>(stream))
+                   : packed_launch<128>(tq, tk, tv, p, static_cast<cudaStream_t>(stream));
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t mlt_mha_packed_workspace_bytes(int num_q, int num_seqs, int H, int H_kv, int D) {
+    if (num_q <= 0 || num_seqs <= 0 || H <= 0 || H_kv <= 0 || D <= 0 || H % H_kv != 0 || H / H_kv > kMhaBlock) return 0;
+    const PackedScratch x = packed_scratch(num_q, num_seqs, H / H_kv, H_kv, D);
+    return x.lists + kPackedMaxSlots * x.slot_bytes;
+}
+
+int mlt_mha_packed_fwd(const void* Q, const void* K, const void* V, const int32_t* cu_q, const int32_t* cu_k, void* O, float* LSE,
+                       int num_q, int num_k, int num_seqs, int H, int H_kv, int D, int causal, float scale, int64_t ldq, int64_t ldk,
+                       int64_t ldv, int64_t ldo, void* workspace, size_t workspace_bytes, void* stream) {
+    bool launch;
+    if (num_k < 0) return MLT_ERR_INVALID_ARG;
+    int rc = packed_check(Q, K, V, O, num_q, num_seqs, H, H_kv, D, scale, ldq, ldo, workspace, &launch);
+    if (rc != MLT_OK || !launch) return rc;
+    if (!cu_q || !cu_k || ldk < static_cast<int64_t>(H_kv) * D || ldv < static_cast<int64_t>(H_kv) * D) return MLT_ERR_INVALID_ARG;
+    if (ldk % 8 != 0 || ldv % 8 != 0) return MLT_ERR_ALIGNMENT;
+    const PackedScratch x = packed_scratch(num_q, num_seqs, H / H_kv, H_kv, D);
+    if (workspace_bytes < x.lists) return MLT_ERR_INVALID_ARG;
+    DeviceInfo dev;
+    rc = get_device(&dev);
+    if (rc != MLT_OK) return rc;
+    if (!dev.packed_ok) return MLT_ERR_UNSUPPORTED;
+    PackedParams p;
+    CUtensorMap tq, tk, tv;
+    rc = packed_fill(&p, &tq, Q, O, LSE, num_q, num_seqs, H, H_kv, D, scale, ldq, ldo, x, workspace,
+                     packed_slots(x, num_q, H_kv, workspace_bytes, dev.sm_count), dev.sm_count);
+    if (rc != MLT_OK) return rc;
+    const uint64_t dims[3] = {static_cast<uint64_t>(D), static_cast<uint64_t>(H_kv), static_cast<uint64_t>(std::max(1, num_k))};
+    const uint32_t box[3] = {64, 1, kMhaBlock};
+    const uint64_t k_strides[2] = {static_cast<uint64_t>(D) * 2, static_cast<uint64_t>(ldk) * 2};
+    const uint64_t v_strides[2] = {static_cast<uint64_t>(D) * 2, static_cast<uint64_t>(ldv) * 2};
+    rc = encode_bf16(&tk, K, 3, dims, k_strides, box);
+    if (rc == MLT_OK) rc = encode_bf16(&tv, V, 3, dims, v_strides, box);
+    if (rc != MLT_OK) return rc;
+    p.cu_q = cu_q;
+    p.cu_k = cu_k;
+    p.num_k = num_k;
+    p.causal = causal ? 1 : 0;
+    return packed_run(tq, tk, tv, p, D, stream);
+}
+
+int mlt_paged_attn_prefill(const void* Q, const void* K_cache, const void* V_cache, const int32_t* cu_tokens, const int32_t* context_lens,
+                           const int32_t* block_table, void* O, float* LSE, int num_tokens, int num_seqs, int H, int H_kv, int D,
+                           int block_size, int max_blocks_per_seq, int num_blocks, float scale, int64_t ldq, int64_t ldo, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+    bool launch;
+    if (max_blocks_per_seq < 0 || num_blocks < 0) return MLT_ERR_INVALID_ARG;
+    int rc = packed_check(Q, K_cache, V_cache, O, num_tokens, num_seqs, H, H_kv, D, scale, ldq, ldo, workspace, &launch);
+    if (rc != MLT_OK || !launch) return rc;
+    if (!cu_tokens || !context_lens || !block_table) return MLT_ERR_INVALID_ARG;
+    if (block_size != 8 && block_size != 16 && block_size != 32) return MLT_ERR_UNSUPPORTED;
+    if (static_cast<int64_t>(num_blocks) * H_kv > INT32_MAX) return MLT_ERR_UNSUPPORTED;
+    const PackedScratch x = packed_scratch(num_tokens, num_seqs, H / H_kv, H_kv, D);
+    if (workspace_bytes < x.lists) return MLT_ERR_INVALID_ARG;
+    DeviceInfo dev;
+    rc = get_device(&dev);
+    if (rc != MLT_OK) return rc;
+    if (!dev.packed_ok) return MLT_ERR_UNSUPPORTED;
+    PackedParams p;
+    CUtensorMap tq, tk, tv;
+    rc = packed_fill(&p, &tq, Q, O, LSE, num_tokens, num_seqs, H, H_kv, D, scale, ldq, ldo, x, workspace,
+                     packed_slots(x, num_tokens, H_kv, workspace_bytes, dev.sm_count), dev.sm_count);
+    if (rc == MLT_OK) rc = packed_cache_maps(&tk, &tv, K_cache, V_cache, num_blocks, H_kv, block_size, D);
+    if (rc != MLT_OK) return rc;
+    p.cu_q = cu_tokens;
+    p.context_lens = context_lens;
+    p.block_table = block_table;
+    p.block_size = block_size;
+    p.max_blocks = max_blocks_per_seq;
+    p.num_blocks = num_blocks;
+    p.causal = 1;
+    return packed_run(tq, tk, tv, p, D, stream);
 }
 
 }  // extern "C"

@@ -1,0 +1,60 @@
+"""The packed and paged attention entry points refuse what they cannot do before any CUDA call (no GPU needed)."""
+import pytest
+
+import __graft_entry__ as entry
+from paper_2503_14985_b200 import binding
+
+BIG = 1 << 40
+
+
+@pytest.fixture(scope="module", autouse=True)
+def lib():
+    entry.build()
+
+
+def packed(**kw):
+    a = dict(Q=16, K=16, V=16, cu_q=16, cu_k=16, O=16, LSE=0, num_q=10, num_k=10, num_seqs=2, H=8, H_kv=2, D=128, causal=1, scale=1.0, ldq=1024,
+             ldk=256, ldv=256, ldo=1024, workspace=256, workspace_bytes=BIG)
+    a.update(kw)
+    return binding.mha_packed_fwd_raw(**a)
+
+
+def prefill(**kw):
+    a = dict(Q=16, K_cache=16, V_cache=16, cu_tokens=16, context_lens=16, block_table=16, O=16, LSE=0, num_tokens=10, num_seqs=2, H=8, H_kv=2, D=128,
+             block_size=16, max_blocks=4, num_blocks=9, scale=1.0, ldq=1024, ldo=1024, workspace=256, workspace_bytes=BIG)
+    a.update(kw)
+    return binding.paged_attn_prefill_raw(**a)
+
+
+@pytest.mark.parametrize("call,tokens", [(packed, "num_q"), (prefill, "num_tokens")])
+def test_shared_refusals(call, tokens):
+    assert call(**{tokens: 0}) == 0 and call(num_seqs=0) == 0          # nothing to do
+    assert call(**{tokens: -1}) == 1 and call(num_seqs=-1) == 1
+    assert call(Q=0) == 1 and call(O=0) == 1 and call(workspace=0) == 1
+    assert call(H=9) == 1 and call(H_kv=0) == 1
+    assert call(scale=0.0) == 1 and call(scale=float("nan")) == 1 and call(scale=float("inf")) == 1
+    assert call(D=96, ldq=4096, ldo=4096) == 2
+    assert call(H=258, H_kv=2, ldq=258 * 128, ldo=258 * 128) == 2      # 129 query heads per KV head
+    assert call(ldq=1016) == 1 and call(ldo=1016) == 1
+    assert call(ldq=1028) == 3 and call(ldo=1028) == 3
+    assert call(Q=18) == 3 and call(O=24) == 3 and call(workspace=8) == 3
+    assert call(workspace_bytes=100) == 1                              # too little for the list of work items
+
+
+def test_packed_refusals():
+    assert packed(K=0) == 1 and packed(cu_q=0) == 1 and packed(cu_k=0) == 1 and packed(num_k=-1) == 1
+    assert packed(ldk=248) == 1 and packed(ldv=248) == 1 and packed(ldk=260) == 3
+
+
+def test_prefill_refusals():
+    assert prefill(K_cache=0) == 1 and prefill(context_lens=0) == 1 and prefill(block_table=0) == 1
+    assert prefill(block_size=12) == 2 and prefill(block_size=64) == 2
+    assert prefill(num_blocks=-1) == 1 and prefill(max_blocks=-1) == 1
+    assert prefill(num_blocks=2 ** 30, H_kv=2) == 2
+
+
+def test_workspace_size():
+    size = binding.mha_packed_workspace_bytes
+    assert size(0, 1, 8, 2, 128) == 0 and size(10, 1, 9, 2, 128) == 0
+    assert size(10, 1, 8, 2, 128) >= 320 * 40 * (128 * 4 + 8)
+    assert size(100000, 100, 32, 8, 128) >= 320 * 256 * (128 * 4 + 8)
