@@ -342,6 +342,31 @@ int mlt_paged_attn_prefill(const void* Q, const void* K_cache, const void* V_cac
                            int64_t ldq, int64_t ldo, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * mlt_paged_attn_decode for a batch whose sequences share long prefixes (one system prompt, one document, samples of one
+ * prompt).  Each prefix is read once for all sequences behind it, as a tensor-core product over their query rows; the tails are
+ * decoded one by one, and the two are joined in FP32.  The result is mlt_paged_attn_decode's on the same arguments.
+ *
+ *   prefix_lens  device, int32, [num_groups];  cu_groups  device, int32, [num_groups + 1], ascending: the sequences
+ *                cu_groups[g] .. cu_groups[g + 1] - 1 have the first prefix_lens[g] / block_size (whole blocks) entries of
+ *                their block tables in common; those of the group's first sequence are used.  Sequences in no group are
+ *                decoded by themselves.  Negative lengths count as 0, lengths beyond the table as the table's.
+ *   workspace    device scratch of mlt_paged_attn_shared_workspace_bytes bytes (MLT_ERR_INVALID_ARG with less); calls that overlap
+ *                on the GPU must not share it
+ * The rest as for mlt_paged_attn_decode, but a bad block-table entry inside a prefix counts as a block of zeros (and is
+ * reported).  seq_lens may be shorter than the prefix, or 0.  A group whose offsets descend or reach outside num_seqs is left
+ * out (its sequences are decoded by themselves) and reported (MLT_ERR_BAD_POSITION).  num_groups == 0: mlt_paged_attn_decode.
+ * MLT_ERR_UNSUPPORTED when num_seqs / (2 * (128 / (H / H_kv))) + num_groups exceeds 1024, or num_blocks * H_kv reaches 2^31.
+ */
+size_t mlt_paged_attn_shared_workspace_bytes(int num_seqs, int num_groups, int H, int H_kv, int D);
+int mlt_paged_attn_decode_shared(const void* Q, const void* K_cache, const void* V_cache,
+                                 const int32_t* block_table, const int32_t* seq_lens,
+                                 const int32_t* prefix_lens, const int32_t* cu_groups,
+                                 void* O, float* LSE,
+                                 int num_seqs, int num_groups, int H, int H_kv, int D,
+                                 int block_size, int max_blocks_per_seq, int num_blocks, float scale,
+                                 void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * The SM clock the last GEMM (which = 0) or attention (which = 1) launch on the current device really ran at, in
  * MHz: CTA 0 of those kernels notes the SM cycle counter and the nanosecond timer at its start and at its end.  (No
  * counterpart in the paper; a measurement aid: under tensor-core load this part runs well below the clock NVML

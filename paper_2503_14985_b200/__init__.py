@@ -10,4 +10,5 @@ from .binding import (MltError, debug_wait_timeout_selftest, gemm, gemm_ex_raw, 
                       paged_attn_workspace_bytes, status_string, version,
                       gemm_f8, gemm_f8_plan, gemm_f8_raw, kv_append, kv_append_f8, kv_append_f8_raw, kv_append_raw, paged_attn_decode_f8,
                       paged_attn_decode_f8_raw, paged_attn_f8_workspace_bytes, quantize_f8, quantize_f8_raw,
-                      mha_packed_fwd, mha_packed_fwd_raw, mha_packed_workspace_bytes, paged_attn_prefill, paged_attn_prefill_raw)
+                      mha_packed_fwd, mha_packed_fwd_raw, mha_packed_workspace_bytes, paged_attn_prefill, paged_attn_prefill_raw,
+                      paged_attn_decode_shared, paged_attn_decode_shared_raw, paged_attn_shared_workspace_bytes)

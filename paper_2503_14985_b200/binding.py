@@ -22,6 +22,7 @@ EXPORTS = ("mlt_gemm", "mlt_gemm_f16", "mlt_gemm_ex", "mlt_gemm_workspace_bytes"
            "mlt_paged_attn_workspace_bytes",
            "mlt_quantize_f8", "mlt_gemm_f8", "mlt_kv_append", "mlt_kv_append_f8", "mlt_paged_attn_decode_f8", "mlt_paged_attn_f8_workspace_bytes",
            "mlt_mha_packed_fwd", "mlt_mha_packed_workspace_bytes", "mlt_paged_attn_prefill",
+           "mlt_paged_attn_decode_shared", "mlt_paged_attn_shared_workspace_bytes",
            "mlt_last_device_error", "mlt_debug_wait_timeout_selftest", "mlt_debug_last_clock_mhz", "mlt_debug_gemm_plan", "mlt_debug_gemm_f8_plan", "mlt_status_string",
            "mlt_version")
 
@@ -86,6 +87,10 @@ def load() -> ctypes.CDLL:
         lib.mlt_mha_packed_fwd.restype = i32
         lib.mlt_paged_attn_prefill.argtypes = [p] * 8 + [i32] * 8 + [ctypes.c_float] + [i64] * 2 + [p, ctypes.c_size_t, p]
         lib.mlt_paged_attn_prefill.restype = i32
+        lib.mlt_paged_attn_shared_workspace_bytes.argtypes = [i32] * 5
+        lib.mlt_paged_attn_shared_workspace_bytes.restype = ctypes.c_size_t
+        lib.mlt_paged_attn_decode_shared.argtypes = [p] * 9 + [i32] * 8 + [ctypes.c_float, p, ctypes.c_size_t, p]
+        lib.mlt_paged_attn_decode_shared.restype = i32
         lib.mlt_last_device_error.argtypes = [p]
         lib.mlt_last_device_error.restype = i32
         lib.mlt_status_string.argtypes = [i32]
@@ -220,6 +225,18 @@ def paged_attn_prefill_raw(Q: int, K_cache: int, V_cache: int, cu_tokens: int, c
     """mlt_paged_attn_prefill with raw device addresses; returns the status code."""
     return load().mlt_paged_attn_prefill(Q, K_cache, V_cache, cu_tokens, context_lens, block_table, O, LSE, num_tokens, num_seqs, H, H_kv, D,
                                          block_size, max_blocks, num_blocks, scale, ldq, ldo, workspace, workspace_bytes, stream)
+
+
+def paged_attn_shared_workspace_bytes(num_seqs: int, num_groups: int, H: int, H_kv: int, D: int) -> int:
+    return int(load().mlt_paged_attn_shared_workspace_bytes(num_seqs, num_groups, H, H_kv, D))
+
+
+def paged_attn_decode_shared_raw(Q: int, K_cache: int, V_cache: int, block_table: int, seq_lens: int, prefix_lens: int, cu_groups: int, O: int,
+                                 LSE: int, num_seqs: int, num_groups: int, H: int, H_kv: int, D: int, block_size: int, max_blocks: int,
+                                 num_blocks: int, scale: float, workspace: int, workspace_bytes: int, stream: int = 0) -> int:
+    """mlt_paged_attn_decode_shared with raw device addresses; returns the status code."""
+    return load().mlt_paged_attn_decode_shared(Q, K_cache, V_cache, block_table, seq_lens, prefix_lens, cu_groups, O, LSE, num_seqs, num_groups,
+                                               H, H_kv, D, block_size, max_blocks, num_blocks, scale, workspace, workspace_bytes, stream)
 
 
 def last_device_error():
@@ -711,5 +728,44 @@ def paged_attn_prefill(Q, K_cache, V_cache, cu_tokens, context_lens, block_table
     _call("mlt_paged_attn_prefill", load().mlt_paged_attn_prefill, held,
           (Q.data_ptr(), K_cache.data_ptr(), V_cache.data_ptr(), cu_tokens.data_ptr(), context_lens.data_ptr(), block_table.data_ptr(),
            O.data_ptr(), lse, T, S, H, H_kv, D, block_size, block_table.shape[1], num_blocks, float(scale), _rows(Q, H, D), ldo,
+           workspace.data_ptr(), workspace.numel() * workspace.element_size()), stream)
+    return O, LSE
+
+
+def paged_attn_decode_shared(Q, K_cache, V_cache, block_table, seq_lens, prefix_lens, cu_groups, *, scale: float, workspace=None, O=None,
+                             LSE=None, return_lse: bool = True, stream=None):
+    """paged_attn_decode for a batch whose sequences share prefixes, which are read once for all sequences behind them.
+
+    Arguments as there, and prefix_lens [groups], cu_groups [groups + 1] int32: the sequences cu_groups[g] .. cu_groups[g + 1] - 1 have
+    the first prefix_lens[g] // block_size entries of their block tables in common.  `workspace`: a contiguous
+    uint8 CUDA tensor of paged_attn_shared_workspace_bytes (a new one without).
+    Returns (O [S, H, D] bfloat16, LSE [S, H] float32 or None), those of paged_attn_decode.
+    """
+    import torch
+    if Q.dtype != torch.bfloat16 or not Q.is_contiguous() or Q.dim() != 3:
+        raise TypeError("Q must be a contiguous [S, H, D] bfloat16 tensor")
+    for t in (K_cache, V_cache):
+        if t.dtype != torch.bfloat16 or not t.is_contiguous() or t.dim() != 4:
+            raise TypeError("the caches must be contiguous 4-D bfloat16 tensors")
+    S, H, D = Q.shape
+    _vectors(block_table, seq_lens, prefix_lens, cu_groups)
+    num_blocks, H_kv, block_size, _ = K_cache.shape
+    if V_cache.shape != K_cache.shape or K_cache.shape[3] != D:
+        raise ValueError("shape mismatch")
+    groups = prefix_lens.numel()
+    if cu_groups.numel() != groups + 1 or seq_lens.numel() != S or block_table.dim() != 2 or block_table.shape[0] != S:
+        raise ValueError("cu_groups must be [groups + 1], prefix_lens [groups], seq_lens [sequences], block_table [sequences, blocks]")
+    O, _, LSE = _out_rows(Q, O, LSE, return_lse, stream)
+    if not O.is_contiguous():
+        raise ValueError("O must be contiguous")
+    workspace = _scratch(Q, workspace, paged_attn_shared_workspace_bytes(S, groups, H, H_kv, D), stream)
+    held = [Q, K_cache, V_cache, block_table, seq_lens, prefix_lens, cu_groups, O, workspace]
+    lse = 0
+    if LSE is not None:
+        held.append(LSE)
+        lse = LSE.data_ptr()
+    _call("mlt_paged_attn_decode_shared", load().mlt_paged_attn_decode_shared, held,
+          (Q.data_ptr(), K_cache.data_ptr(), V_cache.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(), prefix_lens.data_ptr(),
+           cu_groups.data_ptr(), O.data_ptr(), lse, S, groups, H, H_kv, D, block_size, block_table.shape[1], num_blocks, float(scale),
            workspace.data_ptr(), workspace.numel() * workspace.element_size()), stream)
     return O, LSE

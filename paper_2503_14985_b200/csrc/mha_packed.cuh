@@ -66,6 +66,11 @@ struct PackedParams {
     float2* part_ml; // [slots][rows] {m in log2 units, l}
     int max_tiles, max_entries, slots, slot_rows;
     int sm_count;
+    // shared prefix: the sequences' own tails, which the decode kernels of paged.cuh work on
+    PagedParams tail;  // (its seq_lens and table_skip are written by the plan kernel)
+    int* tail_lens;    // = tail.seq_lens
+    int* tail_skip;    // = tail.table_skip
+    int* tail_parts;   // [T, H_kv] partial results of a tail
 };
 
 __host__ __device__ __forceinline__ int packed_blocks(int keys) { return (keys + kMhaBlock - 1) / kMhaBlock; }
@@ -151,6 +156,61 @@ __device__ __forceinline__ int packed_scan(int v, int* red, int& total) {
     const int before = warp ? __shfl_sync(0xffffffffu, r, warp - 1) : 0;
     __syncthreads();
     return v + before;
+}
+
+// The group that sequence s is in, or -1; and the sequence's tokens behind the group's prefix.
+__device__ __forceinline__ int packed_group(const PackedParams& p, int s, int& tail) {
+    int lo = 0, hi = p.S;  // the last group that begins at or before s
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (p.cu_q[mid] <= s) lo = mid; else hi = mid;
+    }
+    const int4 q = p.seqs[lo];
+    const int group = s >= q.x && s - q.x < q.y ? lo : -1;
+    const long long most = static_cast<long long>(p.max_blocks) * p.block_size;
+    const int len = static_cast<int>(max(0ll, min(static_cast<long long>(p.seq_lens[s]), most)));
+    tail = max(0, len - (group >= 0 ? q.z : 0));
+    return group;
+}
+
+// The tails behind the prefixes, and how many partial results the decode kernel makes of each (one CTA).
+__device__ __forceinline__ void packed_plan_tails(const PackedParams& p, int* red) {
+    const int tid = threadIdx.x;
+    const int per = (p.T + kPackedPlanThreads - 1) / kPackedPlanThreads;
+    const int lo = min(p.T, tid * per), hi = min(p.T, lo + per);
+    int chunks = 0, most = 0;
+    for (int s = lo; s < hi; ++s) {
+        int tail;
+        const int group = packed_group(p, s, tail);
+        p.tail_lens[s] = tail;
+        p.tail_skip[s] = group >= 0 ? p.seqs[group].z / p.block_size : 0;
+        const int n = (tail + kPagedChunkTokens - 1) / kPagedChunkTokens;
+        chunks += n;
+        most = max(most, n);
+    }
+    int total;
+    int before = packed_scan(chunks, red, total) - chunks;
+#pragma unroll
+    for (int w = 16; w > 0; w >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, w));
+    if ((tid & 31) == 0) red[tid >> 5] = most;
+    __syncthreads();
+    for (int w = 0; w < 32; ++w) most = max(most, red[w]);
+    __syncthreads();
+    const int quota = paged_quota(static_cast<long long>(total) * p.H_kv, most, max(1, p.tail.balanced_ctas));
+    for (int s = lo; s < hi; ++s) {
+        const int tail = p.tail_lens[s];
+        if (p.tail.balanced) {  // as in paged_decode_mma_kernel: pieces of `quota` chunks across all rows
+            const int n = (tail + kPagedChunkTokens - 1) / kPagedChunkTokens;
+            for (int h = 0; h < p.H_kv; ++h) {
+                const long long start = static_cast<long long>(before) * p.H_kv + static_cast<long long>(h) * n;
+                p.tail_parts[static_cast<int64_t>(s) * p.H_kv + h] = n > 0 ? static_cast<int>((start + n - 1) / quota - start / quota + 1) : 0;
+            }
+            before += n;
+        } else {
+            const int nblk = (tail + p.block_size - 1) / p.block_size, share = paged_split_blocks(p.tail, nblk);
+            for (int h = 0; h < p.H_kv; ++h) p.tail_parts[static_cast<int64_t>(s) * p.H_kv + h] = (nblk + share - 1) / share;
+        }
+    }
 }
 
 // One CTA.  Sequences -> tile pairs -> work items.
@@ -277,6 +337,7 @@ __global__ void __launch_bounds__(kPackedPlanThreads) mha_packed_plan_kernel(con
         }
         total = tiles;
     }
+    if (p.prefix_lens) packed_plan_tails(p, red);
     if (tid == 0) {
         p.hdr->num_items = total * p.H_kv;
         p.hdr->counter = 0;
@@ -929,7 +990,7 @@ mha_packed_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
     }
 }
 
-// Joins the parts of cut key ranges: one warp per (token, head).
+// Joins the parts of cut key ranges, and of tails behind a shared prefix: one warp per (token, head).
 constexpr int kPackedJoinWarps = 8;
 template <int D>
 __global__ void __launch_bounds__(kPackedJoinWarps * 32) mha_packed_join_kernel(const PackedParams p) {
@@ -949,31 +1010,41 @@ __global__ void __launch_bounds__(kPackedJoinWarps * 32) mha_packed_join_kernel(
     }
     const int4 q = p.seqs[lo];
     const int i = tok - q.x;
-    if (i < 0 || i >= q.y) return;  // a token of no sequence
-    const int W2 = 2 * p.W, pair = i / W2, first = pair * W2, t = (i - first) / p.W;
-    const int n = min(W2, q.y - first);
-    if (packed_tile_blocks(q.y, q.z, p.causal, first, n) <= chunk) return;  // not cut: written by its item
-    const int blocks = packed_tile_blocks(q.y, q.z, p.causal, first + t * p.W, min(p.W, n - t * p.W));
-    const int parts = (blocks + chunk - 1) / chunk;
-    const int r = t * kMhaBlock + (i - first - t * p.W) * p.G + h % p.G;
-    const int64_t slot0 = static_cast<int64_t>(p.tile_first[q.w + pair]) * p.H_kv + h / p.G;
-    auto part = [&](int k) { return (slot0 + static_cast<int64_t>(k) * p.H_kv) * p.slot_rows + r; };
+    int parts = 0;
+    int64_t part0 = 0;
+    if (i >= 0 && i < q.y) {
+        const int W2 = 2 * p.W, pair = i / W2, first = pair * W2, t = (i - first) / p.W;
+        const int n = min(W2, q.y - first);
+        // a range that is not cut was written by its item
+        if (!p.prefix_lens && packed_tile_blocks(q.y, q.z, p.causal, first, n) <= chunk) return;
+        const int blocks = packed_tile_blocks(q.y, q.z, p.causal, first + t * p.W, min(p.W, n - t * p.W));
+        parts = (blocks + chunk - 1) / chunk;
+        const int r = t * kMhaBlock + (i - first - t * p.W) * p.G + h % p.G;
+        part0 = (static_cast<int64_t>(p.tile_first[q.w + pair]) * p.H_kv + h / p.G) * p.slot_rows + r;
+    } else if (!p.prefix_lens) {
+        return;  // a token of no sequence
+    }
+    const int64_t step = static_cast<int64_t>(p.H_kv) * p.slot_rows;
+    const int tails = p.prefix_lens ? p.tail_parts[static_cast<int64_t>(tok) * p.H_kv + h / p.G] : 0;
+    const int all = parts + tails;
+    const int64_t tail0 = row * p.tail.splits;
+    auto stat = [&](int k) { return k < parts ? p.part_ml[part0 + k * step] : p.tail.part_ml[tail0 + k - parts]; };
     float m = -INFINITY;
-    for (int k = lane; k < parts; k += 32) m = fmaxf(m, p.part_ml[part(k)].x);
+    for (int k = lane; k < all; k += 32) m = fmaxf(m, stat(k).x);
 #pragma unroll
     for (int w = 16; w > 0; w >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, w));
     float l = 0.0f, o[V] = {};
-    for (int k0 = 0; k0 < parts; k0 += 32) {
+    for (int k0 = 0; k0 < all; k0 += 32) {
         float weight = 0.0f;
-        if (k0 + lane < parts) {
-            const float2 ml = p.part_ml[part(k0 + lane)];
+        if (k0 + lane < all) {
+            const float2 ml = stat(k0 + lane);
             weight = ml.x == -INFINITY ? 0.0f : fast_exp2(ml.x - m);
             l += weight * ml.y;
         }
-        for (int k = 0; k < 32 && k0 + k < parts; ++k) {
+        for (int k = 0; k < 32 && k0 + k < all; ++k) {
             const float w = __shfl_sync(0xffffffffu, weight, k);
-            if (w == 0.0f) continue;
-            const float* src = p.part_o + part(k0 + k) * D + lane * V;
+            if (w == 0.0f) continue;  // (a part without a visible key)
+            const float* src = (k0 + k < parts ? p.part_o + (part0 + (k0 + k) * step) * D : p.tail.part_o + (tail0 + k0 + k - parts) * D) + lane * V;
 #pragma unroll
             for (int e = 0; e < V; ++e) o[e] = fmaf(src[e], w, o[e]);
         }
@@ -995,15 +1066,17 @@ struct PackedScratch {
     size_t seqs, entries, tile_first, part_ml, part_o;  // byte offsets
     size_t lists;                                       // bytes without partial results
     size_t slot_bytes;
+    int64_t slots;                                      // parts that scratch is sized for
     int max_tiles, max_entries, slot_rows, W;
 };
-inline PackedScratch packed_scratch(int64_t T, int64_t S, int G, int H_kv, int D) {
+inline PackedScratch packed_scratch(int64_t T, int64_t S, int G, int H_kv, int D, bool prefix = false) {
     PackedScratch x;
     auto up = [](size_t v) { return (v + 255) & ~size_t(255); };
     x.W = kMhaBlock / G;
     const int64_t tiles = T / (2 * x.W) + S;
     x.max_tiles = static_cast<int>(tiles);
-    x.max_entries = static_cast<int>(std::max<int64_t>(tiles, kPackedMaxSlots / H_kv));
+    x.slots = prefix ? std::max<int64_t>(kPackedMaxSlots, tiles * H_kv) : kPackedMaxSlots;  // (a prefix's results all go to the join)
+    x.max_entries = static_cast<int>(std::max<int64_t>(tiles, x.slots / H_kv));
     x.slot_rows = static_cast<int>(T * G <= kMhaBlock ? T * G : 2 * kMhaBlock);
     x.seqs = 256;
     x.entries = up(x.seqs + static_cast<size_t>(S) * 16);
@@ -1038,10 +1111,14 @@ inline bool packed_launch_one(void (*kernel)(Params...), int64_t grid, int threa
     return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...) == cudaSuccess;
 }
 
-// plan, attention, and (where key ranges may be cut) the join
+// plan, (behind a shared prefix: the tails,) attention, and (where key ranges may be cut) the join
 template <int D>
 int packed_launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const PackedParams& p, cudaStream_t st) {
     if (!packed_launch_one(mha_packed_plan_kernel, 1, kPackedPlanThreads, 0, st, p)) return 4;
+    if (p.prefix_lens) {
+        const int rc = paged_launch_g<D>(p.tail, st);
+        if (rc != 0) return rc;
+    }
     const int64_t most = static_cast<int64_t>(p.slots > 0 ? p.max_entries : p.max_tiles) * p.H_kv;
     if (!packed_launch_one(mha_packed_kernel<D>, std::min<int64_t>(p.sm_count, most), kMhaThreads, PackedSmem<D>::kTotal, st, tq, tk, tv, p)) return 4;
     if (p.slots > 0) {

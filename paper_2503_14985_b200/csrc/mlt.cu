@@ -768,6 +768,7 @@ int paged_prepare(const void* Q, const void* K_cache, const void* V_cache, const
     p->head_groups = 1;
     p->balanced = 0;
     p->balanced_ctas = 0;
+    p->table_skip = nullptr;
     *launch = true;
     return MLT_OK;
 }
@@ -1255,7 +1256,7 @@ int packed_fill(PackedParams* p, CUtensorMap* tq, const void* Q, void* O, float*
 // Parts of cut key ranges that pay: none when there are enough items for two rounds of the SMs as it is.
 int64_t packed_slots(const PackedScratch& x, int64_t T, int H_kv, size_t workspace_bytes, int sm_count) {
     if ((T + 2 * x.W - 1) / (2 * x.W) * H_kv >= 2ll * sm_count) return 0;
-    return std::min<int64_t>(kPackedMaxSlots, static_cast<int64_t>((workspace_bytes - x.lists) / x.slot_bytes));
+    return std::min<int64_t>(x.slots, static_cast<int64_t>((workspace_bytes - x.lists) / x.slot_bytes));
 }
 
 int packed_cache_maps(CUtensorMap* tk, CUtensorMap* tv, const void* K_cache, const void* V_cache, int num_blocks, int H_kv, int block_size, int D) {
@@ -1279,7 +1280,7 @@ extern "C" {
 size_t mlt_mha_packed_workspace_bytes(int num_q, int num_seqs, int H, int H_kv, int D) {
     if (num_q <= 0 || num_seqs <= 0 || H <= 0 || H_kv <= 0 || D <= 0 || H % H_kv != 0 || H / H_kv > kMhaBlock) return 0;
     const PackedScratch x = packed_scratch(num_q, num_seqs, H / H_kv, H_kv, D);
-    return x.lists + kPackedMaxSlots * x.slot_bytes;
+    return x.lists + x.slots * x.slot_bytes;
 }
 
 int mlt_mha_packed_fwd(const void* Q, const void* K, const void* V, const int32_t* cu_q, const int32_t* cu_k, void* O, float* LSE,
@@ -1346,6 +1347,91 @@ int mlt_paged_attn_prefill(const void* Q, const void* K_cache, const void* V_cac
     p.max_blocks = max_blocks_per_seq;
     p.num_blocks = num_blocks;
     p.causal = 1;
+    return packed_run(tq, tk, tv, p, D, stream);
+}
+
+}  // extern "C"
+
+namespace {
+// Scratch of decode behind a shared prefix: the prefix's lists and parts, then the tails' lengths, table offsets, numbers of parts
+// and the parts themselves.
+struct SharedScratch {
+    PackedScratch x;
+    size_t tail_lens, tail_skip, tail_parts, tail_part_o, total;
+};
+SharedScratch shared_scratch(int64_t S, int64_t groups, int H, int H_kv, int D) {
+    SharedScratch w;
+    auto up = [](size_t v) { return (v + 255) & ~size_t(255); };
+    w.x = packed_scratch(S, groups, H / H_kv, H_kv, D, true);
+    w.tail_lens = up(w.x.lists + static_cast<size_t>(w.x.slots) * w.x.slot_bytes);
+    w.tail_skip = up(w.tail_lens + static_cast<size_t>(S) * 4);
+    w.tail_parts = up(w.tail_skip + static_cast<size_t>(S) * 4);
+    w.tail_part_o = up(w.tail_parts + static_cast<size_t>(S) * H_kv * 4);
+    w.total = w.tail_part_o + paged_workspace_bytes(static_cast<int>(S), H, D, kPagedMaxSplits);
+    return w;
+}
+}  // namespace
+
+extern "C" {
+
+size_t mlt_paged_attn_shared_workspace_bytes(int num_seqs, int num_groups, int H, int H_kv, int D) {
+    if (num_seqs <= 0 || num_groups < 0 || H <= 0 || H_kv <= 0 || D <= 0 || H % H_kv != 0 || H / H_kv > kMhaBlock) return 0;
+    if (num_groups == 0) return mlt_paged_attn_workspace_bytes(num_seqs, H, D);
+    return shared_scratch(num_seqs, num_groups, H, H_kv, D).total;
+}
+
+int mlt_paged_attn_decode_shared(const void* Q, const void* K_cache, const void* V_cache, const int32_t* block_table, const int32_t* seq_lens,
+                                 const int32_t* prefix_lens, const int32_t* cu_groups, void* O, float* LSE, int num_seqs, int num_groups,
+                                 int H, int H_kv, int D, int block_size, int max_blocks_per_seq, int num_blocks, float scale,
+                                 void* workspace, size_t workspace_bytes, void* stream) {
+    if (num_groups < 0) return MLT_ERR_INVALID_ARG;
+    if (num_groups == 0)
+        return mlt_paged_attn_decode(Q, K_cache, V_cache, block_table, seq_lens, O, LSE, num_seqs, H, H_kv, D, block_size, max_blocks_per_seq,
+                                     num_blocks, scale, workspace, workspace_bytes, stream);
+    PackedParams p;
+    PagedParams tail;
+    DeviceInfo dev;
+    bool launch = false;
+    if (num_seqs > 0 && H > 0) {
+        if (!prefix_lens || !cu_groups || !workspace) return MLT_ERR_INVALID_ARG;
+        if (!aligned16(workspace)) return MLT_ERR_ALIGNMENT;
+        if (static_cast<int64_t>(num_blocks) * H_kv > INT32_MAX) return MLT_ERR_UNSUPPORTED;
+        // (tile pairs of the groups: the plan keeps them in shared memory)
+        if (H_kv > 0 && H % H_kv == 0 && H / H_kv <= kMhaBlock) {
+            if (num_seqs / (2 * (kMhaBlock / (H / H_kv))) + static_cast<int64_t>(num_groups) > kPackedMaxSplitTiles) return MLT_ERR_UNSUPPORTED;
+            if (D > 0 && workspace_bytes < shared_scratch(num_seqs, num_groups, H, H_kv, D).total) return MLT_ERR_INVALID_ARG;
+        }
+    }
+    int rc = paged_prepare(Q, K_cache, V_cache, block_table, seq_lens, O, LSE, num_seqs, H, H_kv, D, block_size, max_blocks_per_seq, num_blocks,
+                           scale, &tail, &dev, &launch);
+    if (rc != MLT_OK || !launch) return rc;
+    if (!dev.packed_ok) return MLT_ERR_UNSUPPORTED;
+    const SharedScratch w = shared_scratch(num_seqs, num_groups, H, H_kv, D);
+    CUtensorMap tq, tk, tv;
+    const int64_t ld = static_cast<int64_t>(H) * D;
+    rc = packed_fill(&p, &tq, Q, O, LSE, num_seqs, num_groups, H, H_kv, D, scale, ld, ld, w.x, workspace, w.x.slots, dev.sm_count);
+    if (rc == MLT_OK) rc = packed_cache_maps(&tk, &tv, K_cache, V_cache, num_blocks, H_kv, block_size, D);
+    if (rc != MLT_OK) return rc;
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    p.cu_q = cu_groups;
+    p.prefix_lens = prefix_lens;
+    p.seq_lens = seq_lens;
+    p.block_table = block_table;
+    p.block_size = block_size;
+    p.max_blocks = max_blocks_per_seq;
+    p.num_blocks = num_blocks;
+    p.causal = 0;
+    p.tail_lens = reinterpret_cast<int*>(ws + w.tail_lens);
+    p.tail_skip = reinterpret_cast<int*>(ws + w.tail_skip);
+    p.tail_parts = reinterpret_cast<int*>(ws + w.tail_parts);
+    tail.seq_lens = p.tail_lens;
+    tail.table_skip = p.tail_skip;
+    tail.part_o = reinterpret_cast<float*>(ws + w.tail_part_o);
+    tail.splits = kPagedMaxSplits;
+    tail.blocks_per_split = std::max(2, 128 / block_size);  // at least 128 tokens per CTA
+    if (paged_use_balanced(tail, dev.sm_count)) paged_set_balanced(&tail, dev.sm_count);
+    tail.part_ml = reinterpret_cast<float2*>(tail.part_o + static_cast<size_t>(num_seqs) * H * tail.splits * D);
+    p.tail = tail;
     return packed_run(tq, tk, tv, p, D, stream);
 }
 

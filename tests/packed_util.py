@@ -73,7 +73,8 @@ def cu(lens):
 
 
 def paged(lens, Hk, D, bs, seed, width=None, share=None):
-    """A cache whose blocks lie scattered, NaN wherever no sequence looks; share: (rows, blocks) whose first blocks are the same."""
+    """A cache whose blocks lie scattered, NaN wherever no sequence looks; share: (rows, blocks) whose first blocks are the
+    same (one of them must have that many)."""
     rng = np.random.RandomState(seed)
     lens = np.asarray(lens)
     per = -(-lens // bs)
@@ -83,10 +84,9 @@ def paged(lens, Hk, D, bs, seed, width=None, share=None):
     for s in range(len(lens)):
         table[s, : per[s]] = order[at: at + per[s]]
         at += per[s]
-    for rows, held in share or []:
-        for s in rows[1:]:
-            n = min(held, per[s], per[rows[0]])
-            table[s, :n] = table[rows[0], :n]
+    for rows, held in share or []:  # (also for rows that do not reach that far themselves)
+        longest = max(rows, key=lambda s: lens[s])
+        table[rows, :held] = table[longest, :held]
     used = np.zeros((blocks, bs), bool)
     for s in range(len(lens)):
         for i in range(per[s]):

@@ -58,3 +58,22 @@ def test_workspace_size():
     assert size(0, 1, 8, 2, 128) == 0 and size(10, 1, 9, 2, 128) == 0
     assert size(10, 1, 8, 2, 128) >= 320 * 40 * (128 * 4 + 8)
     assert size(100000, 100, 32, 8, 128) >= 320 * 256 * (128 * 4 + 8)
+
+
+def test_shared_refusals():
+    def call(**kw):
+        a = dict(Q=16, K_cache=16, V_cache=16, block_table=16, seq_lens=16, prefix_lens=16, cu_groups=16, O=16, LSE=0, num_seqs=10, num_groups=2, H=8,
+                 H_kv=2, D=128, block_size=16, max_blocks=4, num_blocks=9, scale=1.0, workspace=256, workspace_bytes=BIG)
+        a.update(kw)
+        return binding.paged_attn_decode_shared_raw(**a)
+
+    assert call(num_seqs=0) == 0 and call(num_seqs=0, workspace=0) == 0
+    assert call(num_seqs=0, num_groups=0) == 0
+    assert call(num_groups=-1) == 1 and call(prefix_lens=0) == 1 and call(cu_groups=0) == 1 and call(workspace=0) == 1
+    assert call(workspace=8) == 3 and call(workspace_bytes=10000) == 1
+    assert call(Q=0) == 1 and call(seq_lens=0) == 1 and call(H=7) == 1 and call(scale=-1.0) == 1
+    assert call(H=24, H_kv=2) == 2 and call(D=96) == 2 and call(block_size=64) == 2
+    assert call(num_seqs=60000, num_groups=200) == 2 and call(num_blocks=2 ** 30) == 2
+    size = binding.paged_attn_shared_workspace_bytes
+    assert size(0, 1, 8, 2, 128) == 0 and size(8, 0, 8, 2, 128) == binding.paged_attn_workspace_bytes(8, 8, 128)
+    assert size(8, 1, 8, 2, 128) > binding.paged_attn_workspace_bytes(8, 8, 128)
