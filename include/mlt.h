@@ -367,6 +367,26 @@ int mlt_paged_attn_decode_shared(const void* Q, const void* K_cache, const void*
                                  void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * C[i][n] = sum over groups j of K: scales[n][j] * sum over k in j of X[i][k] * (q[n][k] - zeros[n][j]), for few rows: the
+ * projections of next-token steps, which are bound by the weights' bytes.
+ *
+ *   X       device, BF16, M x K row-major, pitch ldx in elements, a multiple of 8; 16-byte aligned.  Its values must be finite
+ *           (an infinity gives NaN).
+ *   W       device, 4-bit unsigned, N x K, two to a byte, the even k in the lower half; pitch ldw in bytes, a multiple of 16;
+ *           16-byte aligned
+ *   scales  device, BF16, N x (K / group), pitch lds in elements
+ *   zeros   device, uint8, N x (K / group), 0 .. 15, pitch ldz in bytes, or NULL: 8 everywhere
+ *   C       device, BF16 out, M x N, pitch ldc in elements
+ *   group   elements of K per scale: 32, 64 or 128;  K a multiple of it
+ * Products are summed in FP32 in a fixed order, weighted, and summed over the groups in FP32; one rounding to nearest even.  Weights are
+ * never rounded.  Any M: every 16 rows (fewer for very long K) read the weights once more, so that prompts are better off with
+ * mlt_gemm_f8 or mlt_gemm.  M == 0 or N == 0: MLT_OK, nothing launched; K == 0: C is zero-filled.  Needs no scratch.
+ */
+int mlt_gemm_w4(const void* X, const void* W, const void* scales, const void* zeros, void* C,
+                int64_t M, int64_t N, int64_t K, int group,
+                int64_t ldx, int64_t ldw, int64_t lds, int64_t ldz, int64_t ldc, void* stream);
+
+/*
  * The SM clock the last GEMM (which = 0) or attention (which = 1) launch on the current device really ran at, in
  * MHz: CTA 0 of those kernels notes the SM cycle counter and the nanosecond timer at its start and at its end.  (No
  * counterpart in the paper; a measurement aid: under tensor-core load this part runs well below the clock NVML

@@ -11,4 +11,4 @@ from .binding import (MltError, debug_wait_timeout_selftest, gemm, gemm_ex_raw, 
                       gemm_f8, gemm_f8_plan, gemm_f8_raw, kv_append, kv_append_f8, kv_append_f8_raw, kv_append_raw, paged_attn_decode_f8,
                       paged_attn_decode_f8_raw, paged_attn_f8_workspace_bytes, quantize_f8, quantize_f8_raw,
                       mha_packed_fwd, mha_packed_fwd_raw, mha_packed_workspace_bytes, paged_attn_prefill, paged_attn_prefill_raw,
-                      paged_attn_decode_shared, paged_attn_decode_shared_raw, paged_attn_shared_workspace_bytes)
+                      paged_attn_decode_shared, paged_attn_decode_shared_raw, paged_attn_shared_workspace_bytes, gemm_w4, gemm_w4_raw)

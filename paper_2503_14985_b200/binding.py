@@ -22,7 +22,7 @@ EXPORTS = ("mlt_gemm", "mlt_gemm_f16", "mlt_gemm_ex", "mlt_gemm_workspace_bytes"
            "mlt_paged_attn_workspace_bytes",
            "mlt_quantize_f8", "mlt_gemm_f8", "mlt_kv_append", "mlt_kv_append_f8", "mlt_paged_attn_decode_f8", "mlt_paged_attn_f8_workspace_bytes",
            "mlt_mha_packed_fwd", "mlt_mha_packed_workspace_bytes", "mlt_paged_attn_prefill",
-           "mlt_paged_attn_decode_shared", "mlt_paged_attn_shared_workspace_bytes",
+           "mlt_paged_attn_decode_shared", "mlt_paged_attn_shared_workspace_bytes", "mlt_gemm_w4",
            "mlt_last_device_error", "mlt_debug_wait_timeout_selftest", "mlt_debug_last_clock_mhz", "mlt_debug_gemm_plan", "mlt_debug_gemm_f8_plan", "mlt_status_string",
            "mlt_version")
 
@@ -91,6 +91,8 @@ def load() -> ctypes.CDLL:
         lib.mlt_paged_attn_shared_workspace_bytes.restype = ctypes.c_size_t
         lib.mlt_paged_attn_decode_shared.argtypes = [p] * 9 + [i32] * 8 + [ctypes.c_float, p, ctypes.c_size_t, p]
         lib.mlt_paged_attn_decode_shared.restype = i32
+        lib.mlt_gemm_w4.argtypes = [p] * 5 + [i64] * 3 + [i32] + [i64] * 5 + [p]
+        lib.mlt_gemm_w4.restype = i32
         lib.mlt_last_device_error.argtypes = [p]
         lib.mlt_last_device_error.restype = i32
         lib.mlt_status_string.argtypes = [i32]
@@ -237,6 +239,12 @@ def paged_attn_decode_shared_raw(Q: int, K_cache: int, V_cache: int, block_table
     """mlt_paged_attn_decode_shared with raw device addresses; returns the status code."""
     return load().mlt_paged_attn_decode_shared(Q, K_cache, V_cache, block_table, seq_lens, prefix_lens, cu_groups, O, LSE, num_seqs, num_groups,
                                                H, H_kv, D, block_size, max_blocks, num_blocks, scale, workspace, workspace_bytes, stream)
+
+
+def gemm_w4_raw(X: int, W: int, scales: int, zeros: int, C: int, M: int, N: int, K: int, group: int, ldx: int, ldw: int, lds: int, ldz: int,
+                ldc: int, stream: int = 0) -> int:
+    """mlt_gemm_w4 with raw device addresses; returns the status code."""
+    return load().mlt_gemm_w4(X, W, scales, zeros, C, M, N, K, group, ldx, ldw, lds, ldz, ldc, stream)
 
 
 def last_device_error():
@@ -769,3 +777,32 @@ def paged_attn_decode_shared(Q, K_cache, V_cache, block_table, seq_lens, prefix_
            cu_groups.data_ptr(), O.data_ptr(), lse, S, groups, H, H_kv, D, block_size, block_table.shape[1], num_blocks, float(scale),
            workspace.data_ptr(), workspace.numel() * workspace.element_size()), stream)
     return O, LSE
+
+
+def gemm_w4(X, W, scales, zeros=None, C=None, *, stream=None):
+    """C = X @ dequantised(W).T in bfloat16 for few rows X [M, K] bfloat16 and 4-bit weights.
+
+    W [N, K / 2] uint8, two weights to a byte, the even k in the lower half; scales [N, K / group] bfloat16; zeros [N, K / group]
+    uint8 (None: 8): weight (n, k) is scales[n, k / group] * (W(n, k) - zeros[n, k / group]).  group, 32, 64 or 128, follows from
+    the shapes.  Row pitches come from the tensors' strides (X: a multiple of 8 elements, W: of 16 bytes).
+    """
+    import torch
+    if X.dtype != torch.bfloat16 or scales.dtype != torch.bfloat16 or W.dtype != torch.uint8 or (zeros is not None and zeros.dtype != torch.uint8):
+        raise TypeError("X and scales must be bfloat16, W and zeros uint8")
+    (M, K), (N, half), (Ns, groups) = X.shape, W.shape, scales.shape
+    if 2 * half != K or Ns != N or (K and (groups == 0 or K % groups)) or (zeros is not None and zeros.shape != scales.shape):
+        raise ValueError("shape mismatch")
+    group = K // groups if groups else 128
+    if C is None:
+        C = _new(X, (M, N), torch.bfloat16, stream)
+    elif C.dtype != torch.bfloat16 or tuple(C.shape) != (M, N):
+        raise ValueError("C must be bfloat16 [M, N]")
+    held = [X, W, scales, C]
+    z = ldz = 0
+    if zeros is not None:
+        held.append(zeros)
+        z, ldz = zeros.data_ptr(), _pitch(zeros, groups)
+    _call("mlt_gemm_w4", load().mlt_gemm_w4, held,
+          (X.data_ptr(), W.data_ptr(), scales.data_ptr(), z, C.data_ptr(), M, N, K, group, _pitch(X, (K + 7) // 8 * 8), _pitch(W, (half + 15) // 16 * 16),
+           _pitch(scales, groups), ldz, _pitch(C, N)), stream)
+    return C

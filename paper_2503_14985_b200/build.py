@@ -9,7 +9,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libmlt.so")
 SOURCES = ["mlt.cu"]
-HEADERS = ["ptx.cuh", "gemm.cuh", "mha.cuh", "mha_packed.cuh", "paged.cuh", "f8.cuh", "quantize.cuh", "gemm_f8.cuh", "append.cuh", "paged_f8.cuh",
+HEADERS = ["ptx.cuh", "gemm.cuh", "mha.cuh", "mha_packed.cuh", "paged.cuh", "f8.cuh", "quantize.cuh", "gemm_f8.cuh", "gemm_w4.cuh", "append.cuh", "paged_f8.cuh",
            os.path.join("..", "..", "include", "mlt.h")]
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

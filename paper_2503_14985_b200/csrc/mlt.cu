@@ -14,6 +14,7 @@
 #include "append.cuh"
 #include "gemm.cuh"
 #include "gemm_f8.cuh"
+#include "gemm_w4.cuh"
 #include "mha.cuh"
 #include "mha_packed.cuh"
 #include "paged.cuh"
@@ -103,7 +104,7 @@ int get_device(DeviceInfo* out) {
             }
             d.cluster_slots[i] = clusters * S;
         }
-        if (paged_configure() != 0 || !paged_f8_configure()) return MLT_ERR_CUDA;
+        if (paged_configure() != 0 || !paged_f8_configure() || !w4_configure()) return MLT_ERR_CUDA;
         const int f8_rc = gemm_f8_configure();
         if (f8_rc == 1) return MLT_ERR_CUDA;
         d.gemm_f8_ok = f8_rc == 0;
@@ -1436,3 +1437,37 @@ int mlt_paged_attn_decode_shared(const void* Q, const void* K_cache, const void*
 }
 
 }  // extern "C"
+
+extern "C" int mlt_gemm_w4(const void* X, const void* W, const void* scales, const void* zeros, void* C, int64_t M, int64_t N, int64_t K,
+                           int group, int64_t ldx, int64_t ldw, int64_t lds, int64_t ldz, int64_t ldc, void* stream) {
+    if (M < 0 || N < 0 || K < 0) return MLT_ERR_INVALID_ARG;
+    if (M == 0 || N == 0) return MLT_OK;
+    if (!C || (K > 0 && (!X || !W || !scales))) return MLT_ERR_INVALID_ARG;
+    if (group != 32 && group != 64 && group != 128) return MLT_ERR_UNSUPPORTED;
+    if (K % group != 0) return MLT_ERR_INVALID_ARG;
+    if (ldx < K || ldw < K / 2 || lds < K / group || (zeros && ldz < K / group) || ldc < N) return MLT_ERR_INVALID_ARG;
+    if (M > (1 << 19) || N > INT32_MAX - 1024 || K > INT32_MAX - 1024) return MLT_ERR_UNSUPPORTED;
+    if (K > 0 && (!aligned16(X) || !aligned16(W) || ldx % 8 != 0 || ldw % 16 != 0 || (reinterpret_cast<uintptr_t>(scales) & 1u) != 0))
+        return MLT_ERR_ALIGNMENT;
+    if ((reinterpret_cast<uintptr_t>(C) & 1u) != 0) return MLT_ERR_ALIGNMENT;
+    DeviceInfo dev;
+    const int rc = get_device(&dev);
+    if (rc != MLT_OK) return rc;
+    W4Params p = {};
+    p.X = static_cast<const __nv_bfloat16*>(X);
+    p.W = static_cast<const uint8_t*>(W);
+    p.scales = static_cast<const __nv_bfloat16*>(scales);
+    p.zeros = static_cast<const uint8_t*>(zeros);
+    p.C = static_cast<__nv_bfloat16*>(C);
+    p.ldx = ldx;
+    p.ldw = ldw;
+    p.lds = lds;
+    p.ldz = ldz;
+    p.ldc = ldc;
+    p.M = static_cast<int>(M);
+    p.N = static_cast<int>(N);
+    p.K = static_cast<int>(K);
+    int grid = 0;
+    if (!w4_plan(&p, group, dev.sm_count, dev.cluster_slots, &grid)) return MLT_ERR_UNSUPPORTED;
+    return p.rows > 8 ? w4_launch<2>(p, group, grid, static_cast<cudaStream_t>(stream)) : w4_launch<1>(p, group, grid, static_cast<cudaStream_t>(stream));
+}

@@ -77,3 +77,17 @@ def test_shared_refusals():
     size = binding.paged_attn_shared_workspace_bytes
     assert size(0, 1, 8, 2, 128) == 0 and size(8, 0, 8, 2, 128) == binding.paged_attn_workspace_bytes(8, 8, 128)
     assert size(8, 1, 8, 2, 128) > binding.paged_attn_workspace_bytes(8, 8, 128)
+
+
+def test_w4_refusals():
+    def call(**kw):
+        a = dict(X=16, W=16, scales=16, zeros=16, C=16, M=4, N=100, K=256, group=64, ldx=256, ldw=128, lds=4, ldz=4, ldc=100)
+        a.update(kw)
+        return binding.gemm_w4_raw(**a)
+
+    assert call(M=0) == 0 and call(N=0) == 0 and call(M=0, X=0, C=0) == 0
+    assert call(M=-1) == 1 and call(X=0) == 1 and call(W=0) == 1 and call(scales=0) == 1 and call(C=0) == 1
+    assert call(group=16) == 2 and call(group=256) == 2 and call(K=224, group=64) == 1
+    assert call(ldx=248) == 1 and call(ldw=112) == 1 and call(lds=3) == 1 and call(ldz=3) == 1 and call(ldc=99) == 1
+    assert call(ldx=260) == 3 and call(ldw=136) == 3 and call(X=8) == 3 and call(W=24) == 3 and call(scales=17) == 3 and call(C=17) == 3
+    assert call(M=1 << 20) == 2
