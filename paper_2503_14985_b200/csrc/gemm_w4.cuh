@@ -1,22 +1,28 @@
 // Few rows times 4-bit weights:  C[i][n] = sum over groups j of scale[n][j] * sum over k in j of x[i][k] (q[n][k] - z[n][j]).
 //
 // Bound by the weights' bytes (N K / 2, read once).  At the copy bandwidth an SM gets about 46 weights per clock, so what
-// counts besides keeping loads in flight is instructions per weight:
-//  * The weights are the A operand (16 rows) of mma.sync m16n8k16, the rows of x the B operand (8 columns).  A 32-bit word of 8
-//    weights becomes four BF16 pairs by (w >> 4 i) & 0x000F000F | 0x43004300: 128 + q, exact, one shift and one three-input
-//    logic operation per pair.  Nothing is subtracted per weight: the accumulator of a group starts at -(128 + z) sum x, with the
-//    sums of x taken once per CTA, so products and sums stay in FP32 and scales are applied once per group and output.
-//    (Starting value and sum are up to 143 sum |x|, so a group's rounding is 143 * 2^-23 of that at most per addition.)
+// counts besides keeping loads in flight is instructions per weight, above all on the integer pipe (one per two clocks and scheduler):
+//  * The weights are the A operand (16 rows) of mma.sync m16n8k16, the rows of x the B operand (8 columns), both FP16 with FP32
+//    accumulators.  The bits of a 4-bit weight are an FP16 number as they stand, the subnormal q 2^-24: a 32-bit word of 8 weights
+//    becomes four FP16 pairs with one shift and four ANDs, v & 0x000F000F and v & 0x00F000F0 for v = w and v = w >> 8; the x that meet
+//    the latter, 16 q 2^-24, are divided by 16.  The accumulator of a group starts at -z sum x (the sums are taken once per CTA),
+//    products are exact, and the group's scale and the factors are applied once per group and output.
+//  * x is BF16, whose range FP16 lacks: each group of a row is multiplied by the power of two that brings its largest element to
+//    2^14 .. 2^15, and the inverse goes into the group's factor.  An element loses bits only below 2^-27 of that largest one.
 //  * The order of the summation index of an MMA is free.  The pairs of a word are (k, k + 4); x is laid out in shared memory
 //    in that order once per CTA, as the B fragments (16 bytes per lane, no bank conflicts).  A lane's words of a group lie side by
-//    side, so that a quad covers whole groups: a load is 16, 8 or 4 bytes per lane for groups of 128, 64 or 32.
-//  * A warp works on 32 weight rows x 128 of K at a time, so every B fragment serves two MMAs.  The 16 warps of a CTA cut K among
-//    them (and row tiles, where K is short); their partial sums meet in shared memory.  Weights go from global memory straight to
-//    registers, kW4Ahead pieces ahead of their use.
-//  * CTAs are persistent (one per SM); x stays in shared memory for all row tiles of a CTA.  Where x does not fit or there are
-//    fewer tiles than SMs, a cluster cuts K and sums through distributed shared memory, in a fixed order.  More than 16 rows run as
-//    several passes over the weights (from L2, mostly).
+//    side, so that a quad covers whole groups.
+//  * A warp works on pieces of 32 weight rows x 256 of K, so every B fragment serves two MMAs.  Pieces come by TMA in halves of 128 of
+//    K (64-byte swizzle, zeros beyond N and K) into a ring of the warp's own, and a half is requested again as soon as it has been
+//    read; which row of a piece a lane takes is chosen so that the swizzled reads of 16, 8 or 4 bytes (groups of 128, 64, 32)
+//    meet no bank conflicts.
+//  * The 16 warps of a CTA cut K among them (and row tiles, where K is short); their partial sums meet in shared memory.  CTAs are
+//    persistent (one per SM); x stays in shared memory for all row tiles of a CTA.  Where x does not fit or there are fewer tiles than
+//    SMs, a cluster cuts K and sums through distributed shared memory, in a fixed order.  More than 16 rows run as several passes
+//    over the weights (from L2, mostly).
 #pragma once
+
+#include <cuda_fp16.h>
 
 #include <algorithm>
 
@@ -25,140 +31,202 @@
 
 namespace mlt {
 
-constexpr int kW4Threads = 512;
-constexpr int kW4Warps = kW4Threads / 32;
-constexpr int kW4Ahead = 2;        // pieces of 32 rows x 128 of K that a warp has in flight
-constexpr int kW4Step = 128;       // K per piece
+constexpr int kW4Warps = 16;
+constexpr int kW4Threads = kW4Warps * 32;
+constexpr int kW4Step = 256;       // K per piece: 128 bytes of a weight row, in two halves
 constexpr int kW4Tile = 32;        // weight rows per piece
+constexpr int kW4PieceBytes = kW4Tile * kW4Step / 2, kW4HalfBytes = kW4PieceBytes / 2;
+constexpr int kW4MaxRing = 3;      // pieces per warp in shared memory
 constexpr int kW4ColPitch = 36;    // words per column of a warp's partial sums (no bank conflicts)
 constexpr int kW4Smem = 227 * 1024;
 
 struct W4Params {
     const __nv_bfloat16* X;       // [M, K], pitch ldx
-    const uint8_t* W;             // [N, K / 2], pitch ldw bytes
     const __nv_bfloat16* scales;  // [N, K / group], pitch lds
     const uint8_t* zeros;         // [N, K / group], pitch ldz, or null (8)
     __nv_bfloat16* C;             // [M, N], pitch ldc
-    int64_t ldx, ldw, lds, ldz, ldc;
+    int64_t ldx, lds, ldz, ldc;
     int M, N, K;
-    int rows;         // rows of x per pass
+    int wide_scales;  // a piece's scales (zero points) of a row can be read at once
+    int rows;         // rows of x per pass (R of the kernel)
     int steps;        // pieces of K per CTA
-    int k_warps;      // warps that cut them (a power of two); kW4Warps / k_warps row tiles at a time
+    int k_warps;      // warps that cut them
+    int at_once;      // row tiles at a time, kW4Warps / k_warps
+    unsigned char k_of[kW4Warps], tile_of[kW4Warps];  // a warp's first piece of K and its row tile
     int cluster;      // CTAs that cut K
+    int stride;       // row tiles from one set to a CTA's next
+    int ring;         // pieces per warp in flight
+    int red_sets;     // sets of row tiles whose warps' sums fit shared memory
+    int part_sets;    // cluster: sets whose sums do
+    // offsets in shared memory, in bytes
+    int at_x, at_fac, at_red, at_part;
 };
 
-// bytes of shared memory in front of the partial sums: x, then the groups' sums
-__host__ __device__ inline int w4_x_bytes(int rows, int steps) { return rows * steps * kW4Step * 2; }
-__host__ __device__ inline int w4_sum_bytes(int rows, int steps, int group) { return (rows * steps * (kW4Step / group) * 4 + 15) / 16 * 16; }
-template <int MT>
-__host__ __device__ constexpr int w4_red_bytes() { return 2 * kW4Warps * MT * 8 * kW4ColPitch * 4; }
-__host__ __device__ inline int w4_part_bytes(int rows, int k_warps, int cluster) {
-    return cluster > 1 ? 2 * (kW4Warps / k_warps) * kW4Tile * rows * 4 : 0;
+// Row (0..7) of an 8-row group that lane group g reads: with the TMA's 64-byte swizzle (16-byte chunk c of row r at c ^ ((r >> 1) & 3))
+// the lanes that one shared-memory phase serves (8 of 16 bytes, 16 of 8, 32 of 4) then hit different banks.
+template <int VEC>
+__device__ __forceinline__ int w4_row(int g) {
+    return VEC == 2 ? (g & 1) | ((g & 2) << 1) | ((g & 4) >> 1) : g;
 }
 
-// MT: columns of x in units of 8;  VEC: words of a lane per group (group = 32 * VEC)
-template <int MT, int VEC>
-__global__ void __launch_bounds__(kW4Threads, 1) gemm_w4_kernel(const W4Params p) {
+__device__ __forceinline__ void w4_mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// R: rows of x per pass, a power of two (those beyond the last are zeros);  VEC: words of a lane per group (group = 32 * VEC)
+template <int R, int VEC>
+__global__ void __launch_bounds__(kW4Threads, 1) gemm_w4_kernel(const __grid_constant__ CUtensorMap tmap_w, const W4Params p) {
     constexpr int kGroup = 32 * VEC;
     constexpr int kGroups = kW4Step / kGroup;  // groups per piece
-    extern __shared__ __align__(16) uint8_t w4_smem[];
+    constexpr int MT = R > 8 ? 2 : 1;          // columns of x in units of 8
+    constexpr int kColumns = R < 8 ? R : 8;    // of a unit
+    extern __shared__ uint8_t w4_smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(w4_smem_raw) + 1023) & ~uintptr_t(1023));
+    __shared__ uint64_t bars[kW4Warps][2 * kW4MaxRing];
+    __shared__ uint32_t abort_word;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int k_warps = p.k_warps, tiles_at_once = kW4Warps / k_warps;
-    const int kw = warp % k_warps, tw = warp / k_warps;
+    const int k_warps = p.k_warps, tiles_at_once = p.at_once;
+    const int kw = p.k_of[warp], tw = p.tile_of[warp];                 // (warps with tw == tiles_at_once only help with the sums)
     const int rank = p.cluster > 1 ? static_cast<int>(cluster_ctarank()) : 0;
-    const int m0 = blockIdx.y * p.rows, rows = min(p.rows, p.M - m0);
+    const int m0 = blockIdx.y * R, rows = min(R, p.M - m0);
     const int step0 = rank * p.steps;                                  // first piece of K of this CTA
     const int all_steps = (p.K + kW4Step - 1) / kW4Step;
     const int steps = max(0, min(p.steps, all_steps - step0));         // (the last CTAs of a cluster may have fewer, or none)
     const int tiles = (p.N + kW4Tile - 1) / kW4Tile;
-    const int stride = static_cast<int>(gridDim.x) / p.cluster * tiles_at_once;
-    const int first = static_cast<int>(blockIdx.x) / p.cluster * tiles_at_once;
-    uint4* xs = reinterpret_cast<uint4*>(w4_smem);                     // [piece][word][row][t]
-    float* sums = reinterpret_cast<float*>(w4_smem + w4_x_bytes(p.rows, p.steps));  // [group][row]
-    float* red = sums + w4_sum_bytes(p.rows, p.steps, kGroup) / 4;     // [2][warp][column][kW4ColPitch]
-    float* part = red + w4_red_bytes<MT>() / 4;                        // [2][tile][column][row]
+    const int stride = p.stride, first = (p.cluster > 1 ? static_cast<int>(blockIdx.x) / p.cluster : static_cast<int>(blockIdx.x)) * tiles_at_once;
+    uint8_t* ring = smem + warp * p.ring * kW4PieceBytes;
+    uint4* xs = reinterpret_cast<uint4*>(smem + p.at_x);               // [piece][word][row][t]
+    float2* fac = reinterpret_cast<float2*>(smem + p.at_fac);          // [group][row] {sum of x times 2^-24, inverse factor times 2^24}
+    float* red = reinterpret_cast<float*>(smem + p.at_red);            // [p.red_sets][warp][up to 8 columns][kW4ColPitch]
+    float* part = reinterpret_cast<float*>(smem + p.at_part);          // cluster: [p.part_sets][tile][row][weight row]
 
+    if (lane == 0) {
+        for (int i = 0; i < 2 * kW4MaxRing; ++i) mbar_init(&bars[warp][i], 1);
+        if (warp == 0) abort_word = 0;
+        fence_mbar_init();
+    }
     pdl_launch_dependents();
+    __syncthreads();
     cudaGridDependencySynchronize();
 
     // pieces of this warp, in order: row tile, then K
-    struct Piece {
-        uint32_t w[4][4];      // rows g, g + 8, g + 16, g + 24
-        uint32_t sz[kGroups];  // of row g + 8 t: scale in the upper half, 128 + z in the lower
-    };
-    Piece piece[kW4Ahead];
-    int ld_tile = first + tw, ld_step = kw;
-    const int n_groups = p.K / kGroup;
-    auto load = [&](Piece& pc) {
-        if (ld_tile < tiles && ld_step < steps) {
-            const int k_step = (step0 + ld_step) * kW4Step;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int n = min(ld_tile * kW4Tile + 8 * r + g, p.N - 1);
-                const uint8_t* row = p.W + n * p.ldw + k_step / 2 + t * 4 * VEC;
-#pragma unroll
-                for (int q = 0; q < kGroups; ++q) {
-                    const bool in = k_step + q * kGroup < p.K;
-                    if constexpr (VEC == 4) {
-                        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-                        if (in) v = *reinterpret_cast<const uint4*>(row);
-                        pc.w[r][0] = v.x; pc.w[r][1] = v.y; pc.w[r][2] = v.z; pc.w[r][3] = v.w;
-                    } else if constexpr (VEC == 2) {
-                        uint2 v = make_uint2(0u, 0u);
-                        if (in) v = *reinterpret_cast<const uint2*>(row + q * 32);
-                        pc.w[r][2 * q] = v.x; pc.w[r][2 * q + 1] = v.y;
-                    } else {
-                        pc.w[r][q] = in ? *reinterpret_cast<const uint32_t*>(row + q * 16) : 0u;
-                    }
-                }
-            }
-            const int n = min(ld_tile * kW4Tile + 8 * t + g, p.N - 1);
-#pragma unroll
-            for (int q = 0; q < kGroups; ++q) {
-                const int j = k_step / kGroup + q;
-                uint32_t s = 0, z = 8;
-                if (j < n_groups) {
-                    s = *reinterpret_cast<const uint16_t*>(p.scales + n * p.lds + j);
-                    if (p.zeros) z = p.zeros[n * p.ldz + j];
-                }
-                pc.sz[q] = (s << 16) | z;
-            }
+    int ld_tile = tw < tiles_at_once ? first + tw : tiles, ld_step = kw, ld_slot = 0;
+    auto request = [&](int half) {  // half of the next piece, into its slot
+        if (ld_tile < tiles && ld_step < steps && lane == 0) {
+            const int at = 2 * ld_slot + half;
+            mbar_arrive_expect_tx(&bars[warp][at], kW4HalfBytes);
+            tma_load_2d(ring + at * kW4HalfBytes, &tmap_w, &bars[warp][at], (step0 + ld_step) * (kW4Step / 2) + half * (kW4Step / 4), ld_tile * kW4Tile);
         }
+    };
+    auto next_request = [&]() {
+        if (++ld_slot == p.ring) ld_slot = 0;
         ld_step += k_warps;
         if (ld_step >= steps) {
             ld_step = kw;
             ld_tile += stride;
         }
     };
-#pragma unroll
-    for (int i = 0; i < kW4Ahead; ++i) load(piece[i]);
+    for (int i = 0; i < p.ring; ++i) {
+        request(0);
+        request(1);
+        next_request();
+    }
 
     // x, in fragment order: 8 consecutive k become (k, k + 4), (k + 1, k + 5), ...
-    for (int i = threadIdx.x; i < rows * steps * (kW4Step / 8); i += kW4Threads) {
-        const int per_row = steps * (kW4Step / 8);
-        const int row = i / per_row, k8 = i % per_row, k = step0 * kW4Step + k8 * 8;
-        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        if (k < p.K) v = *reinterpret_cast<const uint4*>(p.X + (m0 + row) * p.ldx + k);
-        const int in_step = k8 % 16, q = in_step / (4 * VEC), r = in_step % (4 * VEC);
-        const int word = q * VEC + r % VEC, tt = r / VEC;
-        xs[(((k8 / 16) * 4 + word) * rows + row) * 4 + tt] =
-            make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < rows * steps * kGroups; i += kW4Threads) {
-        const int row = i % rows, j = i / rows;  // group j of the CTA's K
-        float s = 0.0f;
-        for (int e = 0; e < 4 * VEC; ++e) {
-            const int word = j / kGroups * 4 + j % kGroups * VEC + e % VEC;
-            const uint4 v = xs[(word * rows + row) * 4 + e / VEC];
-            float f[8];
-            bf16x8_to_f32(v, f);
-            s += ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+    for (int k8 = threadIdx.x; k8 < steps * (kW4Step / 8); k8 += kW4Threads) {  // (whole warps)
+        const int k = step0 * kW4Step + k8 * 8;
+        const int in_step = k8 % 32, q = in_step / (4 * VEC), r = in_step % (4 * VEC);
+        uint4* to = xs + ((k8 / 32) * 8 + q * VEC + r % VEC) * R * 4 + r / VEC;
+        const __nv_bfloat16* from = p.X + m0 * p.ldx + k;
+        uint4 v[R];
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            v[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (i < rows && k < p.K) v[i] = *reinterpret_cast<const uint4*>(from + i * p.ldx);
         }
-        sums[j * rows + row] = s;
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            float f[8];
+            bf16x8_to_f32(v[i], f);
+            float top = 0.0f, sum = ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(f[e]));
+#pragma unroll
+            for (int w = 1; w < 4 * VEC; w <<= 1) {
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+                sum += __shfl_xor_sync(0xffffffffu, sum, w);
+            }
+            const int up = min(268 - static_cast<int>(__float_as_uint(top) >> 23), 253);  // exponent field of the factor
+            const float mul = __uint_as_float(static_cast<uint32_t>(up) << 23), mul16 = mul * 0.0625f;
+            const __half2 h0 = __floats2half2_rn(f[0] * mul, f[4] * mul), h1 = __floats2half2_rn(f[1] * mul16, f[5] * mul16);
+            const __half2 h2 = __floats2half2_rn(f[2] * mul, f[6] * mul), h3 = __floats2half2_rn(f[3] * mul16, f[7] * mul16);
+            to[i * 4] = make_uint4(*reinterpret_cast<const uint32_t*>(&h0), *reinterpret_cast<const uint32_t*>(&h1),
+                                   *reinterpret_cast<const uint32_t*>(&h2), *reinterpret_cast<const uint32_t*>(&h3));
+            if (r == 0)
+                fac[((k8 / 32) * kGroups + q) * R + i] = make_float2(sum * mul * 5.9604644775390625e-8f, 16777216.0f * __uint_as_float(static_cast<uint32_t>(254 - up) << 23));
+        }
     }
     __syncthreads();
-
+    // scales and zero points of a piece, as they lie in memory: this lane holds those of row 8 t + w4_row(g)
+    const int my_row = w4_row<VEC>(g);
+    const int per_tile = (steps - kw + k_warps - 1) / k_warps;  // pieces of this warp per tile (0 or less: none)
+    int sc_tile = first + tw, sc_step = kw;
+    const int64_t s_on = static_cast<int64_t>(k_warps) * kGroups, s_back = (per_tile - 1) * s_on;
+    const uint16_t* scale_at = reinterpret_cast<const uint16_t*>(p.scales) + (static_cast<int64_t>(sc_tile) * kW4Tile + 8 * t + my_row) * p.lds + (step0 + kw) * kGroups;
+    const uint8_t* zero_at = p.zeros + (static_cast<int64_t>(sc_tile) * kW4Tile + 8 * t + my_row) * p.ldz + (step0 + kw) * kGroups;
+    struct Scales {
+        uint32_t s[kGroups / 2], z[(kGroups + 3) / 4];
+    };
+    auto load_scales = [&](Scales& sc) {
+        if (sc_tile < tiles && sc_step < steps) {
+            const bool in_n = sc_tile * kW4Tile + 8 * t + my_row < p.N;
+            if (p.wide_scales && (step0 + sc_step + 1) * kW4Step <= p.K) {
+                if (in_n) {
+                    if constexpr (kGroups == 8) {
+                        const uint4 v = *reinterpret_cast<const uint4*>(scale_at);
+                        sc.s[0] = v.x; sc.s[1] = v.y; sc.s[2] = v.z; sc.s[3] = v.w;
+                    } else if constexpr (kGroups == 4) {
+                        const uint2 v = *reinterpret_cast<const uint2*>(scale_at);
+                        sc.s[0] = v.x; sc.s[1] = v.y;
+                    } else {
+                        sc.s[0] = *reinterpret_cast<const uint32_t*>(scale_at);
+                    }
+                    if (p.zeros) {
+                        if constexpr (kGroups == 8) {
+                            const uint2 v = *reinterpret_cast<const uint2*>(zero_at);
+                            sc.z[0] = v.x; sc.z[1] = v.y;
+                        } else if constexpr (kGroups == 4) {
+                            sc.z[0] = *reinterpret_cast<const uint32_t*>(zero_at);
+                        } else {
+                            sc.z[0] = *reinterpret_cast<const uint16_t*>(zero_at);
+                        }
+                    }
+                }
+            } else {
+                const int left = in_n ? p.K / kGroup - (step0 + sc_step) * kGroups : 0;
+#pragma unroll
+                for (int i = 0; i < kGroups / 2; ++i) sc.s[i] = 0;
+#pragma unroll
+                for (int q = 0; q < kGroups; ++q)
+                    if (q < left) {
+                        sc.s[q >> 1] |= static_cast<uint32_t>(scale_at[q]) << (16 * (q & 1));
+                        if (p.zeros) sc.z[q >> 2] = (sc.z[q >> 2] & ~(0xFFu << (8 * (q & 3)))) | (static_cast<uint32_t>(zero_at[q]) << (8 * (q & 3)));
+                    }
+            }
+        }
+        sc_step += k_warps;
+        int64_t by = s_on, z_by = s_on;
+        if (sc_step >= steps) {
+            sc_step = kw;
+            sc_tile += stride;
+            by = static_cast<int64_t>(stride) * kW4Tile * p.lds - s_back;
+            z_by = static_cast<int64_t>(stride) * kW4Tile * p.ldz - s_back;
+        }
+        scale_at += by;
+        zero_at += z_by;
+    };
     float acc[2][MT][4];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -166,139 +234,222 @@ __global__ void __launch_bounds__(kW4Threads, 1) gemm_w4_kernel(const W4Params p
         for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[h][m][e] = 0.0f;
-    int my_row[MT], col0[MT], col1[MT];  // columns beyond the rows of x repeat the last one; their sums go nowhere
-#pragma unroll
-    for (int m = 0; m < MT; ++m) {
-        my_row[m] = min(m * 8 + g, rows - 1);
-        col0[m] = min(m * 8 + 2 * t, rows - 1);
-        col1[m] = min(m * 8 + 2 * t + 1, rows - 1);
-    }
+    // (columns beyond R repeat others; their sums go nowhere)
+    const uint4* x_at = xs + (g & (kColumns - 1)) * 4 + t;
+    const int col0 = (2 * t) & (kColumns - 1), col1 = (2 * t + 1) & (kColumns - 1);
+    const int twist = (my_row >> 1) & 3;
+    const int w_at = my_row * 64 + (VEC == 4 ? (t ^ twist) * 16 : VEC == 2 ? ((t >> 1) ^ twist) * 16 + (t & 1) * 8 : twist * 16 + t * 4);
 
-    auto compute = [&](const Piece& pc, int step) {
+    constexpr int kHalfGroups = kGroups / 2;
+    // (One copy of this code, not one per half: unrolled, a row tile's pass runs through more instructions than the cache near
+    // the schedulers holds.)
+    auto compute = [&](int slot, int half, int step, const Scales& sc) {
+        uint32_t s_half[(kHalfGroups + 1) / 2], z_half;  // the half's scales and zero points, from the lowest bits on
+        if constexpr (kHalfGroups == 4) {
+            s_half[0] = half ? sc.s[2] : sc.s[0];
+            s_half[1] = half ? sc.s[3] : sc.s[1];
+            z_half = half ? sc.z[1] : sc.z[0];
+        } else if constexpr (kHalfGroups == 2) {
+            s_half[0] = half ? sc.s[1] : sc.s[0];
+            z_half = sc.z[0] >> (16 * half);
+        } else {
+            s_half[0] = sc.s[0] >> (16 * half);
+            z_half = sc.z[0] >> (8 * half);
+        }
+        const uint8_t* w_half = ring + (2 * slot + half) * kW4HalfBytes;
+        const uint4* x_half = x_at + (2 * step + half) * (4 * R * 4);
+        const float2* fac_half = fac + (2 * step + half) * (kHalfGroups * R);
 #pragma unroll
-        for (int q = 0; q < kGroups; ++q) {
-            float s[4], z[4];
+        for (int q = 0; q < kHalfGroups; ++q) {
+            uint32_t w[4][VEC];  // rows w4_row(g) + 0, 8, 16, 24
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const uint32_t v = __shfl_sync(0xffffffffu, pc.sz[q], (lane & 28) | r);
-                s[r] = __uint_as_float(v & 0xFFFF0000u);
-                z[r] = -__uint_as_float((v << 16) | 0x43000000u);  // -(128 + z)
+                const uint8_t* at = w_half + (w_at ^ (q * 16 * VEC)) + r * 512;
+                if constexpr (VEC == 4) {
+                    const uint4 v = *reinterpret_cast<const uint4*>(at);
+                    w[r][0] = v.x; w[r][1] = v.y; w[r][2] = v.z; w[r][3] = v.w;
+                } else if constexpr (VEC == 2) {
+                    const uint2 v = *reinterpret_cast<const uint2*>(at);
+                    w[r][0] = v.x; w[r][1] = v.y;
+                } else {
+                    w[r][0] = *reinterpret_cast<const uint32_t*>(at);
+                }
             }
-            float c[2][MT][4];
-            const float* sum = sums + (step * kGroups + q) * rows;
+            float s[4], z[4];
+            // scale in the upper half, 128 + z in the lower, both BF16
+            const uint32_t sz = __byte_perm(s_half[q >> 1], __byte_perm(z_half, 0x43u, 0x0040 + q), (q & 1) ? 0x3254 : 0x1054);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const uint32_t v = __shfl_sync(0xffffffffu, sz, (lane & 28) | r);
+                s[r] = __uint_as_float(v & 0xFFFF0000u);
+                z[r] = 128.0f - __uint_as_float(v << 16);  // -z
+            }
+            float c[2][MT][4], u0[MT], u1[MT];
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
-                const float s0 = sum[col0[m]], s1 = sum[col1[m]];
+                const float2 f0 = fac_half[q * R + m * 8 + col0], f1 = fac_half[q * R + m * 8 + col1];
+                u0[m] = f0.y;
+                u1[m] = f1.y;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    c[h][m][0] = z[2 * h] * s0;
-                    c[h][m][1] = z[2 * h] * s1;
-                    c[h][m][2] = z[2 * h + 1] * s0;
-                    c[h][m][3] = z[2 * h + 1] * s1;
+                    c[h][m][0] = z[2 * h] * f0.x;
+                    c[h][m][1] = z[2 * h] * f1.x;
+                    c[h][m][2] = z[2 * h + 1] * f0.x;
+                    c[h][m][3] = z[2 * h + 1] * f1.x;
                 }
             }
 #pragma unroll
             for (int v = 0; v < VEC; ++v) {
-                const int word = q * VEC + v;
                 uint4 b[MT];
 #pragma unroll
-                for (int m = 0; m < MT; ++m) b[m] = xs[((step * 4 + word) * rows + my_row[m]) * 4 + t];
+                for (int m = 0; m < MT; ++m) b[m] = x_half[(q * VEC + v) * (R * 4) + m * 32];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    uint32_t lo[4], hi[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        lo[i] = ((pc.w[2 * h][word] >> (4 * i)) & 0x000F000Fu) | 0x43004300u;
-                        hi[i] = ((pc.w[2 * h + 1][word] >> (4 * i)) & 0x000F000Fu) | 0x43004300u;
-                    }
+                    const uint32_t a0 = w[2 * h][v], a1 = w[2 * h + 1][v], b0 = a0 >> 8, b1 = a1 >> 8;
 #pragma unroll
                     for (int m = 0; m < MT; ++m) {
-                        mma_bf16_16816(c[h][m], lo[0], hi[0], lo[1], hi[1], b[m].x, b[m].y);
-                        mma_bf16_16816(c[h][m], lo[2], hi[2], lo[3], hi[3], b[m].z, b[m].w);
+                        w4_mma(c[h][m], a0 & 0x000F000Fu, a1 & 0x000F000Fu, a0 & 0x00F000F0u, a1 & 0x00F000F0u, b[m].x, b[m].y);
+                        w4_mma(c[h][m], b0 & 0x000F000Fu, b1 & 0x000F000Fu, b0 & 0x00F000F0u, b1 & 0x00F000F0u, b[m].z, b[m].w);
                     }
                 }
             }
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int m = 0; m < MT; ++m)
 #pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    acc[h][m][0] = fmaf(s[2 * h], c[h][m][0], acc[h][m][0]);
-                    acc[h][m][1] = fmaf(s[2 * h], c[h][m][1], acc[h][m][1]);
-                    acc[h][m][2] = fmaf(s[2 * h + 1], c[h][m][2], acc[h][m][2]);
-                    acc[h][m][3] = fmaf(s[2 * h + 1], c[h][m][3], acc[h][m][3]);
+                for (int h = 0; h < 2; ++h) {
+                    acc[h][m][0] = fmaf(s[2 * h] * u0[m], c[h][m][0], acc[h][m][0]);
+                    acc[h][m][1] = fmaf(s[2 * h] * u1[m], c[h][m][1], acc[h][m][1]);
+                    acc[h][m][2] = fmaf(s[2 * h + 1] * u0[m], c[h][m][2], acc[h][m][2]);
+                    acc[h][m][3] = fmaf(s[2 * h + 1] * u1[m], c[h][m][3], acc[h][m][3]);
                 }
         }
     };
 
-    // The warps' sums of one set of tiles meet in one of two buffers, which alternate: a buffer is written again only after a
-    // barrier that every reader of it has passed.  With a cluster the CTAs' sums do the same.
-    auto finish_tiles = [&](int tile, int round) {
-        float* buf = red + (round & 1) * (kW4Warps * MT * 8 * kW4ColPitch);
-        float* mine = buf + warp * (MT * 8 * kW4ColPitch);
+    // The warps' sums of a set of tiles meet in shared memory, 8 rows of x at a time (one warp adds up those of a row, tile and set, a
+    // lane per weight row); with up to 8 rows several sets wait for that.  With a cluster the CTAs' sums are kept until all sets
+    // are done, or there is no room for more, and then do the same.
+    constexpr int pitch = kColumns * kW4ColPitch;  // of a warp's sums
+    auto put_sums = [&](int set, int m) {
+        float* mine = red + (set * kW4Warps + warp) * pitch;
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    mine[(m * 8 + 2 * t + (e & 1)) * kW4ColPitch + h * 16 + (e >> 1) * 8 + g] = acc[h][m][e];
-                    acc[h][m][e] = 0.0f;
-                }
-        __syncthreads();
-        const int outputs = tiles_at_once * rows * kW4Tile;  // (tile, row of x, weight row)
-        float* dst = part + (round & 1) * outputs;
-        for (int i = threadIdx.x; i < outputs; i += kW4Threads) {
-            const int n_in = i % kW4Tile, m = i / kW4Tile % rows, tl = i / (kW4Tile * rows);
-            const float* src = buf + tl * k_warps * (MT * 8 * kW4ColPitch) + m * kW4ColPitch + n_in;
+            for (int e = 0; e < 4; ++e)
+                if (2 * t + (e & 1) < kColumns) mine[(2 * t + (e & 1)) * kW4ColPitch + h * 16 + (e >> 1) * 8 + my_row] = acc[h][m][e];
+    };
+    auto store = [&](int tile, int tl, int row, float sum) {
+        const int n = (tile + tl) * kW4Tile + lane;
+        if (n < p.N) p.C[(m0 + row) * p.ldc + n] = __float2bfloat16(sum);
+    };
+    auto add_sums = [&](int sets, int m, int tile, int kept) {  // tile: the last set's first one;  kept: sets in `part` before these
+        const int cols = min(kColumns, rows - 8 * m);
+        for (int i = warp; i < sets * tiles_at_once * cols; i += kW4Warps) {
+            const int col = i % cols, tl = i / cols % tiles_at_once, set = i / cols / tiles_at_once;
+            const float* src = red + (set * kW4Warps + tl * k_warps) * pitch + col * kW4ColPitch + lane;
             float sum = 0.0f;
-            for (int w = 0; w < k_warps; ++w) sum += src[w * (MT * 8 * kW4ColPitch)];
-            const int n = (tile + tl) * kW4Tile + n_in;
-            if (p.cluster > 1) dst[i] = sum;
-            else if (n < p.N) p.C[(m0 + m) * p.ldc + n] = __float2bfloat16(sum);
-        }
-        if (p.cluster > 1) {
-            cluster_sync_all();
-            const int lo = outputs * rank / p.cluster, hi = outputs * (rank + 1) / p.cluster;
-            for (int i = lo + threadIdx.x; i < hi; i += kW4Threads) {
-                const int n_in = i % kW4Tile, m = i / kW4Tile % rows, tl = i / (kW4Tile * rows);
-                float sum = 0.0f;
-                for (int c = 0; c < p.cluster; ++c) {
-                    float v;
-                    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(map_to_cta(smem_u32(dst + i), static_cast<uint32_t>(c))));
-                    sum += v;
-                }
-                const int n = (tile + tl) * kW4Tile + n_in;
-                if (n < p.N) p.C[(m0 + m) * p.ldc + n] = __float2bfloat16(sum);
-            }
+#pragma unroll 4
+            for (int w = 0; w < k_warps; ++w) sum += src[w * pitch];
+            if (p.cluster > 1) part[(((kept + set) * tiles_at_once + tl) * R + 8 * m + col) * kW4Tile + lane] = sum;
+            else store(tile - (sets - 1 - set) * stride, tl, 8 * m + col, sum);
         }
     };
-
-    int tile = first, step = kw, round = 0;
-    while (tile < tiles) {
+    auto exchange = [&](int sets, int tile) {
+        __syncwarp();
+        cluster_sync_all();
+        for (int i = rank * kW4Warps + warp; i < sets * tiles_at_once * R; i += p.cluster * kW4Warps) {
+            if (i % R >= rows) continue;
+            const uint32_t at = smem_u32(part + i * kW4Tile + lane);
+            float v[8];
 #pragma unroll
-        for (int u = 0; u < kW4Ahead; ++u) {
-            if (tile < tiles) {
-                if (tile + tw < tiles && step < steps) compute(piece[u], step);
-                load(piece[u]);
-                step += k_warps;
-                if (step >= steps) {
-                    finish_tiles(tile, round++);
-                    step = kw;
-                    tile += stride;
-                }
+            for (int c = 0; c < 8; ++c) {
+                v[c] = 0.0f;
+                if (c < p.cluster) asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[c]) : "r"(map_to_cta(at, static_cast<uint32_t>(c))) : "memory");
             }
+            const int row = i % R, tl = i / R % tiles_at_once, set = i / R / tiles_at_once;
+            store(tile - (sets - 1 - set) * stride, tl, row, ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])));
+        }
+        __syncwarp();
+        cluster_sync_all();  // the sums have been read
+    };
+    int in_red = 0, kept = 0;
+    auto tile_done = [&](int tile, bool last) {
+        if constexpr (MT == 1) {
+            put_sums(in_red++, 0);
+            if (in_red == p.red_sets || last) {
+                __syncthreads();
+                add_sums(in_red, 0, tile, kept);
+                kept += in_red;
+                in_red = 0;
+                if (!last) __syncthreads();
+            }
+        } else {
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                put_sums(0, m);
+                __syncthreads();
+                add_sums(1, m, tile, kept);
+                if (m + 1 < MT || !last) __syncthreads();
+            }
+            ++kept;
+        }
+        if (p.cluster > 1 && (last || (in_red == 0 && kept + p.red_sets > p.part_sets))) {
+            exchange(kept, tile);
+            kept = 0;
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[h][m][e] = 0.0f;
+    };
+
+    Scales sc, next_sc;
+#pragma unroll
+    for (int i = 0; i < (kGroups + 3) / 4; ++i) sc.z[i] = 0x08080808u;
+#pragma unroll
+    for (int i = 0; i < kGroups / 2; ++i) sc.s[i] = 0u;
+    next_sc = sc;
+    int tile = first, step = kw, slot = 0;
+    uint32_t phase = 0;  // of the slot in turn
+    bool ok = true;
+    const bool works = tw < tiles_at_once;
+    if (works) load_scales(sc);
+#pragma unroll 1
+    while (tile < tiles) {
+        if (works) {
+            load_scales(next_sc);
+#pragma unroll 1
+            for (int half = 0; half < 2; ++half) {
+                if (tile + tw < tiles && step < steps && ok) {
+                    ok = __all_sync(0xffffffffu, mbar_wait(&bars[warp][2 * slot + half], phase, &abort_word, 0x800 + warp)) != 0;
+                    if (ok) compute(slot, half, step, sc);
+                }
+                __syncwarp();
+                if (ok) request(half);
+            }
+            next_request();
+            sc = next_sc;
+            if (++slot == p.ring) {
+                slot = 0;
+                phase ^= 1;
+            }
+        }
+        step += k_warps;
+        if (step >= steps) {
+            tile_done(tile, tile + stride >= tiles);
+            step = kw;
+            tile += stride;
         }
     }
-    if (p.cluster > 1) cluster_sync_all();  // nobody leaves while its sums are being read
 }
 
-template <int MT, int VEC>
-int w4_launch_one(const W4Params& p, int grid, cudaStream_t st) {
+template <int R, int VEC>
+int w4_launch_one(const CUtensorMap& tw, const W4Params& p, int grid, int smem, cudaStream_t st) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(grid), static_cast<unsigned>((p.M + p.rows - 1) / p.rows));
+    cfg.gridDim = dim3(static_cast<unsigned>(grid), static_cast<unsigned>((p.M + R - 1) / R));
     cfg.blockDim = dim3(kW4Threads);
-    cfg.dynamicSmemBytes = static_cast<size_t>(w4_x_bytes(p.rows, p.steps)) + w4_sum_bytes(p.rows, p.steps, 32 * VEC) + w4_red_bytes<MT>() +
-                           w4_part_bytes(p.rows, p.k_warps, p.cluster);
+    cfg.dynamicSmemBytes = static_cast<size_t>(smem);
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -308,57 +459,93 @@ int w4_launch_one(const W4Params& p, int grid, cudaStream_t st) {
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = p.cluster > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, gemm_w4_kernel<MT, VEC>, p) == cudaSuccess ? 0 : 4;
+    return cudaLaunchKernelEx(&cfg, gemm_w4_kernel<R, VEC>, tw, p) == cudaSuccess ? 0 : 4;
 }
 
-template <int MT>
-int w4_launch(const W4Params& p, int group, int grid, cudaStream_t st) {
-    switch (group) {
-        case 32: return w4_launch_one<MT, 1>(p, grid, st);
-        case 64: return w4_launch_one<MT, 2>(p, grid, st);
-        default: return w4_launch_one<MT, 4>(p, grid, st);
+template <int VEC>
+int w4_launch_rows(const CUtensorMap& tw, const W4Params& p, int grid, int smem, cudaStream_t st) {
+    switch (p.rows) {
+        case 1: return w4_launch_one<1, VEC>(tw, p, grid, smem, st);
+        case 2: return w4_launch_one<2, VEC>(tw, p, grid, smem, st);
+        case 4: return w4_launch_one<4, VEC>(tw, p, grid, smem, st);
+        case 8: return w4_launch_one<8, VEC>(tw, p, grid, smem, st);
+        default: return w4_launch_one<16, VEC>(tw, p, grid, smem, st);
     }
 }
+inline int w4_launch(const CUtensorMap& tw, const W4Params& p, int group, int grid, int smem, cudaStream_t st) {
+    return group == 32 ? w4_launch_rows<1>(tw, p, grid, smem, st) : group == 64 ? w4_launch_rows<2>(tw, p, grid, smem, st)
+                                                                               : w4_launch_rows<4>(tw, p, grid, smem, st);
+}
 
-template <int MT, int VEC>
+template <int R, int VEC>
 bool w4_configure_one() {
-    return cudaFuncSetAttribute(gemm_w4_kernel<MT, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, kW4Smem) == cudaSuccess;
+    return cudaFuncSetAttribute(gemm_w4_kernel<R, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, kW4Smem - 1024) == cudaSuccess;
 }
-inline bool w4_configure() {
-    return w4_configure_one<1, 1>() && w4_configure_one<1, 2>() && w4_configure_one<1, 4>() && w4_configure_one<2, 1>() && w4_configure_one<2, 2>() &&
-           w4_configure_one<2, 4>();
+template <int VEC>
+bool w4_configure_rows() {
+    return w4_configure_one<1, VEC>() && w4_configure_one<2, VEC>() && w4_configure_one<4, VEC>() && w4_configure_one<8, VEC>() &&
+           w4_configure_one<16, VEC>();
 }
+inline bool w4_configure() { return w4_configure_rows<1>() && w4_configure_rows<2>() && w4_configure_rows<4>(); }
 
-// Rows per pass, CTAs per cluster and warps along K; false if not even one row of x fits a cluster of 8.
+// Rows per pass, CTAs per cluster, warps along K and the layout of shared memory; false if not even one row of x fits a cluster of 8.
 // cluster_slots: resident CTAs in clusters of 2, 4, 8.
-inline bool w4_plan(W4Params* p, int group, int sm_count, const int* cluster_slots, int* grid) {
+inline bool w4_plan(W4Params* p, int group, int sm_count, const int* cluster_slots, int* grid, int* smem) {
     const int all_steps = (p->K + kW4Step - 1) / kW4Step, tiles = (p->N + kW4Tile - 1) / kW4Tile;
-    auto steps_of = [&](int c) { return (all_steps + c - 1) / c; };
+    constexpr int kLimit = kW4Smem - 2048;  // 1 KB of static shared memory and its like, 1 KB for the ring's alignment
+    auto steps_of = [&](int c) { return std::max(1, (all_steps + c - 1) / c); };
     auto warps_of = [&](int c) {
-        int kw = 1;
-        while (kw < kW4Warps && 2 * kw <= steps_of(c)) kw *= 2;
-        return kw;
+        const int rounds = (steps_of(c) + kW4Warps - 1) / kW4Warps;
+        return (steps_of(c) + rounds - 1) / rounds;
     };
-    auto fits = [&](int rows, int c) {
-        const int64_t bytes = static_cast<int64_t>(rows) * steps_of(c) * kW4Step * 2 + static_cast<int64_t>(rows) * steps_of(c) * (kW4Step / group) * 4 + 16 +
-                              (rows > 8 ? w4_red_bytes<2>() : w4_red_bytes<1>()) + w4_part_bytes(rows, warps_of(c), c);
-        return bytes <= kW4Smem;
+    auto fixed_bytes = [&](int rows, int c) {  // x and its factors
+        return static_cast<int64_t>(rows) * steps_of(c) * (kW4Step * 2 + kW4Step / group * 8) + 16;
+    };
+    auto at_once_of = [&](int c) { return kW4Warps / warps_of(c); };
+    auto red_bytes = [&](int rows) { return kW4Warps * std::min(rows, 8) * kW4ColPitch * 4; };
+    auto part_bytes = [&](int rows, int c) { return c > 1 ? at_once_of(c) * kW4Tile * rows * 4 : 0; };
+    auto ring_of = [&](int rows, int c) {
+        const int64_t left = kLimit - fixed_bytes(rows, c) - red_bytes(rows) - part_bytes(rows, c);
+        return left < 0 ? 0 : static_cast<int>(std::min<int64_t>(kW4MaxRing, left / (at_once_of(c) * warps_of(c) * kW4PieceBytes)));
     };
     auto slots = [&](int c) { return c == 1 ? sm_count : cluster_slots[c == 2 ? 0 : c == 4 ? 1 : 2]; };
-    int rows = std::min(p->M, 16), c = 1;
-    for (; rows > 0; rows = rows > 8 ? 8 : rows - 1) {
-        for (c = 1; c <= 8 && !(fits(rows, c) && slots(c) >= c); c *= 2) {}
-        if (c <= 8) break;
+    int rows = 1, c = 1;
+    while (rows < 16 && rows < p->M) rows *= 2;
+    for (; rows > 0; rows /= 2) {
+        int best = 0;
+        for (int k = 1; k <= 8 && best == 0; k *= 2)  // the smallest cluster that x and one piece per warp fit
+            if (slots(k) >= k && ring_of(rows, k) > 0) {
+                c = k;
+                best = ring_of(rows, k);
+            }
+        if (best > 0) break;
     }
     if (rows <= 0) return false;
-    // fewer tiles than half the SMs: cut K further, while a warp of the CTAs keeps a piece
+    // fewer tiles than half the SMs: cut K further, while a CTA keeps four pieces
     while (c < 8 && slots(2 * c) >= 2 * c && static_cast<int64_t>(tiles) * 2 * c <= sm_count && all_steps >= 2 * c * 4) c *= 2;
     p->rows = rows;
     p->cluster = c;
     p->steps = steps_of(c);
     p->k_warps = warps_of(c);
-    const int at_once = kW4Warps / p->k_warps;
-    *grid = c * std::max(1, std::min(slots(c) / c, (tiles + at_once - 1) / at_once));
+    p->ring = ring_of(rows, c);
+    const int at_once = at_once_of(c), groups = std::max(1, std::min(slots(c) / c, (tiles + at_once - 1) / at_once));
+    *grid = c * groups;
+    p->at_once = at_once;
+    p->stride = groups * at_once;
+    for (int w = 0; w < kW4Warps; ++w) {
+        p->k_of[w] = static_cast<unsigned char>(w % p->k_warps);
+        p->tile_of[w] = static_cast<unsigned char>(w / p->k_warps);
+    }
+    // The rest of shared memory: a cluster's sums of all sets of tiles first, then sets of the warps' sums.
+    const int sets = (tiles + groups * at_once - 1) / (groups * at_once);
+    p->at_x = at_once * p->k_warps * p->ring * kW4PieceBytes;
+    p->at_fac = p->at_x + rows * p->steps * kW4Step * 2;
+    p->at_red = p->at_fac + (rows * p->steps * (kW4Step / group) * 8 + 15) / 16 * 16;
+    const int room = kLimit - p->at_red, part = part_bytes(rows, c), red = red_bytes(rows);
+    p->part_sets = part ? std::min(sets, (room - red) / part) : 0;
+    p->red_sets = rows > 8 ? 1 : std::max(1, std::min({sets, (room - p->part_sets * part) / red, part ? p->part_sets : sets}));
+    p->at_part = p->at_red + p->red_sets * red;
+    *smem = p->at_part + p->part_sets * part + 1024;
     return true;
 }
 

@@ -1451,23 +1451,32 @@ extern "C" int mlt_gemm_w4(const void* X, const void* W, const void* scales, con
         return MLT_ERR_ALIGNMENT;
     if ((reinterpret_cast<uintptr_t>(C) & 1u) != 0) return MLT_ERR_ALIGNMENT;
     DeviceInfo dev;
-    const int rc = get_device(&dev);
+    int rc = get_device(&dev);
     if (rc != MLT_OK) return rc;
     W4Params p = {};
     p.X = static_cast<const __nv_bfloat16*>(X);
-    p.W = static_cast<const uint8_t*>(W);
     p.scales = static_cast<const __nv_bfloat16*>(scales);
     p.zeros = static_cast<const uint8_t*>(zeros);
     p.C = static_cast<__nv_bfloat16*>(C);
     p.ldx = ldx;
-    p.ldw = ldw;
     p.lds = lds;
     p.ldz = ldz;
     p.ldc = ldc;
     p.M = static_cast<int>(M);
     p.N = static_cast<int>(N);
     p.K = static_cast<int>(K);
-    int grid = 0;
-    if (!w4_plan(&p, group, dev.sm_count, dev.cluster_slots, &grid)) return MLT_ERR_UNSUPPORTED;
-    return p.rows > 8 ? w4_launch<2>(p, group, grid, static_cast<cudaStream_t>(stream)) : w4_launch<1>(p, group, grid, static_cast<cudaStream_t>(stream));
+    const int per_piece = kW4Step / group;  // a piece's scales of a row, if they are aligned
+    p.wide_scales = reinterpret_cast<uintptr_t>(scales) % (2 * per_piece) == 0 && lds % per_piece == 0 &&
+                    (!zeros || (reinterpret_cast<uintptr_t>(zeros) % per_piece == 0 && ldz % per_piece == 0));
+    int grid = 0, smem = 0;
+    if (!w4_plan(&p, group, dev.sm_count, dev.cluster_slots, &grid, &smem)) return MLT_ERR_UNSUPPORTED;
+    CUtensorMap tw = {};
+    if (K > 0) {
+        const uint64_t dims[2] = {static_cast<uint64_t>(K) / 2, static_cast<uint64_t>(N)};
+        const uint64_t strides[1] = {static_cast<uint64_t>(ldw)};
+        const uint32_t box[2] = {kW4Step / 4, kW4Tile};
+        rc = encode_bf16(&tw, W, 2, dims, strides, box, 3, true);
+        if (rc != MLT_OK) return rc;
+    }
+    return w4_launch(tw, p, group, grid, smem, static_cast<cudaStream_t>(stream));
 }

@@ -1,10 +1,9 @@
 """mlt_gemm_w4 against the definition in 64 bits.
 
-Bound of an output element, with T = sum over groups of scale * sum |x| in them: half a BF16 step, 2^-8 |C|; a group's accumulator starts at
--(128 + z) sum x and every value it passes through is at most 143 sum |x| + 143 sum |x|, so each of its at most group / 8 additions
-(and the sum of x, whose group additions are off by 2^-24 of sum |x| each and enter 143-fold) costs at most 2^-23 of 286 sum |x|:
-(group / 8 + group / 4) * 286 * 2^-23 T; scales, and the sums over groups and warps, 2^-22 * 16 per unit of 15 T in at most
-K / group + 24 additions: (K / group + 24) * 15 * 2^-23 T.
+Bound of an output element, with T = sum over groups of |scale| sum |x| in them: half a BF16 step, 2^-8 |C|; a group's products are exact
+and its partial sums at most 15 sum |x|, so each of its at most group / 8 additions costs at most 2^-23 of that: group / 8 * 15 * 2^-23 T;
+an element of x below 2^-27 of its group's largest is off by at most 2^-38 of that one: 15 * group * 2^-38 T; scales, and the sums over
+groups and warps, at most K / group + 24 roundings of 2^-23 in terms of 15 T: (K / group + 24) * 15 * 2^-23 T.
 """
 import numpy as np
 import pytest
@@ -38,7 +37,7 @@ def check(c, x, w, s, z, group):
     wd = ((q.view(N, -1, group) - zz[..., None]) * s.double()[..., None]).reshape(N, K)
     ref = x.double() @ wd.t()
     T = x.double().abs().view(M, -1, group).sum(-1) @ s.double().abs().t()
-    bound = 2.0 ** -8 * ref.abs() + ((group / 8 + group / 4) * 286 + (K / group + 24) * 15) * 2.0 ** -23 * T + 1e-30
+    bound = 2.0 ** -8 * ref.abs() + 15 * (group / 8 + group * 2.0 ** -15 + K / group + 24) * 2.0 ** -23 * T + 1e-30
     err = (c.double() - ref).abs()
     assert torch.isfinite(c).all()
     assert (err <= bound).all(), f"off by {(err / bound).max().item():.3f} of the bound"
