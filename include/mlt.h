@@ -303,7 +303,7 @@ int mlt_paged_attn_decode_f8(const void* Q, const void* K_cache, const void* V_c
  *   O       device, BF16 out, pitch ldo;  LSE  device, FP32 out, [num_q, H], or NULL
  *   causal  non-zero: key j is visible to query i of the same sequence iff j <= i + (keys - queries) (bottom-right
  *           aligned; queries beyond the keys see nothing)
- * H / H_kv is any whole number up to 128.  D in {64, 128}; pitches in elements, multiples of 8.
+ * H / H_kv is any whole number up to 128, H at most 4096.  D in {64, 128}; pitches in elements, multiples of 8.
  * A query that sees no key gives O = 0 and LSE = -inf.  Rows of O and LSE that belong to no sequence (a padded batch) are
  * left as they were.  What lies in K and V behind a sequence's last key (the next sequence, padding) never reaches its results, not
  * even a NaN; inside a sequence a masked V must be finite (it may meet a weight of zero).
@@ -343,19 +343,21 @@ int mlt_paged_attn_prefill(const void* Q, const void* K_cache, const void* V_cac
 
 /*
  * mlt_paged_attn_decode for a batch whose sequences share long prefixes (one system prompt, one document, samples of one
- * prompt).  Each prefix is read once for all sequences behind it, as a tensor-core product over their query rows; the tails are
- * decoded one by one, and the two are joined in FP32.  The result is mlt_paged_attn_decode's on the same arguments.
+ * prompt).  Each prefix is read once for all sequences behind it, as a tensor-core product over their query rows; what lies behind
+ * it is read per sequence, and the two are joined in FP32.  The result is mlt_paged_attn_decode's on the same arguments.
  *
  *   prefix_lens  device, int32, [num_groups];  cu_groups  device, int32, [num_groups + 1], ascending: the sequences
  *                cu_groups[g] .. cu_groups[g + 1] - 1 have the first prefix_lens[g] / block_size (whole blocks) entries of
  *                their block tables in common; those of the group's first sequence are used.  Sequences in no group are
  *                decoded by themselves.  Negative lengths count as 0, lengths beyond the table as the table's.
+ *   H_kv         H / H_kv is any whole number up to 128
  *   workspace    device scratch of mlt_paged_attn_shared_workspace_bytes bytes (MLT_ERR_INVALID_ARG with less); calls that overlap
  *                on the GPU must not share it
- * The rest as for mlt_paged_attn_decode, but a bad block-table entry inside a prefix counts as a block of zeros (and is
- * reported).  seq_lens may be shorter than the prefix, or 0.  A group whose offsets descend or reach outside num_seqs is left
- * out (its sequences are decoded by themselves) and reported (MLT_ERR_BAD_POSITION).  num_groups == 0: mlt_paged_attn_decode.
- * MLT_ERR_UNSUPPORTED when num_seqs / (2 * (128 / (H / H_kv))) + num_groups exceeds 1024, or num_blocks * H_kv reaches 2^31.
+ * The rest as for mlt_paged_attn_decode, but a bad block-table entry counts as a block of zeros (and is reported).
+ * seq_lens may be shorter than the prefix, or 0.  A group whose offsets descend or reach outside num_seqs is left
+ * out (its sequences are decoded by themselves) and reported (MLT_ERR_BAD_POSITION); so are, without any output, groups that
+ * overlap so that their rows do not fit the workspace.
+ * MLT_ERR_UNSUPPORTED when num_seqs + num_seqs / (2 * (128 / (H / H_kv))) + num_groups exceeds 4096, or num_blocks * H_kv reaches 2^31.
  */
 size_t mlt_paged_attn_shared_workspace_bytes(int num_seqs, int num_groups, int H, int H_kv, int D);
 int mlt_paged_attn_decode_shared(const void* Q, const void* K_cache, const void* V_cache,

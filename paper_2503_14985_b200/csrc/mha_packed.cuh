@@ -1,18 +1,21 @@
 // Attention of whole prompts, for sequences of different lengths packed one behind another and grouped heads:
 //   row (token i of sequence s, head h) sees keys j <= lim(i);  p_j = exp(scale q.k_j - m),  O = sum p_j v_j / sum p_j.
-// Keys come from packed rows or from the paged cache; a decode batch that shares a prefix is the same problem with the
-// batch's sequences as the tokens.
+// Keys come from packed rows or from the paged cache.  Decode of a batch with shared prefixes is the same problem: each group of
+// sequences is one "sequence" whose tokens are the group's queries and whose keys are the prefix, and each query has a second one for
+// the keys behind the prefix; the two are joined.
 //
 // The softmax core is that of mha.cuh (two 128-row tiles that take turns on the tensor pipe, one thread per row, running
 // reference maximum, P through tensor memory; its comments give the reasons).  What differs:
 //  * Rows.  The G query heads of a KV head are rows of one tile: row r is token r / G, head r % G, W = 128 / G tokens per
-//    tile (G that do not divide 128 leave up to G - 1 rows unused; these are zeroed once).  A few tokens of many heads then
-//    fill a tile, and K and V are read once for all G heads.  The Q tile is one TMA box [64 of D, G heads, W tokens].
+//    tile (G that do not divide 128 leave up to G - 1 rows unused).  A few tokens of many heads then fill a tile, and K and V are
+//    read once for all G heads.  The Q tile is one TMA box [64 of D, G heads, W tokens] (one token, where there is one).
 //  * Work.  Lengths are on the device, so a one-CTA kernel writes the list of work items (two tiles of a sequence, a range of
 //    key blocks), longest first, and persistent CTAs (one per SM) draw from it by an atomic counter.  The loading warp draws
 //    the next item as soon as it has requested the current one's last keys, so the list's latency hides behind the ring.
-//    With too few items for the SMs (few tokens behind a long context) the plan cuts the key range; the parts go to scratch
-//    as FP32 {m, l, O} and a second kernel joins them.
+//  * Few rows.  With too few items for the SMs (few tokens behind a long context) the plan cuts the key range, and where the rows
+//    fill one tile only, both tiles work on them, each on every other key block ("dual": 128 keys then take 1600 clocks instead of
+//    3000, the latency of one tile's chain S -> softmax -> P V; at the copy bandwidth an SM gets 128 keys in 2800).  The parts go to
+//    scratch as FP32 {m, l, O} and a second kernel joins them.  Warps without a valid row leave the exponentials out.
 //  * Keys from the cache.  One lane per (cache block, 64 columns) issues its own TMA box, so a 128-key tile is one table load
 //    and one issue for the warp.  A block-table entry out of range loads zeros (coordinate beyond the tensor map) and is
 //    reported.  Rows beyond the sequence's last key may hold anything (another sequence, stale cache): scores there are
@@ -31,8 +34,9 @@ namespace mlt {
 constexpr unsigned int kStatusBadSequence = 9;  // a sequence's offsets or positions lie outside the call's tokens or keys
 constexpr int kPackedPlanThreads = 1024;
 constexpr int kPackedBuckets = 2048;
-constexpr int kPackedMaxSplitTiles = 1024;  // key ranges are cut only when there are fewer tile pairs than this
-constexpr int kPackedMaxSlots = 320;        // partial results (256 rows each) that scratch is sized for
+constexpr int kPackedSeqs = 1024;        // sequences that the plan keeps in shared memory (more are read back from scratch)
+constexpr int kPackedSplitTiles = 4096;  // key ranges are cut only when there are no more tile pairs than this
+constexpr int kPackedSplitRows = 320 * 2 * kMhaBlock;  // rows of partial results that scratch is sized for (and see packed_scratch)
 
 struct PackedHeader {  // at the front of the scratch memory, written by the plan kernel
     int num_items;     // entries * H_kv
@@ -42,15 +46,17 @@ struct PackedHeader {  // at the front of the scratch memory, written by the pla
 };
 
 struct PackedParams {
-    // lengths (device): cu_q [S + 1] token offsets; keys per sequence from cu_k (packed), context_lens (paged) or, for a shared
-    // prefix, prefix_lens (floored to whole blocks) with seq_lens as the rows' own limits
+    // lengths (device): cu_q [S + 1] token offsets; keys per sequence from cu_k (packed), context_lens (paged) or, for shared
+    // prefixes, prefix_lens (floored to whole blocks) and seq_lens
     const int* cu_q;
     const int* cu_k;
     const int* context_lens;
     const int* prefix_lens;
     const int* seq_lens;
     const int* block_table;  // [rows, max_blocks]
-    int S, T, num_k, W, G, H, H_kv, causal;
+    int S;                   // sequences (shared prefixes: groups)
+    int all;                 // S, and with shared prefixes the T tails behind them
+    int T, num_k, W, G, H, H_kv, causal;
     int block_size, max_blocks, num_blocks;
     float scale;
     // results
@@ -59,18 +65,16 @@ struct PackedParams {
     int64_t ldo;
     // scratch
     PackedHeader* hdr;
-    int4* seqs;      // [S] {first token, tokens, keys, tile pairs before this sequence}
-    int4* entries;   // [max_entries] {sequence, tile pair, first key block, key blocks}
-    int* tile_first; // [max_tiles] first entry of a tile pair (cut ranges only)
-    float* part_o;   // [slots][rows][D]
-    float2* part_ml; // [slots][rows] {m in log2 units, l}
-    int max_tiles, max_entries, slots, slot_rows;
+    int4* seqs;           // [all] {first token, tokens, keys, tile pairs before this sequence}
+    long long* key_base;  // [all] first key row (packed) or block-table index (paged)
+    int4* entries;        // [max_entries] {sequence, tile pair, first key block, key blocks}
+    int* entry_rows;      // [max_entries] first row of the entry's partial results (of KV head 0)
+    int* tile_rows;       // [max_tiles] that of a tile pair's first entry
+    float* part_o;        // [part_rows][D]
+    float2* part_ml;      // [part_rows] {m in log2 units, l}
+    int max_tiles, max_entries, part_rows;
     int sm_count;
-    // shared prefix: the sequences' own tails, which the decode kernels of paged.cuh work on
-    PagedParams tail;  // (its seq_lens and table_skip are written by the plan kernel)
-    int* tail_lens;    // = tail.seq_lens
-    int* tail_skip;    // = tail.table_skip
-    int* tail_parts;   // [T, H_kv] partial results of a tail
+    int boxes;  // the output tensor maps exist: whole warps' rows leave as TMA boxes (H / H_kv divides 32)
 };
 
 __host__ __device__ __forceinline__ int packed_blocks(int keys) { return (keys + kMhaBlock - 1) / kMhaBlock; }
@@ -81,6 +85,8 @@ __device__ __forceinline__ int packed_tile_blocks(int nq, int nk, int causal, in
     const int last = causal ? nk - nq + first + n : nk;  // keys that the last of them sees
     return packed_blocks(max(0, last));
 }
+// Rows of partial results of a tile pair with n tokens, per part and KV head: two tiles, or one tile's rows twice.
+__device__ __forceinline__ int packed_part_rows(const PackedParams& p, int n) { return n <= p.W ? 2 * n * p.G : 2 * kMhaBlock; }
 
 __device__ __forceinline__ void packed_report(unsigned int code, int a, int b, int c) {
     if (atomicCAS(&g_status[0], 0u, code) == 0u) {
@@ -90,41 +96,60 @@ __device__ __forceinline__ void packed_report(unsigned int code, int a, int b, i
     }
 }
 
-// Tokens of a sequence and its keys; false (and no tokens) if they do not fit the call.
-__device__ __forceinline__ bool packed_sequence(const PackedParams& p, int s, int& q0, int& nq, int& nk) {
-    q0 = p.cu_q[s];
+// Tokens {first, count, keys} of a sequence and where its keys begin; false (and no tokens) if they do not fit the call.
+__device__ __forceinline__ bool packed_sequence(const PackedParams& p, int s, int3& q, long long& base) {
+    q.x = p.cu_q[s];
     const long long q1 = p.cu_q[s + 1];
-    nq = 0;
-    nk = 0;
-    if (q0 < 0 || q1 < q0 || q1 > p.T) return false;
+    q.y = 0;
+    q.z = 0;
+    base = 0;
+    if (q.x < 0 || q1 < q.x || q1 > p.T) return false;
     long long keys;
     if (p.cu_k) {
         const long long k0 = p.cu_k[s], k1 = p.cu_k[s + 1];
         if (k0 < 0 || k1 < k0 || k1 > p.num_k) return false;
         keys = k1 - k0;
+        base = k0;
     } else {
         const long long most = static_cast<long long>(p.max_blocks) * p.block_size;
         if (p.prefix_lens) {
             keys = max(0ll, min(static_cast<long long>(p.prefix_lens[s]), most));
             keys -= keys % p.block_size;
+            base = static_cast<long long>(q.x) * p.max_blocks;  // the group's first sequence
         } else {
-            keys = static_cast<long long>(p.context_lens[s]) + (q1 - q0);
-            if (p.context_lens[s] < 0 || (q1 > q0 && keys > most)) return false;
+            keys = static_cast<long long>(p.context_lens[s]) + (q1 - q.x);
+            if (p.context_lens[s] < 0 || (q1 > q.x && keys > most)) return false;
+            base = static_cast<long long>(s) * p.max_blocks;
         }
     }
-    nq = static_cast<int>(q1 - q0);
-    nk = static_cast<int>(keys);
+    q.y = static_cast<int>(q1 - q.x);
+    q.z = static_cast<int>(keys);
     return true;
 }
 
-// The sequence that holds tile pair i: the last one with at most i pairs before it that has any.
-__device__ __forceinline__ int packed_find_tile(const int4* seqs, int S, int i) {
-    int lo = 0, hi = S;
+// The group (or sequence) that token t is in, or -1.
+__device__ __forceinline__ int packed_owner(const PackedParams& p, int t) {
+    if (p.S == 0) return -1;
+    int lo = 0, hi = p.S;  // the last one that begins at or before the token
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (seqs[mid].w <= i) lo = mid; else hi = mid;
+        if (p.cu_q[mid] <= t) lo = mid; else hi = mid;
     }
-    return lo;
+    return p.cu_q[lo] <= t && t < p.cu_q[lo + 1] ? lo : -1;
+}
+
+// The keys of decoded sequence t behind its group's prefix.
+__device__ __forceinline__ void packed_tail(const PackedParams& p, int t, int3& q, long long& base) {
+    int3 g;
+    long long unused;
+    const int group = packed_owner(p, t);
+    const int prefix = group >= 0 && packed_sequence(p, group, g, unused) ? g.z : 0;
+    const long long most = static_cast<long long>(p.max_blocks) * p.block_size;
+    const int len = static_cast<int>(max(0ll, min(static_cast<long long>(p.seq_lens[t]), most)));
+    q.x = t;
+    q.z = max(0, len - prefix);
+    q.y = q.z > 0 ? 1 : 0;
+    base = static_cast<long long>(t) * p.max_blocks + prefix / p.block_size;
 }
 
 __device__ __forceinline__ int packed_bucket(int blocks) {  // monotone: exact below 512 blocks, then 64 steps per octave
@@ -158,192 +183,183 @@ __device__ __forceinline__ int packed_scan(int v, int* red, int& total) {
     return v + before;
 }
 
-// The group that sequence s is in, or -1; and the sequence's tokens behind the group's prefix.
-__device__ __forceinline__ int packed_group(const PackedParams& p, int s, int& tail) {
-    int lo = 0, hi = p.S;  // the last group that begins at or before s
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (p.cu_q[mid] <= s) lo = mid; else hi = mid;
-    }
-    const int4 q = p.seqs[lo];
-    const int group = s >= q.x && s - q.x < q.y ? lo : -1;
-    const long long most = static_cast<long long>(p.max_blocks) * p.block_size;
-    const int len = static_cast<int>(max(0ll, min(static_cast<long long>(p.seq_lens[s]), most)));
-    tail = max(0, len - (group >= 0 ? q.z : 0));
-    return group;
-}
-
-// The tails behind the prefixes, and how many partial results the decode kernel makes of each (one CTA).
-__device__ __forceinline__ void packed_plan_tails(const PackedParams& p, int* red) {
-    const int tid = threadIdx.x;
-    const int per = (p.T + kPackedPlanThreads - 1) / kPackedPlanThreads;
-    const int lo = min(p.T, tid * per), hi = min(p.T, lo + per);
-    int chunks = 0, most = 0;
-    for (int s = lo; s < hi; ++s) {
-        int tail;
-        const int group = packed_group(p, s, tail);
-        p.tail_lens[s] = tail;
-        p.tail_skip[s] = group >= 0 ? p.seqs[group].z / p.block_size : 0;
-        const int n = (tail + kPagedChunkTokens - 1) / kPagedChunkTokens;
-        chunks += n;
-        most = max(most, n);
-    }
-    int total;
-    int before = packed_scan(chunks, red, total) - chunks;
-#pragma unroll
-    for (int w = 16; w > 0; w >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, w));
-    if ((tid & 31) == 0) red[tid >> 5] = most;
-    __syncthreads();
-    for (int w = 0; w < 32; ++w) most = max(most, red[w]);
-    __syncthreads();
-    const int quota = paged_quota(static_cast<long long>(total) * p.H_kv, most, max(1, p.tail.balanced_ctas));
-    for (int s = lo; s < hi; ++s) {
-        const int tail = p.tail_lens[s];
-        if (p.tail.balanced) {  // as in paged_decode_mma_kernel: pieces of `quota` chunks across all rows
-            const int n = (tail + kPagedChunkTokens - 1) / kPagedChunkTokens;
-            for (int h = 0; h < p.H_kv; ++h) {
-                const long long start = static_cast<long long>(before) * p.H_kv + static_cast<long long>(h) * n;
-                p.tail_parts[static_cast<int64_t>(s) * p.H_kv + h] = n > 0 ? static_cast<int>((start + n - 1) / quota - start / quota + 1) : 0;
-            }
-            before += n;
-        } else {
-            const int nblk = (tail + p.block_size - 1) / p.block_size, share = paged_split_blocks(p.tail, nblk);
-            for (int h = 0; h < p.H_kv; ++h) p.tail_parts[static_cast<int64_t>(s) * p.H_kv + h] = (nblk + share - 1) / share;
-        }
-    }
-}
-
 // One CTA.  Sequences -> tile pairs -> work items.
 __global__ void __launch_bounds__(kPackedPlanThreads) mha_packed_plan_kernel(const PackedParams p) {
     pdl_launch_dependents();
+    extern __shared__ int4 plan_smem[];
+    int4* near_seqs = plan_smem;                                          // [kPackedSeqs]
+    int* hist = reinterpret_cast<int*>(plan_smem + kPackedSeqs);          // [kPackedBuckets], or with cut ranges
+    int2* tile_of_split = reinterpret_cast<int2*>(hist + kPackedBuckets); // [kPackedSplitTiles] {key blocks, tokens}
     __shared__ int red[32];
-    __shared__ int hist[kPackedBuckets];
-    __shared__ int blocks_of[kPackedMaxSplitTiles];
-    __shared__ int best_sh, sum_sh;
+    __shared__ int longest_sh;
     __shared__ unsigned long long pick_sh;
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     for (int i = tid; i < kPackedBuckets; i += kPackedPlanThreads) hist[i] = 0;
-    if (tid == 0) { best_sh = 0; sum_sh = 0; pick_sh = ~0ull; }
+    if (tid == 0) { longest_sh = 0; pick_sh = ~0ull; }
     cudaGridDependencySynchronize();
 
     // sequences: tile pairs and their prefix sums
     const int W2 = 2 * p.W;
-    const int per = (p.S + kPackedPlanThreads - 1) / kPackedPlanThreads;
-    const int s_lo = min(p.S, tid * per), s_hi = min(p.S, s_lo + per);
+    const int per = (p.all + kPackedPlanThreads - 1) / kPackedPlanThreads;
+    const int s_lo = min(p.all, tid * per), s_hi = min(p.all, s_lo + per);
+    int3 q = make_int3(0, 0, 0);
+    long long base = 0;
+    bool ok = true;
+    auto get = [&](int s) {
+        if (s < p.S) ok = packed_sequence(p, s, q, base);
+        else { ok = true; packed_tail(p, s - p.S, q, base); }
+    };
     int mine = 0;
     for (int s = s_lo; s < s_hi; ++s) {
-        int q0, nq, nk;
-        packed_sequence(p, s, q0, nq, nk);
-        mine += (nq + W2 - 1) / W2;
+        get(s);
+        mine += (q.y + W2 - 1) / W2;
     }
     int tiles;
     int before = packed_scan(mine, red, tiles) - mine;
     for (int s = s_lo; s < s_hi; ++s) {
-        int q0, nq, nk;
-        bool ok = packed_sequence(p, s, q0, nq, nk);
-        int n = (nq + W2 - 1) / W2;
+        if (per > 1) get(s);
+        int n = (q.y + W2 - 1) / W2;
         if (before > p.max_tiles - n) {  // more tokens than the call has: the offsets do not ascend
             ok = false;
-            nq = n = 0;
+            q.y = n = 0;
         }
-        if (!ok) packed_report(kStatusBadSequence, s, q0, nk);
-        p.seqs[s] = make_int4(q0, nq, nk, before);
+        if (!ok) packed_report(kStatusBadSequence, s, q.x, q.z);
+        const int4 e = make_int4(q.x, q.y, q.z, before);
+        p.seqs[s] = e;
+        p.key_base[s] = base;
+        if (s < kPackedSeqs) near_seqs[s] = e;
         before += n;
     }
     tiles = min(tiles, p.max_tiles);
     __syncthreads();
 
-    // tile pairs: key blocks of each
-    auto tile_of = [&](int i, int& s, int& pair) -> int {
-        s = packed_find_tile(p.seqs, p.S, i);
-        const int4 q = p.seqs[s];
-        pair = i - q.w;
-        const int first = pair * W2;
-        return packed_tile_blocks(q.y, q.z, p.causal, first, min(W2, q.y - first));
+    // tile pair i: its sequence (the last one with at most i pairs before it), number in it, tokens and key blocks
+    const int4* seqs = p.all <= kPackedSeqs ? near_seqs : p.seqs;
+    struct Tile { int s, pair, n, blocks; };
+    auto tile_at = [&](int i) {
+        Tile t;
+        int lo = 0, hi = p.all;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (seqs[mid].w <= i) lo = mid; else hi = mid;
+        }
+        const int4 e = seqs[lo];
+        t.s = lo;
+        t.pair = i - e.w;
+        t.n = min(W2, e.y - t.pair * W2);
+        t.blocks = packed_tile_blocks(e.y, e.z, p.causal, t.pair * W2, t.n);
+        return t;
     };
-    const bool may_split = p.slots > 0 && tiles <= kPackedMaxSplitTiles;
-    int most = 0, sum = 0;
+    const bool may_split = p.part_rows > 0 && tiles <= kPackedSplitTiles;
+    int most = 0;
     for (int i = tid; i < tiles; i += kPackedPlanThreads) {
-        int s, pair;
-        const int blocks = tile_of(i, s, pair);
-        atomicAdd(&hist[packed_bucket(blocks)], 1);
-        if (may_split) blocks_of[i] = blocks;
-        most = max(most, blocks);
-        sum += min(blocks, 1 << 20);
+        const Tile t = tile_at(i);
+        atomicAdd(&hist[packed_bucket(t.blocks)], 1);
+        if (may_split) tile_of_split[i] = make_int2(t.blocks, t.n);
+        most = max(most, t.blocks);
     }
     if (may_split) {
-        atomicMax(&best_sh, most);
-        atomicAdd(&sum_sh, sum);
+        most = __reduce_max_sync(0xffffffffu, most);
+        if (lane == 0) atomicMax(&longest_sh, most);
     }
     __syncthreads();
 
-    // Cut the key ranges?  Time in key blocks: an item of b blocks takes b + kItem (fill, drain, epilogue); whole ranges end with
-    // the longest, or when the SMs have shared the sum; parts of at most c blocks run in rounds, and joining them costs kJoin.
-    constexpr int kItem = 3, kJoin = 4;
+    // Cut the key ranges?  Time in halves of a key block's: an item of b blocks takes 2 b + 3 (fill, drain, epilogue), with one tile's
+    // rows on both tiles b + 3; equal items run in rounds of one per SM, unequal ones stick out by half of what the longest has
+    // over the average (whole ranges, longest first, by less).  Joining the parts costs kJoin.
+    constexpr int kItem = 3;
+    constexpr float kJoin = 5.0f, kNever = 1e12f;
     int chunk = 0;
     if (may_split) {
-        const int longest = best_sh;
-        if (longest > 1) {
-            const int warp = tid >> 5, lane = tid & 31;
-            for (int n = warp + 1; n <= 160 && n <= longest; n += kPackedPlanThreads / 32) {
-                const int c = (longest + n - 1) / n;
-                int parts = 0;
-                for (int i = lane; i < tiles; i += 32) parts += max(1, (blocks_of[i] + c - 1) / c);
-                parts = __reduce_add_sync(0xffffffffu, parts);
-                const long long items = static_cast<long long>(max(parts, 1)) * p.H_kv;
-                long long cost;
-                if (n == 1 && !p.prefix_lens) {
-                    const long long shared_out = (static_cast<long long>(sum_sh) * p.H_kv + kItem * items) / p.sm_count;
-                    cost = max(static_cast<long long>(c + kItem), shared_out);
-                } else {
-                    cost = (items + p.sm_count - 1) / p.sm_count * (c + kItem) + kJoin;
-                    if (items > p.slots) cost = 1ll << 40;
-                }
-                if (lane == 0) atomicMin(&pick_sh, (static_cast<unsigned long long>(cost) << 16) | static_cast<unsigned long long>(n));
+        const int longest = longest_sh;
+        for (int i = warp; i <= 64; i += kPackedPlanThreads / 32) {
+            // n parts of the longest range: 0 (whole and not joined), 1 .. 16, then 16 per octave up to 128
+            const int n = i <= 16 ? i : ((i - 17) % 16 + 17) << ((i - 17) / 16);
+            if (n > longest || (n == 0 && p.prefix_lens)) continue;  // (a prefix's results always go to the join)
+            const int c = n ? (longest + n - 1) / n : max(longest, 1);
+            float work = 0.0f, rows = 0.0f;
+            int top = 0, entries = 0;
+            for (int k = lane; k < tiles; k += 32) {
+                const int2 t = tile_of_split[k];
+                const int parts = max(1, (t.x + c - 1) / c), each = min(t.x, c);
+                const bool dual = n > 0 && t.y <= p.W;
+                work += static_cast<float>((dual ? t.x : 2 * t.x) + kItem * parts);
+                rows += static_cast<float>(parts * packed_part_rows(p, t.y));
+                top = max(top, (dual ? each : 2 * each) + kItem);
+                entries += parts;
             }
+#pragma unroll
+            for (int w = 16; w > 0; w >>= 1) {
+                work += __shfl_xor_sync(0xffffffffu, work, w);
+                rows += __shfl_xor_sync(0xffffffffu, rows, w);
+            }
+            top = __reduce_max_sync(0xffffffffu, top);
+            entries = __reduce_add_sync(0xffffffffu, entries);
+            const float items = static_cast<float>(max(entries, 1)) * p.H_kv, average = work * p.H_kv / items;
+            const float rounds = n ? ceilf(items / p.sm_count) : fmaxf(items / p.sm_count, 1.0f);
+            float cost = fmaxf(static_cast<float>(top), rounds * average + (top - average) * (n ? 0.5f : 0.25f)) + (n ? kJoin : 0.0f);
+            // (1.0001: the sum of the rows is rounded)
+            if (n && (rows * p.H_kv * 1.0001f > static_cast<float>(p.part_rows) || entries > p.max_entries)) cost = n == 1 && p.prefix_lens ? kNever / 2 : kNever;
+            if (lane == 0) atomicMin(&pick_sh, (static_cast<unsigned long long>(__float_as_uint(cost)) << 16) | static_cast<unsigned long long>(n));
         }
         __syncthreads();
-        const int n = pick_sh == ~0ull ? 1 : static_cast<int>(pick_sh & 0xffff);
-        chunk = n == 1 ? 0 : (longest + n - 1) / n;
-        if (p.prefix_lens && chunk == 0) chunk = max(1, longest);  // a prefix's results always go on to the join
+        const int n = pick_sh == ~0ull ? 0 : static_cast<int>(pick_sh & 0xffff);
+        if (n > 0 || p.prefix_lens) chunk = max(1, n ? (longest + n - 1) / n : longest);
     }
 
     int total;
     if (chunk > 0) {
-        const int blocks = tid < tiles ? blocks_of[tid] : 0;
-        const int parts = tid < tiles ? max(1, (blocks + chunk - 1) / chunk) : 0;
-        const int first = packed_scan(parts, red, total) - parts;
-        if (tid < tiles) {
-            int s, pair;
-            tile_of(tid, s, pair);
-            p.tile_first[tid] = first;
-            for (int k = 0; k < parts; ++k)
-                if (first + k < p.max_entries) p.entries[first + k] = make_int4(s, pair, k * chunk, min(chunk, blocks - k * chunk));
+        int first = 0, first_row = 0;
+        for (int i0 = 0; i0 < tiles; i0 += kPackedPlanThreads) {  // entries in the order of the tile pairs
+            const int i = i0 + tid;
+            Tile t = {0, 0, 0, 0};
+            int parts = 0, rows = 0;
+            if (i < tiles) {
+                t = tile_at(i);
+                parts = max(1, (t.blocks + chunk - 1) / chunk);
+                rows = packed_part_rows(p, t.n) * p.H_kv;
+            }
+            int sum_parts, sum_rows;
+            const int at = first + packed_scan(parts, red, sum_parts) - parts;
+            const int row = first_row + packed_scan(parts * rows, red, sum_rows) - parts * rows;
+            if (i < tiles) {
+                p.tile_rows[i] = row;
+                for (int k = 0; k < parts && at + k < p.max_entries; ++k) {
+                    p.entries[at + k] = make_int4(t.s, t.pair, k * chunk, min(chunk, t.blocks - k * chunk));
+                    p.entry_rows[at + k] = row + k * rows;
+                }
+            }
+            first += sum_parts;
+            first_row += sum_rows;
+            if (first_row > p.part_rows || first > p.max_entries) {  // (only for groups that overlap: scratch is sized for groups that do not)
+                if (tid == 0) packed_report(kStatusBadSequence, p.S, tiles, 0);
+                first = 0;
+                chunk = 0;
+                break;
+            }
         }
-        total = min(total, p.max_entries);
+        total = first;
     } else {
         // longest first: counting sort
         const int a = hist[2 * tid], b = hist[2 * tid + 1];
         const int end = packed_scan(a + b, red, total);
-        __syncthreads();
         hist[2 * tid] = end - a - b;
         hist[2 * tid + 1] = end - b;
         __syncthreads();
         for (int i = tid; i < tiles; i += kPackedPlanThreads) {
-            int s, pair;
-            const int blocks = tile_of(i, s, pair);
-            const int at = atomicAdd(&hist[packed_bucket(blocks)], 1);
-            if (at < p.max_entries) p.entries[at] = make_int4(s, pair, 0, blocks);
+            const Tile t = tile_at(i);
+            const int at = atomicAdd(&hist[packed_bucket(t.blocks)], 1);
+            if (at < p.max_entries) p.entries[at] = make_int4(t.s, t.pair, 0, t.blocks);
         }
         total = tiles;
     }
-    if (p.prefix_lens) packed_plan_tails(p, red);
     if (tid == 0) {
         p.hdr->num_items = total * p.H_kv;
         p.hdr->counter = 0;
         p.hdr->split = chunk;
     }
 }
+constexpr int kPackedPlanSmem = kPackedSeqs * 16 + kPackedBuckets * 4 + kPackedSplitTiles * 8;
 
 template <int D>
 struct PackedSmem {
@@ -351,7 +367,7 @@ struct PackedSmem {
     static constexpr int kChunkBytes = kMhaBlock * 128;
     static constexpr int kStages = (D == 128) ? 4 : 8;
     static constexpr int kBarrierBytes = 512;
-    static constexpr int kItemBytes = 2 * 48;
+    static constexpr int kItemBytes = 2 * 48 + kMhaBlock * 4;  // two work items, and which token and head a row is
     static constexpr int kStageBytes = 8 * 4096;
     static constexpr int kTotal = 2 * kTileBytes + kStages * kTileBytes + kBarrierBytes + kItemBytes + kStageBytes + 1024;
 };
@@ -364,15 +380,20 @@ struct PackedItem {  // 48 bytes in shared memory
     int lim0;        // last visible key of token tok0 (causal: one more per token)
     int b0;          // first key block
     int J[2];        // key blocks of each tile from b0 on
-    int slot;        // partial result, or -1: O and LSE are written
+    int part_row;    // first row of the partial results, or -1: O and LSE are written
     int fix;         // rows of the last V tile to zero: first | (end << 8), or 0
-    int pad[2];
+    int dual;        // both tiles have the same rows, tile t works on blocks b0 + t, b0 + t + 2, ...
+    int row_limits;  // rows see no key beyond their sequence's length either
 };
 
-template <int D>
+// kParts: items may be parts of a key range or have both tiles on one tile's rows.  Calls with enough items without that run the
+// kernel that leaves the code out: what the schedulers fetch is what bounds the softmax warps' neighbours (with it prompts
+// ran 2 to 11 % slower, D = 64 the most).
+template <int D, bool kParts>
 __global__ void __launch_bounds__(kMhaThreads, 1)
-mha_packed_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
-                  const __grid_constant__ CUtensorMap tmap_v, const PackedParams p) {
+mha_packed_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_q1,
+                  const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
+                  const __grid_constant__ CUtensorMap tmap_o, const __grid_constant__ CUtensorMap tmap_part, const PackedParams p) {
     using L = PackedSmem<D>;
     constexpr int kIssuers = (D == 64) ? 2 : 1;
     constexpr int kStages = L::kStages;
@@ -399,6 +420,7 @@ mha_packed_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
     uint32_t* tmem_base_slot = reinterpret_cast<uint32_t*>(v_asked + 2);
     volatile uint32_t* abort_flag = tmem_base_slot + 1;
     PackedItem* items = reinterpret_cast<PackedItem*>(reinterpret_cast<uint8_t*>(bars) + L::kBarrierBytes);
+    int* row_of = reinterpret_cast<int*>(items + 2);  // [128] token in the tile << 16 | head in the group
     static_assert(sizeof(PackedItem) == 48, "item slots");
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -425,6 +447,7 @@ mha_packed_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
         *abort_flag = 0;
         fence_mbar_init();
         prefetch_tensormap(&tmap_q);
+        prefetch_tensormap(&tmap_q1);
         prefetch_tensormap(&tmap_k);
         prefetch_tensormap(&tmap_v);
     }
@@ -432,15 +455,11 @@ mha_packed_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
         tmem_alloc(tmem_base_slot, 512);
         tmem_relinquish();
     }
-    // rows that no token fills (128 - W * G of them): zero for good, so that their scores are finite
-    {
-        const int used = p.W * p.G;
-        for (int i = threadIdx.x; i < (kMhaBlock - used) * 8 * 2 * kChunks; i += kMhaThreads) {
-            const int piece = i & 7, row = used + (i >> 3) % (kMhaBlock - used), tile_chunk = (i >> 3) / (kMhaBlock - used);
-            *reinterpret_cast<uint4*>(smem_q + tile_chunk * L::kChunkBytes + row * 128 + piece * 16) = make_uint4(0u, 0u, 0u, 0u);
-        }
-        fence_proxy_async_smem();
-    }
+    if (threadIdx.x < kMhaBlock) row_of[threadIdx.x] = (static_cast<int>(threadIdx.x) / p.G << 16) | (static_cast<int>(threadIdx.x) % p.G);
+    // Rows that no token fills: their scores need not be right, but a NaN would send the warp through the slow path.  Later items find
+    // rows of earlier ones there.
+    for (int i = threadIdx.x; i < 2 * L::kTileBytes / 16; i += kMhaThreads) reinterpret_cast<uint4*>(smem_q)[i] = make_uint4(0u, 0u, 0u, 0u);
+    fence_proxy_async_smem();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -471,22 +490,41 @@ mha_packed_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
         // ------------------------------- loader and scheduler -------------------------------
         setmaxnreg_dec<kMhaOtherRegs>();
         const int num_items = p.hdr->num_items;
-        const bool split = p.hdr->split != 0;
         const int chunk = p.hdr->split;
         const int W2 = 2 * p.W;
-        const uint32_t q_bytes = static_cast<uint32_t>(p.W) * p.G * 128 * kChunks;  // per tile
-        const int nb = p.cu_k ? 1 : kMhaBlock / p.block_size;                       // cache blocks per tile
+        const int nb = p.cu_k ? 1 : kMhaBlock / p.block_size;     // cache blocks per tile
+        const int lane_block = lane % nb, lane_chunk = lane / nb;  // which this lane loads, and which 64 columns of it
+        const int beyond = max(1, p.num_blocks * p.H_kv);          // coordinate that loads zeros
         int ld_stage = 0;
         uint32_t ld_phase = 0;
         int q_loads = 0;
         bool ok = true;
-        int idx = blockIdx.x;
+        // The next item is drawn while the current one's tiles are loaded, and its entry read: the list's latency (atomic, entry,
+        // sequence, one behind the other) is then off the path.
+        int idx = blockIdx.x, drawn = 0;
+        int4 e = make_int4(0, 0, 0, 0), q = e;
+        long long base = 0;
+        int entry_row = 0;
+        auto read_entry = [&]() {
+            if (idx < num_items) {
+                const int entry = idx / p.H_kv;
+                e = p.entries[entry];
+                if (kParts && chunk > 0) entry_row = p.entry_rows[entry];
+            }
+        };
+        auto read_sequence = [&]() {
+            if (idx < num_items) {
+                q = p.seqs[e.x];
+                base = p.key_base[e.x];
+            }
+        };
+        read_entry();
+        read_sequence();
         for (int n = 0; ok; ++n) {
             PackedItem it = {};
-            int k_first = 0, trow = 0, nk = 0;
+            int nk = 0, total = 0;  // keys of the sequence, key blocks of the item
+            const long long key_base = base;
             if (idx < num_items) {
-                const int4 e = p.entries[idx / p.H_kv];
-                const int4 q = p.seqs[e.x];
                 const int first = e.y * W2;
                 it.valid = 1;
                 it.kvh = idx % p.H_kv;
@@ -495,19 +533,25 @@ mha_packed_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 nk = q.z;
                 it.lim0 = p.causal ? nk - q.y + first : nk - 1;
                 it.b0 = e.z;
+                it.row_limits = p.prefix_lens && e.x < p.S;
+                const bool parts = kParts && chunk > 0 && (p.prefix_lens || it.ntok <= p.W || packed_tile_blocks(q.y, nk, p.causal, first, it.ntok) > chunk);
+                it.part_row = parts ? entry_row + it.kvh * packed_part_rows(p, it.ntok) : -1;
+                it.dual = parts && it.ntok <= p.W;
+                if (kParts && it.dual) {
+                    total = e.w;
+                    it.J[0] = (total + 1) >> 1;
+                    it.J[1] = total >> 1;
+                } else {
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
-                    it.J[t] = min(max(packed_tile_blocks(q.y, nk, p.causal, first + t * p.W, min(p.W, it.ntok - t * p.W)) - e.z, 0), e.w);
-                const bool parts = split && (p.prefix_lens || packed_tile_blocks(q.y, nk, p.causal, first, it.ntok) > chunk);
-                it.slot = parts ? idx : -1;
+                    for (int t = 0; t < 2; ++t)
+                        it.J[t] = min(max(packed_tile_blocks(q.y, nk, p.causal, first + t * p.W, min(p.W, it.ntok - t * p.W)) - e.z, 0), e.w);
+                    total = max(it.J[0], it.J[1]);
+                }
                 // V rows beyond the last key, up to the next cache block (the blocks after that load zeros)
                 const int tail = nk % kMhaBlock;
                 int tail_end = kMhaBlock;
                 if (!p.cu_k) tail_end = (tail + p.block_size - 1) / p.block_size * p.block_size;
-                const int Jm = max(it.J[0], it.J[1]);
-                if (Jm > 0 && it.b0 + Jm == packed_blocks(nk) && tail != 0 && tail < tail_end) it.fix = tail | (tail_end << 8);
-                if (p.cu_k) k_first = p.cu_k[e.x];
-                trow = p.prefix_lens ? q.x : e.x;
+                if (total > 0 && it.b0 + total == packed_blocks(nk) && tail != 0 && tail < tail_end) it.fix = tail | (tail_end << 8);
             }
             if (n >= 2) {
                 ok = wait_all(&item_empty[n & 1], ((n >> 1) - 1) & 1, 0x600);
@@ -519,76 +563,88 @@ mha_packed_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             }
             __syncwarp();
             if (!it.valid) break;
-            const int Jmax = max(it.J[0], it.J[1]);
 
-            // block-table entry of this lane's cache block of key block b, as a coordinate of the tensor map
+            // block-table entry of this lane's cache block of the item's key block b, as a coordinate of the tensor map
             const int nblk = p.cu_k ? 0 : (nk + p.block_size - 1) / p.block_size;
-            const int beyond = max(1, p.num_blocks * p.H_kv);  // loads zeros
             auto table_at = [&](int b) -> int {
-                const int i = b * nb + lane % nb;
-                return (b < it.b0 + Jmax && i < nblk) ? p.block_table[static_cast<int64_t>(trow) * p.max_blocks + i] : -1;
+                const int i = (it.b0 + b) * nb + lane_block;
+                return (b < total && i < nblk) ? p.block_table[key_base + i] : -1;
             };
-            auto coord = [&](int b, int phys) -> int {
-                if (phys >= 0 && phys < p.num_blocks) return phys * p.H_kv + it.kvh;
-                if (b * nb + lane % nb < nblk && lane < nb) packed_report(kStatusBadBlock, b * nb + lane, trow, phys);
-                return beyond;
-            };
-            int next_entry = p.cu_k ? 0 : table_at(it.b0);
-            int z[2] = {0, 0};
-            for (int i = 0; i < 2 * Jmax; ++i) {
-                bool is_k = (i & 1) == 0;
-                int blk = i >> 1;
-                if (D == 64 && i > 0) {  // K_0, K_1, V_0, K_2, V_1, ..., V_{J-1}
-                    if (i == 2 * Jmax - 1) {
-                        is_k = false;
-                        blk = Jmax - 1;
-                    } else {
-                        is_k = (i & 1) == 1;
-                        blk = is_k ? (i + 1) >> 1 : (i >> 1) - 1;
-                    }
-                }
-                if (i == 1) {  // Q: K_0 first, then the tiles once the previous item's last Q K^T has read them
-                    if (q_loads > 0) {
-                        ok = wait_all(q_empty, (q_loads - 1) & 1, 0x110);
-                        if (!ok) break;
-                    }
-                    ++q_loads;
-                    const int tiles = it.ntok > p.W ? 2 : 1;
-                    if (lane == 0) mbar_arrive_expect_tx(q_full, tiles * q_bytes);
-                    __syncwarp();
-                    if (lane < tiles * kChunks) {
-                        const int t = lane / kChunks, c = lane % kChunks;
-                        tma_load_3d(smem_q + t * L::kTileBytes + c * L::kChunkBytes, &tmap_q, q_full, c * 64, it.kvh * p.G, it.tok0 + t * p.W);
-                    }
-                    __syncwarp();
-                }
-                ok = wait_all(&kv_empty[ld_stage], ld_phase ^ 1, 0x100 + ld_stage);
-                if (!ok) break;
+            int next_entry = p.cu_k ? 0 : table_at(0);
+            constexpr int kHeld = kParts ? 4 : 2;
+            int z[4] = {0, 0, 0, 0};  // coordinates of the last kHeld key blocks
+            // key block b of the item, K or V (K blocks in order; V blocks less than kHeld behind)
+            auto load = [&](bool is_k, int b) -> bool {
+                if (!wait_all(&kv_empty[ld_stage], ld_phase ^ 1, 0x100 + ld_stage)) return false;
                 uint8_t* dst = smem_kv + ld_stage * L::kTileBytes;
                 if (lane == 0) mbar_arrive_expect_tx(&kv_full[ld_stage], L::kTileBytes);
                 __syncwarp();
                 const CUtensorMap* map = is_k ? &tmap_k : &tmap_v;
-                const int b = it.b0 + blk;
                 if (p.cu_k) {
-                    if (lane < kChunks) tma_load_3d(dst + lane * L::kChunkBytes, map, &kv_full[ld_stage], lane * 64, it.kvh, k_first + b * kMhaBlock);
+                    if (lane < kChunks)
+                        tma_load_3d(dst + lane * L::kChunkBytes, map, &kv_full[ld_stage], lane * 64, it.kvh, static_cast<int>(key_base) + (it.b0 + b) * kMhaBlock);
                 } else {
                     if (is_k) {
-                        const int zz = coord(b, next_entry);
-                        if (blk & 1) z[1] = zz; else z[0] = zz;
+                        int zz = beyond;
+                        if (next_entry >= 0 && next_entry < p.num_blocks) zz = next_entry * p.H_kv + it.kvh;
+                        else if (lane < nb && (it.b0 + b) * nb + lane < nblk) packed_report(kStatusBadBlock, (it.b0 + b) * nb + lane, it.tok0, next_entry);
+#pragma unroll
+                        for (int i = 0; i < kHeld; ++i)
+                            if ((b & (kHeld - 1)) == i) z[i] = zz;
                         next_entry = table_at(b + 1);
                     }
-                    if (lane < nb * kChunks) {
-                        const int c = lane / nb, piece = lane % nb;
-                        tma_load_3d(dst + c * L::kChunkBytes + piece * p.block_size * 128, map, &kv_full[ld_stage], c * 64, 0, (blk & 1) ? z[1] : z[0]);
-                    }
+                    int at = (b & 1) ? z[1] : z[0];
+                    if (kParts && (b & 2)) at = (b & 1) ? z[3] : z[2];
+                    if (lane_chunk < kChunks)
+                        tma_load_3d(dst + lane_chunk * L::kChunkBytes + lane_block * p.block_size * 128, map, &kv_full[ld_stage], lane_chunk * 64, 0, at);
                 }
                 __syncwarp();
                 if (++ld_stage == kStages) { ld_stage = 0; ld_phase ^= 1; }
+                return true;
+            };
+            // Q: after the first K, once the previous item's last Q K^T has read the tiles
+            auto load_q = [&]() -> bool {
+                if (q_loads > 0 && !wait_all(q_empty, (q_loads - 1) & 1, 0x110)) return false;
+                ++q_loads;
+                const int tiles = kParts && it.dual ? (total > 1 ? 2 : 1) : it.ntok > p.W ? 2 : 1;
+                const bool one = it.ntok == 1;
+                if (lane == 0) mbar_arrive_expect_tx(q_full, static_cast<uint32_t>(tiles) * (one ? 1 : p.W) * p.G * 128 * kChunks);
+                __syncwarp();
+                if (lane < tiles * kChunks) {
+                    const int t = lane / kChunks, c = lane % kChunks;
+                    tma_load_3d(smem_q + t * L::kTileBytes + c * L::kChunkBytes, one ? &tmap_q1 : &tmap_q, q_full, c * 64, it.kvh * p.G,
+                                it.tok0 + (kParts && it.dual ? 0 : t * p.W));
+                }
+                __syncwarp();
+                return true;
+            };
+            // Ring order (the issuing warps walk the same): K of the first step's blocks (one, with `dual` two), then V of a block and K
+            // of the next step's in turn; D = 64: all of a step's next K, then its V.  (One copy of `load`: code that is not
+            // in a loop is fetched cold every time.)
+            const int width = kParts && it.dual ? 2 : 1;
+            int n_k = 0, n_v = 0;
+            for (int i = 0; i < 2 * total && ok; ++i) {
+                const bool is_k = n_k < min(total, kEarlyQK ? (n_v & ~(width - 1)) + 2 * width : n_v + width);
+                if (i == 1) {
+                    ok = load_q();
+                    if (lane == 0) drawn = atomicAdd(&p.hdr->counter, 1);
+                }
+                ok = ok && load(is_k, is_k ? n_k : n_v);
+                n_k += is_k;
+                n_v += !is_k;
+                if (i == min(3, 2 * total - 1)) {
+                    idx = static_cast<int>(gridDim.x) + __shfl_sync(0xffffffffu, drawn, 0);
+                    read_entry();
+                }
             }
             if (!ok) break;
             if (it.fix && lane == 0) mbar_arrive(&v_asked[n & 1]);
-            if (lane == 0) idx = static_cast<int>(gridDim.x) + atomicAdd(&p.hdr->counter, 1);
-            idx = __shfl_sync(0xffffffffu, idx, 0);
+            if (total == 0) {
+                if (lane == 0) drawn = atomicAdd(&p.hdr->counter, 1);
+                idx = static_cast<int>(gridDim.x) + __shfl_sync(0xffffffffu, drawn, 0);
+                read_entry();
+            }
+            read_sequence();
         }
     } else if (warp == 8 || (warp == 10 && kIssuers == 2)) {
         // ------------------------------- UMMA issuer -------------------------------
@@ -637,114 +693,159 @@ mha_packed_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
         for (int n = 0; ok && take_item(n, 0x210); ++n) {
             const PackedItem& it = items[n & 1];
             const int J0 = it.J[0], J1 = it.J[1], Jmax = max(J0, J1);
+            const bool fix = it.fix != 0;
+            const bool dual = kParts && it.dual;
+            const int fix_step = fix ? (dual ? J0 + J1 : Jmax) - 1 : -1;  // the block whose V tile has a tail
             if (Jmax > 0) {
                 ok = wait_all(q_full, n_q & 1, 0x200);
                 if (!ok) break;
                 ++n_q;
             }
-            const bool fix = it.fix != 0;
-            const int fix_step = fix ? Jmax - 1 : -1;  // the step whose V tile has a tail
-            if constexpr (kEarlyQK) {
-                // Step j: Q_t K_{j+1}^T as soon as S_t(j) has been read, then P_t(j) V_j, for this warp's tile
+            if (dual) {
+                // As below, but every tile in the ring belongs to one query tile (tile t: blocks t, t + 2, ...).  D = 64: both issuing
+                // warps walk the whole ring and release every slot.
 #pragma unroll 1
-                for (int j = -1; j < Jmax && ok; ++j) {
-                    if (j + 1 < Jmax) {
-                        const int kslot = stage;
-                        ok = wait_all(&kv_full[kslot], phase, 0x240 + kslot);
+                for (int j = -1; j < J0 && ok; ++j) {
+#pragma unroll 1
+                    for (int i = 0; i < 4 && ok; ++i) {
+                        // D = 128: V and the next K of tile 0, then of tile 1;  D = 64: the next K of both tiles, then V of both
+                        const int t = kEarlyQK ? i & 1 : i >> 1, Jt = t ? J1 : J0;
+                        const bool is_k = kEarlyQK ? i < 2 : (i & 1);
+                        if (is_k ? j + 1 >= Jt : (j < 0 || j >= Jt)) continue;
+                        const int slot = stage;
+                        ok = wait_all(&kv_full[slot], phase, 0x240 + slot);
                         if (!ok) break;
                         if (++stage == kStages) { stage = 0; phase ^= 1; }
-                        tc_fence_after();
-                        for (int t = t_lo; t < t_hi && ok; ++t) {
-                            if (j + 1 >= (t ? J1 : J0)) continue;
-                            if (n_qk[t] > 0) {
-                                ok = wait_all(&s_free[t], (n_qk[t] - 1) & 1, 0x250 + t);
+                        if (t >= t_lo && t < t_hi) {
+                            if (is_k) {
+                                const uint32_t done = t ? n_qk[1] : n_qk[0];
+                                if (kEarlyQK && done > 0) ok = wait_all(&s_free[t], (done - 1) & 1, 0x250 + t);
                                 if (!ok) break;
+                                if (t) ++n_qk[1]; else ++n_qk[0];
                                 tc_fence_after();
+                                issue_qk(t, slot);
+                            } else {
+                                if (2 * j + t == fix_step) ok = wait_all(&v_fixed[n & 1], (fixed >> (n & 1)) & 1, 0x260);
+                                ok = ok && wait_all(&p_full[t], (t ? n_p[1] : n_p[0]) & 1, 0x230 + t);
+                                if (!ok) break;
+                                if (t) ++n_p[1]; else ++n_p[0];
+                                tc_fence_after();
+                                issue_pv(t, slot, j == 0);
+                                if (leader) {
+                                    if (kEarlyQK) umma_commit(&p_free[t]);
+                                    if (j == Jt - 1) umma_commit(&o_full[t]);
+                                }
                             }
-                            ++n_qk[t];
-                            issue_qk(t, kslot);
                         }
-                        if (!ok) break;
-                        if (leader) {
-                            umma_commit(&kv_empty[kslot]);
-                            if (j + 2 == Jmax) umma_commit(q_empty);
-                        }
+                        if (leader) umma_commit(&kv_empty[slot]);
                         __syncwarp();
                     }
-                    if (j >= 0) {
-                        const int vslot = stage;
-                        ok = wait_all(&kv_full[vslot], phase, 0x220 + vslot);
-                        if (!ok) break;
-                        if (j == fix_step) {
-                            ok = wait_all(&v_fixed[n & 1], (fixed >> (n & 1)) & 1, 0x260);
+                    if (ok && j + 2 == J0 && leader) umma_commit(q_empty);  // the item's last Q K^T products are issued
+                    __syncwarp();
+                }
+            } else {
+                if constexpr (kEarlyQK) {
+                    // Step j: Q_t K_{j+1}^T as soon as S_t(j) has been read, then P_t(j) V_j, for this warp's tile
+#pragma unroll 1
+                    for (int j = -1; j < Jmax && ok; ++j) {
+                        if (j + 1 < Jmax) {
+                            const int kslot = stage;
+                            ok = wait_all(&kv_full[kslot], phase, 0x240 + kslot);
                             if (!ok) break;
-                        }
-                        if (++stage == kStages) { stage = 0; phase ^= 1; }
-                        for (int t = t_lo; t < t_hi && ok; ++t) {
-                            const int Jt = t ? J1 : J0;
-                            if (j >= Jt) continue;
-                            ok = wait_all(&p_full[t], n_p[t] & 1, 0x230 + t);
-                            if (!ok) break;
-                            ++n_p[t];
+                            if (++stage == kStages) { stage = 0; phase ^= 1; }
                             tc_fence_after();
-                            issue_pv(t, vslot, j == 0);
+                            for (int t = t_lo; t < t_hi && ok; ++t) {
+                                if (j + 1 >= (t ? J1 : J0)) continue;
+                                if (n_qk[t] > 0) {
+                                    ok = wait_all(&s_free[t], (n_qk[t] - 1) & 1, 0x250 + t);
+                                    if (!ok) break;
+                                    tc_fence_after();
+                                }
+                                ++n_qk[t];
+                                issue_qk(t, kslot);
+                            }
+                            if (!ok) break;
                             if (leader) {
-                                umma_commit(&p_free[t]);
-                                if (j == Jt - 1) umma_commit(&o_full[t]);
+                                umma_commit(&kv_empty[kslot]);
+                                if (j + 2 == Jmax) umma_commit(q_empty);
                             }
                             __syncwarp();
                         }
-                        if (!ok) break;
-                        if (leader) umma_commit(&kv_empty[vslot]);
-                        __syncwarp();
-                    }
-                }
-            } else {
-                // Step j issues P_t(j) V_j and then Q_t K_{j+1}^T for both tiles; step -1 only the first Q K^T products
-#pragma unroll 1
-                for (int j = -1; j < Jmax && ok; ++j) {
-                    int vslot = 0;
-                    if (j >= 0) {
-                        vslot = stage;
-                        ok = wait_all(&kv_full[vslot], phase, 0x220 + vslot);
-                        if (!ok) break;
-                        if (j == fix_step) {
-                            ok = wait_all(&v_fixed[n & 1], (fixed >> (n & 1)) & 1, 0x260);
+                        if (j >= 0) {
+                            const int vslot = stage;
+                            ok = wait_all(&kv_full[vslot], phase, 0x220 + vslot);
                             if (!ok) break;
-                        }
-                        if (++stage == kStages) { stage = 0; phase ^= 1; }
-                    }
-                    const int kslot = stage;  // K_{j+1}, if there is one
-                    bool k_ready = false;
-                    for (int t = 0; t < 2 && ok; ++t) {
-                        const int Jt = t ? J1 : J0;
-                        if (j >= 0 && j < Jt) {
-                            ok = wait_all(&p_full[t], n_p[t] & 1, 0x230 + t);
-                            if (!ok) break;
-                            ++n_p[t];
-                            tc_fence_after();
-                            issue_pv(t, vslot, j == 0);
-                            if (j == Jt - 1 && leader) umma_commit(&o_full[t]);
-                        }
-                        if (j + 1 < Jt) {
-                            if (!k_ready) {
-                                ok = wait_all(&kv_full[kslot], phase, 0x240 + kslot);
+                            if (j == fix_step) {
+                                ok = wait_all(&v_fixed[n & 1], (fixed >> (n & 1)) & 1, 0x260);
                                 if (!ok) break;
-                                tc_fence_after();
-                                k_ready = true;
                             }
-                            issue_qk(t, kslot);
+                            if (++stage == kStages) { stage = 0; phase ^= 1; }
+                            for (int t = t_lo; t < t_hi && ok; ++t) {
+                                const int Jt = t ? J1 : J0;
+                                if (j >= Jt) continue;
+                                ok = wait_all(&p_full[t], n_p[t] & 1, 0x230 + t);
+                                if (!ok) break;
+                                ++n_p[t];
+                                tc_fence_after();
+                                issue_pv(t, vslot, j == 0);
+                                if (leader) {
+                                    umma_commit(&p_free[t]);
+                                    if (j == Jt - 1) umma_commit(&o_full[t]);
+                                }
+                                __syncwarp();
+                            }
+                            if (!ok) break;
+                            if (leader) umma_commit(&kv_empty[vslot]);
+                            __syncwarp();
                         }
                     }
-                    if (!ok) break;
-                    if (leader) {
-                        if (j >= 0) umma_commit(&kv_empty[vslot]);
-                        if (j + 1 < Jmax) umma_commit(&kv_empty[kslot]);
-                        if (j + 2 == Jmax) umma_commit(q_empty);
-                    }
-                    __syncwarp();
-                    if (j + 1 < Jmax) {
-                        if (++stage == kStages) { stage = 0; phase ^= 1; }
+                } else {
+                    // Step j issues P_t(j) V_j and then Q_t K_{j+1}^T for both tiles; step -1 only the first Q K^T products
+#pragma unroll 1
+                    for (int j = -1; j < Jmax && ok; ++j) {
+                        int vslot = 0;
+                        if (j >= 0) {
+                            vslot = stage;
+                            ok = wait_all(&kv_full[vslot], phase, 0x220 + vslot);
+                            if (!ok) break;
+                            if (j == fix_step) {
+                                ok = wait_all(&v_fixed[n & 1], (fixed >> (n & 1)) & 1, 0x260);
+                                if (!ok) break;
+                            }
+                            if (++stage == kStages) { stage = 0; phase ^= 1; }
+                        }
+                        const int kslot = stage;  // K_{j+1}, if there is one
+                        bool k_ready = false;
+                        for (int t = 0; t < 2 && ok; ++t) {
+                            const int Jt = t ? J1 : J0;
+                            if (j >= 0 && j < Jt) {
+                                ok = wait_all(&p_full[t], n_p[t] & 1, 0x230 + t);
+                                if (!ok) break;
+                                ++n_p[t];
+                                tc_fence_after();
+                                issue_pv(t, vslot, j == 0);
+                                if (j == Jt - 1 && leader) umma_commit(&o_full[t]);
+                            }
+                            if (j + 1 < Jt) {
+                                if (!k_ready) {
+                                    ok = wait_all(&kv_full[kslot], phase, 0x240 + kslot);
+                                    if (!ok) break;
+                                    tc_fence_after();
+                                    k_ready = true;
+                                }
+                                issue_qk(t, kslot);
+                            }
+                        }
+                        if (!ok) break;
+                        if (leader) {
+                            if (j >= 0) umma_commit(&kv_empty[vslot]);
+                            if (j + 1 < Jmax) umma_commit(&kv_empty[kslot]);
+                            if (j + 2 == Jmax) umma_commit(q_empty);
+                        }
+                        __syncwarp();
+                        if (j + 1 < Jmax) {
+                            if (++stage == kStages) { stage = 0; phase ^= 1; }
+                        }
                     }
                 }
             }
@@ -760,8 +861,7 @@ mha_packed_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             uint32_t fixed = 0;  // bit: parity of v_asked of an item slot
             for (int n = 0; take_item(n, 0x720); ++n) {
                 const PackedItem& it = items[n & 1];
-                const int Jmax = max(it.J[0], it.J[1]);
-                pos += 2 * Jmax;
+                pos += 2 * (kParts && it.dual ? it.J[0] + it.J[1] : max(it.J[0], it.J[1]));
                 if (it.fix) {  // the item's last ring tile is its last V tile
                     // (a barrier's parity says something only about the phase that is under way and the one before it: the stage's
                     // earlier uses are over once the loader has requested this one)
@@ -799,18 +899,39 @@ mha_packed_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
         bool ok = true;
         for (int n = 0; ok && take_item(n, 0x320); ++n) {
             const PackedItem& it = items[n & 1];
-            const int tile_tok = it.ntok - t * p.W;  // tokens of this tile, if positive
-            if (tile_tok <= 0) {
+            const int dual = kParts ? it.dual : 0;
+            const int tok_shift = dual ? 0 : t * p.W;           // first token of this tile in the pair
+            const int tile_tok = min(it.ntok - tok_shift, p.W);  // its tokens, if positive
+            const int Jt = it.J[t], first_block = it.b0 + (dual ? t : 0), block_step = dual ? 2 : 1;
+            if (tile_tok <= 0 || (dual && Jt == 0)) {
                 drop_item(n);
                 continue;
             }
-            const int Jt = it.J[t], first_block = it.b0;
+            const bool busy = quarter * 32 < tile_tok * p.G;  // this warp has a row of a token
             // last visible key; rows without a token take the last token's, so that they mask no more than their neighbours
             int limit = it.lim0;
-            if (p.causal) limit += t * p.W + min(row_tok, min(tile_tok, p.W) - 1);
-            if (p.seq_lens && row_tok < tile_tok) limit = min(limit, p.seq_lens[it.tok0 + t * p.W + min(row_tok, p.W - 1)] - 1);
+            if (p.causal) limit += tok_shift + min(row_tok, tile_tok - 1);
+            if (kParts && it.row_limits && row_tok < tile_tok) limit = min(limit, p.seq_lens[it.tok0 + tok_shift + row_tok] - 1);
             float m_run = -INFINITY, l_run = 0.0f;
 
+            if (kParts && !busy) {  // nobody reads this warp's rows: P_t may be anything there
+                for (int j = 0; j < Jt && ok; ++j) {
+                    ok = wait_all(&s_full[t], n_s & 1, 0x340 + t);
+                    ++n_s;
+                    if constexpr (kEarlyQK) {
+                        if (ok && lane == 0) mbar_arrive(&s_free[t]);
+                        // (not ahead of the busy warps: a second arrival in p_full's phase would stand for theirs)
+                        if (n_s > 1) ok = ok && wait_all(&p_free[t], n_s & 1, 0x330 + t);
+                    }
+                    __syncwarp();
+                    if (ok && lane == 0) mbar_arrive(&p_full[t]);
+                }
+                if (Jt > 0) ok = ok && wait_all(&o_full[t], n_o & 1, 0x410 + t);
+                n_o += Jt > 0;
+                if (!ok) break;
+                drop_item(n);
+                continue;
+            }
             for (int j = 0; j < Jt; ++j) {
                 ok = wait_all(&s_full[t], n_s & 1, 0x300 + t);
                 if (!ok) break;
@@ -825,7 +946,7 @@ mha_packed_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&s_free[t]);
                 }
-                const int j0 = (first_block + j) * kMhaBlock;
+                const int j0 = (first_block + j * block_step) * kMhaBlock;
                 if (j0 + kMhaBlock - 1 > limit) {
 #pragma unroll
                     for (int q = 0; q < 4; ++q)
@@ -918,65 +1039,91 @@ mha_packed_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 ++n_o;
                 tc_fence_after();
             }
-            // Rows leave in pieces of 128 bytes: each thread puts its row's piece into the warp's staging area (16-byte chunk k of
-            // row r at chunk k ^ (r & 7): no bank conflicts either way), then eight lanes at a time write a row's piece.
-            auto put = [&](int k, uint32_t a, uint32_t b, uint32_t c2, uint32_t d) {
-                *reinterpret_cast<uint4*>(stage_o + lane * 128 + ((k ^ (lane & 7)) * 16)) = make_uint4(a, b, c2, d);
-            };
-            auto send = [&](uint64_t dst) {  // dst: where this thread's row's piece goes, 0: nowhere
-                __syncwarp();
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int row = i * 4 + (lane >> 3), k = lane & 7;
-                    const uint64_t to = __shfl_sync(0xffffffffu, dst, row);
-                    const uint4 v = *reinterpret_cast<const uint4*>(stage_o + row * 128 + ((k ^ (row & 7)) * 16));
-                    if (to) *reinterpret_cast<uint4*>(to + k * 16) = v;
-                }
-                __syncwarp();
-            };
+            // Rows leave in pieces of 128 bytes (64 columns of O, 32 of a partial result): each thread puts its row's piece into the warp's
+            // staging area (16-byte chunk k of row r at chunk k ^ (r & 7), the tensor maps' 128-byte swizzle).  A warp whose 32 rows
+            // are all tokens' stores it as one TMA box; else eight lanes at a time write a row's piece.  (An epilogue of plain
+            // stores alone took 5200 clocks at D = 128: 1600 to convert, 3100 to read the staging area back and store.)
+            // Short loops throughout: what runs once per item is fetched cold.
+            const bool direct = !kParts || it.part_row < 0;
             const bool seen = m_run != -INFINITY;
-            const bool valid = row_tok < min(it.ntok - t * p.W, p.W);
-            const int tok = it.tok0 + t * p.W + row_tok, head = it.kvh * p.G + row_head;
-            if (it.slot < 0) {
-                const float inv_l = seen ? __fdividef(1.0f, l_run) : 0.0f;
-                const uint64_t row_at = valid ? reinterpret_cast<uint64_t>(p.O + static_cast<int64_t>(tok) * p.ldo + head * D) : 0;
+            const int shift = dual ? t * it.ntok * p.G : t * kMhaBlock;  // of a partial result's rows
+            uint8_t* base;       // where the tile's token 0, head 0 goes, and the bytes from one token and from one head to the next
+            int64_t tok_bytes;
+            int head_bytes;
+            if (direct) {
+                base = reinterpret_cast<uint8_t*>(p.O + static_cast<int64_t>(it.tok0 + tok_shift) * p.ldo + it.kvh * p.G * D);
+                tok_bytes = p.ldo * 2;
+                head_bytes = D * 2;
+            } else {
+                base = reinterpret_cast<uint8_t*>(p.part_o + (static_cast<int64_t>(it.part_row) + shift) * D);
+                tok_bytes = p.G * D * 4;
+                head_bytes = D * 4;
+            }
+            base += (lane & 7) * 16;
+            const float inv_l = seen ? __fdividef(1.0f, l_run) : 0.0f;
+            const float2 factor = make_float2(inv_l, inv_l);
+            const int columns = direct ? 64 : 32;  // of a piece
+            const bool boxed = p.boxes && quarter * 32 + 32 <= tile_tok * p.G;
 #pragma unroll 1
-                for (int h = 0; h < D / 32; ++h) {  // 32 columns: half a piece
-                    uint32_t o[32];
-                    if (Jt > 0) {
-                        tmem_ld_32x32b_x32(o_addr + h * 32, o);
-                        tmem_wait_ld();
-                    }
+            for (int h = 0; (direct || Jt > 0) && h < D; h += 32) {
+                uint32_t o[32];
+                if (Jt > 0) tmem_ld_32x32b_x32(o_addr + h, o);
+                if (lane == 0) tma_store_wait_read<0>();  // the staging area's previous box has been read out
+                __syncwarp();
+                tmem_wait_ld();
+                if (Jt == 0) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) o[i] = 0u;
+                }
+                if (!direct) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        *reinterpret_cast<uint4*>(stage_o + lane * 128 + ((k ^ (lane & 7)) * 16)) = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+                } else {
+                    const int first = (h & 32) >> 3;  // chunk
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        uint32_t w[4] = {0u, 0u, 0u, 0u};
-                        if (Jt > 0 && seen) {
+                        uint32_t w[4];
 #pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                w[e] = pack_bf16x2(__uint_as_float(o[8 * k + 2 * e]) * inv_l, __uint_as_float(o[8 * k + 2 * e + 1]) * inv_l);
+                        for (int e = 0; e < 4; ++e) {  // (a row that sees nothing: its O is finite, and times 0)
+                            const float2 v = fmul2(make_float2(__uint_as_float(o[8 * k + 2 * e]), __uint_as_float(o[8 * k + 2 * e + 1])), factor);
+                            w[e] = pack_bf16x2(v.x, v.y);
                         }
-                        put((h & 1) * 4 + k, w[0], w[1], w[2], w[3]);
+                        *reinterpret_cast<uint4*>(stage_o + lane * 128 + (((first + k) ^ (lane & 7)) * 16)) = make_uint4(w[0], w[1], w[2], w[3]);
                     }
-                    if (h & 1) send(row_at ? row_at + (h >> 1) * 128 : 0);
+                    if ((h & 32) == 0) continue;
                 }
-                if (valid && p.LSE)
-                    p.LSE[static_cast<int64_t>(tok) * p.H + head] = seen ? m_run * p.scale + __log2f(l_run) * 0.6931471805599453f : -INFINITY;
-            } else if (Jt > 0) {
-                const int64_t row = static_cast<int64_t>(it.slot) * p.slot_rows + t * kMhaBlock + row_in_tile;
-                const uint64_t row_at = valid ? reinterpret_cast<uint64_t>(p.part_o + row * D) : 0;
-#pragma unroll 1
-                for (int h = 0; h < D / 32; ++h) {
-                    uint32_t o[32];
-                    tmem_ld_32x32b_x32(o_addr + h * 32, o);
-                    tmem_wait_ld();
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) put(k, o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
-                    send(row_at ? row_at + h * 128 : 0);
+                if (boxed) {
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (direct) tma_store_3d(&tmap_o, stage_o, h - 32, it.kvh * p.G, it.tok0 + tok_shift + quarter * 32 / p.G);
+                        else tma_store_2d(&tmap_part, stage_o, h, it.part_row + shift + quarter * 32);
+                        tma_store_commit();
+                    }
+                    continue;
                 }
-                if (valid) p.part_ml[row] = make_float2(seen ? m_run * c : -INFINITY, seen ? l_run : 0.0f);
+                __syncwarp();
+                uint8_t* to = base + (h / columns) * 128;
+#pragma unroll 2
+                for (int i = 0; i < 32; i += 4) {
+                    const int row = i + (lane >> 3), at = row_of[quarter * 32 + row];
+                    const uint4 v = *reinterpret_cast<const uint4*>(stage_o + row * 128 + (((lane & 7) ^ (row & 7)) * 16));
+                    if ((at >> 16) < tile_tok) *reinterpret_cast<uint4*>(to + (at >> 16) * tok_bytes + (at & 0xFFFF) * head_bytes) = v;
+                }
+                __syncwarp();
+            }
+            if (row_tok < tile_tok) {
+                if (!direct) {
+                    if (Jt > 0) p.part_ml[static_cast<int64_t>(it.part_row) + shift + row_in_tile] = make_float2(seen ? m_run * c : -INFINITY, seen ? l_run : 0.0f);
+                } else if (p.LSE) {
+                    p.LSE[static_cast<int64_t>(it.tok0 + tok_shift + row_tok) * p.H + it.kvh * p.G + row_head] =
+                        seen ? m_run * p.scale + __log2f(l_run) * 0.6931471805599453f : -INFINITY;
+                }
             }
             drop_item(n);
         }
+        if (lane == 0) tma_store_wait_all<0>();  // shared memory must outlive the stores that read it
     }
 
     // common exit: every role reaches this, also after an aborted wait
@@ -990,7 +1137,7 @@ mha_packed_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
     }
 }
 
-// Joins the parts of cut key ranges, and of tails behind a shared prefix: one warp per (token, head).
+// Joins the parts of cut key ranges, and a prefix with the tail behind it: one warp per (token, head).
 constexpr int kPackedJoinWarps = 8;
 template <int D>
 __global__ void __launch_bounds__(kPackedJoinWarps * 32) mha_packed_join_kernel(const PackedParams p) {
@@ -1003,50 +1150,82 @@ __global__ void __launch_bounds__(kPackedJoinWarps * 32) mha_packed_join_kernel(
     const int64_t row = static_cast<int64_t>(blockIdx.x) * kPackedJoinWarps + (threadIdx.x >> 5);
     if (row >= static_cast<int64_t>(p.T) * p.H) return;
     const int tok = static_cast<int>(row / p.H), h = static_cast<int>(row % p.H);
-    int lo = 0, hi = p.S;  // the last sequence that begins at or before the token
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (p.cu_q[mid] <= tok) lo = mid; else hi = mid;
+    // This row's parts: up to two runs (a prefix's and a tail's), each of n parts at rows first + k * step, or first + (k / 2) * step +
+    // (k % 2) * half where both tiles had the same rows.
+    int first[2] = {0, 0}, step[2] = {0, 0}, half[2] = {0, 0}, count[2] = {0, 0};
+    auto run = [&](int i, const int4& q, int token) {  // the token's row in sequence q; false: its item has written the result
+        const int W2 = 2 * p.W, pair = token / W2, begin = pair * W2, n = min(W2, q.y - begin);
+        const int whole = packed_tile_blocks(q.y, q.z, p.causal, begin, n), rows = packed_part_rows(p, n), in_pair = token - begin;
+        step[i] = rows * p.H_kv;
+        first[i] = p.tile_rows[q.w + pair] + h / p.G * rows + h % p.G;
+        if (n <= p.W) {
+            half[i] = n * p.G;
+            first[i] += in_pair * p.G;
+            count[i] = whole / chunk * min(2, chunk) + min(2, whole % chunk);  // (a single block is the first tile's alone)
+        } else {
+            if (!p.prefix_lens && whole <= chunk) return false;
+            const int t = in_pair / p.W;
+            first[i] += t * kMhaBlock + (in_pair - t * p.W) * p.G;
+            count[i] = (packed_tile_blocks(q.y, q.z, p.causal, begin + t * p.W, min(p.W, n - t * p.W)) + chunk - 1) / chunk;
+        }
+        return true;
+    };
+    const int owner = packed_owner(p, tok);
+    if (p.prefix_lens) {
+        if (owner >= 0) {
+            const int4 q = p.seqs[owner];
+            if (tok - q.x < q.y) run(0, q, tok - q.x);
+        }
+        const int4 q = p.seqs[p.S + tok];
+        if (q.y > 0) run(1, q, 0);
+    } else {
+        if (owner < 0) return;  // a token of no sequence
+        const int4 q = p.seqs[owner];
+        if (tok - q.x >= q.y || !run(0, q, tok - q.x)) return;
     }
-    const int4 q = p.seqs[lo];
-    const int i = tok - q.x;
-    int parts = 0;
-    int64_t part0 = 0;
-    if (i >= 0 && i < q.y) {
-        const int W2 = 2 * p.W, pair = i / W2, first = pair * W2, t = (i - first) / p.W;
-        const int n = min(W2, q.y - first);
-        // a range that is not cut was written by its item
-        if (!p.prefix_lens && packed_tile_blocks(q.y, q.z, p.causal, first, n) <= chunk) return;
-        const int blocks = packed_tile_blocks(q.y, q.z, p.causal, first + t * p.W, min(p.W, n - t * p.W));
-        parts = (blocks + chunk - 1) / chunk;
-        const int r = t * kMhaBlock + (i - first - t * p.W) * p.G + h % p.G;
-        part0 = (static_cast<int64_t>(p.tile_first[q.w + pair]) * p.H_kv + h / p.G) * p.slot_rows + r;
-    } else if (!p.prefix_lens) {
-        return;  // a token of no sequence
-    }
-    const int64_t step = static_cast<int64_t>(p.H_kv) * p.slot_rows;
-    const int tails = p.prefix_lens ? p.tail_parts[static_cast<int64_t>(tok) * p.H_kv + h / p.G] : 0;
-    const int all = parts + tails;
-    const int64_t tail0 = row * p.tail.splits;
-    auto stat = [&](int k) { return k < parts ? p.part_ml[part0 + k * step] : p.tail.part_ml[tail0 + k - parts]; };
+    const int all = count[0] + count[1];
+    auto part = [&](int k) -> int64_t {
+        const int i = k < count[0] ? 0 : 1;
+        if (i) k -= count[0];
+        // parts of two tiles come in pairs, but for chunks of one block
+        if (half[i] && chunk > 1) return static_cast<int64_t>(first[i]) + static_cast<int64_t>(k >> 1) * step[i] + (k & 1) * half[i];
+        return static_cast<int64_t>(first[i]) + static_cast<int64_t>(k) * step[i];
+    };
     float m = -INFINITY;
-    for (int k = lane; k < all; k += 32) m = fmaxf(m, stat(k).x);
+    for (int k = lane; k < all; k += 32) m = fmaxf(m, p.part_ml[part(k)].x);
 #pragma unroll
     for (int w = 16; w > 0; w >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, w));
     float l = 0.0f, o[V] = {};
     for (int k0 = 0; k0 < all; k0 += 32) {
         float weight = 0.0f;
         if (k0 + lane < all) {
-            const float2 ml = stat(k0 + lane);
+            const float2 ml = p.part_ml[part(k0 + lane)];
             weight = ml.x == -INFINITY ? 0.0f : fast_exp2(ml.x - m);
             l += weight * ml.y;
         }
-        for (int k = 0; k < 32 && k0 + k < all; ++k) {
-            const float w = __shfl_sync(0xffffffffu, weight, k);
-            if (w == 0.0f) continue;  // (a part without a visible key)
-            const float* src = (k0 + k < parts ? p.part_o + (part0 + (k0 + k) * step) * D : p.tail.part_o + (tail0 + k0 + k - parts) * D) + lane * V;
+        for (int k1 = 0; k1 < 32 && k0 + k1 < all; k1 += 4) {  // four parts' loads in flight
+            float v[4][V], w[4];
 #pragma unroll
-            for (int e = 0; e < V; ++e) o[e] = fmaf(src[e], w, o[e]);
+            for (int i = 0; i < 4; ++i) {
+                w[i] = __shfl_sync(0xffffffffu, weight, k1 + i);
+                if (k0 + k1 + i >= all) w[i] = 0.0f;
+#pragma unroll
+                for (int e = 0; e < V; ++e) v[i][e] = 0.0f;
+                if (w[i] != 0.0f) {  // (0: a part without a visible key)
+                    const float* src = p.part_o + part(k0 + k1 + i) * D + lane * V;
+                    if constexpr (V == 4) {
+                        const float4 f = *reinterpret_cast<const float4*>(src);
+                        v[i][0] = f.x; v[i][1] = f.y; v[i][2] = f.z; v[i][3] = f.w;
+                    } else {
+                        const float2 f = *reinterpret_cast<const float2*>(src);
+                        v[i][0] = f.x; v[i][1] = f.y;
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int e = 0; e < V; ++e) o[e] = fmaf(v[i][e], w[i], o[e]);
         }
     }
 #pragma unroll
@@ -1056,44 +1235,55 @@ __global__ void __launch_bounds__(kPackedJoinWarps * 32) mha_packed_join_kernel(
 #pragma unroll
     for (int e = 0; e < V / 2; ++e) packed[e] = pack_bf16x2(o[2 * e] * inv, o[2 * e + 1] * inv);
     __nv_bfloat16* dst = p.O + static_cast<int64_t>(tok) * p.ldo + h * D + lane * V;
-#pragma unroll
-    for (int e = 0; e < V / 2; ++e) reinterpret_cast<uint32_t*>(dst)[e] = packed[e];
+    if constexpr (V == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(packed[0], packed[1]);
+    else *reinterpret_cast<uint32_t*>(dst) = packed[0];
     if (lane == 0 && p.LSE) p.LSE[row] = l > 0.0f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
 }
 
-// Scratch: header, sequences, entries, first entries, partial results.
+// Scratch: header, sequences, key bases, entries, their rows, tile pairs' rows, partial results.
 struct PackedScratch {
-    size_t seqs, entries, tile_first, part_ml, part_o;  // byte offsets
-    size_t lists;                                       // bytes without partial results
-    size_t slot_bytes;
-    int64_t slots;                                      // parts that scratch is sized for
-    int max_tiles, max_entries, slot_rows, W;
+    size_t seqs, key_base, entries, entry_rows, tile_rows;  // byte offsets
+    size_t lists;                                           // bytes without partial results
+    size_t row_bytes;
+    int64_t part_rows;  // rows of partial results that it is sized for
+    int64_t max_tiles, max_entries;
+    int W;
 };
+// S sequences of T tokens in all; prefix: S groups, with a tail behind them for each of the T sequences.
 inline PackedScratch packed_scratch(int64_t T, int64_t S, int G, int H_kv, int D, bool prefix = false) {
     PackedScratch x;
     auto up = [](size_t v) { return (v + 255) & ~size_t(255); };
     x.W = kMhaBlock / G;
-    const int64_t tiles = T / (2 * x.W) + S;
-    x.max_tiles = static_cast<int>(tiles);
-    x.slots = prefix ? std::max<int64_t>(kPackedMaxSlots, tiles * H_kv) : kPackedMaxSlots;  // (a prefix's results all go to the join)
-    x.max_entries = static_cast<int>(std::max<int64_t>(tiles, x.slots / H_kv));
-    x.slot_rows = static_cast<int>(T * G <= kMhaBlock ? T * G : 2 * kMhaBlock);
+    const int64_t pairs = T / (2 * x.W) + S, all = prefix ? S + T : S;
+    x.max_tiles = prefix ? pairs + T : pairs;
+    // A row needs two partial results at least where it is cut (one per tile), and few rows more parts than many.
+    const int64_t rows = T * G * H_kv;
+    x.part_rows = std::min<int64_t>(kPackedSplitRows, 320 * 2 * T * G);
+    if (prefix) x.part_rows += pairs * 2 * kMhaBlock * H_kv + 2 * rows;
+    x.max_entries = std::max<int64_t>(x.max_tiles, std::min<int64_t>(x.part_rows / (2 * H_kv), (1 << 17)));
     x.seqs = 256;
-    x.entries = up(x.seqs + static_cast<size_t>(S) * 16);
-    x.tile_first = up(x.entries + static_cast<size_t>(x.max_entries) * 16);
-    x.lists = up(x.tile_first + static_cast<size_t>(std::min<int64_t>(tiles, kPackedMaxSplitTiles)) * 4);
-    x.slot_bytes = static_cast<size_t>(x.slot_rows) * (static_cast<size_t>(D) * 4 + 8);
+    x.key_base = up(x.seqs + static_cast<size_t>(all) * 16);
+    x.entries = up(x.key_base + static_cast<size_t>(all) * 8);
+    x.entry_rows = up(x.entries + static_cast<size_t>(x.max_entries) * 16);
+    x.tile_rows = up(x.entry_rows + static_cast<size_t>(x.max_entries) * 4);
+    x.lists = up(x.tile_rows + static_cast<size_t>(std::min<int64_t>(x.max_tiles, kPackedSplitTiles)) * 4);
+    x.row_bytes = static_cast<size_t>(D) * 4 + 8;
     return x;
 }
 
 inline int packed_configure() {  // as mha_configure: 0, 1 (a CUDA call failed), 2 (too few registers for the hand-over)
-    if (cudaFuncSetAttribute(mha_packed_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, PackedSmem<64>::kTotal) != cudaSuccess ||
-        cudaFuncSetAttribute(mha_packed_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, PackedSmem<128>::kTotal) != cudaSuccess)
-        return 1;
-    cudaFuncAttributes a64, a128;
-    if (cudaFuncGetAttributes(&a64, mha_packed_kernel<64>) != cudaSuccess || cudaFuncGetAttributes(&a128, mha_packed_kernel<128>) != cudaSuccess)
-        return 1;
-    return a64.numRegs < kMhaMinRegsPerThread || a128.numRegs < kMhaMinRegsPerThread ? 2 : 0;
+    if (cudaFuncSetAttribute(mha_packed_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPackedPlanSmem) != cudaSuccess) return 1;
+    auto one = [](auto* kernel, int smem) {
+        cudaFuncAttributes a;
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess || cudaFuncGetAttributes(&a, kernel) != cudaSuccess)
+            return 1;
+        return a.numRegs < kMhaMinRegsPerThread ? 2 : 0;
+    };
+    const int rc[4] = {one(mha_packed_kernel<64, false>, PackedSmem<64>::kTotal), one(mha_packed_kernel<64, true>, PackedSmem<64>::kTotal),
+                       one(mha_packed_kernel<128, false>, PackedSmem<128>::kTotal), one(mha_packed_kernel<128, true>, PackedSmem<128>::kTotal)};
+    int worst = 0;
+    for (int r : rc) worst = r == 1 || worst == 1 ? 1 : std::max(worst, r);
+    return worst;
 }
 
 template <class... Params, class... Args>
@@ -1111,17 +1301,19 @@ inline bool packed_launch_one(void (*kernel)(Params...), int64_t grid, int threa
     return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...) == cudaSuccess;
 }
 
-// plan, (behind a shared prefix: the tails,) attention, and (where key ranges may be cut) the join
+struct PackedMaps {
+    CUtensorMap q, q1, k, v, o, part;
+};
+
+// plan, attention, and (where key ranges may be cut) the join
 template <int D>
-int packed_launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const PackedParams& p, cudaStream_t st) {
-    if (!packed_launch_one(mha_packed_plan_kernel, 1, kPackedPlanThreads, 0, st, p)) return 4;
-    if (p.prefix_lens) {
-        const int rc = paged_launch_g<D>(p.tail, st);
-        if (rc != 0) return rc;
-    }
-    const int64_t most = static_cast<int64_t>(p.slots > 0 ? p.max_entries : p.max_tiles) * p.H_kv;
-    if (!packed_launch_one(mha_packed_kernel<D>, std::min<int64_t>(p.sm_count, most), kMhaThreads, PackedSmem<D>::kTotal, st, tq, tk, tv, p)) return 4;
-    if (p.slots > 0) {
+int packed_launch(const PackedMaps& m, const PackedParams& p, cudaStream_t st) {
+    if (!packed_launch_one(mha_packed_plan_kernel, 1, kPackedPlanThreads, kPackedPlanSmem, st, p)) return 4;
+    const int64_t most = static_cast<int64_t>(p.part_rows > 0 ? p.max_entries : p.max_tiles) * p.H_kv;
+    if (!packed_launch_one(p.part_rows > 0 ? mha_packed_kernel<D, true> : mha_packed_kernel<D, false>, std::min<int64_t>(p.sm_count, most), kMhaThreads,
+                           PackedSmem<D>::kTotal, st, m.q, m.q1, m.k, m.v, m.o, m.part, p))
+        return 4;
+    if (p.part_rows > 0) {
         const int64_t rows = static_cast<int64_t>(p.T) * p.H;
         if (!packed_launch_one(mha_packed_join_kernel<D>, (rows + kPackedJoinWarps - 1) / kPackedJoinWarps, kPackedJoinWarps * 32, 0, st, p)) return 4;
     }

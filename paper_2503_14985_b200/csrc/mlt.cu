@@ -769,7 +769,6 @@ int paged_prepare(const void* Q, const void* K_cache, const void* V_cache, const
     p->head_groups = 1;
     p->balanced = 0;
     p->balanced_ctas = 0;
-    p->table_skip = nullptr;
     *launch = true;
     return MLT_OK;
 }
@@ -1213,7 +1212,7 @@ int packed_check(const void* Q, const void* K, const void* V, const void* O, int
     const int64_t width = static_cast<int64_t>(H) * D;
     if (D != 64 && D != 128) return MLT_ERR_UNSUPPORTED;
     if (ldq < width || ldo < width) return MLT_ERR_INVALID_ARG;
-    if (H / H_kv > kMhaBlock || H > 65536) return MLT_ERR_UNSUPPORTED;
+    if (H / H_kv > kMhaBlock || H > 4096) return MLT_ERR_UNSUPPORTED;
     if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(O) || !aligned16(workspace) || ldq % 8 != 0 || ldo % 8 != 0)
         return MLT_ERR_ALIGNMENT;
     // work items (tile pairs of all sequences x KV heads) are counted in 32 bits
@@ -1222,11 +1221,11 @@ int packed_check(const void* Q, const void* K, const void* V, const void* O, int
     return MLT_OK;
 }
 
-// Parameters that do not depend on where the keys come from, and the Q tensor map.
-int packed_fill(PackedParams* p, CUtensorMap* tq, const void* Q, void* O, float* LSE, int T, int S, int H, int H_kv, int D, float scale,
-                int64_t ldq, int64_t ldo, const PackedScratch& x, void* workspace, int64_t slots, int sm_count) {
+// Parameters that do not depend on where the keys come from, and the tensor maps of Q (W tokens and one token) and of the results.
+int packed_fill(PackedParams* p, PackedMaps* m, const void* Q, void* O, float* LSE, int T, int S, int H, int H_kv, int D,
+                float scale, int64_t ldq, int64_t ldo, const PackedScratch& x, void* workspace, int64_t part_rows, int sm_count) {
     *p = PackedParams{};
-    p->S = S;
+    p->S = p->all = S;
     p->T = T;
     p->G = H / H_kv;
     p->W = x.W;
@@ -1239,39 +1238,53 @@ int packed_fill(PackedParams* p, CUtensorMap* tq, const void* Q, void* O, float*
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     p->hdr = reinterpret_cast<PackedHeader*>(ws);
     p->seqs = reinterpret_cast<int4*>(ws + x.seqs);
+    p->key_base = reinterpret_cast<long long*>(ws + x.key_base);
     p->entries = reinterpret_cast<int4*>(ws + x.entries);
-    p->tile_first = reinterpret_cast<int*>(ws + x.tile_first);
-    p->max_tiles = x.max_tiles;
-    p->max_entries = x.max_entries;
-    p->slot_rows = x.slot_rows;
-    p->slots = static_cast<int>(slots);
+    p->entry_rows = reinterpret_cast<int*>(ws + x.entry_rows);
+    p->tile_rows = reinterpret_cast<int*>(ws + x.tile_rows);
+    p->max_tiles = static_cast<int>(x.max_tiles);
+    p->max_entries = static_cast<int>(x.max_entries);
+    p->part_rows = static_cast<int>(part_rows);
     p->part_o = reinterpret_cast<float*>(ws + x.lists);
-    p->part_ml = reinterpret_cast<float2*>(p->part_o + static_cast<size_t>(slots) * x.slot_rows * D);
+    p->part_ml = reinterpret_cast<float2*>(p->part_o + static_cast<size_t>(part_rows) * D);
     p->sm_count = sm_count;
     const uint64_t dims[3] = {static_cast<uint64_t>(D), static_cast<uint64_t>(H), static_cast<uint64_t>(T)};
     const uint64_t strides[2] = {static_cast<uint64_t>(D) * 2, static_cast<uint64_t>(ldq) * 2};
-    const uint32_t box[3] = {64, static_cast<uint32_t>(p->G), static_cast<uint32_t>(p->W)};
-    return encode_bf16(tq, Q, 3, dims, strides, box);
+    const uint32_t box[3] = {64, static_cast<uint32_t>(p->G), static_cast<uint32_t>(p->W)}, box1[3] = {64, static_cast<uint32_t>(p->G), 1};
+    int rc = encode_bf16(&m->q, Q, 3, dims, strides, box);
+    if (rc == MLT_OK) rc = encode_bf16(&m->q1, Q, 3, dims, strides, box1);
+    p->boxes = 32 % p->G == 0 && static_cast<int64_t>(T) * p->G >= 32;  // (with fewer rows no warp is full)
+    m->o = m->part = m->q;
+    if (rc == MLT_OK && p->boxes) {
+        const uint64_t o_strides[2] = {static_cast<uint64_t>(D) * 2, static_cast<uint64_t>(ldo) * 2};
+        const uint32_t o_box[3] = {64, static_cast<uint32_t>(p->G), 32 / static_cast<uint32_t>(p->G)};
+        rc = encode_bf16(&m->o, O, 3, dims, o_strides, o_box);
+        if (rc == MLT_OK && part_rows > 0) {
+            const uint64_t p_dims[2] = {static_cast<uint64_t>(D), static_cast<uint64_t>(part_rows)}, p_strides[1] = {static_cast<uint64_t>(D) * 4};
+            const uint32_t p_box[2] = {32, 32};
+            rc = encode_bf16(&m->part, p->part_o, 2, p_dims, p_strides, p_box, 2);
+        }
+    }
+    return rc;
 }
 
-// Parts of cut key ranges that pay: none when there are enough items for two rounds of the SMs as it is.
-int64_t packed_slots(const PackedScratch& x, int64_t T, int H_kv, size_t workspace_bytes, int sm_count) {
+// Rows of partial results of cut key ranges: none when there are enough items for two rounds of the SMs as it is.
+int64_t packed_part_limit(const PackedScratch& x, int64_t T, int H_kv, size_t workspace_bytes, int sm_count) {
     if ((T + 2 * x.W - 1) / (2 * x.W) * H_kv >= 2ll * sm_count) return 0;
-    return std::min<int64_t>(x.slots, static_cast<int64_t>((workspace_bytes - x.lists) / x.slot_bytes));
+    return std::min<int64_t>(x.part_rows, static_cast<int64_t>((workspace_bytes - x.lists) / x.row_bytes));
 }
 
-int packed_cache_maps(CUtensorMap* tk, CUtensorMap* tv, const void* K_cache, const void* V_cache, int num_blocks, int H_kv, int block_size, int D) {
+int packed_cache_maps(PackedMaps* m, const void* K_cache, const void* V_cache, int num_blocks, int H_kv, int block_size, int D) {
     const uint64_t dims[3] = {static_cast<uint64_t>(D), static_cast<uint64_t>(block_size),
                               std::max<uint64_t>(1, static_cast<uint64_t>(num_blocks) * H_kv)};
     const uint64_t strides[2] = {static_cast<uint64_t>(D) * 2, static_cast<uint64_t>(D) * 2 * block_size};
     const uint32_t box[3] = {64, static_cast<uint32_t>(block_size), 1};
-    const int rc = encode_bf16(tk, K_cache, 3, dims, strides, box);
-    return rc != MLT_OK ? rc : encode_bf16(tv, V_cache, 3, dims, strides, box);
+    const int rc = encode_bf16(&m->k, K_cache, 3, dims, strides, box);
+    return rc != MLT_OK ? rc : encode_bf16(&m->v, V_cache, 3, dims, strides, box);
 }
 
-int packed_run(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const PackedParams& p, int D, void* stream) {
-    return D == 64 ? packed_launch<64>(tq, tk, tv, p, static_cast<cudaStream_t>(stream))
-                   : packed_launch<128>(tq, tk, tv, p, static_cast<cudaStream_t>(stream));
+int packed_run(const PackedMaps& m, const PackedParams& p, int D, void* stream) {
+    return D == 64 ? packed_launch<64>(m, p, static_cast<cudaStream_t>(stream)) : packed_launch<128>(m, p, static_cast<cudaStream_t>(stream));
 }
 
 }  // namespace
@@ -1281,7 +1294,7 @@ extern "C" {
 size_t mlt_mha_packed_workspace_bytes(int num_q, int num_seqs, int H, int H_kv, int D) {
     if (num_q <= 0 || num_seqs <= 0 || H <= 0 || H_kv <= 0 || D <= 0 || H % H_kv != 0 || H / H_kv > kMhaBlock) return 0;
     const PackedScratch x = packed_scratch(num_q, num_seqs, H / H_kv, H_kv, D);
-    return x.lists + x.slots * x.slot_bytes;
+    return x.lists + static_cast<size_t>(x.part_rows) * x.row_bytes;
 }
 
 int mlt_mha_packed_fwd(const void* Q, const void* K, const void* V, const int32_t* cu_q, const int32_t* cu_k, void* O, float* LSE,
@@ -1300,22 +1313,22 @@ int mlt_mha_packed_fwd(const void* Q, const void* K, const void* V, const int32_
     if (rc != MLT_OK) return rc;
     if (!dev.packed_ok) return MLT_ERR_UNSUPPORTED;
     PackedParams p;
-    CUtensorMap tq, tk, tv;
-    rc = packed_fill(&p, &tq, Q, O, LSE, num_q, num_seqs, H, H_kv, D, scale, ldq, ldo, x, workspace,
-                     packed_slots(x, num_q, H_kv, workspace_bytes, dev.sm_count), dev.sm_count);
+    PackedMaps m;
+    rc = packed_fill(&p, &m, Q, O, LSE, num_q, num_seqs, H, H_kv, D, scale, ldq, ldo, x, workspace,
+                     packed_part_limit(x, num_q, H_kv, workspace_bytes, dev.sm_count), dev.sm_count);
     if (rc != MLT_OK) return rc;
     const uint64_t dims[3] = {static_cast<uint64_t>(D), static_cast<uint64_t>(H_kv), static_cast<uint64_t>(std::max(1, num_k))};
     const uint32_t box[3] = {64, 1, kMhaBlock};
     const uint64_t k_strides[2] = {static_cast<uint64_t>(D) * 2, static_cast<uint64_t>(ldk) * 2};
     const uint64_t v_strides[2] = {static_cast<uint64_t>(D) * 2, static_cast<uint64_t>(ldv) * 2};
-    rc = encode_bf16(&tk, K, 3, dims, k_strides, box);
-    if (rc == MLT_OK) rc = encode_bf16(&tv, V, 3, dims, v_strides, box);
+    rc = encode_bf16(&m.k, K, 3, dims, k_strides, box);
+    if (rc == MLT_OK) rc = encode_bf16(&m.v, V, 3, dims, v_strides, box);
     if (rc != MLT_OK) return rc;
     p.cu_q = cu_q;
     p.cu_k = cu_k;
     p.num_k = num_k;
     p.causal = causal ? 1 : 0;
-    return packed_run(tq, tk, tv, p, D, stream);
+    return packed_run(m, p, D, stream);
 }
 
 int mlt_paged_attn_prefill(const void* Q, const void* K_cache, const void* V_cache, const int32_t* cu_tokens, const int32_t* context_lens,
@@ -1336,10 +1349,10 @@ int mlt_paged_attn_prefill(const void* Q, const void* K_cache, const void* V_cac
     if (rc != MLT_OK) return rc;
     if (!dev.packed_ok) return MLT_ERR_UNSUPPORTED;
     PackedParams p;
-    CUtensorMap tq, tk, tv;
-    rc = packed_fill(&p, &tq, Q, O, LSE, num_tokens, num_seqs, H, H_kv, D, scale, ldq, ldo, x, workspace,
-                     packed_slots(x, num_tokens, H_kv, workspace_bytes, dev.sm_count), dev.sm_count);
-    if (rc == MLT_OK) rc = packed_cache_maps(&tk, &tv, K_cache, V_cache, num_blocks, H_kv, block_size, D);
+    PackedMaps m;
+    rc = packed_fill(&p, &m, Q, O, LSE, num_tokens, num_seqs, H, H_kv, D, scale, ldq, ldo, x, workspace,
+                     packed_part_limit(x, num_tokens, H_kv, workspace_bytes, dev.sm_count), dev.sm_count);
+    if (rc == MLT_OK) rc = packed_cache_maps(&m, K_cache, V_cache, num_blocks, H_kv, block_size, D);
     if (rc != MLT_OK) return rc;
     p.cu_q = cu_tokens;
     p.context_lens = context_lens;
@@ -1348,92 +1361,53 @@ int mlt_paged_attn_prefill(const void* Q, const void* K_cache, const void* V_cac
     p.max_blocks = max_blocks_per_seq;
     p.num_blocks = num_blocks;
     p.causal = 1;
-    return packed_run(tq, tk, tv, p, D, stream);
+    return packed_run(m, p, D, stream);
 }
 
 }  // extern "C"
-
-namespace {
-// Scratch of decode behind a shared prefix: the prefix's lists and parts, then the tails' lengths, table offsets, numbers of parts
-// and the parts themselves.
-struct SharedScratch {
-    PackedScratch x;
-    size_t tail_lens, tail_skip, tail_parts, tail_part_o, total;
-};
-SharedScratch shared_scratch(int64_t S, int64_t groups, int H, int H_kv, int D) {
-    SharedScratch w;
-    auto up = [](size_t v) { return (v + 255) & ~size_t(255); };
-    w.x = packed_scratch(S, groups, H / H_kv, H_kv, D, true);
-    w.tail_lens = up(w.x.lists + static_cast<size_t>(w.x.slots) * w.x.slot_bytes);
-    w.tail_skip = up(w.tail_lens + static_cast<size_t>(S) * 4);
-    w.tail_parts = up(w.tail_skip + static_cast<size_t>(S) * 4);
-    w.tail_part_o = up(w.tail_parts + static_cast<size_t>(S) * H_kv * 4);
-    w.total = w.tail_part_o + paged_workspace_bytes(static_cast<int>(S), H, D, kPagedMaxSplits);
-    return w;
-}
-}  // namespace
 
 extern "C" {
 
 size_t mlt_paged_attn_shared_workspace_bytes(int num_seqs, int num_groups, int H, int H_kv, int D) {
     if (num_seqs <= 0 || num_groups < 0 || H <= 0 || H_kv <= 0 || D <= 0 || H % H_kv != 0 || H / H_kv > kMhaBlock) return 0;
-    if (num_groups == 0) return mlt_paged_attn_workspace_bytes(num_seqs, H, D);
-    return shared_scratch(num_seqs, num_groups, H, H_kv, D).total;
+    const PackedScratch x = packed_scratch(num_seqs, num_groups, H / H_kv, H_kv, D, true);
+    return x.lists + static_cast<size_t>(x.part_rows) * x.row_bytes;
 }
 
 int mlt_paged_attn_decode_shared(const void* Q, const void* K_cache, const void* V_cache, const int32_t* block_table, const int32_t* seq_lens,
                                  const int32_t* prefix_lens, const int32_t* cu_groups, void* O, float* LSE, int num_seqs, int num_groups,
                                  int H, int H_kv, int D, int block_size, int max_blocks_per_seq, int num_blocks, float scale,
                                  void* workspace, size_t workspace_bytes, void* stream) {
-    if (num_groups < 0) return MLT_ERR_INVALID_ARG;
-    if (num_groups == 0)
-        return mlt_paged_attn_decode(Q, K_cache, V_cache, block_table, seq_lens, O, LSE, num_seqs, H, H_kv, D, block_size, max_blocks_per_seq,
-                                     num_blocks, scale, workspace, workspace_bytes, stream);
-    PackedParams p;
-    PagedParams tail;
-    DeviceInfo dev;
-    bool launch = false;
-    if (num_seqs > 0 && H > 0) {
-        if (!prefix_lens || !cu_groups || !workspace) return MLT_ERR_INVALID_ARG;
-        if (!aligned16(workspace)) return MLT_ERR_ALIGNMENT;
-        if (static_cast<int64_t>(num_blocks) * H_kv > INT32_MAX) return MLT_ERR_UNSUPPORTED;
-        // (tile pairs of the groups: the plan keeps them in shared memory)
-        if (H_kv > 0 && H % H_kv == 0 && H / H_kv <= kMhaBlock) {
-            if (num_seqs / (2 * (kMhaBlock / (H / H_kv))) + static_cast<int64_t>(num_groups) > kPackedMaxSplitTiles) return MLT_ERR_UNSUPPORTED;
-            if (D > 0 && workspace_bytes < shared_scratch(num_seqs, num_groups, H, H_kv, D).total) return MLT_ERR_INVALID_ARG;
-        }
-    }
-    int rc = paged_prepare(Q, K_cache, V_cache, block_table, seq_lens, O, LSE, num_seqs, H, H_kv, D, block_size, max_blocks_per_seq, num_blocks,
-                           scale, &tail, &dev, &launch);
-    if (rc != MLT_OK || !launch) return rc;
-    if (!dev.packed_ok) return MLT_ERR_UNSUPPORTED;
-    const SharedScratch w = shared_scratch(num_seqs, num_groups, H, H_kv, D);
-    CUtensorMap tq, tk, tv;
+    bool launch;
+    if (num_groups < 0 || max_blocks_per_seq < 0 || num_blocks < 0) return MLT_ERR_INVALID_ARG;
     const int64_t ld = static_cast<int64_t>(H) * D;
-    rc = packed_fill(&p, &tq, Q, O, LSE, num_seqs, num_groups, H, H_kv, D, scale, ld, ld, w.x, workspace, w.x.slots, dev.sm_count);
-    if (rc == MLT_OK) rc = packed_cache_maps(&tk, &tv, K_cache, V_cache, num_blocks, H_kv, block_size, D);
+    int rc = packed_check(Q, K_cache, V_cache, O, num_seqs, std::max(1, num_groups), H, H_kv, D, scale, ld, ld, workspace, &launch);
+    if (rc != MLT_OK || !launch) return rc;
+    if (!block_table || !seq_lens || !cu_groups || (num_groups > 0 && !prefix_lens)) return MLT_ERR_INVALID_ARG;
+    if (block_size != 8 && block_size != 16 && block_size != 32) return MLT_ERR_UNSUPPORTED;
+    if (static_cast<int64_t>(num_blocks) * H_kv > INT32_MAX) return MLT_ERR_UNSUPPORTED;
+    const PackedScratch x = packed_scratch(num_seqs, num_groups, H / H_kv, H_kv, D, true);
+    if (x.max_tiles > kPackedSplitTiles || x.part_rows > INT32_MAX) return MLT_ERR_UNSUPPORTED;
+    if (workspace_bytes < x.lists + static_cast<size_t>(x.part_rows) * x.row_bytes) return MLT_ERR_INVALID_ARG;
+    DeviceInfo dev;
+    rc = get_device(&dev);
     if (rc != MLT_OK) return rc;
-    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    if (!dev.packed_ok) return MLT_ERR_UNSUPPORTED;
+    PackedParams p;
+    PackedMaps m;
+    rc = packed_fill(&p, &m, Q, O, LSE, num_seqs, num_groups, H, H_kv, D, scale, ld, ld, x, workspace, x.part_rows, dev.sm_count);
+    if (rc == MLT_OK) rc = packed_cache_maps(&m, K_cache, V_cache, num_blocks, H_kv, block_size, D);
+    if (rc != MLT_OK) return rc;
+    p.all = num_groups + num_seqs;
     p.cu_q = cu_groups;
-    p.prefix_lens = prefix_lens;
+    p.prefix_lens = num_groups > 0 ? prefix_lens : seq_lens;  // (of no group: not read, but tells the kernels what the tokens are)
     p.seq_lens = seq_lens;
     p.block_table = block_table;
     p.block_size = block_size;
     p.max_blocks = max_blocks_per_seq;
     p.num_blocks = num_blocks;
     p.causal = 0;
-    p.tail_lens = reinterpret_cast<int*>(ws + w.tail_lens);
-    p.tail_skip = reinterpret_cast<int*>(ws + w.tail_skip);
-    p.tail_parts = reinterpret_cast<int*>(ws + w.tail_parts);
-    tail.seq_lens = p.tail_lens;
-    tail.table_skip = p.tail_skip;
-    tail.part_o = reinterpret_cast<float*>(ws + w.tail_part_o);
-    tail.splits = kPagedMaxSplits;
-    tail.blocks_per_split = std::max(2, 128 / block_size);  // at least 128 tokens per CTA
-    if (paged_use_balanced(tail, dev.sm_count)) paged_set_balanced(&tail, dev.sm_count);
-    tail.part_ml = reinterpret_cast<float2*>(tail.part_o + static_cast<size_t>(num_seqs) * H * tail.splits * D);
-    p.tail = tail;
-    return packed_run(tq, tk, tv, p, D, stream);
+    return packed_run(m, p, D, stream);
 }
 
 }  // extern "C"

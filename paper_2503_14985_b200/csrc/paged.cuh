@@ -48,18 +48,7 @@ struct PagedParams {
     int head_groups;       // CTAs per KV head (1, or 2 when 8 query heads per KV head run as two groups of 4)
     int balanced;          // grouped-head kernel: equal work per CTA (see paged_decode_mma_kernel); splits = kPagedMaxSplits
     int balanced_ctas;     // ... and the grid it is launched with (the combine kernel repeats the arithmetic)
-    // Tails behind a shared prefix: seq_lens are the tails' lengths, which begin table_skip[s] blocks into a sequence's row; the
-    // partial results are joined with the prefix's elsewhere, and each sequence is split evenly (the tables' width says
-    // nothing about the tails), into pieces of at least blocks_per_split.
-    const int* table_skip; // [num_seqs] or null
 };
-
-// KV blocks per CTA of a sequence of nblk blocks.
-__host__ __device__ __forceinline__ int paged_split_blocks(const PagedParams& p, int nblk) {
-    if (!p.table_skip) return p.blocks_per_split;
-    const int even = ((nblk + p.splits - 1) / p.splits + 1) & ~1;  // (a multiple of 16 tokens also with 8-token blocks)
-    return even > p.blocks_per_split ? even : p.blocks_per_split;
-}
 
 __device__ __forceinline__ void bf16x8_to_f32(const uint4& v, float (&f)[8]) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -146,9 +135,8 @@ paged_decode_kernel(const PagedParams p) {
     // a length beyond what the block table can reach is cut at the table's end: no entry past the row is read
     const int len = max(0, min(p.seq_lens[s], p.max_blocks * BS));
     const int nblk = (len + BS - 1) / BS;
-    const int share = paged_split_blocks(p, nblk);
-    const int b0 = sp * share;
-    const int b1 = min(nblk, b0 + share);
+    const int b0 = sp * p.blocks_per_split;
+    const int b1 = min(nblk, b0 + p.blocks_per_split);
     if (p.splits > 1 && b0 >= nblk && !(sp == 0)) return;  // nothing of this sequence here (split 0 reports an empty one)
 
     // this lane's 8 columns of the G query rows
@@ -170,7 +158,7 @@ paged_decode_kernel(const PagedParams p) {
     }
     (void)my_g;
 
-    const int* table = p.block_table + static_cast<int64_t>(s) * p.max_blocks + (p.table_skip ? p.table_skip[s] : 0);
+    const int* table = p.block_table + static_cast<int64_t>(s) * p.max_blocks;
     for (int b = b0 + warp; b < b1; b += kPagedWarps) {
         const int phys = table[b];
         if (phys < 0 || phys >= p.num_blocks) {  // never dereference a bad table entry: report and skip the block
@@ -423,9 +411,8 @@ paged_decode_mma_kernel(const PagedParams p) {
         seg_kvh = blockIdx.y;
         const int len = max(0, min(p.seq_lens[seg_s], p.max_blocks * BS));
         const int nblk = (len + BS - 1) / BS;
-        const int share = paged_split_blocks(p, nblk);
-        const int b0 = blockIdx.x * share;  // even for BS = 8 (the host sees to it): a multiple of 16 tokens
-        const int b1 = min(nblk, b0 + share);
+        const int b0 = blockIdx.x * p.blocks_per_split;  // even for BS = 8 (the host sees to it): a multiple of 16 tokens
+        const int b1 = min(nblk, b0 + p.blocks_per_split);
         if (p.splits > 1 && b0 >= nblk && blockIdx.x != 0) return;  // nothing of this sequence here (split 0 reports an empty one)
         seg_tok_begin = b0 * BS;
         seg_tok_end = min(len, b1 * BS);
@@ -525,7 +512,7 @@ paged_decode_mma_kernel(const PagedParams p) {
             for (int i = 0; i < 4; ++i) oacc[h][nt][i] = 0.0f;
     float m_run = -INFINITY, l_part = 0.0f;  // head g: running max (log2 units, equal in the 4 lanes of a group), this lane's share of the sum
 
-    const int* table = p.block_table + static_cast<int64_t>(s) * p.max_blocks + (p.table_skip ? p.table_skip[s] : 0);
+    const int* table = p.block_table + static_cast<int64_t>(s) * p.max_blocks;
     const int64_t head_off = static_cast<int64_t>(kvh) * BS * D;
     const int64_t blk_stride = static_cast<int64_t>(p.H_kv) * BS * D;
 
@@ -877,7 +864,7 @@ int paged_launch_bs(const PagedParams& p, cudaStream_t st) {
         }
     }
     if (cudaGetLastError() != cudaSuccess) return 4;
-    if (p.splits > 1 && !p.table_skip) {
+    if (p.splits > 1) {
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(p.num_seqs * p.H);
         cfg.blockDim = dim3(D);

@@ -58,17 +58,19 @@ def test_shared(lens, prefix, groups, H, Hk, D, bs):
         check_rows(o[s: s + 1], lse[s: s + 1], ref, f"sequence {s}")
 
 
-def test_equals_plain_decode_without_prefixes():
-    """No group, or groups without a whole block in common: what mlt_paged_attn_decode gives, within the two paths' bounds."""
+@pytest.mark.parametrize("prefix,groups", [([], [0]), ([15], [0, 4]), ([64, 0], [1, 2, 4])])
+def test_without_whole_blocks_in_common(prefix, groups):
+    """No group, groups without a whole block in common, a group of one: plain decode (and mlt_paged_attn_decode within both paths' bounds)."""
     lens, H, Hk, D, bs = [100, 7, 0, 2000], 16, 4, 128, 16
     kc, vc, table = paged(lens, Hk, D, bs, seed=3)
+    if groups[0] == 1:
+        table[1, :4] = table[3, :4]  # (the second sequence is shorter than its prefix: its row goes on all the same)
     q = torch.randn(4, H, D, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda", dtype=torch.bfloat16)
-    ws = torch.empty(mlt.paged_attn_shared_workspace_bytes(4, 0, H, Hk, D), dtype=torch.uint8, device="cuda")
+    o, lse = run_shared(q, kc, vc, table, lens, prefix, groups, 0.1)
+    ws = torch.empty(mlt.paged_attn_workspace_bytes(4, H, D), dtype=torch.uint8, device="cuda")
     plain, plain_lse = mlt.paged_attn_decode(q, kc, vc, table, i32(lens), scale=0.1, workspace=ws)
-    none, none_lse = mlt.paged_attn_decode_shared(q, kc, vc, table, i32(lens), i32([]), i32([0]), scale=0.1, workspace=ws)
-    assert torch.equal(plain, none) and torch.equal(plain_lse, none_lse)
-    o, lse = run_shared(q, kc, vc, table, lens, [15], [0, 4], 0.1)
     for s, n in enumerate(lens):
         ref = rows_reference(q[s: s + 1].double(), gathered(kc, table[s], n), gathered(vc, table[s], n), torch.ones(1, n, dtype=torch.bool, device="cuda"), 0.1)
         check_rows(o[s: s + 1], lse[s: s + 1], ref, f"sequence {s}")
+        check_rows(plain[s: s + 1], plain_lse[s: s + 1], ref, f"sequence {s}, plain")
     assert_device_healthy()
