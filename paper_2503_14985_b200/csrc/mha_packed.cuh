@@ -138,6 +138,21 @@ __device__ __forceinline__ int packed_owner(const PackedParams& p, int t) {
     return p.cu_q[lo] <= t && t < p.cu_q[lo + 1] ? lo : -1;
 }
 
+// The same by a whole warp: 33 parts per step instead of two.
+__device__ __forceinline__ int packed_owner_warp(const PackedParams& p, int t) {
+    if (p.S == 0) return -1;
+    const int lane = threadIdx.x & 31;
+    int lo = 0, hi = p.S;  // cu_q[lo] <= t (or lo = 0), cu_q[hi] > t (or hi = S)
+    while (hi - lo > 1) {
+        const int step = max(1, (hi - lo + 32) / 33), at = lo + (lane + 1) * step;
+        const unsigned int below = __ballot_sync(0xffffffffu, at < hi && p.cu_q[at] <= t);
+        const int n = below ? 32 - __clz(below) : 0;  // (sorted: the lanes below are the first n)
+        hi = min(hi, lo + (n + 1) * step);
+        lo += n * step;
+    }
+    return p.cu_q[lo] <= t && t < p.cu_q[lo + 1] ? lo : -1;
+}
+
 // The keys of decoded sequence t behind its group's prefix.
 __device__ __forceinline__ void packed_tail(const PackedParams& p, int t, int3& q, long long& base) {
     int3 g;
@@ -189,13 +204,15 @@ __global__ void __launch_bounds__(kPackedPlanThreads) mha_packed_plan_kernel(con
     extern __shared__ int4 plan_smem[];
     int4* near_seqs = plan_smem;                                          // [kPackedSeqs]
     int* hist = reinterpret_cast<int*>(plan_smem + kPackedSeqs);          // [kPackedBuckets], or with cut ranges
-    int2* tile_of_split = reinterpret_cast<int2*>(hist + kPackedBuckets); // [kPackedSplitTiles] {key blocks, tokens}
+    int4* near_tiles = reinterpret_cast<int4*>(hist + kPackedBuckets);    // [kPackedSplitTiles] {sequence, pair, tokens, key blocks}
+    int* near_rows = reinterpret_cast<int*>(near_tiles + kPackedSplitTiles);  // [kPackedSplitTiles]
     __shared__ int red[32];
     __shared__ int longest_sh;
-    __shared__ unsigned long long pick_sh;
+    __shared__ float best_cost[32];
+    __shared__ int best_n[32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     for (int i = tid; i < kPackedBuckets; i += kPackedPlanThreads) hist[i] = 0;
-    if (tid == 0) { longest_sh = 0; pick_sh = ~0ull; }
+    if (tid == 0) longest_sh = 0;
     cudaGridDependencySynchronize();
 
     // sequences: tile pairs and their prefix sums
@@ -236,7 +253,8 @@ __global__ void __launch_bounds__(kPackedPlanThreads) mha_packed_plan_kernel(con
     // tile pair i: its sequence (the last one with at most i pairs before it), number in it, tokens and key blocks
     const int4* seqs = p.all <= kPackedSeqs ? near_seqs : p.seqs;
     struct Tile { int s, pair, n, blocks; };
-    auto tile_at = [&](int i) {
+    const bool near = tiles <= kPackedSplitTiles;
+    auto find_tile = [&](int i) {
         Tile t;
         int lo = 0, hi = p.all;
         while (hi - lo > 1) {
@@ -250,12 +268,17 @@ __global__ void __launch_bounds__(kPackedPlanThreads) mha_packed_plan_kernel(con
         t.blocks = packed_tile_blocks(e.y, e.z, p.causal, t.pair * W2, t.n);
         return t;
     };
-    const bool may_split = p.part_rows > 0 && tiles <= kPackedSplitTiles;
+    auto tile_at = [&](int i) {
+        if (!near) return find_tile(i);
+        const int4 t = near_tiles[i];
+        return Tile{t.x, t.y, t.z, t.w};
+    };
+    const bool may_split = p.part_rows > 0 && near;
     int most = 0;
     for (int i = tid; i < tiles; i += kPackedPlanThreads) {
-        const Tile t = tile_at(i);
+        const Tile t = find_tile(i);
         atomicAdd(&hist[packed_bucket(t.blocks)], 1);
-        if (may_split) tile_of_split[i] = make_int2(t.blocks, t.n);
+        if (near) near_tiles[i] = make_int4(t.s, t.pair, t.n, t.blocks);
         most = max(most, t.blocks);
     }
     if (may_split) {
@@ -272,19 +295,21 @@ __global__ void __launch_bounds__(kPackedPlanThreads) mha_packed_plan_kernel(con
     int chunk = 0;
     if (may_split) {
         const int longest = longest_sh;
-        for (int i = warp; i <= 64; i += kPackedPlanThreads / 32) {
-            // n parts of the longest range: 0 (whole and not joined), 1 .. 16, then 16 per octave up to 128
-            const int n = i <= 16 ? i : ((i - 17) % 16 + 17) << ((i - 17) / 16);
-            if (n > longest || (n == 0 && p.prefix_lens)) continue;  // (a prefix's results always go to the join)
-            const int c = n ? (longest + n - 1) / n : max(longest, 1);
+        float mine_cost = 3e38f;
+        // n parts of the longest range, a warp per n: 0 (whole and not joined), 1 .. 12, then 4 to 8 per octave up to 128
+        constexpr unsigned char kParts[32] = {0, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15, 16, 18, 20, 22, 24, 28, 32, 36, 40, 48, 56, 64, 80, 96, 112, 128};
+        const int mine_n = kParts[warp];
+        if (mine_n <= longest && (mine_n > 0 || !p.prefix_lens)) {  // (a prefix's results always go to the join)
+            const int n = mine_n, c = n ? (longest + n - 1) / n : max(longest, 1);
+            const float per_block = 1.0f / c;
             float work = 0.0f, rows = 0.0f;
             int top = 0, entries = 0;
             for (int k = lane; k < tiles; k += 32) {
-                const int2 t = tile_of_split[k];
-                const int parts = max(1, (t.x + c - 1) / c), each = min(t.x, c);
-                const bool dual = n > 0 && t.y <= p.W;
-                work += static_cast<float>((dual ? t.x : 2 * t.x) + kItem * parts);
-                rows += static_cast<float>(parts * packed_part_rows(p, t.y));
+                const int tokens = near_tiles[k].z, blocks = near_tiles[k].w;
+                const int parts = max(1, __float2int_rd((blocks + c - 0.5f) * per_block)), each = min(blocks, c);  // (rounded up)
+                const bool dual = n > 0 && tokens <= p.W;
+                work += static_cast<float>((dual ? blocks : 2 * blocks) + kItem * parts);
+                rows += static_cast<float>(parts * packed_part_rows(p, tokens));
                 top = max(top, (dual ? each : 2 * each) + kItem);
                 entries += parts;
             }
@@ -297,38 +322,45 @@ __global__ void __launch_bounds__(kPackedPlanThreads) mha_packed_plan_kernel(con
             entries = __reduce_add_sync(0xffffffffu, entries);
             const float items = static_cast<float>(max(entries, 1)) * p.H_kv, average = work * p.H_kv / items;
             const float rounds = n ? ceilf(items / p.sm_count) : fmaxf(items / p.sm_count, 1.0f);
-            float cost = fmaxf(static_cast<float>(top), rounds * average + (top - average) * (n ? 0.5f : 0.25f)) + (n ? kJoin : 0.0f);
+            mine_cost = fmaxf(static_cast<float>(top), rounds * average + (top - average) * (n ? 0.5f : 0.25f)) + (n ? kJoin : 0.0f);
             // (1.0001: the sum of the rows is rounded)
-            if (n && (rows * p.H_kv * 1.0001f > static_cast<float>(p.part_rows) || entries > p.max_entries)) cost = n == 1 && p.prefix_lens ? kNever / 2 : kNever;
-            if (lane == 0) atomicMin(&pick_sh, (static_cast<unsigned long long>(__float_as_uint(cost)) << 16) | static_cast<unsigned long long>(n));
+            if (n && (rows * p.H_kv * 1.0001f > static_cast<float>(p.part_rows) || entries > p.max_entries))
+                mine_cost = n == 1 && p.prefix_lens ? kNever / 2 : kNever;
+        }
+        if (lane == 0) {
+            best_cost[warp] = mine_cost;
+            best_n[warp] = mine_n;
         }
         __syncthreads();
-        const int n = pick_sh == ~0ull ? 0 : static_cast<int>(pick_sh & 0xffff);
+        const uint32_t key = __float_as_uint(best_cost[lane]);  // (costs are positive: their bits are in their order)
+        const unsigned int at = __ballot_sync(0xffffffffu, key == __reduce_min_sync(0xffffffffu, key));
+        const int n = best_n[__ffs(at) - 1];
         if (n > 0 || p.prefix_lens) chunk = max(1, n ? (longest + n - 1) / n : longest);
     }
 
     int total;
     if (chunk > 0) {
+        // parts of equal length, longest first: a tile pair's whole parts and its last one are counted, then placed
+        for (int i = tid; i < kPackedBuckets; i += kPackedPlanThreads) hist[i] = 0;
+        __syncthreads();
+        auto whole_of = [&](const Tile& t) { return packed_bucket((t.n <= p.W ? 1 : 2) * chunk); };
+        auto last_of = [&](const Tile& t) { return packed_bucket((t.n <= p.W ? 1 : 2) * (t.blocks % chunk)); };
         int first = 0, first_row = 0;
-        for (int i0 = 0; i0 < tiles; i0 += kPackedPlanThreads) {  // entries in the order of the tile pairs
+        for (int i0 = 0; i0 < tiles; i0 += kPackedPlanThreads) {
             const int i = i0 + tid;
-            Tile t = {0, 0, 0, 0};
             int parts = 0, rows = 0;
             if (i < tiles) {
-                t = tile_at(i);
+                const Tile t = tile_at(i);
                 parts = max(1, (t.blocks + chunk - 1) / chunk);
                 rows = packed_part_rows(p, t.n) * p.H_kv;
+                if (t.blocks >= chunk) atomicAdd(&hist[whole_of(t)], t.blocks / chunk);
+                if (t.blocks % chunk != 0 || t.blocks == 0) atomicAdd(&hist[last_of(t)], 1);
             }
             int sum_parts, sum_rows;
-            const int at = first + packed_scan(parts, red, sum_parts) - parts;
+            packed_scan(parts, red, sum_parts);
             const int row = first_row + packed_scan(parts * rows, red, sum_rows) - parts * rows;
-            if (i < tiles) {
-                p.tile_rows[i] = row;
-                for (int k = 0; k < parts && at + k < p.max_entries; ++k) {
-                    p.entries[at + k] = make_int4(t.s, t.pair, k * chunk, min(chunk, t.blocks - k * chunk));
-                    p.entry_rows[at + k] = row + k * rows;
-                }
-            }
+            if (i < tiles) p.tile_rows[i] = row;
+            if (i < tiles) near_rows[i] = row;
             first += sum_parts;
             first_row += sum_rows;
             if (first_row > p.part_rows || first > p.max_entries) {  // (only for groups that overlap: scratch is sized for groups that do not)
@@ -339,6 +371,31 @@ __global__ void __launch_bounds__(kPackedPlanThreads) mha_packed_plan_kernel(con
             }
         }
         total = first;
+        if (total > 0) {
+            int sum;
+            __syncthreads();
+            const int a = hist[2 * tid], b = hist[2 * tid + 1];
+            const int end = packed_scan(a + b, red, sum);
+            hist[2 * tid] = end - a - b;
+            hist[2 * tid + 1] = end - b;
+            __syncthreads();
+            for (int i = tid; i < tiles; i += kPackedPlanThreads) {
+                const Tile t = tile_at(i);
+                const int rows = packed_part_rows(p, t.n) * p.H_kv, row = near_rows[i], whole = t.blocks / chunk;
+                if (whole > 0) {
+                    const int at = atomicAdd(&hist[whole_of(t)], whole);
+                    for (int k = 0; k < whole; ++k) {
+                        p.entries[at + k] = make_int4(t.s, t.pair, k * chunk, chunk);
+                        p.entry_rows[at + k] = row + k * rows;
+                    }
+                }
+                if (t.blocks % chunk != 0 || t.blocks == 0) {
+                    const int at = atomicAdd(&hist[last_of(t)], 1);
+                    p.entries[at] = make_int4(t.s, t.pair, whole * chunk, t.blocks - whole * chunk);
+                    p.entry_rows[at] = row + whole * rows;
+                }
+            }
+        }
     } else {
         // longest first: counting sort
         const int a = hist[2 * tid], b = hist[2 * tid + 1];
@@ -359,7 +416,7 @@ __global__ void __launch_bounds__(kPackedPlanThreads) mha_packed_plan_kernel(con
         p.hdr->split = chunk;
     }
 }
-constexpr int kPackedPlanSmem = kPackedSeqs * 16 + kPackedBuckets * 4 + kPackedSplitTiles * 8;
+constexpr int kPackedPlanSmem = kPackedSeqs * 16 + kPackedBuckets * 4 + kPackedSplitTiles * 20;
 
 template <int D>
 struct PackedSmem {
@@ -1170,7 +1227,7 @@ __global__ void __launch_bounds__(kPackedJoinWarps * 32) mha_packed_join_kernel(
         }
         return true;
     };
-    const int owner = packed_owner(p, tok);
+    const int owner = packed_owner_warp(p, tok);
     if (p.prefix_lens) {
         if (owner >= 0) {
             const int4 q = p.seqs[owner];

@@ -1268,9 +1268,10 @@ int packed_fill(PackedParams* p, PackedMaps* m, const void* Q, void* O, float* L
     return rc;
 }
 
-// Rows of partial results of cut key ranges: none when there are enough items for two rounds of the SMs as it is.
-int64_t packed_part_limit(const PackedScratch& x, int64_t T, int H_kv, size_t workspace_bytes, int sm_count) {
-    if ((T + 2 * x.W - 1) / (2 * x.W) * H_kv >= 2ll * sm_count) return 0;
+// Rows of partial results of cut key ranges: none when there are enough items for two rounds of the SMs as it is, or no sequence
+// can have more than two key blocks (most_keys).
+int64_t packed_part_limit(const PackedScratch& x, int64_t T, int64_t most_keys, int H_kv, size_t workspace_bytes, int sm_count) {
+    if ((T + 2 * x.W - 1) / (2 * x.W) * H_kv >= 2ll * sm_count || most_keys <= 2 * kMhaBlock) return 0;
     return std::min<int64_t>(x.part_rows, static_cast<int64_t>((workspace_bytes - x.lists) / x.row_bytes));
 }
 
@@ -1315,7 +1316,7 @@ int mlt_mha_packed_fwd(const void* Q, const void* K, const void* V, const int32_
     PackedParams p;
     PackedMaps m;
     rc = packed_fill(&p, &m, Q, O, LSE, num_q, num_seqs, H, H_kv, D, scale, ldq, ldo, x, workspace,
-                     packed_part_limit(x, num_q, H_kv, workspace_bytes, dev.sm_count), dev.sm_count);
+                     packed_part_limit(x, num_q, num_k, H_kv, workspace_bytes, dev.sm_count), dev.sm_count);
     if (rc != MLT_OK) return rc;
     const uint64_t dims[3] = {static_cast<uint64_t>(D), static_cast<uint64_t>(H_kv), static_cast<uint64_t>(std::max(1, num_k))};
     const uint32_t box[3] = {64, 1, kMhaBlock};
@@ -1351,7 +1352,7 @@ int mlt_paged_attn_prefill(const void* Q, const void* K_cache, const void* V_cac
     PackedParams p;
     PackedMaps m;
     rc = packed_fill(&p, &m, Q, O, LSE, num_tokens, num_seqs, H, H_kv, D, scale, ldq, ldo, x, workspace,
-                     packed_part_limit(x, num_tokens, H_kv, workspace_bytes, dev.sm_count), dev.sm_count);
+                     packed_part_limit(x, num_tokens, static_cast<int64_t>(max_blocks_per_seq) * block_size, H_kv, workspace_bytes, dev.sm_count), dev.sm_count);
     if (rc == MLT_OK) rc = packed_cache_maps(&m, K_cache, V_cache, num_blocks, H_kv, block_size, D);
     if (rc != MLT_OK) return rc;
     p.cu_q = cu_tokens;
