@@ -69,7 +69,7 @@ struct PackedParams {
     long long* key_base;  // [all] first key row (packed) or block-table index (paged)
     int4* entries;        // [max_entries] {sequence, tile pair, first key block, key blocks}
     int* entry_rows;      // [max_entries] first row of the entry's partial results (of KV head 0)
-    int* tile_rows;       // [max_tiles] that of a tile pair's first entry
+    int2* tile_info;      // [max_tiles] that of a tile pair's first entry, and the pair's entries
     float* part_o;        // [part_rows][D]
     float2* part_ml;      // [part_rows] {m in log2 units, l}
     int max_tiles, max_entries, part_rows;
@@ -176,8 +176,9 @@ __device__ __forceinline__ int packed_bucket(int blocks) {  // monotone: exact b
     return kPackedBuckets - 1 - min(key, kPackedBuckets - 1);
 }
 
-// Inclusive scan over the CTA (1024 threads); `red` holds 32 words.  Ends with all threads past their use of `red`.
-__device__ __forceinline__ int packed_scan(int v, int* red, int& total) {
+// Inclusive scan over the CTA (1024 threads); `red` holds 32 words.  Ends with all threads past their use of `red`.  (A function of its own:
+// the plan runs once, and what it costs is fetching its instructions.)
+__device__ __noinline__ int packed_scan(int v, int* red, int& total) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
     for (int w = 1; w < 32; w <<= 1) {
@@ -227,12 +228,14 @@ __global__ void __launch_bounds__(kPackedPlanThreads) mha_packed_plan_kernel(con
         else { ok = true; packed_tail(p, s - p.S, q, base); }
     };
     int mine = 0;
+#pragma unroll 1
     for (int s = s_lo; s < s_hi; ++s) {
         get(s);
         mine += (q.y + W2 - 1) / W2;
     }
     int tiles;
     int before = packed_scan(mine, red, tiles) - mine;
+#pragma unroll 1
     for (int s = s_lo; s < s_hi; ++s) {
         if (per > 1) get(s);
         int n = (q.y + W2 - 1) / W2;
@@ -257,6 +260,7 @@ __global__ void __launch_bounds__(kPackedPlanThreads) mha_packed_plan_kernel(con
     auto find_tile = [&](int i) {
         Tile t;
         int lo = 0, hi = p.all;
+#pragma unroll 1
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
             if (seqs[mid].w <= i) lo = mid; else hi = mid;
@@ -275,6 +279,7 @@ __global__ void __launch_bounds__(kPackedPlanThreads) mha_packed_plan_kernel(con
     };
     const bool may_split = p.part_rows > 0 && near;
     int most = 0;
+#pragma unroll 1
     for (int i = tid; i < tiles; i += kPackedPlanThreads) {
         const Tile t = find_tile(i);
         atomicAdd(&hist[packed_bucket(t.blocks)], 1);
@@ -304,6 +309,7 @@ __global__ void __launch_bounds__(kPackedPlanThreads) mha_packed_plan_kernel(con
             const float per_block = 1.0f / c;
             float work = 0.0f, rows = 0.0f;
             int top = 0, entries = 0;
+#pragma unroll 1
             for (int k = lane; k < tiles; k += 32) {
                 const int tokens = near_tiles[k].z, blocks = near_tiles[k].w;
                 const int parts = max(1, __float2int_rd((blocks + c - 0.5f) * per_block)), each = min(blocks, c);  // (rounded up)
@@ -346,6 +352,7 @@ __global__ void __launch_bounds__(kPackedPlanThreads) mha_packed_plan_kernel(con
         auto whole_of = [&](const Tile& t) { return packed_bucket((t.n <= p.W ? 1 : 2) * chunk); };
         auto last_of = [&](const Tile& t) { return packed_bucket((t.n <= p.W ? 1 : 2) * (t.blocks % chunk)); };
         int first = 0, first_row = 0;
+#pragma unroll 1
         for (int i0 = 0; i0 < tiles; i0 += kPackedPlanThreads) {
             const int i = i0 + tid;
             int parts = 0, rows = 0;
@@ -359,7 +366,7 @@ __global__ void __launch_bounds__(kPackedPlanThreads) mha_packed_plan_kernel(con
             int sum_parts, sum_rows;
             packed_scan(parts, red, sum_parts);
             const int row = first_row + packed_scan(parts * rows, red, sum_rows) - parts * rows;
-            if (i < tiles) p.tile_rows[i] = row;
+            if (i < tiles) p.tile_info[i] = make_int2(row, parts);
             if (i < tiles) near_rows[i] = row;
             first += sum_parts;
             first_row += sum_rows;
@@ -379,11 +386,13 @@ __global__ void __launch_bounds__(kPackedPlanThreads) mha_packed_plan_kernel(con
             hist[2 * tid] = end - a - b;
             hist[2 * tid + 1] = end - b;
             __syncthreads();
+#pragma unroll 1
             for (int i = tid; i < tiles; i += kPackedPlanThreads) {
                 const Tile t = tile_at(i);
                 const int rows = packed_part_rows(p, t.n) * p.H_kv, row = near_rows[i], whole = t.blocks / chunk;
                 if (whole > 0) {
                     const int at = atomicAdd(&hist[whole_of(t)], whole);
+#pragma unroll 1
                     for (int k = 0; k < whole; ++k) {
                         p.entries[at + k] = make_int4(t.s, t.pair, k * chunk, chunk);
                         p.entry_rows[at + k] = row + k * rows;
@@ -403,6 +412,7 @@ __global__ void __launch_bounds__(kPackedPlanThreads) mha_packed_plan_kernel(con
         hist[2 * tid] = end - a - b;
         hist[2 * tid + 1] = end - b;
         __syncthreads();
+#pragma unroll 1
         for (int i = tid; i < tiles; i += kPackedPlanThreads) {
             const Tile t = tile_at(i);
             const int at = atomicAdd(&hist[packed_bucket(t.blocks)], 1);
@@ -960,7 +970,7 @@ mha_packed_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             const int tok_shift = dual ? 0 : t * p.W;           // first token of this tile in the pair
             const int tile_tok = min(it.ntok - tok_shift, p.W);  // its tokens, if positive
             const int Jt = it.J[t], first_block = it.b0 + (dual ? t : 0), block_step = dual ? 2 : 1;
-            if (tile_tok <= 0 || (dual && Jt == 0)) {
+            if (tile_tok <= 0) {
                 drop_item(n);
                 continue;
             }
@@ -1172,7 +1182,7 @@ mha_packed_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             }
             if (row_tok < tile_tok) {
                 if (!direct) {
-                    if (Jt > 0) p.part_ml[static_cast<int64_t>(it.part_row) + shift + row_in_tile] = make_float2(seen ? m_run * c : -INFINITY, seen ? l_run : 0.0f);
+                    p.part_ml[static_cast<int64_t>(it.part_row) + shift + row_in_tile] = make_float2(seen ? m_run * c : -INFINITY, seen ? l_run : 0.0f);
                 } else if (p.LSE) {
                     p.LSE[static_cast<int64_t>(it.tok0 + tok_shift + row_tok) * p.H + it.kvh * p.G + row_head] =
                         seen ? m_run * p.scale + __log2f(l_run) * 0.6931471805599453f : -INFINITY;
@@ -1194,82 +1204,77 @@ mha_packed_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
     }
 }
 
-// Joins the parts of cut key ranges, and a prefix with the tail behind it: one warp per (token, head).
+// Joins the parts of cut key ranges, and a prefix with the tail behind it: one warp per (token, head).  Compact on purpose (short
+// loops, no 64-bit division): most of its time is fetching its instructions and a chain of dependent loads.
 constexpr int kPackedJoinWarps = 8;
 template <int D>
 __global__ void __launch_bounds__(kPackedJoinWarps * 32) mha_packed_join_kernel(const PackedParams p) {
     pdl_launch_dependents();
     constexpr int V = D / 32;  // elements per lane
     cudaGridDependencySynchronize();
-    const int chunk = p.hdr->split;
-    if (chunk == 0) return;
-    const int lane = threadIdx.x & 31;
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * kPackedJoinWarps + (threadIdx.x >> 5);
-    if (row >= static_cast<int64_t>(p.T) * p.H) return;
-    const int tok = static_cast<int>(row / p.H), h = static_cast<int>(row % p.H);
-    // This row's parts: up to two runs (a prefix's and a tail's), each of n parts at rows first + k * step, or first + (k / 2) * step +
-    // (k % 2) * half where both tiles had the same rows.
+    if (p.hdr->split == 0) return;
+    const int lane = threadIdx.x & 31, tok = blockIdx.x, h = blockIdx.y * kPackedJoinWarps + (threadIdx.x >> 5);
+    if (h >= p.H) return;
+    const int kvh = h / p.G, W2 = 2 * p.W;
+    // This row's parts: a run from its sequence's (or group's) tile pair and, behind a prefix, one from its tail.  Part k lies at
+    // first + k * step, or, where both tiles had the same rows, at first + (k / 2) * step + (k % 2) * half.
     int first[2] = {0, 0}, step[2] = {0, 0}, half[2] = {0, 0}, count[2] = {0, 0};
-    auto run = [&](int i, const int4& q, int token) {  // the token's row in sequence q; false: its item has written the result
-        const int W2 = 2 * p.W, pair = token / W2, begin = pair * W2, n = min(W2, q.y - begin);
-        const int whole = packed_tile_blocks(q.y, q.z, p.causal, begin, n), rows = packed_part_rows(p, n), in_pair = token - begin;
-        step[i] = rows * p.H_kv;
-        first[i] = p.tile_rows[q.w + pair] + h / p.G * rows + h % p.G;
-        if (n <= p.W) {
-            half[i] = n * p.G;
-            first[i] += in_pair * p.G;
-            count[i] = whole / chunk * min(2, chunk) + min(2, whole % chunk);  // (a single block is the first tile's alone)
-        } else {
-            if (!p.prefix_lens && whole <= chunk) return false;
-            const int t = in_pair / p.W;
-            first[i] += t * kMhaBlock + (in_pair - t * p.W) * p.G;
-            count[i] = (packed_tile_blocks(q.y, q.z, p.causal, begin + t * p.W, min(p.W, n - t * p.W)) + chunk - 1) / chunk;
-        }
-        return true;
-    };
     const int owner = packed_owner_warp(p, tok);
-    if (p.prefix_lens) {
-        if (owner >= 0) {
-            const int4 q = p.seqs[owner];
-            if (tok - q.x < q.y) run(0, q, tok - q.x);
+    if (owner < 0 && !p.prefix_lens) return;  // a token of no sequence
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        if (i == 0 ? owner < 0 : p.prefix_lens == nullptr) continue;
+        const int4 q = p.seqs[i == 0 ? owner : p.S + tok];
+        const int at = tok - q.x;
+        if (at >= q.y) {  // left out by the plan (not written), or no key behind the prefix
+            if (!p.prefix_lens) return;
+            continue;
         }
-        const int4 q = p.seqs[p.S + tok];
-        if (q.y > 0) run(1, q, 0);
-    } else {
-        if (owner < 0) return;  // a token of no sequence
-        const int4 q = p.seqs[owner];
-        if (tok - q.x >= q.y || !run(0, q, tok - q.x)) return;
+        const int pair = at / W2, in_pair = at - pair * W2, n = min(W2, q.y - pair * W2);
+        const int2 info = p.tile_info[q.w + pair];
+        const bool dual = n <= p.W;
+        if (!p.prefix_lens && !dual && info.y == 1) return;  // not cut: written by its item
+        const int rows = packed_part_rows(p, n), t = !dual && in_pair >= p.W;
+        first[i] = info.x + kvh * rows + t * kMhaBlock + (in_pair - t * p.W) * p.G + h - kvh * p.G;
+        step[i] = rows * p.H_kv;
+        half[i] = n * p.G;
+        count[i] = info.y << dual;
+        if (!dual) half[i] = -1;
     }
-    const int all = count[0] + count[1];
-    auto part = [&](int k) -> int64_t {
-        const int i = k < count[0] ? 0 : 1;
+    auto row_of = [&](int k) -> int {  // parts of both runs, one behind the other
+        const int i = k >= count[0];
         if (i) k -= count[0];
-        // parts of two tiles come in pairs, but for chunks of one block
-        if (half[i] && chunk > 1) return static_cast<int64_t>(first[i]) + static_cast<int64_t>(k >> 1) * step[i] + (k & 1) * half[i];
-        return static_cast<int64_t>(first[i]) + static_cast<int64_t>(k) * step[i];
+        const int f = i ? first[1] : first[0], s = i ? step[1] : step[0], d = i ? half[1] : half[0];
+        return d < 0 ? f + k * s : f + (k >> 1) * s + (k & 1) * d;
     };
+    const int all = count[0] + count[1];
     float m = -INFINITY;
-    for (int k = lane; k < all; k += 32) m = fmaxf(m, p.part_ml[part(k)].x);
+#pragma unroll 1
+    for (int k = lane; k < all; k += 32) m = fmaxf(m, p.part_ml[row_of(k)].x);
 #pragma unroll
     for (int w = 16; w > 0; w >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, w));
     float l = 0.0f, o[V] = {};
+#pragma unroll 1
     for (int k0 = 0; k0 < all; k0 += 32) {
         float weight = 0.0f;
+        int row = 0;
         if (k0 + lane < all) {
-            const float2 ml = p.part_ml[part(k0 + lane)];
+            row = row_of(k0 + lane);
+            const float2 ml = p.part_ml[row];
             weight = ml.x == -INFINITY ? 0.0f : fast_exp2(ml.x - m);
             l += weight * ml.y;
         }
-        for (int k1 = 0; k1 < 32 && k0 + k1 < all; k1 += 4) {  // four parts' loads in flight
-            float v[4][V], w[4];
+        const int n = min(32, all - k0);
+#pragma unroll 1
+        for (int k = 0; k < n; k += 8) {  // eight parts' loads in flight
+            float v[8][V], w[8];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                w[i] = __shfl_sync(0xffffffffu, weight, k1 + i);
-                if (k0 + k1 + i >= all) w[i] = 0.0f;
+            for (int i = 0; i < 8; ++i) {
+                w[i] = __shfl_sync(0xffffffffu, weight, k + i);
+                const float* src = p.part_o + static_cast<int64_t>(__shfl_sync(0xffffffffu, row, k + i)) * D + lane * V;
 #pragma unroll
                 for (int e = 0; e < V; ++e) v[i][e] = 0.0f;
-                if (w[i] != 0.0f) {  // (0: a part without a visible key)
-                    const float* src = p.part_o + part(k0 + k1 + i) * D + lane * V;
+                if (w[i] != 0.0f) {  // (0: a part without a visible key, or none)
                     if constexpr (V == 4) {
                         const float4 f = *reinterpret_cast<const float4*>(src);
                         v[i][0] = f.x; v[i][1] = f.y; v[i][2] = f.z; v[i][3] = f.w;
@@ -1280,26 +1285,26 @@ __global__ void __launch_bounds__(kPackedJoinWarps * 32) mha_packed_join_kernel(
                 }
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 8; ++i)
 #pragma unroll
                 for (int e = 0; e < V; ++e) o[e] = fmaf(v[i][e], w[i], o[e]);
         }
     }
 #pragma unroll
     for (int w = 16; w > 0; w >>= 1) l += __shfl_xor_sync(0xffffffffu, l, w);
-    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+    const float inv = l > 0.0f ? __fdividef(1.0f, l) : 0.0f;
     uint32_t packed[V / 2];
 #pragma unroll
     for (int e = 0; e < V / 2; ++e) packed[e] = pack_bf16x2(o[2 * e] * inv, o[2 * e + 1] * inv);
     __nv_bfloat16* dst = p.O + static_cast<int64_t>(tok) * p.ldo + h * D + lane * V;
     if constexpr (V == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(packed[0], packed[1]);
     else *reinterpret_cast<uint32_t*>(dst) = packed[0];
-    if (lane == 0 && p.LSE) p.LSE[row] = l > 0.0f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+    if (lane == 0 && p.LSE) p.LSE[static_cast<int64_t>(tok) * p.H + h] = l > 0.0f ? (m + __log2f(l)) * 0.6931471805599453f : -INFINITY;
 }
 
-// Scratch: header, sequences, key bases, entries, their rows, tile pairs' rows, partial results.
+// Scratch: header, sequences, key bases, entries, their rows, the tile pairs' parts, partial results.
 struct PackedScratch {
-    size_t seqs, key_base, entries, entry_rows, tile_rows;  // byte offsets
+    size_t seqs, key_base, entries, entry_rows, tile_info;  // byte offsets
     size_t lists;                                           // bytes without partial results
     size_t row_bytes;
     int64_t part_rows;  // rows of partial results that it is sized for
@@ -1322,8 +1327,8 @@ inline PackedScratch packed_scratch(int64_t T, int64_t S, int G, int H_kv, int D
     x.key_base = up(x.seqs + static_cast<size_t>(all) * 16);
     x.entries = up(x.key_base + static_cast<size_t>(all) * 8);
     x.entry_rows = up(x.entries + static_cast<size_t>(x.max_entries) * 16);
-    x.tile_rows = up(x.entry_rows + static_cast<size_t>(x.max_entries) * 4);
-    x.lists = up(x.tile_rows + static_cast<size_t>(std::min<int64_t>(x.max_tiles, kPackedSplitTiles)) * 4);
+    x.tile_info = up(x.entry_rows + static_cast<size_t>(x.max_entries) * 4);
+    x.lists = up(x.tile_info + static_cast<size_t>(std::min<int64_t>(x.max_tiles, kPackedSplitTiles)) * 8);
     x.row_bytes = static_cast<size_t>(D) * 4 + 8;
     return x;
 }
@@ -1344,9 +1349,9 @@ inline int packed_configure() {  // as mha_configure: 0, 1 (a CUDA call failed),
 }
 
 template <class... Params, class... Args>
-inline bool packed_launch_one(void (*kernel)(Params...), int64_t grid, int threads, int smem, cudaStream_t st, Args&&... args) {
+inline bool packed_launch_one(void (*kernel)(Params...), dim3 grid, int threads, int smem, cudaStream_t st, Args&&... args) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(grid));
+    cfg.gridDim = grid;
     cfg.blockDim = dim3(static_cast<unsigned>(threads));
     cfg.dynamicSmemBytes = static_cast<size_t>(smem);
     cfg.stream = st;
@@ -1365,14 +1370,13 @@ struct PackedMaps {
 // plan, attention, and (where key ranges may be cut) the join
 template <int D>
 int packed_launch(const PackedMaps& m, const PackedParams& p, cudaStream_t st) {
-    if (!packed_launch_one(mha_packed_plan_kernel, 1, kPackedPlanThreads, kPackedPlanSmem, st, p)) return 4;
+    if (!packed_launch_one(mha_packed_plan_kernel, dim3(1), kPackedPlanThreads, kPackedPlanSmem, st, p)) return 4;
     const int64_t most = static_cast<int64_t>(p.part_rows > 0 ? p.max_entries : p.max_tiles) * p.H_kv;
-    if (!packed_launch_one(p.part_rows > 0 ? mha_packed_kernel<D, true> : mha_packed_kernel<D, false>, std::min<int64_t>(p.sm_count, most), kMhaThreads,
+    if (!packed_launch_one(p.part_rows > 0 ? mha_packed_kernel<D, true> : mha_packed_kernel<D, false>, dim3(static_cast<unsigned>(std::min<int64_t>(p.sm_count, most))), kMhaThreads,
                            PackedSmem<D>::kTotal, st, m.q, m.q1, m.k, m.v, m.o, m.part, p))
         return 4;
     if (p.part_rows > 0) {
-        const int64_t rows = static_cast<int64_t>(p.T) * p.H;
-        if (!packed_launch_one(mha_packed_join_kernel<D>, (rows + kPackedJoinWarps - 1) / kPackedJoinWarps, kPackedJoinWarps * 32, 0, st, p)) return 4;
+        if (!packed_launch_one(mha_packed_join_kernel<D>, dim3(p.T, (p.H + kPackedJoinWarps - 1) / kPackedJoinWarps), kPackedJoinWarps * 32, 0, st, p)) return 4;
     }
     return 0;
 }

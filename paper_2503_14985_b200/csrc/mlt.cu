@@ -1241,7 +1241,7 @@ int packed_fill(PackedParams* p, PackedMaps* m, const void* Q, void* O, float* L
     p->key_base = reinterpret_cast<long long*>(ws + x.key_base);
     p->entries = reinterpret_cast<int4*>(ws + x.entries);
     p->entry_rows = reinterpret_cast<int*>(ws + x.entry_rows);
-    p->tile_rows = reinterpret_cast<int*>(ws + x.tile_rows);
+    p->tile_info = reinterpret_cast<int2*>(ws + x.tile_info);
     p->max_tiles = static_cast<int>(x.max_tiles);
     p->max_entries = static_cast<int>(x.max_entries);
     p->part_rows = static_cast<int>(part_rows);
