@@ -1112,7 +1112,7 @@ mha_packed_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             // stores alone took 5200 clocks at D = 128: 1600 to convert, 3100 to read the staging area back and store.)
             // Short loops throughout: what runs once per item is fetched cold.
             const bool direct = !kParts || it.part_row < 0;
-            const bool seen = m_run != -INFINITY;
+            const bool seen = Jt > 0 && limit >= first_block * kMhaBlock;  // (by the mask: a row of NaN has no maximum either)
             const int shift = dual ? t * it.ntok * p.G : t * kMhaBlock;  // of a partial result's rows
             uint8_t* base;       // where the tile's token 0, head 0 goes, and the bytes from one token and from one head to the next
             int64_t tok_bytes;
@@ -1292,14 +1292,14 @@ __global__ void __launch_bounds__(kPackedJoinWarps * 32) mha_packed_join_kernel(
     }
 #pragma unroll
     for (int w = 16; w > 0; w >>= 1) l += __shfl_xor_sync(0xffffffffu, l, w);
-    const float inv = l > 0.0f ? __fdividef(1.0f, l) : 0.0f;
+    const float inv = l != 0.0f ? __fdividef(1.0f, l) : 0.0f;  // (NaN stays NaN)
     uint32_t packed[V / 2];
 #pragma unroll
     for (int e = 0; e < V / 2; ++e) packed[e] = pack_bf16x2(o[2 * e] * inv, o[2 * e + 1] * inv);
     __nv_bfloat16* dst = p.O + static_cast<int64_t>(tok) * p.ldo + h * D + lane * V;
     if constexpr (V == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(packed[0], packed[1]);
     else *reinterpret_cast<uint32_t*>(dst) = packed[0];
-    if (lane == 0 && p.LSE) p.LSE[static_cast<int64_t>(tok) * p.H + h] = l > 0.0f ? (m + __log2f(l)) * 0.6931471805599453f : -INFINITY;
+    if (lane == 0 && p.LSE) p.LSE[static_cast<int64_t>(tok) * p.H + h] = l != 0.0f ? (m + __log2f(l)) * 0.6931471805599453f : -INFINITY;
 }
 
 // Scratch: header, sequences, key bases, entries, their rows, the tile pairs' parts, partial results.
