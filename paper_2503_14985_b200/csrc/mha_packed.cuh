@@ -428,6 +428,25 @@ __global__ void __launch_bounds__(kPackedPlanThreads) mha_packed_plan_kernel(con
 }
 constexpr int kPackedPlanSmem = kPackedSeqs * 16 + kPackedBuckets * 4 + kPackedSplitTiles * 20;
 
+// exp2_poly2 (see mha.cuh) with a polynomial of degree 5 (minimax for the relative error on [-1/2, 1/2], 2.2e-7): what is left is the
+// resolution of the exponent, 252 * 2^-25, 5e-6 of the result.  (The cubic's 7.5e-5 showed in the LSE of rows that see one or
+// two keys; two more packed FMAs for one in eight or four exponentials.)
+__device__ __forceinline__ float2 exp2_poly2_fine(float s0, float s1, float cs, float ns) {
+    constexpr float kMagic = 12582912.0f - kPolyLow;  // 1.5 * 2^23 - 125
+    const float2 u = make_float2(fma_sat(s0, cs, ns), fma_sat(s1, cs, ns));
+    const float2 span = make_float2(kPolySpan, kPolySpan), magic = make_float2(kMagic, kMagic);
+    const float2 t = ffma2(u, span, magic);
+    const float2 f = ffma2(u, span, fsub2(magic, t));
+    float2 y = ffma2(f, make_float2(0.0013276472f, 0.0013276472f), make_float2(0.009675541f, 0.009675541f));
+    y = ffma2(y, f, make_float2(0.05550713f, 0.05550713f));
+    y = ffma2(y, f, make_float2(0.2402212f, 0.2402212f));
+    y = ffma2(y, f, make_float2(0.69314694f, 0.69314694f));
+    y = ffma2(y, f, make_float2(1.0f, 1.0f));
+    y.x = __int_as_float(__float_as_int(y.x) + (__float_as_int(t.x) << 23));
+    y.y = __int_as_float(__float_as_int(y.y) + (__float_as_int(t.y) << 23));
+    return y;
+}
+
 template <int D>
 struct PackedSmem {
     static constexpr int kTileBytes = kMhaBlock * D * 2;
@@ -1042,7 +1061,7 @@ mha_packed_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                     uint32_t pk[16];
                     auto exp_pair = [&](int k, bool poly) {
                         const float s0 = __uint_as_float(s[k >> 5][k & 31]), s1 = __uint_as_float(s[k >> 5][(k & 31) + 1]);
-                        if (poly) return exp2_poly2(s0, s1, cs, ns);
+                        if (poly) return exp2_poly2_fine(s0, s1, cs, ns);
                         float2 x = ffma2(make_float2(s0, s1), c2, n2);
                         x.x = fast_exp2(x.x);
                         x.y = fast_exp2(x.y);
