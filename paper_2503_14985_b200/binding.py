@@ -637,22 +637,25 @@ def _out_rows(Q, O, LSE, return_lse, stream):
     """O [T, H, D] with its token pitch, and LSE [T, H] or None: the caller's, checked, or new ones."""
     import torch
     T, H, D = Q.shape
+    ldo = H * D
     if O is None:
         O = _new(Q, (T, H, D), torch.bfloat16, stream)
     elif O.dtype != torch.bfloat16 or O.shape != Q.shape:
         raise ValueError("O must be bfloat16 of Q's shape")
+    else:
+        ldo = _rows(O, H, D)
     if LSE is None and return_lse:
         LSE = _new(Q, (T, H), torch.float32, stream)
     elif LSE is not None and (LSE.dtype != torch.float32 or tuple(LSE.shape) != (T, H) or not LSE.is_contiguous()):
         raise ValueError("LSE must be contiguous float32 [T, H]")
-    return O, _rows(O, H, D), LSE
+    return O, ldo, LSE
 
 
 def _scratch(Q, workspace, need, stream):
     """The caller's workspace, or a new one of the size that is always enough."""
     import torch
     if workspace is None:
-        return _new(Q, (need,), torch.uint8, stream)
+        return _new(Q, (need(),), torch.uint8, stream)
     if not workspace.is_contiguous():
         raise TypeError("workspace must be contiguous")
     return workspace
@@ -690,7 +693,7 @@ def mha_packed_fwd(Q, K, V, cu_q, cu_k=None, *, causal: bool, scale: float, O=No
     if S < 0 or cu_k.numel() != S + 1:
         raise ValueError("cu_q and cu_k must be [sequences + 1]")
     O, ldo, LSE = _out_rows(Q, O, LSE, return_lse, stream)
-    workspace = _scratch(Q, workspace, mha_packed_workspace_bytes(T, S, H, H_kv, D), stream)
+    workspace = _scratch(Q, workspace, lambda: mha_packed_workspace_bytes(T, S, H, H_kv, D), stream)
     held = [Q, K, V, cu_q, cu_k, O, workspace]
     lse = 0
     if LSE is not None:
@@ -727,7 +730,7 @@ def paged_attn_prefill(Q, K_cache, V_cache, cu_tokens, context_lens, block_table
     if cu_tokens.numel() != S + 1 or block_table.dim() != 2 or block_table.shape[0] != S:
         raise ValueError("cu_tokens must be [sequences + 1], context_lens [sequences], block_table [sequences, blocks]")
     O, ldo, LSE = _out_rows(Q, O, LSE, return_lse, stream)
-    workspace = _scratch(Q, workspace, mha_packed_workspace_bytes(T, S, H, H_kv, D), stream)
+    workspace = _scratch(Q, workspace, lambda: mha_packed_workspace_bytes(T, S, H, H_kv, D), stream)
     held = [Q, K_cache, V_cache, cu_tokens, context_lens, block_table, O, workspace]
     lse = 0
     if LSE is not None:
@@ -766,7 +769,7 @@ def paged_attn_decode_shared(Q, K_cache, V_cache, block_table, seq_lens, prefix_
     O, _, LSE = _out_rows(Q, O, LSE, return_lse, stream)
     if not O.is_contiguous():
         raise ValueError("O must be contiguous")
-    workspace = _scratch(Q, workspace, paged_attn_shared_workspace_bytes(S, groups, H, H_kv, D), stream)
+    workspace = _scratch(Q, workspace, lambda: paged_attn_shared_workspace_bytes(S, groups, H, H_kv, D), stream)
     held = [Q, K_cache, V_cache, block_table, seq_lens, prefix_lens, cu_groups, O, workspace]
     lse = 0
     if LSE is not None:

@@ -11,7 +11,8 @@
 //    read once for all G heads.  The Q tile is one TMA box [64 of D, G heads, W tokens] (one token, where there is one).
 //  * Work.  Lengths are on the device, so a one-CTA kernel writes the list of work items (two tiles of a sequence, a range of
 //    key blocks), longest first, and persistent CTAs (one per SM) draw from it by an atomic counter.  The loading warp draws
-//    the next item as soon as it has requested the current one's last keys, so the list's latency hides behind the ring.
+//    the next item while it requests the current one's keys, so the list's latency hides behind the ring.  A call of one short
+//    sequence with an SM for each item needs no list: 37 tokens of 32 heads take 10.6 us without the plan kernel, 13.5 with it.
 //  * Few rows.  With too few items for the SMs (few tokens behind a long context) the plan cuts the key range, and where the rows
 //    fill one tile only, both tiles work on them, each on every other key block ("dual": 128 keys then take 1600 clocks instead of
 //    3000, the latency of one tile's chain S -> softmax -> P V; at the copy bandwidth an SM gets 128 keys in 2800).  The parts go to
@@ -20,8 +21,9 @@
 //    and one issue for the warp.  A block-table entry out of range loads zeros (coordinate beyond the tensor map) and is
 //    reported.  Rows beyond the sequence's last key may hold anything (another sequence, stale cache): scores there are
 //    masked, and a spare warp zeroes those rows of V in shared memory, because a weight of 0 must not meet a NaN.
-//  * Output rows of a tile may belong to a sequence only in part, so they leave as plain 16-byte stores (eight lanes per
-//    128-byte piece of a row) instead of TMA boxes.
+//  * Output rows of a tile may belong to a sequence only in part.  A warp whose 32 rows are all valid sends them as a TMA box
+//    through shared memory, any other as 16-byte stores (eight lanes per 128-byte piece of a row): the epilogue took 4500 to
+//    5200 clocks with plain stores alone, 3200 with boxes.
 #pragma once
 
 #include <utility>
@@ -74,6 +76,7 @@ struct PackedParams {
     float2* part_ml;      // [part_rows] {m in log2 units, l}
     int max_tiles, max_entries, part_rows;
     int sm_count;
+    int single;  // one sequence, no cut ranges, an SM for each item: the items follow from its lengths, without a plan
     int boxes;  // the output tensor maps exist: whole warps' rows leave as TMA boxes (H / H_kv divides 32)
 };
 
@@ -474,8 +477,8 @@ struct PackedItem {  // 48 bytes in shared memory
 
 // kParts: items may be parts of a key range or have both tiles on one tile's rows.  Calls with enough items without that run the
 // kernel that leaves the code out: what the schedulers fetch is what bounds the softmax warps' neighbours (with it prompts
-// ran 2 to 11 % slower, D = 64 the most).
-template <int D, bool kParts>
+// ran 2 to 11 % slower, D = 64 the most).  kOne: PackedParams::single.
+template <int D, bool kParts, bool kOne>
 __global__ void __launch_bounds__(kMhaThreads, 1)
 mha_packed_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_q1,
                   const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
@@ -575,9 +578,19 @@ mha_packed_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
     if (warp == 9) {
         // ------------------------------- loader and scheduler -------------------------------
         setmaxnreg_dec<kMhaOtherRegs>();
-        const int num_items = p.hdr->num_items;
-        const int chunk = p.hdr->split;
         const int W2 = 2 * p.W;
+        int num_items, chunk = 0;
+        int4 e = make_int4(0, 0, 0, 0), q = e;
+        long long base = 0;
+        if constexpr (kOne) {
+            int3 only;
+            if (!packed_sequence(p, 0, only, base) && blockIdx.x == 0 && lane == 0) packed_report(kStatusBadSequence, 0, only.x, only.z);
+            q = make_int4(only.x, only.y, only.z, 0);
+            num_items = (only.y + W2 - 1) / W2 * p.H_kv;
+        } else {
+            num_items = p.hdr->num_items;
+            chunk = p.hdr->split;
+        }
         const int nb = p.cu_k ? 1 : kMhaBlock / p.block_size;     // cache blocks per tile
         const int lane_block = lane % nb, lane_chunk = lane / nb;  // which this lane loads, and which 64 columns of it
         const int beyond = max(1, p.num_blocks * p.H_kv);          // coordinate that loads zeros
@@ -588,18 +601,23 @@ mha_packed_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
         // The next item is drawn while the current one's tiles are loaded, and its entry read: the list's latency (atomic, entry,
         // sequence, one behind the other) is then off the path.
         int idx = blockIdx.x, drawn = 0;
-        int4 e = make_int4(0, 0, 0, 0), q = e;
-        long long base = 0;
         int entry_row = 0;
         auto read_entry = [&]() {
             if (idx < num_items) {
                 const int entry = idx / p.H_kv;
-                e = p.entries[entry];
-                if (kParts && chunk > 0) entry_row = p.entry_rows[entry];
+                if (kOne) {
+                    e = make_int4(0, entry, 0, INT32_MAX);
+                } else {
+                    e = p.entries[entry];
+                    if (kParts && chunk > 0) entry_row = p.entry_rows[entry];
+                }
             }
         };
+        auto draw = [&]() {
+            if (!kOne && lane == 0) drawn = atomicAdd(&p.hdr->counter, 1);
+        };
         auto read_sequence = [&]() {
-            if (idx < num_items) {
+            if (!kOne && idx < num_items) {
                 q = p.seqs[e.x];
                 base = p.key_base[e.x];
             }
@@ -713,7 +731,7 @@ mha_packed_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 const bool is_k = n_k < min(total, kEarlyQK ? (n_v & ~(width - 1)) + 2 * width : n_v + width);
                 if (i == 1) {
                     ok = load_q();
-                    if (lane == 0) drawn = atomicAdd(&p.hdr->counter, 1);
+                    draw();
                 }
                 ok = ok && load(is_k, is_k ? n_k : n_v);
                 n_k += is_k;
@@ -726,7 +744,7 @@ mha_packed_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             if (!ok) break;
             if (it.fix && lane == 0) mbar_arrive(&v_asked[n & 1]);
             if (total == 0) {
-                if (lane == 0) drawn = atomicAdd(&p.hdr->counter, 1);
+                draw();
                 idx = static_cast<int>(gridDim.x) + __shfl_sync(0xffffffffu, drawn, 0);
                 read_entry();
             }
@@ -1360,8 +1378,9 @@ inline int packed_configure() {  // as mha_configure: 0, 1 (a CUDA call failed),
             return 1;
         return a.numRegs < kMhaMinRegsPerThread ? 2 : 0;
     };
-    const int rc[4] = {one(mha_packed_kernel<64, false>, PackedSmem<64>::kTotal), one(mha_packed_kernel<64, true>, PackedSmem<64>::kTotal),
-                       one(mha_packed_kernel<128, false>, PackedSmem<128>::kTotal), one(mha_packed_kernel<128, true>, PackedSmem<128>::kTotal)};
+    const int rc[6] = {one(mha_packed_kernel<64, false, false>, PackedSmem<64>::kTotal), one(mha_packed_kernel<128, false, false>, PackedSmem<128>::kTotal),
+                       one(mha_packed_kernel<64, true, false>, PackedSmem<64>::kTotal), one(mha_packed_kernel<128, true, false>, PackedSmem<128>::kTotal),
+                       one(mha_packed_kernel<64, false, true>, PackedSmem<64>::kTotal), one(mha_packed_kernel<128, false, true>, PackedSmem<128>::kTotal)};
     int worst = 0;
     for (int r : rc) worst = r == 1 || worst == 1 ? 1 : std::max(worst, r);
     return worst;
@@ -1389,10 +1408,11 @@ struct PackedMaps {
 // plan, attention, and (where key ranges may be cut) the join
 template <int D>
 int packed_launch(const PackedMaps& m, const PackedParams& p, cudaStream_t st) {
-    if (!packed_launch_one(mha_packed_plan_kernel, dim3(1), kPackedPlanThreads, kPackedPlanSmem, st, p)) return 4;
+    if (!p.single && !packed_launch_one(mha_packed_plan_kernel, dim3(1), kPackedPlanThreads, kPackedPlanSmem, st, p)) return 4;
     const int64_t most = static_cast<int64_t>(p.part_rows > 0 ? p.max_entries : p.max_tiles) * p.H_kv;
-    if (!packed_launch_one(p.part_rows > 0 ? mha_packed_kernel<D, true> : mha_packed_kernel<D, false>, dim3(static_cast<unsigned>(std::min<int64_t>(p.sm_count, most))), kMhaThreads,
-                           PackedSmem<D>::kTotal, st, m.q, m.q1, m.k, m.v, m.o, m.part, p))
+    const auto kernel = p.part_rows > 0 ? mha_packed_kernel<D, true, false> : p.single ? mha_packed_kernel<D, false, true> : mha_packed_kernel<D, false, false>;
+    if (!packed_launch_one(kernel, dim3(static_cast<unsigned>(std::min<int64_t>(p.sm_count, most))), kMhaThreads, PackedSmem<D>::kTotal, st, m.q, m.q1, m.k,
+                           m.v, m.o, m.part, p))
         return 4;
     if (p.part_rows > 0) {
         if (!packed_launch_one(mha_packed_join_kernel<D>, dim3(p.T, (p.H + kPackedJoinWarps - 1) / kPackedJoinWarps), kPackedJoinWarps * 32, 0, st, p)) return 4;

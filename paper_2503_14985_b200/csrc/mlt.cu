@@ -1248,6 +1248,7 @@ int packed_fill(PackedParams* p, PackedMaps* m, const void* Q, void* O, float* L
     p->part_o = reinterpret_cast<float*>(ws + x.lists);
     p->part_ml = reinterpret_cast<float2*>(p->part_o + static_cast<size_t>(part_rows) * D);
     p->sm_count = sm_count;
+    p->single = S == 1 && part_rows == 0 && x.max_tiles * H_kv <= sm_count;
     const uint64_t dims[3] = {static_cast<uint64_t>(D), static_cast<uint64_t>(H), static_cast<uint64_t>(T)};
     const uint64_t strides[2] = {static_cast<uint64_t>(D) * 2, static_cast<uint64_t>(ldq) * 2};
     const uint32_t box[3] = {64, static_cast<uint32_t>(p->G), static_cast<uint32_t>(p->W)}, box1[3] = {64, static_cast<uint32_t>(p->G), 1};
@@ -1303,6 +1304,7 @@ int mlt_mha_packed_fwd(const void* Q, const void* K, const void* V, const int32_
                        int64_t ldv, int64_t ldo, void* workspace, size_t workspace_bytes, void* stream) {
     bool launch;
     if (num_k < 0) return MLT_ERR_INVALID_ARG;
+    if (num_k == 0) K = V = Q;  // no row of either is read, but their tensor maps want an address
     int rc = packed_check(Q, K, V, O, num_q, num_seqs, H, H_kv, D, scale, ldq, ldo, workspace, &launch);
     if (rc != MLT_OK || !launch) return rc;
     if (!cu_q || !cu_k || ldk < static_cast<int64_t>(H_kv) * D || ldv < static_cast<int64_t>(H_kv) * D) return MLT_ERR_INVALID_ARG;

@@ -104,6 +104,26 @@ def test_offsets_that_do_not_fit_are_left_out_and_reported(bad_q, bad_k, left_ou
         assert (o[:10] == 776).all()
 
 
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("at_q,at_k,T,M", [([3, 20], [5, 90], 30, 100), ([0, 37], [0, 0], 37, 0), ([4, 4], [0, 9], 9, 9), ([0, 200], [0, 180], 200, 256),
+                                           ([2, 40], [0, 9], 39, 9), ([-1, 9], [0, 9], 9, 9), ([0, 9], [7, 3], 9, 9), ([0, 9], [0, 10], 9, 9)])
+def test_one_short_sequence(at_q, at_k, T, M, causal):
+    """One sequence that may leave rows in front and behind, without keys, without tokens, and with offsets that do not fit."""
+    q, k, v = randn(T, 8, 64, seed=1), randn(M, 2, 64, seed=2), randn(M, 2, 64, seed=3)
+    o = torch.full((T, 8, 64), 776.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((T, 8), 776.0, device="cuda")
+    mlt.mha_packed_fwd(q, k, v, i32(at_q), i32(at_k), causal=causal, scale=0.125, O=o, LSE=lse)
+    fits = 0 <= at_q[0] <= at_q[1] <= T and 0 <= at_k[0] <= at_k[1] <= M
+    rc, detail = mlt.last_device_error()
+    assert rc == (0 if fits else 9)
+    a, b = at_q if fits else (0, 0)
+    rows = slice(a, b)
+    kk, vv = (x[at_k[0]: at_k[1]].double() for x in (k, v)) if fits else (k[:0].double(), v[:0].double())
+    check_rows(o[rows], lse[rows], rows_reference(q[rows].double(), kk, vv, visible(b - a, kk.shape[0], causal), 0.125))
+    for x in (o, lse):
+        assert (x[:a] == 776).all() and (x[b:] == 776).all()
+
+
 def test_bad_blocks_and_positions():
     H, Hk, D, bs = 4, 2, 64, 16
     kc, vc, table = paged([100, 60, 40], Hk, D, bs, seed=5)
@@ -240,7 +260,7 @@ def test_caches_and_rows_beyond_32_bits():
     k, v = x[:, :256].unflatten(1, (2, 128)), x[:, 256:512].unflatten(1, (2, 128))
     q = x[:, 512:1536].unflatten(1, (8, 128))
     at = i32([T - 700, T - 690, T])
-    o, lse = mlt.mha_packed_fwd(q, k, v, at, at, causal=True, scale=0.1, O=x[:, 2048:3072].unflatten(1, (8, 128)))
+    o, lse = mlt.mha_packed_fwd(q, k, v, at, at, causal=True, scale=0.1, O=x[:, 2064:3088].unflatten(1, (8, 128)))
     ref = rows_reference(q[-690:].double(), k[-690:].double(), v[-690:].double(), visible(690, 690, True), float(np.float32(0.1)))
     check_rows(o[-690:], lse[-690:], ref)
     assert_device_healthy()
