@@ -16,10 +16,15 @@
 //    K (64-byte swizzle, zeros beyond N and K) into a ring of the warp's own, and a half is requested again as soon as it has been
 //    read; which row of a piece a lane takes is chosen so that the swizzled reads of 16, 8 or 4 bytes (groups of 128, 64, 32)
 //    meet no bank conflicts.
-//  * The 16 warps of a CTA cut K among them (and row tiles, where K is short); their partial sums meet in shared memory.  CTAs are
-//    persistent (one per SM); x stays in shared memory for all row tiles of a CTA.  Where x does not fit or there are fewer tiles than
-//    SMs, a cluster cuts K and sums through distributed shared memory, in a fixed order.  More than 16 rows run as several passes
-//    over the weights (from L2, mostly).
+//  * CTAs are persistent (one per SM) and keep x in shared memory.  The pieces of all row tiles of a CTA, in order (row tile, then
+//    K), are one list of which each of the 16 warps takes a sixteenth, wherever that cuts a tile's K; the sums of the runs meet
+//    once, behind the only barrier.  (Against one set of row tiles at a time, K cut over the warps and a barrier per set:
+//    16 x 28672 x 4096 38.7 -> 29.9 us, 16 x 4096 x 28672 56 -> 42.7, 1 x 28672 x 4096 18.6 -> 16.4; 1 x 4096 x 4096, one tile per CTA
+//    either way, 5.3 -> 5.7.)  Where x does not fit or there are fewer tiles than SMs, a cluster cuts K and sums through
+//    distributed shared memory, in a fixed order.  More than 16 rows run as several passes over the weights (from L2, mostly).
+// Times are those of graphs of ten calls.  58.7 MB of weights (28672 x 4096) take 12.3 us to read by TMA or by plain loads and nothing
+// else, 9 at the copy bandwidth.  With 1 row the kernel is 1.3 of that; with 16 the matrix instructions (m16n8k16 at 16 weights and 8
+// columns) and what turns the words into them bound it.
 #pragma once
 
 #include <cuda_fp16.h>
@@ -50,16 +55,13 @@ struct W4Params {
     int wide_scales;  // a piece's scales (zero points) of a row can be read at once
     int rows;         // rows of x per pass (R of the kernel)
     int steps;        // pieces of K per CTA
-    int k_warps;      // warps that cut them
-    int at_once;      // row tiles at a time, kW4Warps / k_warps
-    unsigned char k_of[kW4Warps], tile_of[kW4Warps];  // a warp's first piece of K and its row tile
     int cluster;      // CTAs that cut K
-    int stride;       // row tiles from one set to a CTA's next
+    int tiles_each, tiles_over;  // row tiles of a CTA or cluster (the first tiles_over have one more)
+    int sets;         // sets of row tiles that those are cut into
+    int set_tiles;    // row tiles of a set, at most
     int ring;         // pieces per warp in flight
-    int red_sets;     // sets of row tiles whose warps' sums fit shared memory
-    int part_sets;    // cluster: sets whose sums do
     // offsets in shared memory, in bytes
-    int at_x, at_fac, at_red, at_part;
+    int at_x, at_fac, at_sums;
 };
 
 // Row (0..7) of an 8-row group that lane group g reads: with the TMA's 64-byte swizzle (16-byte chunk c of row r at c ^ ((r >> 1) & 3))
@@ -87,20 +89,18 @@ __global__ void __launch_bounds__(kW4Threads, 1) gemm_w4_kernel(const __grid_con
     __shared__ uint64_t bars[kW4Warps][2 * kW4MaxRing];
     __shared__ uint32_t abort_word;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int k_warps = p.k_warps, tiles_at_once = p.at_once;
-    const int kw = p.k_of[warp], tw = p.tile_of[warp];                 // (warps with tw == tiles_at_once only help with the sums)
     const int rank = p.cluster > 1 ? static_cast<int>(cluster_ctarank()) : 0;
     const int m0 = blockIdx.y * R, rows = min(R, p.M - m0);
     const int step0 = rank * p.steps;                                  // first piece of K of this CTA
     const int all_steps = (p.K + kW4Step - 1) / kW4Step;
     const int steps = max(0, min(p.steps, all_steps - step0));         // (the last CTAs of a cluster may have fewer, or none)
-    const int tiles = (p.N + kW4Tile - 1) / kW4Tile;
-    const int stride = p.stride, first = (p.cluster > 1 ? static_cast<int>(blockIdx.x) / p.cluster : static_cast<int>(blockIdx.x)) * tiles_at_once;
+    const int owner = static_cast<int>(blockIdx.x) >> (31 - __clz(p.cluster));  // (1, 2, 4 or 8 CTAs)
+    const int first = owner * p.tiles_each + min(owner, p.tiles_over), end = first + p.tiles_each + (owner < p.tiles_over);
     uint8_t* ring = smem + warp * p.ring * kW4PieceBytes;
     uint4* xs = reinterpret_cast<uint4*>(smem + p.at_x);               // [piece][word][row][t]
     float2* fac = reinterpret_cast<float2*>(smem + p.at_fac);          // [group][row] {sum of x times 2^-24, inverse factor times 2^24}
-    float* red = reinterpret_cast<float*>(smem + p.at_red);            // [p.red_sets][warp][up to 8 columns][kW4ColPitch]
-    float* part = reinterpret_cast<float*>(smem + p.at_part);          // cluster: [p.part_sets][tile][row][weight row]
+    float* sums = reinterpret_cast<float*>(smem + p.at_sums);          // [row tile of the set][row of x][kW4ColPitch]
+    constexpr int kSums = R * kW4ColPitch;                             // floats per tile
 
     if (lane == 0) {
         for (int i = 0; i < 2 * kW4MaxRing; ++i) mbar_init(&bars[warp][i], 1);
@@ -111,28 +111,41 @@ __global__ void __launch_bounds__(kW4Threads, 1) gemm_w4_kernel(const __grid_con
     __syncthreads();
     cudaGridDependencySynchronize();
 
-    // pieces of this warp, in order: row tile, then K
-    int ld_tile = tw < tiles_at_once ? first + tw : tiles, ld_step = kw, ld_slot = 0;
+    // A set of row tiles is n * steps pieces in order (row tile, then K), of which each warp takes a sixteenth.
+    int sets_left = p.sets, tile0 = first, n = 0, u = 0, u_end = 0;
+    int ld_tile = 0, ld_step = 0, ld_u = 0, ld_slot = 0;
     auto request = [&](int half) {  // half of the next piece, into its slot
-        if (ld_tile < tiles && ld_step < steps && lane == 0) {
+        if (ld_u < u_end && lane == 0) {
             const int at = 2 * ld_slot + half;
             mbar_arrive_expect_tx(&bars[warp][at], kW4HalfBytes);
             tma_load_2d(ring + at * kW4HalfBytes, &tmap_w, &bars[warp][at], (step0 + ld_step) * (kW4Step / 2) + half * (kW4Step / 4), ld_tile * kW4Tile);
         }
     };
     auto next_request = [&]() {
+        if (ld_u >= u_end) return;
+        ++ld_u;
         if (++ld_slot == p.ring) ld_slot = 0;
-        ld_step += k_warps;
-        if (ld_step >= steps) {
-            ld_step = kw;
-            ld_tile += stride;
+        if (++ld_step == steps) {
+            ld_step = 0;
+            ++ld_tile;
         }
     };
-    for (int i = 0; i < p.ring; ++i) {
-        request(0);
-        request(1);
-        next_request();
-    }
+    auto tile_of = [&](int unit) { return n == 1 || steps == 0 ? 0 : unit / steps; };
+    auto run_start = [&](int w) { return n * steps * w / kW4Warps; };
+    auto begin_set = [&]() {
+        n = min(p.set_tiles, end - tile0);
+        u = run_start(warp);
+        u_end = run_start(warp + 1);
+        ld_u = u;
+        ld_tile = tile0 + tile_of(u);
+        ld_step = u - (ld_tile - tile0) * steps;
+        for (int i = 0; i < p.ring; ++i) {
+            request(0);
+            request(1);
+            next_request();
+        }
+    };
+    begin_set();
 
     // x, in fragment order: 8 consecutive k become (k, k + 4), (k + 1, k + 5), ...
     for (int k8 = threadIdx.x; k8 < steps * (kW4Step / 8); k8 += kW4Threads) {  // (whole warps)
@@ -171,16 +184,14 @@ __global__ void __launch_bounds__(kW4Threads, 1) gemm_w4_kernel(const __grid_con
     __syncthreads();
     // scales and zero points of a piece, as they lie in memory: this lane holds those of row 8 t + w4_row(g)
     const int my_row = w4_row<VEC>(g);
-    const int per_tile = (steps - kw + k_warps - 1) / k_warps;  // pieces of this warp per tile (0 or less: none)
-    int sc_tile = first + tw, sc_step = kw;
-    const int64_t s_on = static_cast<int64_t>(k_warps) * kGroups, s_back = (per_tile - 1) * s_on;
-    const uint16_t* scale_at = reinterpret_cast<const uint16_t*>(p.scales) + (static_cast<int64_t>(sc_tile) * kW4Tile + 8 * t + my_row) * p.lds + (step0 + kw) * kGroups;
-    const uint8_t* zero_at = p.zeros + (static_cast<int64_t>(sc_tile) * kW4Tile + 8 * t + my_row) * p.ldz + (step0 + kw) * kGroups;
+    int sc_tile = 0, sc_step = 0, sc_u = 0;
+    const uint16_t* scale_at = nullptr;
+    const uint8_t* zero_at = nullptr;
     struct Scales {
         uint32_t s[kGroups / 2], z[(kGroups + 3) / 4];
     };
     auto load_scales = [&](Scales& sc) {
-        if (sc_tile < tiles && sc_step < steps) {
+        if (sc_u < u_end) {
             const bool in_n = sc_tile * kW4Tile + 8 * t + my_row < p.N;
             if (p.wide_scales && (step0 + sc_step + 1) * kW4Step <= p.K) {
                 if (in_n) {
@@ -216,13 +227,13 @@ __global__ void __launch_bounds__(kW4Threads, 1) gemm_w4_kernel(const __grid_con
                     }
             }
         }
-        sc_step += k_warps;
-        int64_t by = s_on, z_by = s_on;
-        if (sc_step >= steps) {
-            sc_step = kw;
-            sc_tile += stride;
-            by = static_cast<int64_t>(stride) * kW4Tile * p.lds - s_back;
-            z_by = static_cast<int64_t>(stride) * kW4Tile * p.ldz - s_back;
+        ++sc_u;
+        int64_t by = kGroups, z_by = kGroups;
+        if (++sc_step == steps) {
+            sc_step = 0;
+            ++sc_tile;
+            by += kW4Tile * p.lds - static_cast<int64_t>(steps) * kGroups;
+            z_by += kW4Tile * p.ldz - static_cast<int64_t>(steps) * kGroups;
         }
         scale_at += by;
         zero_at += z_by;
@@ -325,83 +336,65 @@ __global__ void __launch_bounds__(kW4Threads, 1) gemm_w4_kernel(const __grid_con
         }
     };
 
-    // The warps' sums of a set of tiles meet in shared memory, 8 rows of x at a time (one warp adds up those of a row, tile and set, a
-    // lane per weight row); with up to 8 rows several sets wait for that.  With a cluster the CTAs' sums are kept until all sets
-    // are done, or there is no room for more, and then do the same.
-    constexpr int pitch = kColumns * kW4ColPitch;  // of a warp's sums
-    auto put_sums = [&](int set, int m) {
-        float* mine = red + (set * kW4Warps + warp) * pitch;
+    // Sums.  A warp's pieces of a row tile are a run of K.  A run that ends with its tile while the warp has more to do leaves its
+    // sums in the tile's place (there is at most one such run per tile), a warp's last run in the warp's ring, which is empty by
+    // then.  Behind one barrier a warp per (tile, row of x) adds the runs up in the order of K, a lane per weight row.  With a
+    // cluster the CTA's sums take the tile's place, and the CTAs' are added in order.
+    auto put_sums = [&](float* to) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (2 * t + (e & 1) < kColumns) mine[(2 * t + (e & 1)) * kW4ColPitch + h * 16 + (e >> 1) * 8 + my_row] = acc[h][m][e];
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (2 * t + (e & 1) < kColumns) to[(8 * m + 2 * t + (e & 1)) * kW4ColPitch + h * 16 + (e >> 1) * 8 + my_row] = acc[h][m][e];
+                    acc[h][m][e] = 0.0f;
+                }
     };
-    auto store = [&](int tile, int tl, int row, float sum) {
-        const int n = (tile + tl) * kW4Tile + lane;
-        if (n < p.N) p.C[(m0 + row) * p.ldc + n] = __float2bfloat16(sum);
+    auto store = [&](int i, int row, float sum) {
+        const int col = (tile0 + i) * kW4Tile + lane;
+        if (col < p.N) p.C[(m0 + row) * p.ldc + col] = __float2bfloat16(sum);
     };
-    auto add_sums = [&](int sets, int m, int tile, int kept) {  // tile: the last set's first one;  kept: sets in `part` before these
-        const int cols = min(kColumns, rows - 8 * m);
-        for (int i = warp; i < sets * tiles_at_once * cols; i += kW4Warps) {
-            const int col = i % cols, tl = i / cols % tiles_at_once, set = i / cols / tiles_at_once;
-            const float* src = red + (set * kW4Warps + tl * k_warps) * pitch + col * kW4ColPitch + lane;
+    auto add_sums = [&]() {
+        for (int item = warp; item < n * R; item += kW4Warps) {
+            const int i = item / R, row = item % R, from = i * steps, to = from + steps;
+            if (row >= rows) continue;
+            float* place = sums + i * kSums + row * kW4ColPitch + lane;
             float sum = 0.0f;
-#pragma unroll 4
-            for (int w = 0; w < k_warps; ++w) sum += src[w * pitch];
-            if (p.cluster > 1) part[(((kept + set) * tiles_at_once + tl) * R + 8 * m + col) * kW4Tile + lane] = sum;
-            else store(tile - (sets - 1 - set) * stride, tl, 8 * m + col, sum);
+            for (int w = n == 1 ? 0 : i * kW4Warps / n; w < kW4Warps && run_start(w) < to; w += 4) {
+                float v[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int a = run_start(w + j), b = run_start(w + j + 1);
+                    v[j] = 0.0f;
+                    if (w + j < kW4Warps && a < to && b > max(a, from))
+                        v[j] = b > to ? *place : reinterpret_cast<const float*>(smem + (w + j) * p.ring * kW4PieceBytes)[row * kW4ColPitch + lane];
+                }
+                sum += v[0];
+                sum += v[1];
+                sum += v[2];
+                sum += v[3];
+            }
+            if (p.cluster > 1) *place = sum;
+            else store(i, row, sum);
         }
-    };
-    auto exchange = [&](int sets, int tile) {
+        if (p.cluster == 1) return;
         __syncwarp();
         cluster_sync_all();
-        for (int i = rank * kW4Warps + warp; i < sets * tiles_at_once * R; i += p.cluster * kW4Warps) {
-            if (i % R >= rows) continue;
-            const uint32_t at = smem_u32(part + i * kW4Tile + lane);
+        for (int item = rank * kW4Warps + warp; item < n * R; item += p.cluster * kW4Warps) {
+            const int i = item / R, row = item % R;
+            if (row >= rows) continue;
+            const uint32_t at = smem_u32(sums + i * kSums + row * kW4ColPitch + lane);
             float v[8];
 #pragma unroll
             for (int c = 0; c < 8; ++c) {
                 v[c] = 0.0f;
                 if (c < p.cluster) asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[c]) : "r"(map_to_cta(at, static_cast<uint32_t>(c))) : "memory");
             }
-            const int row = i % R, tl = i / R % tiles_at_once, set = i / R / tiles_at_once;
-            store(tile - (sets - 1 - set) * stride, tl, row, ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])));
+            store(i, row, ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])));
         }
         __syncwarp();
         cluster_sync_all();  // the sums have been read
-    };
-    int in_red = 0, kept = 0;
-    auto tile_done = [&](int tile, bool last) {
-        if constexpr (MT == 1) {
-            put_sums(in_red++, 0);
-            if (in_red == p.red_sets || last) {
-                __syncthreads();
-                add_sums(in_red, 0, tile, kept);
-                kept += in_red;
-                in_red = 0;
-                if (!last) __syncthreads();
-            }
-        } else {
-#pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                put_sums(0, m);
-                __syncthreads();
-                add_sums(1, m, tile, kept);
-                if (m + 1 < MT || !last) __syncthreads();
-            }
-            ++kept;
-        }
-        if (p.cluster > 1 && (last || (in_red == 0 && kept + p.red_sets > p.part_sets))) {
-            exchange(kept, tile);
-            kept = 0;
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[h][m][e] = 0.0f;
     };
 
     Scales sc, next_sc;
@@ -410,18 +403,25 @@ __global__ void __launch_bounds__(kW4Threads, 1) gemm_w4_kernel(const __grid_con
 #pragma unroll
     for (int i = 0; i < kGroups / 2; ++i) sc.s[i] = 0u;
     next_sc = sc;
-    int tile = first, step = kw, slot = 0;
+    int slot = 0;
     uint32_t phase = 0;  // of the slot in turn
     bool ok = true;
-    const bool works = tw < tiles_at_once;
-    if (works) load_scales(sc);
 #pragma unroll 1
-    while (tile < tiles) {
-        if (works) {
+    for (;;) {
+        int i = tile_of(u), step = u - i * steps;  // row tile of the set, and piece of K, of unit u
+        sc_u = u;
+        sc_tile = tile0 + i;
+        sc_step = step;
+        const int64_t row = static_cast<int64_t>(sc_tile) * kW4Tile + 8 * t + my_row;
+        scale_at = reinterpret_cast<const uint16_t*>(p.scales) + row * p.lds + (step0 + step) * kGroups;
+        zero_at = p.zeros + row * p.ldz + (step0 + step) * kGroups;
+        load_scales(sc);
+#pragma unroll 1
+        while (u < u_end) {
             load_scales(next_sc);
 #pragma unroll 1
             for (int half = 0; half < 2; ++half) {
-                if (tile + tw < tiles && step < steps && ok) {
+                if (ok) {
                     ok = __all_sync(0xffffffffu, mbar_wait(&bars[warp][2 * slot + half], phase, &abort_word, 0x800 + warp)) != 0;
                     if (ok) compute(slot, half, step, sc);
                 }
@@ -434,13 +434,20 @@ __global__ void __launch_bounds__(kW4Threads, 1) gemm_w4_kernel(const __grid_con
                 slot = 0;
                 phase ^= 1;
             }
+            ++u;
+            if (++step == steps || u == u_end) {
+                put_sums(u == u_end ? reinterpret_cast<float*>(ring) : sums + i * kSums);
+                step = 0;
+                ++i;
+            }
         }
-        step += k_warps;
-        if (step >= steps) {
-            tile_done(tile, tile + stride >= tiles);
-            step = kw;
-            tile += stride;
-        }
+        __syncthreads();
+        add_sums();
+        tile0 += n;
+        if (--sets_left == 0) break;
+        fence_proxy_async_smem();  // the rings have been written and read as sums
+        __syncthreads();
+        begin_set();
     }
 }
 
@@ -494,31 +501,30 @@ inline bool w4_plan(W4Params* p, int group, int sm_count, const int* cluster_slo
     const int all_steps = (p->K + kW4Step - 1) / kW4Step, tiles = (p->N + kW4Tile - 1) / kW4Tile;
     constexpr int kLimit = kW4Smem - 2048;  // 1 KB of static shared memory and its like, 1 KB for the ring's alignment
     auto steps_of = [&](int c) { return std::max(1, (all_steps + c - 1) / c); };
-    auto warps_of = [&](int c) {
-        const int rounds = (steps_of(c) + kW4Warps - 1) / kW4Warps;
-        return (steps_of(c) + rounds - 1) / rounds;
-    };
     auto fixed_bytes = [&](int rows, int c) {  // x and its factors
         return static_cast<int64_t>(rows) * steps_of(c) * (kW4Step * 2 + kW4Step / group * 8) + 16;
     };
-    auto at_once_of = [&](int c) { return kW4Warps / warps_of(c); };
-    auto red_bytes = [&](int rows) { return kW4Warps * std::min(rows, 8) * kW4ColPitch * 4; };
-    auto part_bytes = [&](int rows, int c) { return c > 1 ? at_once_of(c) * kW4Tile * rows * 4 : 0; };
+    auto sum_bytes = [&](int rows) { return rows * kW4ColPitch * 4; };  // of a row tile
     auto ring_of = [&](int rows, int c) {
-        const int64_t left = kLimit - fixed_bytes(rows, c) - red_bytes(rows) - part_bytes(rows, c);
-        return left < 0 ? 0 : static_cast<int>(std::min<int64_t>(kW4MaxRing, left / (at_once_of(c) * warps_of(c) * kW4PieceBytes)));
+        const int64_t left = kLimit - fixed_bytes(rows, c) - sum_bytes(rows);
+        return left < 0 ? 0 : static_cast<int>(std::min<int64_t>(kW4MaxRing, left / (kW4Warps * kW4PieceBytes)));
     };
     auto slots = [&](int c) { return c == 1 ? sm_count : cluster_slots[c == 2 ? 0 : c == 4 ? 1 : 2]; };
-    int rows = 1, c = 1;
+    auto most_tiles = [&](int c) {  // of a cluster
+        const int owners = std::max(1, std::min(slots(c) / c, tiles));
+        return (tiles + owners - 1) / owners;
+    };
+    auto room = [&](int rows, int c) {  // row tiles that a set can have
+        return static_cast<int>((kLimit - fixed_bytes(rows, c) - ring_of(rows, c) * kW4Warps * kW4PieceBytes) / sum_bytes(rows));
+    };
+    // The smallest cluster that x and one piece per warp fit, and beside them the sums of four row tiles, or of all that there are
+    // (16 x 28672 x 4864: sets of one tile 54 us, a cluster of two 48).
+    int rows = 1, c = 0;
     while (rows < 16 && rows < p->M) rows *= 2;
     for (; rows > 0; rows /= 2) {
-        int best = 0;
-        for (int k = 1; k <= 8 && best == 0; k *= 2)  // the smallest cluster that x and one piece per warp fit
-            if (slots(k) >= k && ring_of(rows, k) > 0) {
-                c = k;
-                best = ring_of(rows, k);
-            }
-        if (best > 0) break;
+        for (int k = 8; k >= 1; k /= 2)
+            if (slots(k) >= k && ring_of(rows, k) > 0 && (c == 0 || room(rows, k) >= std::min(4, most_tiles(k)))) c = k;
+        if (c > 0) break;
     }
     if (rows <= 0) return false;
     // fewer tiles than half the SMs: cut K further, while a CTA keeps four pieces
@@ -526,26 +532,18 @@ inline bool w4_plan(W4Params* p, int group, int sm_count, const int* cluster_slo
     p->rows = rows;
     p->cluster = c;
     p->steps = steps_of(c);
-    p->k_warps = warps_of(c);
     p->ring = ring_of(rows, c);
-    const int at_once = at_once_of(c), groups = std::max(1, std::min(slots(c) / c, (tiles + at_once - 1) / at_once));
-    *grid = c * groups;
-    p->at_once = at_once;
-    p->stride = groups * at_once;
-    for (int w = 0; w < kW4Warps; ++w) {
-        p->k_of[w] = static_cast<unsigned char>(w % p->k_warps);
-        p->tile_of[w] = static_cast<unsigned char>(w / p->k_warps);
-    }
-    // The rest of shared memory: a cluster's sums of all sets of tiles first, then sets of the warps' sums.
-    const int sets = (tiles + groups * at_once - 1) / (groups * at_once);
-    p->at_x = at_once * p->k_warps * p->ring * kW4PieceBytes;
+    const int owners = std::max(1, std::min(slots(c) / c, tiles)), most = most_tiles(c);
+    *grid = c * owners;
+    p->at_x = kW4Warps * p->ring * kW4PieceBytes;
     p->at_fac = p->at_x + rows * p->steps * kW4Step * 2;
-    p->at_red = p->at_fac + (rows * p->steps * (kW4Step / group) * 8 + 15) / 16 * 16;
-    const int room = kLimit - p->at_red, part = part_bytes(rows, c), red = red_bytes(rows);
-    p->part_sets = part ? std::min(sets, (room - red) / part) : 0;
-    p->red_sets = rows > 8 ? 1 : std::max(1, std::min({sets, (room - p->part_sets * part) / red, part ? p->part_sets : sets}));
-    p->at_part = p->at_red + p->red_sets * red;
-    *smem = p->at_part + p->part_sets * part + 1024;
+    p->at_sums = p->at_fac + (rows * p->steps * (kW4Step / group) * 8 + 15) / 16 * 16;
+    p->tiles_each = tiles / owners;
+    p->tiles_over = tiles % owners;
+    const int at_most = (kLimit - p->at_sums) / sum_bytes(rows);
+    p->sets = (most + at_most - 1) / at_most;
+    p->set_tiles = (most + p->sets - 1) / p->sets;
+    *smem = p->at_sums + p->set_tiles * sum_bytes(rows) + 1024;
     return true;
 }
 

@@ -65,6 +65,16 @@ def test_gemm_w4(M, N, K, group, zeros):
     assert_device_healthy()
 
 
+@pytest.mark.parametrize("M,N,K,group", [(16, 80000, 4096, 128), (15, 10000, 28672, 32), (16, 10000, 4864, 128), (11, 5000, 9728, 64)])
+def test_several_sets_of_row_tiles(M, N, K, group):
+    """A CTA's row tiles are more than the memory beside x holds sums of (the first two, with and without clusters), or would be."""
+    x, w, s, z = inputs(M, N, K, group, True, seed=N)
+    c = mlt.gemm_w4(x, w, s, z)
+    check(c, x, w, s, z, group)
+    assert torch.equal(c, mlt.gemm_w4(x, w, s, z)), "two calls differ"
+    assert_device_healthy()
+
+
 def test_exact_on_small_integers():
     """Whole numbers that BF16 and FP32 hold: every output is exact."""
     g = torch.Generator(device="cuda").manual_seed(5)
