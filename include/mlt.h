@@ -299,7 +299,7 @@ int mlt_paged_attn_decode_f8(const void* Q, const void* K_cache, const void* V_c
  *   Q       device, BF16; token t, head h, element d at t * ldq + h * D + d
  *   K, V    device, BF16; key j, KV head at j * ldk + h * D + d (likewise ldv); query head h reads KV head h / (H / H_kv)
  *   cu_q, cu_k  device, int32, [num_seqs + 1]: sequence s has the queries cu_q[s] .. cu_q[s + 1] - 1 and the keys
- *           cu_k[s] .. cu_k[s + 1] - 1 (either may be none); they may be the same array
+ *           cu_k[s] .. cu_k[s + 1] - 1 (either may be none; with num_k == 0 K and V are not read); they may be the same array
  *   O       device, BF16 out, pitch ldo;  LSE  device, FP32 out, [num_q, H], or NULL
  *   causal  non-zero: key j is visible to query i of the same sequence iff j <= i + (keys - queries) (bottom-right
  *           aligned; queries beyond the keys see nothing)
@@ -354,7 +354,8 @@ int mlt_paged_attn_prefill(const void* Q, const void* K_cache, const void* V_cac
  *   workspace    device scratch of mlt_paged_attn_shared_workspace_bytes bytes (MLT_ERR_INVALID_ARG with less); calls that overlap
  *                on the GPU must not share it
  * The rest as for mlt_paged_attn_decode, but a bad block-table entry counts as a block of zeros (and is reported).
- * seq_lens may be shorter than the prefix, or 0.  A group whose offsets descend or reach outside num_seqs is left
+ * seq_lens may be shorter than the prefix, or 0; the prefix's blocks are read to their end all the same, so a shared V must be
+ * finite there.  A group whose offsets descend or reach outside num_seqs is left
  * out (its sequences are decoded by themselves) and reported (MLT_ERR_BAD_POSITION); so are, without any output, groups that
  * overlap so that their rows do not fit the workspace.
  * MLT_ERR_UNSUPPORTED when num_seqs + num_seqs / (2 * (128 / (H / H_kv))) + num_groups exceeds 4096, or num_blocks * H_kv reaches 2^31.
@@ -381,7 +382,8 @@ int mlt_paged_attn_decode_shared(const void* Q, const void* K_cache, const void*
  *   C       device, BF16 out, M x N, pitch ldc in elements
  *   group   elements of K per scale: 32, 64 or 128;  K a multiple of it
  * Products are summed in FP32 in a fixed order, weighted, and summed over the groups in FP32; one rounding to nearest even.  Weights are
- * never rounded.  Any M: every 16 rows (fewer for very long K) read the weights once more, so that prompts are better off with
+ * never rounded.  X is brought to FP16 under a power of two of each row's group: exactly, but for elements below 2^-27 of the group's
+ * largest, which are off by at most 2^-38 of that one.  Any M: every 16 rows (fewer for very long K) read the weights once more, so that prompts are better off with
  * mlt_gemm_f8 or mlt_gemm.  M == 0 or N == 0: MLT_OK, nothing launched; K == 0: C is zero-filled.  Needs no scratch.
  */
 int mlt_gemm_w4(const void* X, const void* W, const void* scales, const void* zeros, void* C,

@@ -1,5 +1,6 @@
-"""B200 (sm_100a) dense hot path: BF16 GEMM, FlashAttention-2 style MHA forward, paged decode, and the 8-bit serving path
-(E4M3 quantiser, scaled GEMM, cache append with rotation, decode over an E4M3 cache).
+"""B200 (sm_100a) dense hot path: BF16 GEMM, FlashAttention-2 style MHA forward, paged decode, the 8-bit serving path
+(E4M3 quantiser, scaled GEMM, cache append with rotation, decode over an E4M3 cache) and the BF16 serving path (attention of
+packed prompts and of new tokens over the paged cache, decode behind shared prefixes, few rows times 4-bit weights).
 
 `binding` wraps the C ABI of include/mlt.h (libmlt.so, built by `build`);
 `inputs` holds the seeded synthetic workloads.  Nothing here computes on the CPU.

@@ -24,6 +24,10 @@
 //  * Output rows of a tile may belong to a sequence only in part.  A warp whose 32 rows are all valid sends them as a TMA box
 //    through shared memory, any other as 16-byte stores (eight lanes per 128-byte piece of a row): the epilogue took 4500 to
 //    5200 clocks with plain stores alone, 3200 with boxes.
+// Measured (32 heads over 8, D = 128, device time in graphs): 4 prompts of 4k to 8k, causal, 1090 to 1270 us (1.0 to 1.2 PFLOP/s; a pair
+// of 128-row blocks takes 3250 clocks, 2048 of them products); 8 of 500 to 1500 102 us (720 TFLOP/s, tensor pipe 38 %, exponential unit
+// 37 %); 24 sequences of 100 to 1024 with D = 64 173 us (360 TFLOP/s).  Behind long contexts the bytes of the cache bound it: 32 x 5 tokens,
+// 32 heads over 4, 2k to 4k 77 us, 2.5 TB/s over the call, of which plan, first latencies, last parts and join are about 25 us.
 #pragma once
 
 #include <utility>
