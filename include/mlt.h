@@ -304,6 +304,7 @@ int mlt_paged_attn_decode_f8(const void* Q, const void* K_cache, const void* V_c
  *   causal  non-zero: key j is visible to query i of the same sequence iff j <= i + (keys - queries) (bottom-right
  *           aligned; queries beyond the keys see nothing)
  * H / H_kv is any whole number up to 128, H at most 4096.  D in {64, 128}; pitches in elements, multiples of 8.
+ * num_q / (2 * (128 / (H / H_kv))) + num_seqs must be below 2^20, and that times H_kv at most 2^30 (MLT_ERR_UNSUPPORTED).
  * A query that sees no key gives O = 0 and LSE = -inf.  Rows of O and LSE that belong to no sequence (a padded batch) are
  * left as they were.  What lies in K and V behind a sequence's last key (the next sequence, padding) never reaches its results, not
  * even a NaN; inside a sequence a masked V must be finite (it may meet a weight of zero).

@@ -41,6 +41,7 @@ constexpr unsigned int kStatusBadSequence = 9;  // a sequence's offsets or posit
 constexpr int kPackedPlanThreads = 1024;
 constexpr int kPackedBuckets = 2048;
 constexpr int kPackedSeqs = 1024;        // sequences that the plan keeps in shared memory (more are read back from scratch)
+constexpr int kPackedMaxTiles = 1 << 20;  // tile pairs of a call, so that 1024 threads' sums of that many fit 32 bits
 constexpr int kPackedSplitTiles = 4096;  // key ranges are cut only when there are no more tile pairs than this
 constexpr int kPackedSplitRows = 320 * 2 * kMhaBlock;  // rows of partial results that scratch is sized for (and see packed_scratch)
 
@@ -238,7 +239,7 @@ __global__ void __launch_bounds__(kPackedPlanThreads) mha_packed_plan_kernel(con
 #pragma unroll 1
     for (int s = s_lo; s < s_hi; ++s) {
         get(s);
-        mine += (q.y + W2 - 1) / W2;
+        mine = min(mine + (q.y + W2 - 1) / W2, p.max_tiles + 1);  // (offsets that do not ascend could sum up to more than 32 bits hold)
     }
     int tiles;
     int before = packed_scan(mine, red, tiles) - mine;

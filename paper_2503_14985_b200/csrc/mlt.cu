@@ -1215,8 +1215,9 @@ int packed_check(const void* Q, const void* K, const void* V, const void* O, int
     if (H / H_kv > kMhaBlock || H > 4096) return MLT_ERR_UNSUPPORTED;
     if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(O) || !aligned16(workspace) || ldq % 8 != 0 || ldo % 8 != 0)
         return MLT_ERR_ALIGNMENT;
-    // work items (tile pairs of all sequences x KV heads) are counted in 32 bits
-    if ((static_cast<int64_t>(T) / (2 * (kMhaBlock / (H / H_kv))) + S) * H_kv > INT32_MAX / 2) return MLT_ERR_UNSUPPORTED;
+    // tile pairs of all sequences, and work items (x KV heads), are counted in 32 bits
+    const int64_t pairs = static_cast<int64_t>(T) / (2 * (kMhaBlock / (H / H_kv))) + S;
+    if (pairs >= kPackedMaxTiles || pairs * H_kv > INT32_MAX / 2) return MLT_ERR_UNSUPPORTED;
     *launch = true;
     return MLT_OK;
 }

@@ -124,6 +124,42 @@ def test_one_short_sequence(at_q, at_k, T, M, causal):
         assert (x[:a] == 776).all() and (x[b:] == 776).all()
 
 
+def test_offsets_whose_tiles_sum_up_beyond_32_bits():
+    """0, T, 0, T, ...: every second sequence fits by itself, together they have 2.3e9 tile pairs."""
+    T, S = 1 << 16, 140000
+    q, k = torch.zeros(T, 128, 64, dtype=torch.bfloat16, device="cuda"), randn(8, 1, 64)
+    at_q = torch.zeros(S + 1, dtype=torch.int32, device="cuda")
+    at_q[1::2] = T
+    o, lse = mlt.mha_packed_fwd(q, k, k, at_q, torch.zeros_like(at_q), causal=False, scale=0.125)
+    assert mlt.last_device_error()[0] == 9
+    assert (o == 0).all() and (lse == -math.inf).all()                  # (the first ones are within the call's tokens; no keys)
+    assert_device_healthy()
+
+
+@pytest.mark.parametrize("G,Hk,D", [(128, 1, 64), (128, 2, 128), (100, 1, 128), (64, 2, 64), (33, 3, 64)])
+def test_many_heads_per_kv_head(G, Hk, D):
+    H, bs = G * Hk, 16
+    new, ctx = [1, 5, 0, 40], [700, 0, 9, 33]
+    total = [a + b for a, b in zip(new, ctx)]
+    kc, vc, table = paged(total, Hk, D, bs, seed=G)
+    q = randn(sum(new), H, D, seed=1)
+    o, lse = mlt.paged_attn_prefill(q, kc, vc, cu(new), i32(ctx), table, scale=0.11)
+    a = 0
+    for s, n in enumerate(new):
+        kk, vv = gathered(kc, table[s], total[s]), gathered(vc, table[s], total[s])
+        ref = rows_reference(q[a: a + n].double(), kk, vv, visible(n, total[s], True), float(np.float32(0.11)))
+        check_rows(o[a: a + n], lse[a: a + n], ref, f"sequence {s}")
+        a += n
+    lens = [total[0], total[0] - 30, 0, 5]
+    shared = table[:1].repeat(4, 1).contiguous()
+    q = randn(4, H, D, seed=2)
+    o, lse = mlt.paged_attn_decode_shared(q, kc, vc, shared, i32(lens), i32([640]), i32([0, 3]), scale=0.11)
+    kk, vv = gathered(kc, table[0], total[0]), gathered(vc, table[0], total[0])
+    for s, n in enumerate(lens):
+        check_rows(o[s: s + 1], lse[s: s + 1], rows_reference(q[s: s + 1].double(), kk[:n], vv[:n], visible(1, n, True), float(np.float32(0.11))), f"shared {s}")
+    assert_device_healthy()
+
+
 def test_bad_blocks_and_positions():
     H, Hk, D, bs = 4, 2, 64, 16
     kc, vc, table = paged([100, 60, 40], Hk, D, bs, seed=5)

@@ -41,6 +41,12 @@ def test_shared_refusals(call, tokens):
     assert call(workspace_bytes=100) == 1                              # too little for the list of work items
 
 
+def test_counts_that_do_not_fit():
+    for call in (packed, prefill):
+        assert call(num_seqs=1 << 20) == 2                             # tile pairs
+        assert call(num_seqs=(1 << 18) + 1, H=4096, H_kv=4096, ldq=4096 * 128, ldo=4096 * 128) == 2  # times KV heads
+
+
 def test_packed_refusals():
     assert packed(K=0) == 1 and packed(cu_q=0) == 1 and packed(cu_k=0) == 1 and packed(num_k=-1) == 1
     assert packed(ldk=248) == 1 and packed(ldv=248) == 1 and packed(ldk=260) == 3
