@@ -309,7 +309,7 @@ int mlt_paged_attn_decode_f8(const void* Q, const void* K_cache, const void* V_c
  * left as they were.  What lies in K and V behind a sequence's last key (the next sequence, padding) never reaches its results, not
  * even a NaN; inside a sequence a masked V must be finite (it may meet a weight of zero).
  * A sequence whose offsets descend or reach outside num_q or num_k is left out and reported (MLT_ERR_BAD_POSITION,
- * mlt_last_device_error).  num_q == 0 or num_seqs == 0: MLT_OK, nothing launched.
+ * mlt_last_device_error); so are, of sequences that repeat others' queries, those with which the lists no longer hold all tiles.  num_q == 0 or num_seqs == 0: MLT_OK, nothing launched.
  * P is rounded to BF16 for the second product; S, m, l and O accumulate in FP32.  With few queries behind many keys the key
  * range is cut and the parts are joined in FP32.
  *
@@ -358,7 +358,7 @@ int mlt_paged_attn_prefill(const void* Q, const void* K_cache, const void* V_cac
  * seq_lens may be shorter than the prefix, or 0; the prefix's blocks are read to their end all the same, so a shared V must be
  * finite there.  A group whose offsets descend or reach outside num_seqs is left
  * out (its sequences are decoded by themselves) and reported (MLT_ERR_BAD_POSITION); so are, without any output, groups that
- * overlap so that their rows do not fit the workspace.
+ * overlap so that their tiles or rows do not fit the workspace.
  * MLT_ERR_UNSUPPORTED when num_seqs + num_seqs / (2 * (128 / (H / H_kv))) + num_groups exceeds 4096, or num_blocks * H_kv reaches 2^31.
  */
 size_t mlt_paged_attn_shared_workspace_bytes(int num_seqs, int num_groups, int H, int H_kv, int D);

@@ -216,12 +216,12 @@ __global__ void __launch_bounds__(kPackedPlanThreads) mha_packed_plan_kernel(con
     int4* near_tiles = reinterpret_cast<int4*>(hist + kPackedBuckets);    // [kPackedSplitTiles] {sequence, pair, tokens, key blocks}
     int* near_rows = reinterpret_cast<int*>(near_tiles + kPackedSplitTiles);  // [kPackedSplitTiles]
     __shared__ int red[32];
-    __shared__ int longest_sh;
+    __shared__ int longest_sh, kept_sh;
     __shared__ float best_cost[32];
     __shared__ int best_n[32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     for (int i = tid; i < kPackedBuckets; i += kPackedPlanThreads) hist[i] = 0;
-    if (tid == 0) longest_sh = 0;
+    if (tid == 0) longest_sh = kept_sh = 0;
     cudaGridDependencySynchronize();
 
     // sequences: tile pairs and their prefix sums
@@ -241,13 +241,17 @@ __global__ void __launch_bounds__(kPackedPlanThreads) mha_packed_plan_kernel(con
         get(s);
         mine = min(mine + (q.y + W2 - 1) / W2, p.max_tiles + 1);  // (offsets that do not ascend could sum up to more than 32 bits hold)
     }
-    int tiles;
-    int before = packed_scan(mine, red, tiles) - mine;
+    int pairs, kept = 0;
+    int before = packed_scan(mine, red, pairs) - mine;
+    // Offsets that do not ascend can have more tile pairs than the call's tokens make, which is what the lists and the scratch are sized
+    // for.  The sequences from the one on that does not fit are left out; with shared prefixes, where a token's group and its tail
+    // belong together, all are.
+    const bool too_many = pairs > p.max_tiles;
 #pragma unroll 1
     for (int s = s_lo; s < s_hi; ++s) {
         if (per > 1) get(s);
         int n = (q.y + W2 - 1) / W2;
-        if (before > p.max_tiles - n) {  // more tokens than the call has: the offsets do not ascend
+        if (before > p.max_tiles - n) {
             ok = false;
             q.y = n = 0;
         }
@@ -257,9 +261,13 @@ __global__ void __launch_bounds__(kPackedPlanThreads) mha_packed_plan_kernel(con
         p.key_base[s] = base;
         if (s < kPackedSeqs) near_seqs[s] = e;
         before += n;
+        if (n > 0) kept = before;
     }
-    tiles = min(tiles, p.max_tiles);
+    kept = __reduce_max_sync(0xffffffffu, kept);
+    if (lane == 0) atomicMax(&kept_sh, kept);
     __syncthreads();
+    // (up to the end of the last sequence that is kept: the numbers behind it belong to no tile)
+    const int tiles = too_many && p.prefix_lens ? 0 : kept_sh;
 
     // tile pair i: its sequence (the last one with at most i pairs before it), number in it, tokens and key blocks
     const int4* seqs = p.all <= kPackedSeqs ? near_seqs : p.seqs;
@@ -285,7 +293,7 @@ __global__ void __launch_bounds__(kPackedPlanThreads) mha_packed_plan_kernel(con
         const int4 t = near_tiles[i];
         return Tile{t.x, t.y, t.z, t.w};
     };
-    const bool may_split = p.part_rows > 0 && near;
+    const bool may_split = p.part_rows > 0 && near && !(too_many && p.prefix_lens);
     int most = 0;
 #pragma unroll 1
     for (int i = tid; i < tiles; i += kPackedPlanThreads) {
@@ -376,9 +384,11 @@ __global__ void __launch_bounds__(kPackedPlanThreads) mha_packed_plan_kernel(con
             const int row = first_row + packed_scan(parts * rows, red, sum_rows) - parts * rows;
             if (i < tiles) p.tile_info[i] = make_int2(row, parts);
             if (i < tiles) near_rows[i] = row;
+            // (only for groups that overlap: scratch is sized for groups that do not)
+            const bool no_room = sum_rows > p.part_rows - first_row || sum_parts > p.max_entries - first;
             first += sum_parts;
             first_row += sum_rows;
-            if (first_row > p.part_rows || first > p.max_entries) {  // (only for groups that overlap: scratch is sized for groups that do not)
+            if (no_room) {
                 if (tid == 0) packed_report(kStatusBadSequence, p.S, tiles, 0);
                 first = 0;
                 chunk = 0;
