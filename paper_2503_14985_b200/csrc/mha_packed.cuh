@@ -49,7 +49,7 @@ struct PackedHeader {  // at the front of the scratch memory, written by the pla
     int num_items;     // entries * H_kv
     int counter;       // items handed out beyond the first one of each CTA
     int split;         // key blocks per part, 0: no range is cut
-    int pad;
+    int irregular;     // a sequence is left out: the offsets need not ascend
 };
 
 struct PackedParams {
@@ -161,6 +161,19 @@ __device__ __forceinline__ int packed_owner_warp(const PackedParams& p, int t) {
     return p.cu_q[lo] <= t && t < p.cu_q[lo + 1] ? lo : -1;
 }
 
+// The same where offsets need not ascend, so that no search by halves finds what is kept: behind shared prefixes what the plan gave the
+// token's tail, else the first sequence that is kept and has the token.
+__device__ __noinline__ int packed_owner_any(const PackedParams& p, int t) {
+    if (p.prefix_lens) return packed_owner(p, t);
+    for (int s0 = 0; s0 < p.S; s0 += 32) {
+        const int s = s0 + static_cast<int>(threadIdx.x & 31);
+        const int4 q = s < p.S ? p.seqs[s] : make_int4(0, 0, 0, 0);
+        const unsigned int has = __ballot_sync(0xffffffffu, q.x <= t && t - q.x < q.y);
+        if (has) return s0 + __ffs(has) - 1;
+    }
+    return -1;
+}
+
 // The keys of decoded sequence t behind its group's prefix.
 __device__ __forceinline__ void packed_tail(const PackedParams& p, int t, int3& q, long long& base) {
     int3 g;
@@ -216,12 +229,12 @@ __global__ void __launch_bounds__(kPackedPlanThreads) mha_packed_plan_kernel(con
     int4* near_tiles = reinterpret_cast<int4*>(hist + kPackedBuckets);    // [kPackedSplitTiles] {sequence, pair, tokens, key blocks}
     int* near_rows = reinterpret_cast<int*>(near_tiles + kPackedSplitTiles);  // [kPackedSplitTiles]
     __shared__ int red[32];
-    __shared__ int longest_sh, kept_sh;
+    __shared__ int longest_sh, kept_sh, irregular_sh;
     __shared__ float best_cost[32];
     __shared__ int best_n[32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     for (int i = tid; i < kPackedBuckets; i += kPackedPlanThreads) hist[i] = 0;
-    if (tid == 0) longest_sh = kept_sh = 0;
+    if (tid == 0) longest_sh = kept_sh = irregular_sh = 0;
     cudaGridDependencySynchronize();
 
     // sequences: tile pairs and their prefix sums
@@ -255,7 +268,10 @@ __global__ void __launch_bounds__(kPackedPlanThreads) mha_packed_plan_kernel(con
             ok = false;
             q.y = n = 0;
         }
-        if (!ok) packed_report(kStatusBadSequence, s, q.x, q.z);
+        if (!ok) {
+            packed_report(kStatusBadSequence, s, q.x, q.z);
+            irregular_sh = 1;
+        }
         const int4 e = make_int4(q.x, q.y, q.z, before);
         p.seqs[s] = e;
         p.key_base[s] = base;
@@ -442,6 +458,7 @@ __global__ void __launch_bounds__(kPackedPlanThreads) mha_packed_plan_kernel(con
         p.hdr->num_items = total * p.H_kv;
         p.hdr->counter = 0;
         p.hdr->split = chunk;
+        p.hdr->irregular = irregular_sh;
     }
 }
 constexpr int kPackedPlanSmem = kPackedSeqs * 16 + kPackedBuckets * 4 + kPackedSplitTiles * 20;
@@ -1271,7 +1288,7 @@ __global__ void __launch_bounds__(kPackedJoinWarps * 32) mha_packed_join_kernel(
     // This row's parts: a run from its sequence's (or group's) tile pair and, behind a prefix, one from its tail.  Part k lies at
     // first + k * step, or, where both tiles had the same rows, at first + (k / 2) * step + (k % 2) * half.
     int first[2] = {0, 0}, step[2] = {0, 0}, half[2] = {0, 0}, count[2] = {0, 0};
-    const int owner = packed_owner_warp(p, tok);
+    const int owner = p.hdr->irregular ? packed_owner_any(p, tok) : packed_owner_warp(p, tok);
     if (owner < 0 && !p.prefix_lens) return;  // a token of no sequence
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
