@@ -331,7 +331,8 @@ int mlt_mha_packed_fwd(const void* Q, const void* K, const void* V, const int32_
  *   Q       device, BF16, pitch ldq, rotated;  K_cache, V_cache  device, BF16, [num_blocks, H_kv, block_size, D]
  *   token t of sequence s sees the positions 0 .. context_lens[s] + t - cu_tokens[s] of its cache
  *   O, LSE, workspace (mlt_mha_packed_workspace_bytes) and the rest as for mlt_mha_packed_fwd
- * block_size in {8, 16, 32}; num_blocks * H_kv must be below 2^31.  A block-table entry outside [0, num_blocks) that a
+ * block_size in {8, 16, 32}; num_blocks * H_kv must be below 2^31, max_blocks_per_seq * block_size at most 2^31 - 128
+ * (MLT_ERR_UNSUPPORTED).  A block-table entry outside [0, num_blocks) that a
  * sequence reaches counts as a block of zeros and is reported (MLT_ERR_BAD_BLOCK).  A sequence whose offsets do not fit
  * num_tokens, whose context is negative, or whose positions do not fit the table is left out and reported (MLT_ERR_BAD_POSITION).
  */
@@ -359,7 +360,8 @@ int mlt_paged_attn_prefill(const void* Q, const void* K_cache, const void* V_cac
  * finite there.  A group whose offsets descend or reach outside num_seqs is left
  * out (its sequences are decoded by themselves) and reported (MLT_ERR_BAD_POSITION); so are, without any output, groups that
  * overlap so that their tiles or rows do not fit the workspace.
- * MLT_ERR_UNSUPPORTED when num_seqs + num_seqs / (2 * (128 / (H / H_kv))) + num_groups exceeds 4096, or num_blocks * H_kv reaches 2^31.
+ * MLT_ERR_UNSUPPORTED when num_seqs + num_seqs / (2 * (128 / (H / H_kv))) + num_groups exceeds 4096, num_blocks * H_kv reaches 2^31, or
+ * max_blocks_per_seq * block_size exceeds 2^31 - 128.
  */
 size_t mlt_paged_attn_shared_workspace_bytes(int num_seqs, int num_groups, int H, int H_kv, int D);
 int mlt_paged_attn_decode_shared(const void* Q, const void* K_cache, const void* V_cache,

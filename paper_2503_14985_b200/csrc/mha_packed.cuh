@@ -42,6 +42,7 @@ constexpr int kPackedPlanThreads = 1024;
 constexpr int kPackedBuckets = 2048;
 constexpr int kPackedSeqs = 1024;        // sequences that the plan keeps in shared memory (more are read back from scratch)
 constexpr int kPackedMaxTiles = 1 << 20;  // tile pairs of a call, so that 1024 threads' sums of that many fit 32 bits
+constexpr int kPackedMaxKeys = INT32_MAX - 127;  // keys that a block table's row spans, so that positions in whole key blocks fit 32 bits
 constexpr int kPackedSplitTiles = 4096;  // key ranges are cut only when there are no more tile pairs than this
 constexpr int kPackedSplitRows = 320 * 2 * kMhaBlock;  // rows of partial results that scratch is sized for (and see packed_scratch)
 

@@ -1346,6 +1346,7 @@ int mlt_paged_attn_prefill(const void* Q, const void* K_cache, const void* V_cac
     if (!cu_tokens || !context_lens || !block_table) return MLT_ERR_INVALID_ARG;
     if (block_size != 8 && block_size != 16 && block_size != 32) return MLT_ERR_UNSUPPORTED;
     if (static_cast<int64_t>(num_blocks) * H_kv > INT32_MAX) return MLT_ERR_UNSUPPORTED;
+    if (static_cast<int64_t>(max_blocks_per_seq) * block_size > kPackedMaxKeys) return MLT_ERR_UNSUPPORTED;
     const PackedScratch x = packed_scratch(num_tokens, num_seqs, H / H_kv, H_kv, D);
     if (workspace_bytes < x.lists) return MLT_ERR_INVALID_ARG;
     DeviceInfo dev;
@@ -1390,6 +1391,7 @@ int mlt_paged_attn_decode_shared(const void* Q, const void* K_cache, const void*
     if (!block_table || !seq_lens || !cu_groups || (num_groups > 0 && !prefix_lens)) return MLT_ERR_INVALID_ARG;
     if (block_size != 8 && block_size != 16 && block_size != 32) return MLT_ERR_UNSUPPORTED;
     if (static_cast<int64_t>(num_blocks) * H_kv > INT32_MAX) return MLT_ERR_UNSUPPORTED;
+    if (static_cast<int64_t>(max_blocks_per_seq) * block_size > kPackedMaxKeys) return MLT_ERR_UNSUPPORTED;
     const PackedScratch x = packed_scratch(num_seqs, num_groups, H / H_kv, H_kv, D, true);
     if (x.max_tiles > kPackedSplitTiles || x.part_rows > INT32_MAX) return MLT_ERR_UNSUPPORTED;
     if (workspace_bytes < x.lists + static_cast<size_t>(x.part_rows) * x.row_bytes) return MLT_ERR_INVALID_ARG;
