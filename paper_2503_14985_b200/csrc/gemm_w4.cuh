@@ -9,6 +9,10 @@
 //    products are exact, and the group's scale and the factors are applied once per group and output.
 //  * x is BF16, whose range FP16 lacks: each group of a row is multiplied by the power of two that brings its largest element to
 //    2^14 .. 2^15, and the inverse goes into the group's factor.  An element loses bits only below 2^-27 of that largest one.
+//    (The smallest BF16 numbers would need more than an FP32 power of two, but 2^126 already makes whole multiples of 2^-7 of them.)
+//  * Range.  The inverse times 2^24 need not fit FP32, so 2^12 of it are kept for the end: a group's sum times 2^-12 fits whatever x
+//    is, and meets the scale only then (two columns at a time: one by one, 16 x 4096 x 28672 took 46.1 us instead of 43.6).  Sums over groups overflow where 2^12 times as much would.  What is smaller than 2^-114 is
+//    rounded at 2^-138.  The sum of x itself is taken in units of 2^8.
 //  * The order of the summation index of an MMA is free.  The pairs of a word are (k, k + 4); x is laid out in shared memory
 //    in that order once per CTA, as the B fragments (16 bytes per lane, no bank conflicts).  A lane's words of a group lie side by
 //    side, so that a quad covers whole groups.
@@ -44,6 +48,7 @@ constexpr int kW4PieceBytes = kW4Tile * kW4Step / 2, kW4HalfBytes = kW4PieceByte
 constexpr int kW4MaxRing = 3;      // pieces per warp in shared memory
 constexpr int kW4ColPitch = 36;    // words per column of a warp's partial sums (no bank conflicts)
 constexpr int kW4Smem = 227 * 1024;
+constexpr float kW4SumUnit = 0.00390625f;  // 2^-8: 128 elements of any BF16 value add up to less than FP32's largest
 
 struct W4Params {
     const __nv_bfloat16* X;       // [M, K], pitch ldx
@@ -98,7 +103,7 @@ __global__ void __launch_bounds__(kW4Threads, 1) gemm_w4_kernel(const __grid_con
     const int first = owner * p.tiles_each + min(owner, p.tiles_over), end = first + p.tiles_each + (owner < p.tiles_over);
     uint8_t* ring = smem + warp * p.ring * kW4PieceBytes;
     uint4* xs = reinterpret_cast<uint4*>(smem + p.at_x);               // [piece][word][row][t]
-    float2* fac = reinterpret_cast<float2*>(smem + p.at_fac);          // [group][row] {sum of x times 2^-24, inverse factor times 2^24}
+    float2* fac = reinterpret_cast<float2*>(smem + p.at_fac);          // [group][row] {scaled sum of x times 2^-24, inverse factor times 2^12}
     float* sums = reinterpret_cast<float*>(smem + p.at_sums);          // [row tile of the set][row of x][kW4ColPitch]
     constexpr int kSums = R * kW4ColPitch;                             // floats per tile
 
@@ -163,7 +168,13 @@ __global__ void __launch_bounds__(kW4Threads, 1) gemm_w4_kernel(const __grid_con
         for (int i = 0; i < R; ++i) {
             float f[8];
             bf16x8_to_f32(v[i], f);
-            float top = 0.0f, sum = ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+            float top = 0.0f, sum = f[0] * kW4SumUnit, sum1 = f[4] * kW4SumUnit;
+#pragma unroll
+            for (int e = 1; e < 4; ++e) {
+                sum = fmaf(f[e], kW4SumUnit, sum);
+                sum1 = fmaf(f[e + 4], kW4SumUnit, sum1);
+            }
+            sum += sum1;
 #pragma unroll
             for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(f[e]));
 #pragma unroll
@@ -178,7 +189,7 @@ __global__ void __launch_bounds__(kW4Threads, 1) gemm_w4_kernel(const __grid_con
             to[i * 4] = make_uint4(*reinterpret_cast<const uint32_t*>(&h0), *reinterpret_cast<const uint32_t*>(&h1),
                                    *reinterpret_cast<const uint32_t*>(&h2), *reinterpret_cast<const uint32_t*>(&h3));
             if (r == 0)
-                fac[((k8 / 32) * kGroups + q) * R + i] = make_float2(sum * mul * 5.9604644775390625e-8f, 16777216.0f * __uint_as_float(static_cast<uint32_t>(254 - up) << 23));
+                fac[((k8 / 32) * kGroups + q) * R + i] = make_float2(sum * mul * 1.52587890625e-5f, __uint_as_float(static_cast<uint32_t>(266 - up) << 23));
         }
     }
     __syncthreads();
@@ -328,10 +339,14 @@ __global__ void __launch_bounds__(kW4Threads, 1) gemm_w4_kernel(const __grid_con
             for (int m = 0; m < MT; ++m)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    acc[h][m][0] = fmaf(s[2 * h] * u0[m], c[h][m][0], acc[h][m][0]);
-                    acc[h][m][1] = fmaf(s[2 * h] * u1[m], c[h][m][1], acc[h][m][1]);
-                    acc[h][m][2] = fmaf(s[2 * h + 1] * u0[m], c[h][m][2], acc[h][m][2]);
-                    acc[h][m][3] = fmaf(s[2 * h + 1] * u1[m], c[h][m][3], acc[h][m][3]);
+#pragma unroll
+                    for (int e = 0; e < 4; e += 2) {
+                        const float sc_row = s[2 * h + e / 2];
+                        const float2 sum = fmul2(make_float2(c[h][m][e], c[h][m][e + 1]), make_float2(u0[m], u1[m]));
+                        const float2 to = ffma2(sum, make_float2(sc_row, sc_row), make_float2(acc[h][m][e], acc[h][m][e + 1]));
+                        acc[h][m][e] = to.x;
+                        acc[h][m][e + 1] = to.y;
+                    }
                 }
         }
     };
@@ -353,7 +368,7 @@ __global__ void __launch_bounds__(kW4Threads, 1) gemm_w4_kernel(const __grid_con
     };
     auto store = [&](int i, int row, float sum) {
         const int col = (tile0 + i) * kW4Tile + lane;
-        if (col < p.N) p.C[(m0 + row) * p.ldc + col] = __float2bfloat16(sum);
+        if (col < p.N) p.C[(m0 + row) * p.ldc + col] = __float2bfloat16(sum * 4096.0f);
     };
     auto add_sums = [&]() {
         for (int item = warp; item < n * R; item += kW4Warps) {
