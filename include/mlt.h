@@ -387,9 +387,11 @@ int mlt_paged_attn_decode_shared(const void* Q, const void* K_cache, const void*
  * Products are summed in FP32 in a fixed order, weighted, and summed over the groups in FP32; one rounding to nearest even.  Weights are
  * never rounded.  X is brought to FP16 under a power of two of each row's group: exactly, but for elements below 2^-27 of the group's
  * largest, which are off by at most 2^-38 of that one.  That goes for every finite x and scale; near the lower end of the range a
- * group's sum is rounded at 2^-138 before its scale, and an addition over groups at 2^-138.  Any M: every 16 rows (fewer for very
- * long K) read the weights once more, so that prompts are better off with
- * mlt_gemm_f8 or mlt_gemm.  M == 0 or N == 0: MLT_OK, nothing launched; K == 0: C is zero-filled.  Needs no scratch.
+ * group's sum is rounded at 2^-138 before its scale, and an addition over groups at 2^-138.
+ * Every 16 rows read the weights once more, so that prompts are better off with mlt_gemm_f8 or mlt_gemm.  A pass has 16 rows up to
+ * K = 34816 (group 32; 36864 with 64, 38912 with 128), then 8, 4, 2 or 1, each up to about twice the K.  MLT_ERR_UNSUPPORTED when M
+ * exceeds 2^19 or 65535 passes, or K what a pass of one row may have: 583680, 618496 or 636928.
+ * M == 0 or N == 0: MLT_OK, nothing launched; K == 0: C is zero-filled.  Needs no scratch.
  */
 int mlt_gemm_w4(const void* X, const void* W, const void* scales, const void* zeros, void* C,
                 int64_t M, int64_t N, int64_t K, int group,

@@ -510,27 +510,40 @@ bool w4_configure_rows() {
 }
 inline bool w4_configure() { return w4_configure_rows<1>() && w4_configure_rows<2>() && w4_configure_rows<4>(); }
 
-// Rows per pass, CTAs per cluster, warps along K and the layout of shared memory; false if not even one row of x fits a cluster of 8.
+// Pieces per warp that fit beside `rows` rows of x and the sums of one row tile, K cut over c CTAs (0: not even one).
+constexpr int kW4Limit = kW4Smem - 2048;  // 1 KB of static shared memory and its like, 1 KB for the ring's alignment
+inline int w4_steps(int K, int c) {
+    const int all_steps = (K + kW4Step - 1) / kW4Step;
+    return std::max(1, (all_steps + c - 1) / c);
+}
+inline int64_t w4_fixed_bytes(int K, int group, int rows, int c) {  // x and its factors
+    return static_cast<int64_t>(rows) * w4_steps(K, c) * (kW4Step * 2 + kW4Step / group * 8) + 16;
+}
+inline int w4_sum_bytes(int rows) { return rows * kW4ColPitch * 4; }  // of a row tile
+inline int w4_ring(int K, int group, int rows, int c) {
+    const int64_t left = kW4Limit - w4_fixed_bytes(K, group, rows, c) - w4_sum_bytes(rows);
+    return left < 0 ? 0 : static_cast<int>(std::min<int64_t>(kW4MaxRing, left / (kW4Warps * kW4PieceBytes)));
+}
+// Whether M rows, as many at a time as a cluster of 8 holds, are no more passes than a grid has.
+inline bool w4_fits(int64_t M, int K, int group) {
+    int rows = 16;
+    while (rows > 0 && w4_ring(K, group, rows, 8) == 0) rows /= 2;
+    return rows > 0 && (M + rows - 1) / rows <= 65535;
+}
+
+// Rows per pass, CTAs per cluster, warps along K and the layout of shared memory; false if not even one row of x fits a cluster of 8, or
+// there are more passes than a grid has.
 // cluster_slots: resident CTAs in clusters of 2, 4, 8.
 inline bool w4_plan(W4Params* p, int group, int sm_count, const int* cluster_slots, int* grid, int* smem) {
     const int all_steps = (p->K + kW4Step - 1) / kW4Step, tiles = (p->N + kW4Tile - 1) / kW4Tile;
-    constexpr int kLimit = kW4Smem - 2048;  // 1 KB of static shared memory and its like, 1 KB for the ring's alignment
-    auto steps_of = [&](int c) { return std::max(1, (all_steps + c - 1) / c); };
-    auto fixed_bytes = [&](int rows, int c) {  // x and its factors
-        return static_cast<int64_t>(rows) * steps_of(c) * (kW4Step * 2 + kW4Step / group * 8) + 16;
-    };
-    auto sum_bytes = [&](int rows) { return rows * kW4ColPitch * 4; };  // of a row tile
-    auto ring_of = [&](int rows, int c) {
-        const int64_t left = kLimit - fixed_bytes(rows, c) - sum_bytes(rows);
-        return left < 0 ? 0 : static_cast<int>(std::min<int64_t>(kW4MaxRing, left / (kW4Warps * kW4PieceBytes)));
-    };
+    auto ring_of = [&](int rows, int c) { return w4_ring(p->K, group, rows, c); };
     auto slots = [&](int c) { return c == 1 ? sm_count : cluster_slots[c == 2 ? 0 : c == 4 ? 1 : 2]; };
     auto most_tiles = [&](int c) {  // of a cluster
         const int owners = std::max(1, std::min(slots(c) / c, tiles));
         return (tiles + owners - 1) / owners;
     };
     auto room = [&](int rows, int c) {  // row tiles that a set can have
-        return static_cast<int>((kLimit - fixed_bytes(rows, c) - ring_of(rows, c) * kW4Warps * kW4PieceBytes) / sum_bytes(rows));
+        return static_cast<int>((kW4Limit - w4_fixed_bytes(p->K, group, rows, c) - ring_of(rows, c) * kW4Warps * kW4PieceBytes) / w4_sum_bytes(rows));
     };
     // The smallest cluster that x and one piece per warp fit, and beside them the sums of four row tiles, or of all that there are
     // (16 x 28672 x 4864: sets of one tile 54 us, a cluster of two 48).
@@ -541,12 +554,12 @@ inline bool w4_plan(W4Params* p, int group, int sm_count, const int* cluster_slo
             if (slots(k) >= k && ring_of(rows, k) > 0 && (c == 0 || room(rows, k) >= std::min(4, most_tiles(k)))) c = k;
         if (c > 0) break;
     }
-    if (rows <= 0) return false;
+    if (rows <= 0 || (p->M + rows - 1) / rows > 65535) return false;
     // fewer tiles than half the SMs: cut K further, while a CTA keeps four pieces
     while (c < 8 && slots(2 * c) >= 2 * c && static_cast<int64_t>(tiles) * 2 * c <= sm_count && all_steps >= 2 * c * 4) c *= 2;
     p->rows = rows;
     p->cluster = c;
-    p->steps = steps_of(c);
+    p->steps = w4_steps(p->K, c);
     p->ring = ring_of(rows, c);
     const int owners = std::max(1, std::min(slots(c) / c, tiles)), most = most_tiles(c);
     *grid = c * owners;
@@ -555,10 +568,10 @@ inline bool w4_plan(W4Params* p, int group, int sm_count, const int* cluster_slo
     p->at_sums = p->at_fac + (rows * p->steps * (kW4Step / group) * 8 + 15) / 16 * 16;
     p->tiles_each = tiles / owners;
     p->tiles_over = tiles % owners;
-    const int at_most = (kLimit - p->at_sums) / sum_bytes(rows);
+    const int at_most = (kW4Limit - p->at_sums) / w4_sum_bytes(rows);
     p->sets = (most + at_most - 1) / at_most;
     p->set_tiles = (most + p->sets - 1) / p->sets;
-    *smem = p->at_sums + p->set_tiles * sum_bytes(rows) + 1024;
+    *smem = p->at_sums + p->set_tiles * w4_sum_bytes(rows) + 1024;
     return true;
 }
 

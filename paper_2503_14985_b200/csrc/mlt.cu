@@ -1427,6 +1427,7 @@ extern "C" int mlt_gemm_w4(const void* X, const void* W, const void* scales, con
     if (K % group != 0) return MLT_ERR_INVALID_ARG;
     if (ldx < K || ldw < K / 2 || lds < K / group || (zeros && ldz < K / group) || ldc < N) return MLT_ERR_INVALID_ARG;
     if (M > (1 << 19) || N > INT32_MAX - 1024 || K > INT32_MAX - 1024) return MLT_ERR_UNSUPPORTED;
+    if (!w4_fits(M, static_cast<int>(K), group)) return MLT_ERR_UNSUPPORTED;
     if (K > 0 && (!aligned16(X) || !aligned16(W) || ldx % 8 != 0 || ldw % 16 != 0 || (reinterpret_cast<uintptr_t>(scales) & 1u) != 0))
         return MLT_ERR_ALIGNMENT;
     if ((reinterpret_cast<uintptr_t>(C) & 1u) != 0) return MLT_ERR_ALIGNMENT;
