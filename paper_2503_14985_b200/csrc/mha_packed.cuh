@@ -46,7 +46,7 @@ constexpr int kPackedMaxKeys = INT32_MAX - 127;  // keys that a block table's ro
 constexpr int kPackedSplitTiles = 4096;  // key ranges are cut only when there are no more tile pairs than this
 constexpr int kPackedSplitRows = 320 * 2 * kMhaBlock;  // rows of partial results that scratch is sized for (and see packed_scratch)
 
-struct PackedHeader {  // at the front of the scratch memory, written by the plan kernel
+struct alignas(16) PackedHeader {  // at the front of the scratch memory, written by the plan kernel
     int num_items;     // entries * H_kv
     int counter;       // items handed out beyond the first one of each CTA
     int split;         // key blocks per part, 0: no range is cut
@@ -137,14 +137,14 @@ __device__ __forceinline__ bool packed_sequence(const PackedParams& p, int s, in
 }
 
 // The group (or sequence) that token t is in, or -1.
-__device__ __forceinline__ int packed_owner(const PackedParams& p, int t) {
-    if (p.S == 0) return -1;
-    int lo = 0, hi = p.S;  // the last one that begins at or before the token
+__device__ __forceinline__ int packed_owner(const int* cu_q, int S, int t) {
+    if (S == 0) return -1;
+    int lo = 0, hi = S;  // the last one that begins at or before the token
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (p.cu_q[mid] <= t) lo = mid; else hi = mid;
+        if (cu_q[mid] <= t) lo = mid; else hi = mid;
     }
-    return p.cu_q[lo] <= t && t < p.cu_q[lo + 1] ? lo : -1;
+    return cu_q[lo] <= t && t < cu_q[lo + 1] ? lo : -1;
 }
 
 // The same by a whole warp: 33 parts per step instead of two.
@@ -162,13 +162,14 @@ __device__ __forceinline__ int packed_owner_warp(const PackedParams& p, int t) {
     return p.cu_q[lo] <= t && t < p.cu_q[lo + 1] ? lo : -1;
 }
 
-// The same where offsets need not ascend, so that no search by halves finds what is kept: behind shared prefixes what the plan gave the
-// token's tail, else the first sequence that is kept and has the token.
-__device__ __noinline__ int packed_owner_any(const PackedParams& p, int t) {
-    if (p.prefix_lens) return packed_owner(p, t);
-    for (int s0 = 0; s0 < p.S; s0 += 32) {
+// The same where offsets need not ascend, so that no search by halves finds what is kept: behind shared prefixes (cu_q given) what the plan
+// gave the token's tail, else the first sequence that is kept and has the token.  (A call of its own, and not with all parameters, which it
+// would put on the stack: the join of 32 x 5 tokens took 5 us longer.)
+__device__ __noinline__ int packed_owner_any(const int* cu_q, const int4* seqs, int S, int t) {
+    if (cu_q) return packed_owner(cu_q, S, t);
+    for (int s0 = 0; s0 < S; s0 += 32) {
         const int s = s0 + static_cast<int>(threadIdx.x & 31);
-        const int4 q = s < p.S ? p.seqs[s] : make_int4(0, 0, 0, 0);
+        const int4 q = s < S ? seqs[s] : make_int4(0, 0, 0, 0);
         const unsigned int has = __ballot_sync(0xffffffffu, q.x <= t && t - q.x < q.y);
         if (has) return s0 + __ffs(has) - 1;
     }
@@ -179,7 +180,7 @@ __device__ __noinline__ int packed_owner_any(const PackedParams& p, int t) {
 __device__ __forceinline__ void packed_tail(const PackedParams& p, int t, int3& q, long long& base) {
     int3 g;
     long long unused;
-    const int group = packed_owner(p, t);
+    const int group = packed_owner(p.cu_q, p.S, t);
     const int prefix = group >= 0 && packed_sequence(p, group, g, unused) ? g.z : 0;
     const long long most = static_cast<long long>(p.max_blocks) * p.block_size;
     const int len = static_cast<int>(max(0ll, min(static_cast<long long>(p.seq_lens[t]), most)));
@@ -1282,14 +1283,15 @@ __global__ void __launch_bounds__(kPackedJoinWarps * 32) mha_packed_join_kernel(
     pdl_launch_dependents();
     constexpr int V = D / 32;  // elements per lane
     cudaGridDependencySynchronize();
-    if (p.hdr->split == 0) return;
+    const PackedHeader hdr = *p.hdr;
+    if (hdr.split == 0) return;
     const int lane = threadIdx.x & 31, tok = blockIdx.x, h = blockIdx.y * kPackedJoinWarps + (threadIdx.x >> 5);
     if (h >= p.H) return;
     const int kvh = h / p.G, W2 = 2 * p.W;
     // This row's parts: a run from its sequence's (or group's) tile pair and, behind a prefix, one from its tail.  Part k lies at
     // first + k * step, or, where both tiles had the same rows, at first + (k / 2) * step + (k % 2) * half.
     int first[2] = {0, 0}, step[2] = {0, 0}, half[2] = {0, 0}, count[2] = {0, 0};
-    const int owner = p.hdr->irregular ? packed_owner_any(p, tok) : packed_owner_warp(p, tok);
+    const int owner = hdr.irregular ? packed_owner_any(p.prefix_lens ? p.cu_q : nullptr, p.seqs, p.S, tok) : packed_owner_warp(p, tok);
     if (owner < 0 && !p.prefix_lens) return;  // a token of no sequence
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
