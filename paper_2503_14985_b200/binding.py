@@ -783,7 +783,8 @@ def paged_attn_decode_shared(Q, K_cache, V_cache, block_table, seq_lens, prefix_
 
 
 def gemm_w4(X, W, scales, zeros=None, C=None, *, stream=None):
-    """C = X @ dequantised(W).T in bfloat16 for few rows X [M, K] bfloat16 and 4-bit weights.
+    """C = X @ dequantised(W).T in bfloat16 for few rows X [M, K] bfloat16 and 4-bit weights (up to 8 rows faster than gemm_f8 and gemm,
+    from 17 on slower than both).
 
     W [N, K / 2] uint8, two weights to a byte, the even k in the lower half; scales [N, K / group] bfloat16; zeros [N, K / group]
     uint8 (None: 8): weight (n, k) is scales[n, k / group] * (W(n, k) - zeros[n, k / group]).  group, 32, 64 or 128, follows from

@@ -25,7 +25,8 @@
 //    once, behind the only barrier.  (Against one set of row tiles at a time, K cut over the warps and a barrier per set:
 //    16 x 28672 x 4096 38.7 -> 29.9 us, 16 x 4096 x 28672 56 -> 42.7, 1 x 28672 x 4096 18.6 -> 16.4; 1 x 4096 x 4096, one tile per CTA
 //    either way, 5.3 -> 5.7.)  Where x does not fit or there are fewer tiles than SMs, a cluster cuts K and sums through
-//    distributed shared memory, in a fixed order.  More than 16 rows run as several passes over the weights (from L2, mostly).
+//    distributed shared memory, in a fixed order.  More than 16 rows run as several passes over the weights (from L2, mostly), one behind the
+//    other: 28672 x 4096 with group 128 takes 32 us with 16 rows, 59 with 32, 112 with 64.
 // Times are those of graphs of ten calls.  58.7 MB of weights (28672 x 4096) take 12.3 us to read by TMA or by plain loads and nothing
 // else, 9 at the copy bandwidth.  With 1 row the kernel is 1.3 of that; with 16 the matrix instructions (m16n8k16 at 16 weights and 8
 // columns) and what turns the words into them bound it.

@@ -12,7 +12,7 @@
 //  * Work.  Lengths are on the device, so a one-CTA kernel writes the list of work items (two tiles of a sequence, a range of
 //    key blocks), longest first, and persistent CTAs (one per SM) draw from it by an atomic counter.  The loading warp draws
 //    the next item while it requests the current one's keys, so the list's latency hides behind the ring.  A call of one short
-//    sequence with an SM for each item needs no list: 37 tokens of 32 heads take 10.6 us without the plan kernel, 13.5 with it.
+//    sequence with an SM for each item needs no list: 37 tokens of 32 heads take 10.3 us without the plan kernel, 13.5 with it.
 //  * Few rows.  With too few items for the SMs (few tokens behind a long context) the plan cuts the key range, and where the rows
 //    fill one tile only, both tiles work on them, each on every other key block ("dual": 128 keys then take 1600 clocks instead of
 //    3000, the latency of one tile's chain S -> softmax -> P V; at the copy bandwidth an SM gets 128 keys in 2800).  The parts go to
