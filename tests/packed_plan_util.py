@@ -1,7 +1,6 @@
 """The plan of the packed attention (which tiles, key ranges and scratch rows its work items have) run on the CPU from the kernel's own text, and
 what must hold for every plan: the attention and join kernels read and write where it says, without checks of their own."""
 import ctypes
-import hashlib
 import os
 import re
 import subprocess
@@ -36,15 +35,15 @@ def load():
     if _lib is None:
         source = plan_source()
         host = os.path.join(HERE, "packed_plan_host.cpp")
-        with open(host) as f:
-            key = hashlib.sha256((source + f.read()).encode()).hexdigest()[:16]
-        folder = tempfile.mkdtemp(prefix="packed_plan_" + key)
-        with open(os.path.join(folder, "packed_plan_source.inc"), "w") as f:
-            f.write(source)
-        out = os.path.join(folder, "plan.so")
-        res = subprocess.run(["g++", "-std=c++17", "-O2", "-U_FORTIFY_SOURCE", "-w", "-shared", "-fPIC", "-I", folder, "-o", out, host], capture_output=True, text=True)
-        assert res.returncode == 0, res.stderr
-        _lib = ctypes.CDLL(out)
+        with tempfile.TemporaryDirectory(prefix="packed_plan_") as folder:
+            with open(os.path.join(folder, "packed_plan_source.inc"), "w") as f:
+                f.write(source)
+            out = os.path.join(folder, "plan.so")
+            # (_FORTIFY_SOURCE takes a jump to another stack for an error)
+            res = subprocess.run(["g++", "-std=c++17", "-O2", "-U_FORTIFY_SOURCE", "-w", "-shared", "-fPIC", "-I", folder, "-o", out, host], capture_output=True,
+                                 text=True)
+            assert res.returncode == 0, res.stderr
+            _lib = ctypes.CDLL(out)
         _lib.packed_scratch_layout.restype = ctypes.c_longlong
     return _lib
 
